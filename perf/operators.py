@@ -277,8 +277,8 @@ def _own(s):
         return r.logprobs, r.entropy, grad
     if c["form"] == "step":
         return hr.distill_step(s["z"], s["ids"], s["teacher"], s["weights"], scale=c["scale"])
-    loss, norm = hr.distill_forward(s["z"], s["ids"], s["teacher"], scale=c["scale"])
-    return loss, hr.distill_backward(s["z"], s["ids"], s["teacher"], norm, s["weights"], scale=c["scale"])
+    loss, norm, q = hr.distill_forward(s["z"], s["ids"], s["teacher"], scale=c["scale"])
+    return loss, hr.distill_backward(s["z"], s["ids"], q, norm, s["weights"], scale=c["scale"])
 
 
 def run(state):
