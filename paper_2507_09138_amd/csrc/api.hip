@@ -11,6 +11,7 @@
 #include <thread>
 
 #include "common.h"
+#include "entry.h"
 
 // Scratch memory of hr_ivf_search_static, the entry point for callers that cannot allocate: a
 // fixed array in the library's device image, one copy per GPU, held until the process ends.  In
@@ -105,7 +106,7 @@ using namespace hr;
 
 static thread_local char g_err[512] = "";
 
-static int fail(int code, const char* fmt, ...)
+int hr::fail(int code, const char* fmt, ...)
 {
     va_list ap;
     va_start(ap, fmt);
@@ -113,12 +114,6 @@ static int fail(int code, const char* fmt, ...)
     va_end(ap);
     return code;
 }
-
-#define HR_HIP(call)                                                                      \
-    do {                                                                                  \
-        hipError_t e_ = (call);                                                           \
-        if (e_ != hipSuccess) return fail(HR_ERR_HIP, "%s: %s", #call, hipGetErrorString(e_)); \
-    } while (0)
 
 static constexpr uint64_t kMagic = 0x4852495646313031ULL;   // "HRIVF101"
 
@@ -376,10 +371,7 @@ static int check_batch(const hr_ivf_index* ix, int64_t nq, int nprobe, int k, in
 
 static int check_ws(const Plan& p, const void* ws, size_t bytes)
 {
-    if (!ws) return fail(HR_ERR_WORKSPACE, "workspace is null");
-    if (((uintptr_t)ws) % HR_WORKSPACE_ALIGN) return fail(HR_ERR_WORKSPACE, "workspace not %d-byte aligned", HR_WORKSPACE_ALIGN);
-    if (bytes < p.total) return fail(HR_ERR_WORKSPACE, "workspace has %zu bytes, need %zu", bytes, p.total);
-    return HR_OK;
+    return check_workspace(ws, bytes, p.total);
 }
 
 extern "C" {

@@ -1,0 +1,331 @@
+"""ctypes binding of hr_scores.h: products in 8 bits, log probabilities and distillation over matrices of scores.
+
+As in ``binding``: functions with the names of the C entry points take tensors (or raw addresses) and sizes; the others
+check their tensors, allocate results and workspace on the current stream of the tensors' device, and call those.
+Matrices may be slices of columns of wider ones (rows contiguous); others are copied first.
+"""
+import ctypes
+from typing import NamedTuple, Optional
+
+import torch
+
+from .binding import _DTYPE, _addr, _check, _stream, HR_K_MAX, HrError, hr_last_error, lib
+
+HR_I8_K_MAX, HR_LIST_MAX, HR_ROW_MAX = 131071, 512, 1 << 30
+
+_c, _p = ctypes, ctypes.c_void_p
+_i32, _i64, _f32, _size = _c.c_int32, _c.c_int64, _c.c_float, _c.c_size_t
+_rows_args = [_p, _i64, _i32, _i64, _i64, _f32]
+lib.hr_i8_quantize.argtypes = [_p, _i64, _i32, _i64, _i64, _p, _i64, _p, _p]
+lib.hr_i8_workspace_bytes.argtypes = [_i64, _i64, _i64]
+lib.hr_i8_workspace_bytes.restype = _size
+lib.hr_i8_product.argtypes = [_p, _i64, _p, _p, _i64, _p, _p, _i64, _i64, _i64, _p, _i64, _i32, _p, _size, _p]
+lib.hr_i8_linear.argtypes = [_p, _i64, _i32, _p, _i64, _p, _p, _i64, _i64, _i64, _p, _i64, _i32, _p, _size, _p]
+lib.hr_logprobs_workspace_bytes.argtypes = [_i64, _i64, _i32]
+lib.hr_logprobs_workspace_bytes.restype = _size
+lib.hr_logprobs.argtypes = _rows_args + [_p, _i32, _i32, _p, _p, _p, _p, _p, _p, _size, _p]
+lib.hr_logprobs_backward.argtypes = _rows_args + [_p, _i32, _p, _p, _p, _p, _p, _i64, _p]
+lib.hr_distill_workspace_bytes.argtypes = [_i64, _i64, _i32]
+lib.hr_distill_workspace_bytes.restype = _size
+lib.hr_distill_forward.argtypes = _rows_args + [_p, _p, _i32, _p, _p, _p, _p, _size, _p]
+lib.hr_distill_backward.argtypes = _rows_args + [_p, _p, _i32, _p, _p, _p, _i64, _p]
+lib.hr_distill_step.argtypes = _rows_args + [_p, _p, _i32, _p, _p, _p, _p, _p, _i64, _p, _size, _p]
+
+
+# ---- the C entry points by name
+
+def hr_i8_quantize(x, ldx, dtype, m, k, q, ldq, scale, stream=None):
+    _check(lib.hr_i8_quantize(_addr(x), ldx, dtype, m, k, _addr(q), ldq, _addr(scale), _stream(stream)))
+
+
+def hr_i8_workspace_bytes(m, n, k):
+    return int(lib.hr_i8_workspace_bytes(m, n, k))
+
+
+def hr_i8_product(a, lda, a_scale, b, ldb, b_scale, bias, m, n, k, out, ldo, out_dtype, workspace, workspace_bytes, stream=None):
+    _check(lib.hr_i8_product(_addr(a), lda, _addr(a_scale), _addr(b), ldb, _addr(b_scale), _addr(bias), m, n, k, _addr(out), ldo,
+                             out_dtype, _addr(workspace), workspace_bytes, _stream(stream)))
+
+
+def hr_i8_linear(x, ldx, x_dtype, b, ldb, b_scale, bias, m, n, k, out, ldo, out_dtype, workspace, workspace_bytes, stream=None):
+    _check(lib.hr_i8_linear(_addr(x), ldx, x_dtype, _addr(b), ldb, _addr(b_scale), _addr(bias), m, n, k, _addr(out), ldo, out_dtype,
+                            _addr(workspace), workspace_bytes, _stream(stream)))
+
+
+def hr_logprobs_workspace_bytes(rows, n, k):
+    return int(lib.hr_logprobs_workspace_bytes(rows, n, k))
+
+
+def hr_logprobs(logits, ld, dtype, rows, n, scale, given, ngiven, k, out_logprobs, out_entropy, out_norm, out_top_ids, out_top_logprobs,
+                workspace, workspace_bytes, stream=None):
+    _check(lib.hr_logprobs(_addr(logits), ld, dtype, rows, n, scale, _addr(given), ngiven, k, _addr(out_logprobs), _addr(out_entropy),
+                           _addr(out_norm), _addr(out_top_ids), _addr(out_top_logprobs), _addr(workspace), workspace_bytes,
+                           _stream(stream)))
+
+
+def hr_logprobs_backward(logits, ld, dtype, rows, n, scale, given, ngiven, entropy, norm, grad_logprobs, grad_entropy, grad_logits,
+                         ldg, stream=None):
+    _check(lib.hr_logprobs_backward(_addr(logits), ld, dtype, rows, n, scale, _addr(given), ngiven, _addr(entropy), _addr(norm),
+                                    _addr(grad_logprobs), _addr(grad_entropy), _addr(grad_logits), ldg, _stream(stream)))
+
+
+def hr_distill_workspace_bytes(rows, n, k):
+    return int(lib.hr_distill_workspace_bytes(rows, n, k))
+
+
+def hr_distill_forward(logits, ld, dtype, rows, n, scale, ids, teacher, k, out_loss, out_norm, out_q, workspace, workspace_bytes,
+                       stream=None):
+    _check(lib.hr_distill_forward(_addr(logits), ld, dtype, rows, n, scale, _addr(ids), _addr(teacher), k, _addr(out_loss),
+                                  _addr(out_norm), _addr(out_q), _addr(workspace), workspace_bytes, _stream(stream)))
+
+
+def hr_distill_backward(logits, ld, dtype, rows, n, scale, ids, q, k, norm, weights, grad_logits, ldg, stream=None):
+    _check(lib.hr_distill_backward(_addr(logits), ld, dtype, rows, n, scale, _addr(ids), _addr(q), k, _addr(norm), _addr(weights),
+                                   _addr(grad_logits), ldg, _stream(stream)))
+
+
+def hr_distill_step(logits, ld, dtype, rows, n, scale, ids, teacher, k, weights, out_loss, out_norm, out_q, grad_logits, ldg, workspace,
+                    workspace_bytes, stream=None):
+    _check(lib.hr_distill_step(_addr(logits), ld, dtype, rows, n, scale, _addr(ids), _addr(teacher), k, _addr(weights), _addr(out_loss),
+                               _addr(out_norm), _addr(out_q), _addr(grad_logits), ldg, _addr(workspace), workspace_bytes,
+                               _stream(stream)))
+
+
+# ---- tensors in, tensors out
+
+def _matrix(t, name, dtypes, shape=(None, None)):
+    """A device matrix of one of the types whose rows are contiguous, and the distance between its rows."""
+    if not isinstance(t, torch.Tensor) or not t.is_cuda:
+        raise HrError(-1, f"{name} must be a device tensor")
+    if t.dtype not in dtypes:
+        raise HrError(-1, f"{name} has dtype {t.dtype}, want one of {[str(d) for d in dtypes]}")
+    if t.dim() != 2 or any(w is not None and g != w for g, w in zip(t.shape, shape)):
+        raise HrError(-1, f"{name} has shape {tuple(t.shape)}, want {tuple('*' if w is None else w for w in shape)}")
+    rows, cols = t.shape
+    ld = t.stride(0)
+    if (cols > 1 and t.stride(1) != 1) or (rows > 1 and ld < cols):
+        t = t.contiguous()
+        ld = cols
+    return t, (ld if rows > 1 else max(cols, 1))
+
+
+def _like(t, name, dtype, shape, device):
+    """A contiguous tensor of this type and shape on the device."""
+    if not isinstance(t, torch.Tensor) or t.device != device:
+        raise HrError(-1, f"{name} must be a tensor on {device}")
+    if t.dtype != dtype or t.shape != shape:
+        raise HrError(-1, f"{name} is {t.dtype} {tuple(t.shape)}, want {dtype} {tuple(shape)}")
+    return t.contiguous()
+
+
+def _result(out, name, dtype, shape, device):
+    """Where a result matrix goes, and the distance between its rows: a new one, or the caller's."""
+    if out is None:
+        return torch.empty(shape, dtype=dtype, device=device), max(shape[1], 1)
+    if not isinstance(out, torch.Tensor) or out.device != device or out.dtype != dtype or out.shape != shape:
+        raise HrError(-1, f"{name} must be a {dtype} tensor of shape {tuple(shape)} on {device}")
+    ld = out.stride(0)
+    if (shape[1] > 1 and out.stride(1) != 1) or (shape[0] > 1 and ld < shape[1]):
+        raise HrError(-1, f"{name} must have contiguous rows that do not overlap")
+    return out, (ld if shape[0] > 1 else max(shape[1], 1))
+
+
+def _workspace(need, device):
+    if need == 0:
+        raise HrError(-1, hr_last_error())
+    return torch.empty(need, dtype=torch.uint8, device=device)
+
+
+class _on:
+    """The device whose tensors a call takes is the current one during the call."""
+
+    def __init__(self, device):
+        self.guard = None if device.index == torch.cuda.current_device() else torch.cuda.device(device)
+
+    def __enter__(self):
+        if self.guard is not None:
+            self.guard.__enter__()
+
+    def __exit__(self, *exc):
+        if self.guard is not None:
+            self.guard.__exit__(*exc)
+
+
+def _padded(n):
+    return (n + 63) // 64 * 64
+
+
+def quantize_rows(x):
+    """Rows of x [m, k] in 8 bits: (int8 [m, k], float32 scale [m]).  The rows lie a multiple of 64 bytes apart."""
+    x, ld = _matrix(x, "x", _DTYPE)
+    m, k = x.shape
+    q = torch.empty(m, _padded(k), dtype=torch.int8, device=x.device)
+    scale = torch.empty(m, dtype=torch.float32, device=x.device)
+    with _on(x.device):
+        hr_i8_quantize(x, ld, _DTYPE[x.dtype], m, k, q, q.shape[1], scale)
+    return q[:, :k], scale
+
+
+def _i8_matrix(t, name, shape=(None, None)):
+    """An int8 matrix, copied where the library would read behind its memory (rows on 16-byte boundaries of a length that is not)."""
+    t, ld = _matrix(t, name, (torch.int8,), shape)
+    rows, k = t.shape
+    if k % 16 and rows and ld % 16 == 0 and t.data_ptr() % 16 == 0 and \
+            t.storage_offset() + (rows - 1) * ld + (k + 15) // 16 * 16 > t.untyped_storage().nbytes():
+        copy = torch.zeros(rows, _padded(k), dtype=torch.int8, device=t.device)
+        copy[:, :k] = t
+        return copy[:, :k], copy.shape[1]
+    return t, ld
+
+
+def _out_type(dtype):
+    if dtype not in _DTYPE:
+        raise HrError(-1, f"dtype {dtype}: want float32, float16 or bfloat16")
+    return _DTYPE[dtype]
+
+
+def i8_product(a, a_scale, b, b_scale, bias=None, dtype=torch.float32, out=None):
+    """a [m, k] times b [n, k] transposed, both int8, in the scales [m] and [n] of their rows, plus bias [n]: [m, n] in dtype."""
+    a, lda = _i8_matrix(a, "a")
+    m, k = a.shape
+    b, ldb = _i8_matrix(b, "b", (None, k))
+    n, dev = b.shape[0], a.device
+    code = _out_type(dtype)
+    a_scale, b_scale = _like(a_scale, "a_scale", torch.float32, (m,), dev), _like(b_scale, "b_scale", torch.float32, (n,), dev)
+    if b.device != dev:
+        raise HrError(-1, f"b is on {b.device}, a on {dev}")
+    bias = None if bias is None else _like(bias, "bias", torch.float32, (n,), dev)
+    out, ldo = _result(out, "out", dtype, (m, n), dev)
+    with _on(dev):
+        ws = _workspace(hr_i8_workspace_bytes(m, n, k), dev)
+        hr_i8_product(a, lda, a_scale, b, ldb, b_scale, bias, m, n, k, out, ldo, code, ws, ws.numel())
+    return out
+
+
+def i8_linear(x, b, b_scale, bias=None, dtype=torch.float32, out=None):
+    """Rows of floats x [m, k], quantised row by row, times b [n, k] int8 transposed: [m, n] in dtype."""
+    x, ldx = _matrix(x, "x", _DTYPE)
+    m, k = x.shape
+    b, ldb = _i8_matrix(b, "b", (None, k))
+    n, dev = b.shape[0], x.device
+    code = _out_type(dtype)
+    b_scale = _like(b_scale, "b_scale", torch.float32, (n,), dev)
+    if b.device != dev:
+        raise HrError(-1, f"b is on {b.device}, x on {dev}")
+    bias = None if bias is None else _like(bias, "bias", torch.float32, (n,), dev)
+    out, ldo = _result(out, "out", dtype, (m, n), dev)
+    with _on(dev):
+        ws = _workspace(hr_i8_workspace_bytes(m, n, k), dev)
+        hr_i8_linear(x, ldx, _DTYPE[x.dtype], b, ldb, b_scale, bias, m, n, k, out, ldo, code, ws, ws.numel())
+    return out
+
+
+class Logprobs(NamedTuple):
+    """What ``logprobs`` finds: ln p of the given entries, entropy and norm of every row, its best alternatives."""
+    logprobs: Optional[torch.Tensor]
+    entropy: torch.Tensor
+    norm: torch.Tensor
+    top_ids: Optional[torch.Tensor]
+    top_logprobs: Optional[torch.Tensor]
+
+
+def _list(ids, name, rows, device):
+    if not isinstance(ids, torch.Tensor) or ids.dtype not in (torch.int64, torch.int32):
+        raise HrError(-1, f"{name} must be an integer tensor")
+    if ids.device != device or ids.dim() != 2 or ids.shape[0] != rows or ids.shape[1] > HR_LIST_MAX:
+        raise HrError(-1, f"{name} must be a [{rows}, 0..{HR_LIST_MAX}] tensor on {device}")
+    return ids.to(torch.int64).contiguous()
+
+
+def logprobs(logits, given=None, k=0, scale=1.0):
+    """softmax(scale * logits) of every row [rows, n]: log probabilities of the given entries [rows, g], entropy, the k best."""
+    z, ld = _matrix(logits, "logits", _DTYPE)
+    rows, n = z.shape
+    dev = z.device
+    given = None if given is None else _list(given, "given", rows, dev)
+    g = 0 if given is None else given.shape[1]
+    lp = None if given is None else torch.empty(rows, g, dtype=torch.float32, device=dev)
+    entropy = torch.empty(rows, dtype=torch.float32, device=dev)
+    norm = torch.empty(rows, 2, dtype=torch.float32, device=dev)
+    ids = top = None
+    if k > 0:
+        ids = torch.empty(rows, k, dtype=torch.int64, device=dev)
+        top = torch.empty(rows, k, dtype=torch.float32, device=dev)
+    with _on(dev):
+        ws = _workspace(hr_logprobs_workspace_bytes(rows, n, k), dev)
+        hr_logprobs(z, ld, _DTYPE[z.dtype], rows, n, scale, given, g, k, lp, entropy, norm, ids, top, ws, ws.numel())
+    return Logprobs(lp, entropy, norm, ids, top)
+
+
+def logprobs_backward(logits, given, result, grad_logprobs=None, grad_entropy=None, scale=1.0, out=None):
+    """Gradient with respect to the logits, given those with respect to the result's logprobs [rows, g] and entropy [rows]
+    (None: 0).  ``out`` may be the logits themselves."""
+    z, ld = _matrix(logits, "logits", _DTYPE)
+    rows, n = z.shape
+    dev = z.device
+    given = None if given is None else _list(given, "given", rows, dev)
+    g = 0 if given is None else given.shape[1]
+    entropy = _like(result.entropy, "result.entropy", torch.float32, (rows,), dev)
+    norm = _like(result.norm, "result.norm", torch.float32, (rows, 2), dev)
+    if grad_logprobs is not None:
+        if given is None:
+            raise HrError(-1, "grad_logprobs without given entries")
+        grad_logprobs = _like(grad_logprobs, "grad_logprobs", torch.float32, (rows, g), dev)
+    if grad_entropy is not None:
+        grad_entropy = _like(grad_entropy, "grad_entropy", torch.float32, (rows,), dev)
+    grad, ldg = _result(out, "out", z.dtype, (rows, n), dev)
+    with _on(dev):
+        hr_logprobs_backward(z, ld, _DTYPE[z.dtype], rows, n, scale, given, g, entropy, norm, grad_logprobs, grad_entropy, grad, ldg)
+    return grad
+
+
+def _taught(logits, ids, name, values):
+    z, ld = _matrix(logits, "logits", _DTYPE)
+    rows = z.shape[0]
+    ids = _list(ids, "ids", rows, z.device)
+    if ids.shape[1] < 1:
+        raise HrError(-1, "ids has no columns")
+    return z, ld, ids, _like(values, name, torch.float32, ids.shape, z.device)
+
+
+def distill_forward(logits, ids, teacher, scale=1.0):
+    """Loss [rows] of the logits [rows, n] against a teacher's scores [rows, k] of the entries ids [rows, k] (-1: empty), and what
+    ``distill_backward`` needs: (loss, norm, q)."""
+    z, ld, ids, teacher = _taught(logits, ids, "teacher", teacher)
+    rows, n = z.shape
+    k, dev = ids.shape[1], z.device
+    loss = torch.empty(rows, dtype=torch.float32, device=dev)
+    norm = torch.empty(rows, 2, dtype=torch.float32, device=dev)
+    q = torch.empty(rows, k, dtype=torch.float32, device=dev)
+    with _on(dev):
+        ws = _workspace(hr_distill_workspace_bytes(rows, n, k), dev)
+        hr_distill_forward(z, ld, _DTYPE[z.dtype], rows, n, scale, ids, teacher, k, loss, norm, q, ws, ws.numel())
+    return loss, norm, q
+
+
+def distill_backward(logits, ids, q, norm, weights=None, scale=1.0, out=None):
+    """Gradient with respect to the logits; weights [rows]: that of the caller's loss with respect to every row's (None: 1).
+    ``out`` may be the logits themselves."""
+    z, ld, ids, q = _taught(logits, ids, "q", q)
+    rows, n = z.shape
+    dev = z.device
+    norm = _like(norm, "norm", torch.float32, (rows, 2), dev)
+    weights = None if weights is None else _like(weights, "weights", torch.float32, (rows,), dev)
+    grad, ldg = _result(out, "out", z.dtype, (rows, n), dev)
+    with _on(dev):
+        hr_distill_backward(z, ld, _DTYPE[z.dtype], rows, n, scale, ids, q, ids.shape[1], norm, weights, grad, ldg)
+    return grad
+
+
+def distill_step(logits, ids, teacher, weights=None, scale=1.0, out=None):
+    """``distill_forward`` and ``distill_backward`` in one, for weights known beforehand: (loss [rows], gradient [rows, n])."""
+    z, ld, ids, teacher = _taught(logits, ids, "teacher", teacher)
+    rows, n = z.shape
+    k, dev = ids.shape[1], z.device
+    weights = None if weights is None else _like(weights, "weights", torch.float32, (rows,), dev)
+    loss = torch.empty(rows, dtype=torch.float32, device=dev)
+    grad, ldg = _result(out, "out", z.dtype, (rows, n), dev)
+    with _on(dev):
+        ws = _workspace(hr_distill_workspace_bytes(rows, n, k), dev)
+        hr_distill_step(z, ld, _DTYPE[z.dtype], rows, n, scale, ids, teacher, k, weights, loss, None, None, grad, ldg, ws, ws.numel())
+    return loss, grad
