@@ -31,27 +31,47 @@ __device__ __forceinline__ float order_value(uint32_t key)
 template <typename T>
 struct Row {
     static constexpr int E = 16 / sizeof(T);
+    using V = T __attribute__((ext_vector_type(E)));
     const T* z;
     int n, before, nchunks;             // before: places of chunk 0 in front of the row
+    int lo, hi;                         // chunks lo .. hi-1 are the row's throughout
 
     __device__ __forceinline__ Row(const void* base, int64_t offset, int n_) : z((const T*)base + offset), n(n_)
     {
         before = (int)(((uintptr_t)z & 15) / sizeof(T));
         nchunks = (int)(((int64_t)before + n + E - 1) / E);
+        lo = before > 0;
+        hi = (int)(((int64_t)before + n) / E);
     }
-    // scores of chunk c, -inf where it is not the row's; returns the entry of its first place (negative in front of the row)
+    __device__ __forceinline__ int first(int c) const { return c * E - before; }      // entry of a chunk's first place
+    // A chunk as it lies in memory; what lies at the edges or behind the row is some other chunk of it, to be replaced by fix().
+    // (A row that is no whole chunk has nothing that could be loaded: 0.)
+    __device__ __forceinline__ V raw(int c) const
+    {
+        if (hi <= lo) return V{};
+        c = c < lo ? lo : (c < hi ? c : hi - 1);
+        return *(const V*)(z + first(c));
+    }
+    // The same where the chunk is the row's in part or not at all: -inf in the places that are not.
+    __device__ __forceinline__ void fix(int c, float* v) const
+    {
+        if (c >= lo && c < hi) return;
+#pragma unroll
+        for (int e = 0; e < E; ++e) {
+            const int i = first(c) + e;
+            v[e] = c < nchunks && i >= 0 && i < n ? (float)z[i] : -INFINITY;
+        }
+    }
+    __device__ __forceinline__ void unpack(int c, V t, float* v) const
+    {
+#pragma unroll
+        for (int e = 0; e < E; ++e) v[e] = (float)t[e];
+        fix(c, v);
+    }
     __device__ __forceinline__ int load(int c, float* v) const
     {
-        const int first = c * E - before;
-        if (first >= 0 && first + E <= n) {
-            const vec_of<T> t = *(const vec_of<T>*)(z + first);
-#pragma unroll
-            for (int e = 0; e < E; ++e) v[e] = (float)t[e];
-        } else {
-#pragma unroll
-            for (int e = 0; e < E; ++e) v[e] = first + e >= 0 && first + e < n ? (float)z[first + e] : -INFINITY;
-        }
-        return first;
+        unpack(c, raw(c), v);
+        return first(c);
     }
     __device__ __forceinline__ float at(int64_t i) const { return i >= 0 && i < n ? (float)z[i] : -INFINITY; }
 };
@@ -116,18 +136,16 @@ struct RowStat {
         s0 *= f;
         m = to;
     }
-    template <int E>
-    __device__ __forceinline__ void add(const float* v, float c2)
+    // a chunk, top its largest score
+    template <int E, bool ENTROPY>
+    __device__ __forceinline__ void add(const float* v, float top, float c2)
     {
-        float top = m;
-#pragma unroll
-        for (int e = 0; e < E; ++e) top = fmaxf(top, v[e]);
         if (top > m) rescale(top, c2);
 #pragma unroll
         for (int e = 0; e < E; ++e) {
             const float x = (v[e] - m) * c2, t = __builtin_amdgcn_exp2f(x);
             s0 += t;
-            s1 = fmaf(fmaxf(x, kLowest2), t, s1);
+            if (ENTROPY) s1 = fmaf(fmaxf(x, kLowest2), t, s1);
         }
     }
     __device__ __forceinline__ void merge(float m2, float a, float b, float c2)
@@ -154,16 +172,66 @@ struct RowStat {
     }
 };
 
-// of a whole row, to all threads of a workgroup
-template <typename T, int THREADS>
-__device__ __forceinline__ RowStat row_stats(const Row<T>& row, float c2, RowShared<THREADS>& sh)
+// Largest scores of stretches of a row: what the search for its best entries starts from.  A slot is 2^shift chunks.
+template <int THREADS>
+struct Slots {
+    static constexpr int kMax = 4 * THREADS;
+    uint32_t key[kMax];
+    // few enough slots: chunks one by one, or 2, 4, 8, 16 .. of them together
+    static __host__ __device__ int shift_for(int nchunks)
+    {
+        int s = 0;
+        while (nchunks > kMax << s) ++s;
+        return s;
+    }
+};
+
+// largest of 2^min(shift, 4) neighbouring lanes
+__device__ __forceinline__ float neighbours_max(float v, int shift)
 {
+    auto step = [&](auto ctrl) __attribute__((always_inline)) {
+        v = fmaxf(v, __builtin_bit_cast(float, __builtin_amdgcn_update_dpp(0, __builtin_bit_cast(int, v), decltype(ctrl)::value, 0xf, 0xf, false)));
+    };
+    using std::integral_constant;
+    if (shift >= 1) step(integral_constant<int, 0xb1>{});       // quad_perm: lane ^ 1
+    if (shift >= 2) step(integral_constant<int, 0x4e>{});       // quad_perm: lane ^ 2
+    if (shift >= 3) step(integral_constant<int, 0x141>{});      // row_half_mirror: the other four of eight lanes
+    if (shift >= 4) step(integral_constant<int, 0x140>{});      // row_mirror: the other eight of sixteen
+    return v;
+}
+
+// Maximum and sums of chunks begin .. end-1 of a row (begin a multiple of 16), to all threads of a workgroup.  A thread asks for
+// four chunks at a time; with several waves per SIMD that is enough under way.  TOP: the slots' largest scores as well
+// (slots of the row's chunk 0 on; they have to be cleared before if shift > 4).
+template <typename T, int THREADS, bool ENTROPY, bool TOP>
+__device__ __forceinline__ RowStat row_stats(const Row<T>& row, int begin, int end, float c2, RowShared<THREADS>& sh, uint32_t* slots, int shift)
+{
+    constexpr int U = 4, E = Row<T>::E;
     RowStat st;
     st.clear();
-    for (int c = threadIdx.x; c < row.nchunks; c += THREADS) {
-        float v[Row<T>::E];
-        row.load(c, v);
-        st.template add<Row<T>::E>(v, c2);
+    for (int c0 = begin; c0 < end; c0 += U * THREADS) {
+        typename Row<T>::V raw[U];
+#pragma unroll
+        for (int u = 0; u < U; ++u) raw[u] = row.raw(c0 + u * THREADS + (int)threadIdx.x);
+#pragma unroll
+        for (int u = 0; u < U; ++u) {
+            const int c = c0 + u * THREADS + (int)threadIdx.x;
+            if (c0 + u * THREADS < end) {
+                float v[E];
+                row.unpack(c < end ? c : row.nchunks, raw[u], v);
+                float top = v[0];
+#pragma unroll
+                for (int e = 1; e < E; ++e) top = fmaxf(top, v[e]);
+                st.template add<E, ENTROPY>(v, top, c2);
+                if (TOP) {
+                    top = neighbours_max(top, shift);
+                    if (c < end && (c & ((1 << (shift < 4 ? shift : 4)) - 1)) == 0) {
+                        if (shift <= 4) slots[c >> shift] = order_key(top);
+                        else atomicMax(&slots[c >> shift], order_key(top));
+                    }
+                }
+            }
+        }
     }
     for (int d = 32; d > 0; d >>= 1) st.merge(__shfl_xor(st.m, d), __shfl_xor(st.s0, d), __shfl_xor(st.s1, d), c2);
     if (THREADS > 64) {

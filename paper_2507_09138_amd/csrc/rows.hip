@@ -10,85 +10,178 @@
 
 namespace hr {
 
-// ---- best k of a row: keys of (score, entry) in one 64-bit number, larger is better, no two alike
+// ---- best k of a row
+// The entries among the best k lie in slots whose largest score is among the k best of the slots' (k slots hold k entries
+// that are at least as good as the k-th slot's best one).  So the pass over the row only keeps every slot's largest score;
+// a bound is found among those by bisection, the few slots that reach it are read again (from L2), and their entries at or above the
+// bound are ranked.  Keys of (score, entry) are 64-bit numbers, larger is better, no two alike: equal scores go by entry.
 __device__ __forceinline__ uint64_t entry_key(float z, int i) { return (uint64_t)order_key(z) << 32 | (uint32_t)~i; }
-constexpr uint64_t kNoKey = (uint64_t)kNoCandidate << 32 | 0xffffffffu;      // every candidate's is larger
 
 template <int THREADS>
-struct TopBuffer {
-    static constexpr int kCap = 1024;
+struct TopShared {
+    static constexpr int kCap = THREADS >= 256 ? 1024 : 512;      // a chunk has to fit in beside HR_K_MAX kept entries
+    Slots<THREADS> slots;
+    uint16_t picked[Slots<THREADS>::kMax];
     uint64_t key[kCap];
-    int fill, valid;
-    uint64_t bound;                     // key of the k-th best seen so far
+    uint64_t best[HR_K_MAX];
+    uint64_t bound;                     // entries at or below it are not among the best
+    int npicked, fill, valid;
+    int count[2][THREADS / 64];
 };
 
-// The best k of the first `fill` keys go to the front, best first (ranked by counting); returns how many there are.
+// How many lanes of the workgroup say yes, summed over `mine` questions each (mine is a wave's count); one barrier.
 template <int THREADS>
-__device__ int rank_best(TopBuffer<THREADS>& b, int fill, int k)
+__device__ __forceinline__ int group_count(int wave_count, TopShared<THREADS>& t, int turn)
 {
-    uint64_t mine[TopBuffer<THREADS>::kCap / THREADS];
-    int rank[TopBuffer<THREADS>::kCap / THREADS];
+    if (THREADS == 64) return wave_count;
+    if (lane_id() == 0) t.count[turn & 1][threadIdx.x / 64] = wave_count;
     __syncthreads();
-    for (int r = 0; r * THREADS < fill; ++r) {
-        const int i = r * THREADS + threadIdx.x;
-        mine[r] = i < fill ? b.key[i] : 0;
-        rank[r] = i < fill ? 0 : TopBuffer<THREADS>::kCap;
-        for (int j = 0; j < fill; ++j) rank[r] += b.key[j] > mine[r];
-    }
-    __syncthreads();
-    for (int r = 0; r * THREADS < fill; ++r)
-        if (rank[r] < k) b.key[rank[r]] = mine[r];
-    __syncthreads();
-    return fill < k ? fill : k;
+    int n = 0;
+    for (int w = 0; w < THREADS / 64; ++w) n += t.count[turn & 1][w];
+    return n;
 }
 
-// Offers the chunk [c, c + THREADS) of the row, a chunk per thread, to the buffer.
-template <typename T, int THREADS>
-__device__ void offer_chunks(const Row<T>& row, int c, TopBuffer<THREADS>& b, int k)
+// A lower bound, as an order_key, of the k-th largest of the slots, such that few more than k reach it where they differ
+// (bisection between the smallest and the largest, given up as soon as k .. 1.5 k + 8 are left).  Empty slots are never reached.
+template <int THREADS>
+__device__ uint32_t slot_bound(TopShared<THREADS>& t, int nslots, int k, uint32_t largest)
 {
-    float v[Row<T>::E];
-    int first = 0;
-    bool pending = c + (int)threadIdx.x < row.nchunks;
-    if (pending) first = row.load(c + threadIdx.x, v);
-    for (;;) {
-        if (threadIdx.x == 0) b.valid = TopBuffer<THREADS>::kCap;
+    constexpr int PER = Slots<THREADS>::kMax / THREADS;
+    uint32_t mine[PER];
+    uint32_t least = 0xffffffffu;
+#pragma unroll
+    for (int i = 0; i < PER; ++i) {
+        const int s = i * THREADS + threadIdx.x;
+        mine[i] = s < nslots ? t.slots.key[s] : 0;
+        if (mine[i] > kNoCandidate && mine[i] < least) least = mine[i];
+    }
+    int turn = 0;
+    auto reach = [&](uint32_t bound) {
+        int n = 0;
+#pragma unroll
+        for (int i = 0; i < PER; ++i) n += __popcll(__ballot(mine[i] >= bound));
+        return group_count<THREADS>(n, t, turn++);
+    };
+    const int enough = k + k / 2 + 8;
+    least = wave_min(least);
+    if (THREADS > 64) {
+        if (lane_id() == 0) t.count[1][threadIdx.x / 64] = (int)least;
         __syncthreads();
-        int cnt = 0;
-        if (pending)
-            for (int e = 0; e < Row<T>::E; ++e) cnt += entry_key(v[e], first + e) > b.bound;
-        if (pending && cnt == 0) pending = false;
-        if (pending) {
-            int pos = atomicAdd(&b.fill, cnt);
-            if (pos + cnt <= TopBuffer<THREADS>::kCap) {
-                for (int e = 0; e < Row<T>::E; ++e) {
-                    const uint64_t key = entry_key(v[e], first + e);
-                    if (key > b.bound) b.key[pos++] = key;
+        for (int w = 0; w < THREADS / 64; ++w) least = min(least, (uint32_t)t.count[1][w]);
+    }
+    if (least > largest || reach(least) <= enough) return kNoCandidate + 1;
+    uint32_t lo = least, hi = largest;                   // lo is reached by more than enough, hi + 1 by none
+    while (lo < hi) {
+        const uint32_t mid = lo + (hi - lo) / 2 + 1;
+        const int n = reach(mid);
+        if (n < k) hi = mid - 1;
+        else {
+            lo = mid;
+            if (n <= enough) break;
+        }
+    }
+    return lo;
+}
+
+// The best k of the first `fill` keys go to the front, best first; returns how many there are.  16 lanes count how many keys
+// beat one.
+template <int THREADS>
+__device__ int rank_best(TopShared<THREADS>& t, int fill, int k)
+{
+    const int sub = threadIdx.x & 15;
+    __syncthreads();
+    for (int i = threadIdx.x / 16; i < fill; i += THREADS / 16) {
+        const uint64_t mine = t.key[i];
+        int n = 0;
+        for (int j = sub; j < fill; j += 16) n += t.key[j] > mine;
+        n += __builtin_amdgcn_update_dpp(0, n, 0xb1, 0xf, 0xf, false);
+        n += __builtin_amdgcn_update_dpp(0, n, 0x4e, 0xf, 0xf, false);
+        n += __builtin_amdgcn_update_dpp(0, n, 0x141, 0xf, 0xf, false);
+        n += __builtin_amdgcn_update_dpp(0, n, 0x140, 0xf, 0xf, false);
+        if (sub == 0 && n < k) t.best[n] = mine;
+    }
+    __syncthreads();
+    const int found = fill < k ? fill : k;
+    for (int i = threadIdx.x; i < found; i += THREADS) t.key[i] = t.best[i];
+    __syncthreads();
+    return found;
+}
+
+// The best k of a row whose slots are filled: keys in t.key, best first; returns how many there are.
+template <typename T, int THREADS>
+__device__ int best_entries(const Row<T>& row, int shift, int k, uint32_t largest, TopShared<THREADS>& t)
+{
+    constexpr int E = Row<T>::E;
+    const int nslots = (row.nchunks + (1 << shift) - 1) >> shift;
+    __syncthreads();
+    const uint32_t bound = slot_bound<THREADS>(t, nslots, k, largest);
+    if (threadIdx.x == 0) {
+        t.fill = t.npicked = 0;
+        t.bound = ((uint64_t)bound << 32) - 1;
+    }
+    __syncthreads();
+    for (int s = threadIdx.x; s < nslots; s += THREADS)
+        if (t.slots.key[s] >= bound) t.picked[atomicAdd(&t.npicked, 1)] = (uint16_t)s;
+    __syncthreads();
+    const int64_t chunks = (int64_t)t.npicked << shift;
+    for (int64_t c0 = 0; c0 < chunks; c0 += THREADS) {
+        const int64_t i = c0 + threadIdx.x;
+        float v[E];
+        int first = 0;
+        bool pending = i < chunks;
+        if (pending) first = row.load(((int)t.picked[i >> shift] << shift) + (int)(i & ((1 << shift) - 1)), v);
+        // Entries above the bound are appended.  Where the buffer has no room for a chunk's, the best k of what it holds are
+        // kept, the k-th is the new bound, and the chunk is offered again: the buffer has room for one at least.
+        for (;;) {
+            if (threadIdx.x == 0) t.valid = TopShared<THREADS>::kCap;
+            __syncthreads();
+            int cnt = 0;
+            if (pending)
+                for (int e = 0; e < E; ++e) cnt += entry_key(v[e], first + e) > t.bound;
+            pending = pending && cnt > 0;
+            if (pending) {
+                int pos = atomicAdd(&t.fill, cnt);
+                if (pos + cnt <= TopShared<THREADS>::kCap) {
+                    for (int e = 0; e < E; ++e) {
+                        const uint64_t key = entry_key(v[e], first + e);
+                        if (key > t.bound) t.key[pos++] = key;
+                    }
+                    pending = false;
+                } else {
+                    atomicMin(&t.valid, pos);
                 }
-                pending = false;
-            } else {
-                atomicMin(&b.valid, pos);
             }
+            if (!__syncthreads_or(pending)) break;
+            const int kept = rank_best(t, min(t.valid, t.fill), k);
+            if (threadIdx.x == 0) {
+                t.fill = kept;
+                if (kept == k) t.bound = t.key[k - 1];
+            }
+            __syncthreads();
         }
-        // (a chunk that found no room: the best k are kept, the k-th is the new bound, and it is offered again)
-        if (!__syncthreads_or(pending)) return;
-        const int kept = rank_best(b, b.valid < b.fill ? b.valid : b.fill, k);
-        if (threadIdx.x == 0) {
-            b.fill = kept;
-            if (kept == k) b.bound = b.key[k - 1];
-        }
-        __syncthreads();
     }
+    return rank_best(t, t.fill, k);
 }
 
-template <typename T, int THREADS>
+template <typename T, int THREADS, bool TOP>
 __global__ __launch_bounds__(THREADS) void k_logprobs(LogprobsArgs a)
 {
     __shared__ RowShared<THREADS> sh;
-    __shared__ TopBuffer<THREADS> buf;
+    __shared__ std::conditional_t<TOP, TopShared<THREADS>, char> top_;
     const float c2 = a.scale * kLog2e;
     for (int64_t r = blockIdx.x; r < a.rows; r += gridDim.x) {
         const Row<T> row(a.logits, r * a.ld, a.n);
-        const RowStat st = row_stats<T, THREADS>(row, c2, sh);
+        uint32_t* slots = nullptr;
+        int shift = 0;
+        if constexpr (TOP) {
+            slots = top_.slots.key;
+            shift = Slots<THREADS>::shift_for(row.nchunks);
+            if (shift > 4) {
+                for (int i = threadIdx.x; i < Slots<THREADS>::kMax; i += THREADS) slots[i] = 0;
+                __syncthreads();
+            }
+        }
+        const RowStat st = row_stats<T, THREADS, true, TOP>(row, 0, row.nchunks, c2, sh, slots, shift);
         const float logsum = st.log_sum();
         if (threadIdx.x == 0) {
             if (a.norm) { a.norm[2 * r] = st.top(); a.norm[2 * r + 1] = logsum; }
@@ -96,16 +189,13 @@ __global__ __launch_bounds__(THREADS) void k_logprobs(LogprobsArgs a)
         }
         for (int j = threadIdx.x; j < a.ngiven; j += THREADS)
             a.logprobs[r * a.ngiven + j] = st.log_p(row.at(a.given[r * a.ngiven + j]), a.scale, logsum);
-        if (a.k > 0) {
-            if (threadIdx.x == 0) { buf.fill = 0; buf.bound = kNoKey; }
-            __syncthreads();
+        if constexpr (TOP) {
             const bool some = logsum == logsum;
-            for (int c = 0; some && c < row.nchunks; c += THREADS) offer_chunks<T, THREADS>(row, c, buf, a.k);
-            const int found = some ? rank_best(buf, buf.fill, a.k) : 0;
+            const int found = some ? best_entries<T, THREADS>(row, shift, a.k, order_key(st.m), top_) : 0;
             for (int j = threadIdx.x; j < a.k; j += THREADS) {
                 const bool there = j < found;
-                const float z = there ? order_value((uint32_t)(buf.key[j] >> 32)) : -INFINITY;
-                a.top_ids[r * a.k + j] = there ? (int64_t)(uint32_t)~(uint32_t)buf.key[j] : -1;
+                const float z = there ? order_value((uint32_t)(top_.key[j] >> 32)) : -INFINITY;
+                a.top_ids[r * a.k + j] = there ? (int64_t)(uint32_t)~(uint32_t)top_.key[j] : -1;
                 a.top_logprobs[r * a.k + j] = some ? st.log_p(z, a.scale, logsum) : NAN;
             }
             __syncthreads();
@@ -114,8 +204,8 @@ __global__ __launch_bounds__(THREADS) void k_logprobs(LogprobsArgs a)
 }
 
 // ---- gradients:  g_i = p_i (A + B ln p_i) + sum of the list's c_j with id_j = i
-template <typename T, int THREADS>
-__device__ void row_gradient(const Row<T>& row, T* out, float m, float logsum, float scale, float A, float B, bool zero, int count,
+template <typename T, int THREADS, bool ENTROPY>
+__device__ __forceinline__ void row_gradient(const Row<T>& row, int begin, int end, T* out, float m, float logsum, float scale, float A, float B, bool zero, int count,
                              ListShared& list)
 {
     // scores of listed entries are read before anything is written: the gradient may take the place of the scores
@@ -126,14 +216,25 @@ __device__ void row_gradient(const Row<T>& row, T* out, float m, float logsum, f
     // (p is 0 from 2^-158 on) and the product brought back.
     const float c2 = scale * kLog2e, l2 = logsum * kLog2e - 32.0f, b2 = B * kLn2, a2 = A - 32.0f * b2;
     auto grad = [&](float z) {
-        const float x = (z - m) * c2 - l2;
-        return __builtin_amdgcn_exp2f(x) * fmaf(b2, fmaxf(x, kLowest2), a2) * 0x1p-32f;
+        const float x = fmaf(z - m, c2, -l2), p = __builtin_amdgcn_exp2f(x);
+        return ENTROPY ? p * fmaf(b2, fmaxf(x, kLowest2), a2) * 0x1p-32f : p * A * 0x1p-32f;
     };
-    for (int c = threadIdx.x; c < row.nchunks; c += THREADS) {
-        float v[Row<T>::E];
-        const int first = row.load(c, v);
-        for (int e = 0; e < Row<T>::E; ++e) v[e] = zero ? 0.0f : grad(v[e]);
-        store_chunk<T>(out, row.n, first, v);
+    constexpr int U = 4;
+    for (int c0 = begin; c0 < end; c0 += U * THREADS) {
+        typename Row<T>::V raw[U];
+#pragma unroll
+        for (int u = 0; u < U; ++u) raw[u] = row.raw(c0 + u * THREADS + (int)threadIdx.x);
+#pragma unroll
+        for (int u = 0; u < U; ++u) {
+            const int c = c0 + u * THREADS + (int)threadIdx.x;
+            if (c < end) {
+                float v[Row<T>::E];
+                row.unpack(c, raw[u], v);
+#pragma unroll
+                for (int e = 0; e < Row<T>::E; ++e) v[e] = zero ? 0.0f : grad(v[e]);
+                store_chunk<T>(out, row.n, row.first(c), v);
+            }
+        }
     }
     if (zero) return;
     __syncthreads();
@@ -169,7 +270,7 @@ __global__ __launch_bounds__(THREADS) void k_logprobs_backward(LogprobsBackwardA
         const float gh = a.grad_entropy ? a.grad_entropy[r] : 0.0f;
         const float A = -a.scale * (sum + (gh != 0.0f ? gh * a.entropy[r] : 0.0f));
         const float m = a.norm[2 * r];
-        row_gradient<T, THREADS>(row, (T*)a.grad + r * a.ldg, m, a.norm[2 * r + 1], a.scale, A, -a.scale * gh, m == -INFINITY, a.ngiven, list);
+        row_gradient<T, THREADS, true>(row, 0, row.nchunks, (T*)a.grad + r * a.ldg, m, a.norm[2 * r + 1], a.scale, A, -a.scale * gh, m == -INFINITY, a.ngiven, list);
     }
 }
 
@@ -217,7 +318,7 @@ __global__ __launch_bounds__(THREADS) void k_distill(DistillArgs a)
     __shared__ ListShared list;
     for (int64_t r = blockIdx.x; r < a.rows; r += gridDim.x) {
         const Row<T> row(a.logits, r * a.ld, a.n);
-        const RowStat st = row_stats<T, THREADS>(row, a.scale * kLog2e, sh);
+        const RowStat st = row_stats<T, THREADS, false, false>(row, 0, row.nchunks, a.scale * kLog2e, sh, nullptr, 0);
         const float logsum = st.log_sum();
         bool some;
         const float loss = teacher_list<T, THREADS>(row, a.ids + r * a.k, a.teacher + r * a.k, a.k, a.scale, st, logsum, list, sh, some);
@@ -229,7 +330,7 @@ __global__ __launch_bounds__(THREADS) void k_distill(DistillArgs a)
         if (STEP) {
             const float w = (a.weights ? a.weights[r] : 1.0f) * a.scale;
             for (int j = threadIdx.x; j < a.k; j += THREADS) list.c[j] *= -w;
-            row_gradient<T, THREADS>(row, (T*)a.grad + r * a.ldg, st.top(), logsum, a.scale, w, 0.0f, !some || w == 0.0f, a.k, list);
+            row_gradient<T, THREADS, false>(row, 0, row.nchunks, (T*)a.grad + r * a.ldg, st.top(), logsum, a.scale, w, 0.0f, !some || w == 0.0f, a.k, list);
         }
     }
 }
@@ -252,27 +353,65 @@ __global__ __launch_bounds__(THREADS) void k_distill_backward(DistillArgs a)
             some |= counts;
         }
         some = __syncthreads_or(some);
-        row_gradient<T, THREADS>(row, (T*)a.grad + r * a.ldg, a.norm[2 * r], a.norm[2 * r + 1], a.scale, w, 0.0f, !some || w == 0.0f, a.k, list);
+        row_gradient<T, THREADS, false>(row, 0, row.nchunks, (T*)a.grad + r * a.ldg, a.norm[2 * r], a.norm[2 * r + 1], a.scale, w, 0.0f, !some || w == 0.0f, a.k, list);
     }
 }
 
 // ---- launches
-constexpr int kRowThreads = 256;
 static unsigned row_grid(int64_t rows) { return (unsigned)(rows < (1 << 20) ? rows : 1 << 20); }      // (a launch may not have 2^32 threads)
 
-#define HR_ROWS_LAUNCH(kernel, dtype, ...)                                                                                        \
-    switch (dtype) {                                                                                                              \
-    case HR_F32: hipLaunchKernelGGL((kernel<float, kRowThreads __VA_ARGS__>), dim3(row_grid(a.rows)), dim3(kRowThreads), 0, s, a); break;   \
-    case HR_F16: hipLaunchKernelGGL((kernel<_Float16, kRowThreads __VA_ARGS__>), dim3(row_grid(a.rows)), dim3(kRowThreads), 0, s, a); break; \
-    default: hipLaunchKernelGGL((kernel<__bf16, kRowThreads __VA_ARGS__>), dim3(row_grid(a.rows)), dim3(kRowThreads), 0, s, a); break;      \
-    }                                                                                                                             \
-    return hipGetLastError()
+// Threads of the workgroup that takes a row: four chunks of it or more for each.
+static int row_threads(int dtype, int64_t n)
+{
+    const int64_t chunks = n * (int64_t)element_bytes(dtype) / 16;
+    return chunks <= 256 ? 64 : (chunks <= 2048 ? 256 : 1024);
+}
 
-static hipError_t launch_logprobs(int dtype, const LogprobsArgs& a, hipStream_t s) { HR_ROWS_LAUNCH(k_logprobs, dtype); }
-static hipError_t launch_logprobs_backward(int dtype, const LogprobsBackwardArgs& a, hipStream_t s) { HR_ROWS_LAUNCH(k_logprobs_backward, dtype); }
-static hipError_t launch_distill(int dtype, const DistillArgs& a, hipStream_t s) { HR_ROWS_LAUNCH(k_distill, dtype, , false); }
-static hipError_t launch_distill_step(int dtype, const DistillArgs& a, hipStream_t s) { HR_ROWS_LAUNCH(k_distill, dtype, , true); }
-static hipError_t launch_distill_backward(int dtype, const DistillArgs& a, hipStream_t s) { HR_ROWS_LAUNCH(k_distill_backward, dtype); }
+// f(element, threads) with the type and the number as compile-time values
+template <typename F>
+static void with_row_type(int dtype, int threads, F&& f)
+{
+    auto type = [&](auto e) {
+        using std::integral_constant;
+        if (threads == 64) f(e, integral_constant<int, 64>{});
+        else if (threads == 256) f(e, integral_constant<int, 256>{});
+        else f(e, integral_constant<int, 1024>{});
+    };
+    if (dtype == HR_F32) type(float{});
+    else if (dtype == HR_F16) type(_Float16{});
+    else type(__bf16{});
+}
+
+#define HR_ROWS_LAUNCH(kernel) hipLaunchKernelGGL(kernel, dim3(row_grid(a.rows)), dim3(decltype(threads)::value), 0, s, a)
+
+static hipError_t launch_logprobs(int dtype, const LogprobsArgs& a, hipStream_t s)
+{
+    with_row_type(dtype, row_threads(dtype, a.n), [&](auto e, auto threads) {
+        if (a.k > 0) HR_ROWS_LAUNCH((k_logprobs<decltype(e), decltype(threads)::value, true>));
+        else HR_ROWS_LAUNCH((k_logprobs<decltype(e), decltype(threads)::value, false>));
+    });
+    return hipGetLastError();
+}
+static hipError_t launch_logprobs_backward(int dtype, const LogprobsBackwardArgs& a, hipStream_t s)
+{
+    with_row_type(dtype, row_threads(dtype, a.n), [&](auto e, auto threads) { HR_ROWS_LAUNCH((k_logprobs_backward<decltype(e), decltype(threads)::value>)); });
+    return hipGetLastError();
+}
+static hipError_t launch_distill(int dtype, const DistillArgs& a, hipStream_t s)
+{
+    with_row_type(dtype, row_threads(dtype, a.n), [&](auto e, auto threads) { HR_ROWS_LAUNCH((k_distill<decltype(e), decltype(threads)::value, false>)); });
+    return hipGetLastError();
+}
+static hipError_t launch_distill_step(int dtype, const DistillArgs& a, hipStream_t s)
+{
+    with_row_type(dtype, row_threads(dtype, a.n), [&](auto e, auto threads) { HR_ROWS_LAUNCH((k_distill<decltype(e), decltype(threads)::value, true>)); });
+    return hipGetLastError();
+}
+static hipError_t launch_distill_backward(int dtype, const DistillArgs& a, hipStream_t s)
+{
+    with_row_type(dtype, row_threads(dtype, a.n), [&](auto e, auto threads) { HR_ROWS_LAUNCH((k_distill_backward<decltype(e), decltype(threads)::value>)); });
+    return hipGetLastError();
+}
 
 }  // namespace hr
 
