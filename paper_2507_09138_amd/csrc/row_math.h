@@ -27,14 +27,15 @@ __device__ __forceinline__ float order_value(uint32_t key)
 }
 
 // A row of n scores.  Chunks are the 16-byte pieces of memory it lies in, so that every load is aligned wherever the row
-// starts; the first and the last may hold fewer of its entries.
+// starts.  Chunks lo .. hi-1 are the row's throughout; what it has of the chunk before and of the one behind (fewer than E
+// entries each, the edges) is taken entry by entry.
 template <typename T>
 struct Row {
     static constexpr int E = 16 / sizeof(T);
     using V = T __attribute__((ext_vector_type(E)));
     const T* z;
     int n, before, nchunks;             // before: places of chunk 0 in front of the row
-    int lo, hi;                         // chunks lo .. hi-1 are the row's throughout
+    int lo, hi;
 
     __device__ __forceinline__ Row(const void* base, int64_t offset, int n_) : z((const T*)base + offset), n(n_)
     {
@@ -43,54 +44,79 @@ struct Row {
         lo = before > 0;
         hi = (int)(((int64_t)before + n) / E);
     }
+    __device__ __forceinline__ bool edges() const { return lo > 0 || hi < nchunks; }
     __device__ __forceinline__ int first(int c) const { return c * E - before; }      // entry of a chunk's first place
-    // A chunk as it lies in memory; what lies at the edges or behind the row is some other chunk of it, to be replaced by fix().
-    // (A row that is no whole chunk has nothing that could be loaded: 0.)
+    // chunk c, or where it is not the row's throughout the nearest one that is (there has to be one)
     __device__ __forceinline__ V raw(int c) const
     {
-        if (hi <= lo) return V{};
-        c = c < lo ? lo : (c < hi ? c : hi - 1);
-        return *(const V*)(z + first(c));
+        c = min(max(c, lo), hi - 1);
+        return *(const V*)((const char*)z - before * (int)sizeof(T) + (uint32_t)c * 16u);
     }
-    // The same where the chunk is the row's in part or not at all: -inf in the places that are not.
-    __device__ __forceinline__ void fix(int c, float* v) const
+    // entry of the edges that thread t < 2 E looks after, or -1
+    __device__ __forceinline__ int edge(int t) const
     {
-        if (c >= lo && c < hi) return;
-#pragma unroll
-        for (int e = 0; e < E; ++e) {
-            const int i = first(c) + e;
-            v[e] = c < nchunks && i >= 0 && i < n ? (float)z[i] : -INFINITY;
-        }
+        const int i = t < E ? (lo > 0 ? t : n) : (hi < nchunks && hi >= lo ? first(hi) + t - E : n);
+        return t < 2 * E && i < n && (t >= E || i < E - before) ? i : -1;
     }
-    __device__ __forceinline__ void unpack(int c, V t, float* v) const
-    {
-#pragma unroll
-        for (int e = 0; e < E; ++e) v[e] = (float)t[e];
-        fix(c, v);
-    }
+    // a chunk's scores, whichever it is: -inf in the places that are not the row's
     __device__ __forceinline__ int load(int c, float* v) const
     {
-        unpack(c, raw(c), v);
+        if (c >= lo && c < hi) {
+            const V t = raw(c);
+#pragma unroll
+            for (int e = 0; e < E; ++e) v[e] = (float)t[e];
+        } else {
+#pragma unroll
+            for (int e = 0; e < E; ++e) v[e] = (float)at(first(c) + e);
+        }
         return first(c);
     }
     __device__ __forceinline__ float at(int64_t i) const { return i >= 0 && i < n ? (float)z[i] : -INFINITY; }
 };
 
-// A chunk that Row::load read, to a row of the output; vector stores where that row is aligned as well.
-template <typename T>
-__device__ __forceinline__ void store_chunk(T* out, int n, int first, const float* v)
+// f(raw chunk, c, in) for the chunks of begin .. end-1 (begin a multiple of 16) that are the row's throughout, U at a time for
+// every thread, all threads alike: in is false for a thread that has none.  The next U chunks are asked for before the last ones
+// are worked on; what is asked for behind the row's end is its last chunk, again.
+// first() is called once, behind the first request.
+template <int U, int THREADS, typename T, typename F, typename G>
+__device__ __forceinline__ void for_chunks(const Row<T>& row, int begin, int end, F&& f, G&& first)
 {
-    constexpr int E = 16 / sizeof(T);
-    if (first >= 0 && first + E <= n && ((uintptr_t)(out + first) & 15) == 0) {
-        vec_of<T> t;
-#pragma unroll
-        for (int e = 0; e < E; ++e) t[e] = (T)v[e];
-        *(vec_of<T>*)(out + first) = t;
-    } else {
-#pragma unroll
-        for (int e = 0; e < E; ++e)
-            if (first + e >= 0 && first + e < n) out[first + e] = (T)v[e];
+    const int stop = min(end, row.hi);
+    if (stop <= max(begin, row.lo)) {
+        first();
+        return;
     }
+    typename Row<T>::V a[U], b[U];
+    auto load = [&](typename Row<T>::V* r, int c0) __attribute__((always_inline)) {
+#pragma unroll
+        for (int u = 0; u < U; ++u) r[u] = row.raw(c0 + u * THREADS + (int)threadIdx.x);
+    };
+    auto work = [&](typename Row<T>::V* r, int c0) __attribute__((always_inline)) {
+#pragma unroll
+        for (int u = 0; u < U; ++u) {
+            const int c = c0 + u * THREADS + (int)threadIdx.x;
+            if (c0 + u * THREADS < stop) f(r[u], c, c >= row.lo && c < stop);
+        }
+    };
+    load(a, begin);
+    first();
+    for (int c0 = begin; c0 < stop; c0 += 2 * U * THREADS) {
+        load(b, c0 + U * THREADS);
+        work(a, c0);
+        load(a, c0 + 2 * U * THREADS);
+        work(b, c0 + U * THREADS);
+    }
+}
+
+// Chunk c of the row in the output, which may be aligned otherwise.
+template <typename T>
+__device__ __forceinline__ void store_chunk(T* out, const float* v)
+{
+    vec_of<T> t;
+#pragma unroll
+    for (int e = 0; e < 16 / (int)sizeof(T); ++e) t[e] = (T)v[e];
+    if (((uintptr_t)out & 15) == 0) __builtin_nontemporal_store(t, (vec_of<T>*)out);
+    else __builtin_memcpy(out, &t, 16);
 }
 
 template <int THREADS>
@@ -103,25 +129,37 @@ struct ListShared {
     float c[HR_LIST_MAX], z[HR_LIST_MAX];
 };
 
-// Sum / largest over a workgroup, to all threads, in the same order every time.
-template <int THREADS, typename F>
-__device__ __forceinline__ float group_fold(float v, RowShared<THREADS>& sh, F f)
+// Folds over the lanes of a wave and over a workgroup, to all of them, in the same order every time.
+__device__ __forceinline__ float bits_float(uint32_t v) { return __builtin_bit_cast(float, v); }
+__device__ __forceinline__ float lanes_max(float v)          // (a NaN is left out)
 {
-    for (int d = 32; d > 0; d >>= 1) v = f(v, __shfl_xor(v, d));
-    if (THREADS > 64) {
-        __syncthreads();
-        if (lane_id() == 0) sh.part[0][threadIdx.x / 64] = v;
-        __syncthreads();
-        v = sh.part[0][0];
-        for (int w = 1; w < THREADS / 64; ++w) v = f(v, sh.part[0][w]);
-    }
-    return v;
+    return bits_float(wave_fold(__builtin_bit_cast(uint32_t, v), [](uint32_t x, uint32_t y) { return __builtin_bit_cast(uint32_t, fmaxf(bits_float(x), bits_float(y))); }));
+}
+__device__ __forceinline__ float lanes_sum(float v)
+{
+    return bits_float((uint32_t)__builtin_amdgcn_readlane(__builtin_bit_cast(int, wave_add(v)), 63));
+}
+// one number of every wave, a lane each; rest elsewhere
+template <int THREADS>
+__device__ __forceinline__ float of_waves(float* part, float v, float rest)
+{
+    __syncthreads();
+    if (lane_id() == 0) part[threadIdx.x / 64] = v;
+    __syncthreads();
+    return lane_id() < THREADS / 64 ? part[lane_id()] : rest;
 }
 template <int THREADS>
-__device__ __forceinline__ float group_sum(float v, RowShared<THREADS>& sh) { return group_fold<THREADS>(v, sh, [](float x, float y) { return x + y; }); }
-// (a NaN stays: what is compared with it is not larger)
+__device__ __forceinline__ float group_sum(float v, RowShared<THREADS>& sh)
+{
+    v = lanes_sum(v);
+    return THREADS == 64 ? v : lanes_sum(of_waves<THREADS>(sh.part[0], v, 0.0f));
+}
 template <int THREADS>
-__device__ __forceinline__ float group_max(float v, RowShared<THREADS>& sh) { return group_fold<THREADS>(v, sh, [](float x, float y) { return fmaxf(x, y); }); }
+__device__ __forceinline__ float group_max(float v, RowShared<THREADS>& sh)
+{
+    v = lanes_max(v);
+    return THREADS == 64 ? v : lanes_max(of_waves<THREADS>(sh.part[0], v, -INFINITY));
+}
 
 // Maximum and sums of scores.  An empty one has the lowest finite number as its maximum, so that differences from it are
 // -inf or finite, never NaN, except where a score is NaN or +inf: then S0 becomes NaN and stays it.
@@ -148,14 +186,25 @@ struct RowStat {
             if (ENTROPY) s1 = fmaf(fmaxf(x, kLowest2), t, s1);
         }
     }
-    __device__ __forceinline__ void merge(float m2, float a, float b, float c2)
+    // of all lanes of a wave together: what every lane has is brought to the largest maximum, then added up
+    __device__ __forceinline__ void fold_lanes(float c2)
     {
-        RowStat o{m2, a, b};
-        const float top = fmaxf(m, m2);
-        if (m < top) rescale(top, c2);
-        if (m2 < top) o.rescale(top, c2);
-        s0 += o.s0;
-        s1 += o.s1;
+        rescale(lanes_max(m), c2);
+        s0 = lanes_sum(s0);
+        s1 = lanes_sum(s1);
+    }
+    template <int THREADS>
+    __device__ __forceinline__ void fold(float c2, RowShared<THREADS>& sh)
+    {
+        fold_lanes(c2);
+        if (THREADS == 64) return;
+        __syncthreads();
+        const int w = threadIdx.x / 64, i = lane_id();
+        if (i == 0) { sh.part[0][w] = m; sh.part[1][w] = s0; sh.part[2][w] = s1; }
+        __syncthreads();
+        clear();
+        if (i < THREADS / 64) { m = sh.part[0][i]; s0 = sh.part[1][i]; s1 = sh.part[2][i]; }
+        fold_lanes(c2);
     }
     __device__ __forceinline__ float top() const { return s0 == 0.0f ? -INFINITY : m; }
     __device__ __forceinline__ float log_sum() const { return s0 == 0.0f ? 0.0f : logf(s0); }
@@ -200,48 +249,42 @@ __device__ __forceinline__ float neighbours_max(float v, int shift)
     return v;
 }
 
-// Maximum and sums of chunks begin .. end-1 of a row (begin a multiple of 16), to all threads of a workgroup.  A thread asks for
-// four chunks at a time; with several waves per SIMD that is enough under way.  TOP: the slots' largest scores as well
-// (slots of the row's chunk 0 on; they have to be cleared before if shift > 4).
-template <typename T, int THREADS, bool ENTROPY, bool TOP>
-__device__ __forceinline__ RowStat row_stats(const Row<T>& row, int begin, int end, float c2, RowShared<THREADS>& sh, uint32_t* slots, int shift)
+// Maximum and sums of chunks begin .. end-1 of a row (begin a multiple of 16; the edges if begin is 0), to all threads of a workgroup.
+// TOP: the slots' largest scores as well; the slots have to be cleared before.
+// first() is called once while the first chunks are on their way.
+template <typename T, int THREADS, bool ENTROPY, bool TOP, typename G>
+__device__ __forceinline__ RowStat row_stats(const Row<T>& row, int begin, int end, float c2, RowShared<THREADS>& sh, uint32_t* slots, int shift, G&& first)
 {
-    constexpr int U = 4, E = Row<T>::E;
+    constexpr int E = Row<T>::E;
     RowStat st;
     st.clear();
-    for (int c0 = begin; c0 < end; c0 += U * THREADS) {
-        typename Row<T>::V raw[U];
+    for_chunks<4, THREADS>(row, begin, end, [&](const typename Row<T>::V& raw, int c, bool in) __attribute__((always_inline)) {
+        float v[E];
 #pragma unroll
-        for (int u = 0; u < U; ++u) raw[u] = row.raw(c0 + u * THREADS + (int)threadIdx.x);
+        for (int e = 0; e < E; ++e) v[e] = (float)raw[e];
+        float top = v[0];
 #pragma unroll
-        for (int u = 0; u < U; ++u) {
-            const int c = c0 + u * THREADS + (int)threadIdx.x;
-            if (c0 + u * THREADS < end) {
-                float v[E];
-                row.unpack(c < end ? c : row.nchunks, raw[u], v);
-                float top = v[0];
-#pragma unroll
-                for (int e = 1; e < E; ++e) top = fmaxf(top, v[e]);
-                st.template add<E, ENTROPY>(v, top, c2);
-                if (TOP) {
-                    top = neighbours_max(top, shift);
-                    if (c < end && (c & ((1 << (shift < 4 ? shift : 4)) - 1)) == 0) {
-                        if (shift <= 4) slots[c >> shift] = order_key(top);
-                        else atomicMax(&slots[c >> shift], order_key(top));
-                    }
-                }
+        for (int e = 1; e < E; ++e) top = fmaxf(top, v[e]);
+        if (in) st.template add<E, ENTROPY>(v, top, c2);
+        if (TOP) {
+            top = neighbours_max(in ? top : -INFINITY, shift);
+            const int group = (1 << min(shift, 4)) - 1;
+            if ((c & group) == 0) {
+                if (shift <= 4) slots[c >> shift] = order_key(top);
+                else atomicMax(&slots[c >> shift], order_key(top));
             }
         }
+    }, first);
+    if (begin == 0 && row.edges()) {
+        const int i = row.edge(threadIdx.x);
+        if (TOP) __syncthreads();
+        if (i >= 0) {
+            const float v = (float)row.z[i];
+            st.template add<1, ENTROPY>(&v, v, c2);
+            if (TOP) atomicMax(&slots[(i + row.before) / E >> shift], order_key(v));
+        }
     }
-    for (int d = 32; d > 0; d >>= 1) st.merge(__shfl_xor(st.m, d), __shfl_xor(st.s0, d), __shfl_xor(st.s1, d), c2);
-    if (THREADS > 64) {
-        const int w = threadIdx.x / 64;
-        __syncthreads();
-        if (lane_id() == 0) { sh.part[0][w] = st.m; sh.part[1][w] = st.s0; sh.part[2][w] = st.s1; }
-        __syncthreads();
-        st = RowStat{sh.part[0][0], sh.part[1][0], sh.part[2][0]};
-        for (int i = 1; i < THREADS / 64; ++i) st.merge(sh.part[0][i], sh.part[1][i], sh.part[2][i], c2);
-    }
+    st.fold<THREADS>(c2, sh);
     return st;
 }
 

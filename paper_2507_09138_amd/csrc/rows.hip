@@ -5,10 +5,14 @@
 //   ln p_i = s (z_i - m) - ln S0,      entropy = ln S0 - S1 / S0  (two terms that are not negative: nothing cancels).
 // Every thread keeps m, S0, S1 of the chunks it has seen (float32; a larger maximum rescales the sums) and the threads' are
 // merged in a fixed order at the end.  Exponents are counted in base 2: one multiplication by s / ln 2 serves scale and base.
+#include <stdlib.h>
 #include "entry.h"
 #include "row_math.h"
 
 namespace hr {
+
+// entries of a row's list that a thread looks after
+template <int THREADS> constexpr int kListPer = (HR_LIST_MAX + THREADS - 1) / THREADS;
 
 // ---- best k of a row
 // The entries among the best k lie in slots whose largest score is among the k best of the slots' (k slots hold k entries
@@ -26,23 +30,11 @@ struct TopShared {
     uint64_t best[HR_K_MAX];
     uint64_t bound;                     // entries at or below it are not among the best
     int npicked, fill, valid;
-    int count[2][THREADS / 64];
+    uint64_t count[2][THREADS / 64];
 };
 
-// How many lanes of the workgroup say yes, summed over `mine` questions each (mine is a wave's count); one barrier.
-template <int THREADS>
-__device__ __forceinline__ int group_count(int wave_count, TopShared<THREADS>& t, int turn)
-{
-    if (THREADS == 64) return wave_count;
-    if (lane_id() == 0) t.count[turn & 1][threadIdx.x / 64] = wave_count;
-    __syncthreads();
-    int n = 0;
-    for (int w = 0; w < THREADS / 64; ++w) n += t.count[turn & 1][w];
-    return n;
-}
-
 // A lower bound, as an order_key, of the k-th largest of the slots, such that few more than k reach it where they differ
-// (bisection between the smallest and the largest, given up as soon as k .. 1.5 k + 8 are left).  Empty slots are never reached.
+// (the range between the smallest and the largest is cut until k .. 1.5 k + 8 are left).  Empty slots are never reached.
 template <int THREADS>
 __device__ uint32_t slot_bound(TopShared<THREADS>& t, int nslots, int k, uint32_t largest)
 {
@@ -55,30 +47,43 @@ __device__ uint32_t slot_bound(TopShared<THREADS>& t, int nslots, int k, uint32_
         mine[i] = s < nslots ? t.slots.key[s] : 0;
         if (mine[i] > kNoCandidate && mine[i] < least) least = mine[i];
     }
-    int turn = 0;
-    auto reach = [&](uint32_t bound) {
-        int n = 0;
-#pragma unroll
-        for (int i = 0; i < PER; ++i) n += __popcll(__ballot(mine[i] >= bound));
-        return group_count<THREADS>(n, t, turn++);
-    };
     const int enough = k + k / 2 + 8;
     least = wave_min(least);
     if (THREADS > 64) {
-        if (lane_id() == 0) t.count[1][threadIdx.x / 64] = (int)least;
+        if (lane_id() == 0) t.count[1][threadIdx.x / 64] = least;
         __syncthreads();
         for (int w = 0; w < THREADS / 64; ++w) least = min(least, (uint32_t)t.count[1][w]);
     }
-    if (least > largest || reach(least) <= enough) return kNoCandidate + 1;
-    uint32_t lo = least, hi = largest;                   // lo is reached by more than enough, hi + 1 by none
-    while (lo < hi) {
-        const uint32_t mid = lo + (hi - lo) / 2 + 1;
-        const int n = reach(mid);
-        if (n < k) hi = mid - 1;
-        else {
-            lo = mid;
-            if (n <= enough) break;
+    // lo is reached by k or more, hi + 1 by fewer
+    uint32_t lo = kNoCandidate + 1, hi = largest;
+    if (least > largest) return lo;
+    for (int turn = 0; lo < hi; ++turn) {
+        // three bounds at once split what is left in four; the first time the smallest slot is the lowest of them
+        const uint32_t part = (hi - lo) / 4, b1 = turn ? lo + part + 1 : least, b2 = turn ? lo + 2 * part + 1 : least + (hi - least) / 3,
+                       b3 = turn ? lo + 3 * part + 1 : least + (hi - least) / 3 * 2;
+        int n1 = 0, n2 = 0, n3 = 0;
+#pragma unroll
+        for (int i = 0; i < PER; ++i) {
+            n1 += __popcll(__ballot(mine[i] >= b1));
+            n2 += __popcll(__ballot(mine[i] >= b2));
+            n3 += __popcll(__ballot(mine[i] >= b3));
         }
+        uint64_t n = (uint64_t)n3 << 32 | (uint32_t)n2 << 16 | (uint32_t)n1;
+        if (THREADS > 64) {
+            if (lane_id() == 0) t.count[turn & 1][threadIdx.x / 64] = n;
+            __syncthreads();
+            n = 0;
+            for (int w = 0; w < THREADS / 64; ++w) n += t.count[turn & 1][w];
+        }
+        n1 = (int)(n & 0xffff);
+        n2 = (int)(n >> 16 & 0xffff);
+        n3 = (int)(n >> 32);
+        int reached;
+        if (n3 >= k) { lo = b3; reached = n3; }
+        else if (n2 >= k) { lo = b2; hi = b3 - 1; reached = n2; }
+        else if (n1 >= k) { lo = b1; hi = b2 - 1; reached = n1; }
+        else { hi = b1 - 1; reached = Slots<THREADS>::kMax; if (turn == 0) return lo; }
+        if (reached <= enough) break;
     }
     return lo;
 }
@@ -176,19 +181,27 @@ __global__ __launch_bounds__(THREADS) void k_logprobs(LogprobsArgs a)
         if constexpr (TOP) {
             slots = top_.slots.key;
             shift = Slots<THREADS>::shift_for(row.nchunks);
-            if (shift > 4) {
-                for (int i = threadIdx.x; i < Slots<THREADS>::kMax; i += THREADS) slots[i] = 0;
-                __syncthreads();
-            }
+            for (int i = threadIdx.x; i < Slots<THREADS>::kMax; i += THREADS) slots[i] = 0;
+            __syncthreads();
         }
-        const RowStat st = row_stats<T, THREADS, true, TOP>(row, 0, row.nchunks, c2, sh, slots, shift);
+        float z[kListPer<THREADS>];
+        const RowStat st = row_stats<T, THREADS, true, TOP>(row, 0, row.nchunks, c2, sh, slots, shift, [&] {
+#pragma unroll
+            for (int i = 0; i < kListPer<THREADS>; ++i) {
+                const int j = i * THREADS + threadIdx.x;
+                if (i * THREADS < a.ngiven) z[i] = j < a.ngiven ? row.at(a.given[r * a.ngiven + j]) : 0.0f;
+            }
+        });
         const float logsum = st.log_sum();
         if (threadIdx.x == 0) {
             if (a.norm) { a.norm[2 * r] = st.top(); a.norm[2 * r + 1] = logsum; }
             if (a.entropy) a.entropy[r] = st.entropy(logsum);
         }
-        for (int j = threadIdx.x; j < a.ngiven; j += THREADS)
-            a.logprobs[r * a.ngiven + j] = st.log_p(row.at(a.given[r * a.ngiven + j]), a.scale, logsum);
+#pragma unroll
+        for (int i = 0; i < kListPer<THREADS>; ++i) {
+            const int j = i * THREADS + threadIdx.x;
+            if (j < a.ngiven) a.logprobs[r * a.ngiven + j] = st.log_p(z[i], a.scale, logsum);
+        }
         if constexpr (TOP) {
             const bool some = logsum == logsum;
             const int found = some ? best_entries<T, THREADS>(row, shift, a.k, order_key(st.m), top_) : 0;
@@ -204,13 +217,11 @@ __global__ __launch_bounds__(THREADS) void k_logprobs(LogprobsArgs a)
 }
 
 // ---- gradients:  g_i = p_i (A + B ln p_i) + sum of the list's c_j with id_j = i
+// list.id, list.c, list.z: entries (-1: none), coefficients and scores, read before this: the gradient may take the place of the scores.
 template <typename T, int THREADS, bool ENTROPY>
 __device__ __forceinline__ void row_gradient(const Row<T>& row, int begin, int end, T* out, float m, float logsum, float scale, float A, float B, bool zero, int count,
                              ListShared& list)
 {
-    // scores of listed entries are read before anything is written: the gradient may take the place of the scores
-    __syncthreads();
-    for (int j = threadIdx.x; j < count; j += THREADS) list.z[j] = list.id[j] >= 0 ? row.at(list.id[j]) : -INFINITY;
     __syncthreads();
     // The exponential instruction gives 0 below 2^-126, but p times ln p and the coefficients may be above that: it is taken of x + 32
     // (p is 0 from 2^-158 on) and the product brought back.
@@ -219,22 +230,16 @@ __device__ __forceinline__ void row_gradient(const Row<T>& row, int begin, int e
         const float x = fmaf(z - m, c2, -l2), p = __builtin_amdgcn_exp2f(x);
         return ENTROPY ? p * fmaf(b2, fmaxf(x, kLowest2), a2) * 0x1p-32f : p * A * 0x1p-32f;
     };
-    constexpr int U = 4;
-    for (int c0 = begin; c0 < end; c0 += U * THREADS) {
-        typename Row<T>::V raw[U];
+    constexpr int E = Row<T>::E;
+    for_chunks<4, THREADS>(row, begin, end, [&](const typename Row<T>::V& raw, int c, bool in) __attribute__((always_inline)) {
+        float v[E];
 #pragma unroll
-        for (int u = 0; u < U; ++u) raw[u] = row.raw(c0 + u * THREADS + (int)threadIdx.x);
-#pragma unroll
-        for (int u = 0; u < U; ++u) {
-            const int c = c0 + u * THREADS + (int)threadIdx.x;
-            if (c < end) {
-                float v[Row<T>::E];
-                row.unpack(c, raw[u], v);
-#pragma unroll
-                for (int e = 0; e < Row<T>::E; ++e) v[e] = zero ? 0.0f : grad(v[e]);
-                store_chunk<T>(out, row.n, row.first(c), v);
-            }
-        }
+        for (int e = 0; e < E; ++e) v[e] = zero ? 0.0f : grad((float)raw[e]);
+        if (in) store_chunk<T>(out + row.first(c), v);
+    }, [] {});
+    if (begin == 0 && row.edges()) {
+        const int i = row.edge(threadIdx.x);
+        if (i >= 0) out[i] = (T)(zero ? 0.0f : grad((float)row.z[i]));
     }
     if (zero) return;
     __syncthreads();
@@ -260,10 +265,12 @@ __global__ __launch_bounds__(THREADS) void k_logprobs_backward(LogprobsBackwardA
         float sum = 0.0f;
         for (int j = threadIdx.x; j < a.ngiven; j += THREADS) {
             const int64_t id = a.given[r * a.ngiven + j];
-            const bool there = row.at(id) != -INFINITY;
+            const float z = row.at(id);
+            const bool there = z != -INFINITY;
             const float g = there ? a.grad_logprobs[r * a.ngiven + j] : 0.0f;
             list.id[j] = there ? (int)id : -1;
             list.c[j] = g * a.scale;
+            list.z[j] = z;
             sum += g;
         }
         sum = group_sum<THREADS>(sum, sh);
@@ -275,41 +282,60 @@ __global__ __launch_bounds__(THREADS) void k_logprobs_backward(LogprobsBackwardA
 }
 
 // ---- a teacher's list
-// q of the entries that count into list.c (0 for the others), their ids into list.id (-1 for the others); returns the loss
+// What a thread holds of it: read() while the row's first chunks are on their way, finish() with the row's sums.
 template <typename T, int THREADS>
-__device__ float teacher_list(const Row<T>& row, const int64_t* ids, const float* teacher, int k, float scale, const RowStat& st, float logsum,
-                              ListShared& list, RowShared<THREADS>& sh, bool& some)
-{
-    __syncthreads();
-    float top = -FLT_MAX;
-    int n = 0;
-    for (int j = threadIdx.x; j < k; j += THREADS) {
-        const float z = row.at(ids[j]), t = teacher[j];
-        const bool counts = z != -INFINITY && t != -INFINITY;
-        list.id[j] = counts ? (int)ids[j] : -1;
-        list.z[j] = z;
-        if (counts) { top = fmaxf(top, t); n = 1; }
+struct Teacher {
+    static constexpr int PER = kListPer<THREADS>;
+    int id[PER];                        // -1: does not count
+    float t[PER], z[PER];
+
+    __device__ __forceinline__ void read(const Row<T>& row, const int64_t* ids, const float* teacher, int k)
+    {
+#pragma unroll
+        for (int i = 0; i < PER; ++i) {
+            const int j = i * THREADS + threadIdx.x;
+            id[i] = -1;
+            t[i] = z[i] = -INFINITY;
+            if (i * THREADS < k && j < k) {
+                const int64_t at = ids[j];
+                t[i] = teacher[j];
+                z[i] = row.at(at);
+                id[i] = (int)at;
+            }
+        }
     }
-    top = group_max<THREADS>(top, sh);
-    some = __syncthreads_or(n);
-    float sum = 0.0f;
-    for (int j = threadIdx.x; j < k; j += THREADS) {
-        const float e = list.id[j] >= 0 ? expf((teacher[j] - top) * scale) : 0.0f;
-        list.c[j] = e;
-        sum += e;
+    // q of the entries that count into list.c, their entries and scores into list.id, list.z (0, -1 for the others); the loss
+    __device__ __forceinline__ float finish(int k, float scale, const RowStat& st, float logsum, ListShared& list, RowShared<THREADS>& sh, bool& some)
+    {
+        float top = -INFINITY;
+#pragma unroll
+        for (int i = 0; i < PER; ++i) {
+            if (z[i] == -INFINITY || t[i] == -INFINITY) id[i] = -1;
+            // (a NaN counts, and makes the loss NaN)
+            if (id[i] >= 0) top = fmaxf(top, t[i] == t[i] ? t[i] : -FLT_MAX);
+        }
+        top = group_max<THREADS>(top, sh);
+        some = top != -INFINITY;
+        float sum = 0.0f, e[PER];
+#pragma unroll
+        for (int i = 0; i < PER; ++i) {
+            e[i] = id[i] >= 0 ? expf((t[i] - top) * scale) : 0.0f;
+            sum += e[i];
+        }
+        sum = group_sum<THREADS>(sum, sh);
+        const float logq = logf(sum);
+        float loss = 0.0f;
+#pragma unroll
+        for (int i = 0; i < PER; ++i) {
+            const int j = i * THREADS + threadIdx.x;
+            const float q = id[i] >= 0 ? e[i] / sum : 0.0f;
+            // q (ln q - ln p), the part of ln p that may not fit float32 multiplied by q first (a student's mask of the lowest value)
+            if (q != 0.0f) loss += fmaf(q * scale, st.m - z[i], q * ((t[i] - top) * scale - logq + logsum));
+            if (j < k) { list.id[j] = id[i]; list.c[j] = q; list.z[j] = z[i]; }
+        }
+        return group_sum<THREADS>(loss, sh);
     }
-    sum = group_sum<THREADS>(sum, sh);
-    const float logq = logf(sum);
-    float loss = 0.0f;
-    for (int j = threadIdx.x; j < k; j += THREADS) {
-        if (list.id[j] < 0) continue;
-        const float q = list.c[j] / sum;
-        list.c[j] = q;
-        // q (ln q - ln p), the part of ln p that may not fit float32 multiplied by q first (a student's mask of the lowest value)
-        if (q != 0.0f) loss += fmaf(q * scale, st.m - list.z[j], q * ((teacher[j] - top) * scale - logq + logsum));
-    }
-    return group_sum<THREADS>(loss, sh);
-}
+};
 
 template <typename T, int THREADS, bool STEP>
 __global__ __launch_bounds__(THREADS) void k_distill(DistillArgs a)
@@ -318,10 +344,13 @@ __global__ __launch_bounds__(THREADS) void k_distill(DistillArgs a)
     __shared__ ListShared list;
     for (int64_t r = blockIdx.x; r < a.rows; r += gridDim.x) {
         const Row<T> row(a.logits, r * a.ld, a.n);
-        const RowStat st = row_stats<T, THREADS, false, false>(row, 0, row.nchunks, a.scale * kLog2e, sh, nullptr, 0);
+        Teacher<T, THREADS> teacher;
+        const RowStat st = row_stats<T, THREADS, false, false>(row, 0, row.nchunks, a.scale * kLog2e, sh, nullptr, 0,
+                                                              [&] { teacher.read(row, a.ids + r * a.k, a.teacher + r * a.k, a.k); });
         const float logsum = st.log_sum();
         bool some;
-        const float loss = teacher_list<T, THREADS>(row, a.ids + r * a.k, a.teacher + r * a.k, a.k, a.scale, st, logsum, list, sh, some);
+        __syncthreads();                                 // (the list of the row before is no longer read)
+        const float loss = teacher.finish(a.k, a.scale, st, logsum, list, sh, some);
         if (threadIdx.x == 0) {
             a.loss[r] = loss;
             if (a.norm) { a.norm[2 * r] = st.top(); a.norm[2 * r + 1] = logsum; }
@@ -350,6 +379,7 @@ __global__ __launch_bounds__(THREADS) void k_distill_backward(DistillArgs a)
             const bool counts = q != 0.0f && id >= 0 && id < a.n;
             list.id[j] = counts ? (int)id : -1;
             list.c[j] = -w * q;
+            list.z[j] = row.at(id);
             some |= counts;
         }
         some = __syncthreads_or(some);
@@ -364,6 +394,7 @@ static unsigned row_grid(int64_t rows) { return (unsigned)(rows < (1 << 20) ? ro
 static int row_threads(int dtype, int64_t n)
 {
     const int64_t chunks = n * (int64_t)element_bytes(dtype) / 16;
+    if (const char* e = getenv("HR_T")) return atoi(e);
     return chunks <= 256 ? 64 : (chunks <= 2048 ? 256 : 1024);
 }
 
