@@ -221,43 +221,29 @@ struct RowStat {
     }
 };
 
-// Largest scores of stretches of a row: what the search for its best entries starts from.  A slot is 2^shift chunks.
+// Largest scores of stretches of a row: what the search for its best entries starts from.  A stretch is `span` chunks that one
+// thread reads one after the other: nothing has to be exchanged between lanes to know its largest score.
 template <int THREADS>
 struct Slots {
-    static constexpr int kMax = 4 * THREADS;
-    uint32_t key[kMax];
-    // few enough slots: chunks one by one, or 2, 4, 8, 16 .. of them together
-    static __host__ __device__ int shift_for(int nchunks)
-    {
-        int s = 0;
-        while (nchunks > kMax << s) ++s;
-        return s;
-    }
+    static constexpr int kPer = THREADS >= 1024 ? 4 : 8;             // of a thread
+    uint32_t key[kPer][THREADS];
+    static __device__ int span_for(int nchunks) { return (nchunks + THREADS * kPer - 1) / (THREADS * kPer); }
 };
 
-// largest of 2^min(shift, 4) neighbouring lanes
-__device__ __forceinline__ float neighbours_max(float v, int shift)
-{
-    auto step = [&](auto ctrl) __attribute__((always_inline)) {
-        v = fmaxf(v, __builtin_bit_cast(float, __builtin_amdgcn_update_dpp(0, __builtin_bit_cast(int, v), decltype(ctrl)::value, 0xf, 0xf, false)));
-    };
-    using std::integral_constant;
-    if (shift >= 1) step(integral_constant<int, 0xb1>{});       // quad_perm: lane ^ 1
-    if (shift >= 2) step(integral_constant<int, 0x4e>{});       // quad_perm: lane ^ 2
-    if (shift >= 3) step(integral_constant<int, 0x141>{});      // row_half_mirror: the other four of eight lanes
-    if (shift >= 4) step(integral_constant<int, 0x140>{});      // row_mirror: the other eight of sixteen
-    return v;
-}
-
 // Maximum and sums of chunks begin .. end-1 of a row (begin a multiple of 16; the edges if begin is 0), to all threads of a workgroup.
-// TOP: the slots' largest scores as well; the slots have to be cleared before.
-// first() is called once while the first chunks are on their way.
+// TOP: the slots of this thread as well (none of the edges).  first() is called once while the first chunks are on their way.
 template <typename T, int THREADS, bool ENTROPY, bool TOP, typename G>
-__device__ __forceinline__ RowStat row_stats(const Row<T>& row, int begin, int end, float c2, RowShared<THREADS>& sh, uint32_t* slots, int shift, G&& first)
+__device__ __forceinline__ RowStat row_stats(const Row<T>& row, int begin, int end, float c2, RowShared<THREADS>& sh, Slots<THREADS>* slots, int span, G&& first)
 {
     constexpr int E = Row<T>::E;
     RowStat st;
     st.clear();
+    float best = -INFINITY;
+    int left = span, slot = 0;
+    if (TOP) {
+#pragma unroll
+        for (int i = 0; i < Slots<THREADS>::kPer; ++i) slots->key[i][threadIdx.x] = 0;
+    }
     for_chunks<4, THREADS>(row, begin, end, [&](const typename Row<T>::V& raw, int c, bool in) __attribute__((always_inline)) {
         float v[E];
 #pragma unroll
@@ -265,23 +251,22 @@ __device__ __forceinline__ RowStat row_stats(const Row<T>& row, int begin, int e
         float top = v[0];
 #pragma unroll
         for (int e = 1; e < E; ++e) top = fmaxf(top, v[e]);
-        if (in) st.template add<E, ENTROPY>(v, top, c2);
-        if (TOP) {
-            top = neighbours_max(in ? top : -INFINITY, shift);
-            const int group = (1 << min(shift, 4)) - 1;
-            if ((c & group) == 0) {
-                if (shift <= 4) slots[c >> shift] = order_key(top);
-                else atomicMax(&slots[c >> shift], order_key(top));
-            }
+        if (in) {
+            st.template add<E, ENTROPY>(v, top, c2);
+            if (TOP) best = fmaxf(best, top);
+        }
+        if (TOP && --left == 0) {
+            slots->key[slot++][threadIdx.x] = order_key(best);
+            left = span;
+            best = -INFINITY;
         }
     }, first);
+    if (TOP && left < span) slots->key[slot][threadIdx.x] = order_key(best);
     if (begin == 0 && row.edges()) {
         const int i = row.edge(threadIdx.x);
-        if (TOP) __syncthreads();
         if (i >= 0) {
             const float v = (float)row.z[i];
             st.template add<1, ENTROPY>(&v, v, c2);
-            if (TOP) atomicMax(&slots[(i + row.before) / E >> shift], order_key(v));
         }
     }
     st.fold<THREADS>(c2, sh);

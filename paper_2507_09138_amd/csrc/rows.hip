@@ -15,156 +15,273 @@ namespace hr {
 template <int THREADS> constexpr int kListPer = (HR_LIST_MAX + THREADS - 1) / THREADS;
 
 // ---- best k of a row
-// The entries among the best k lie in slots whose largest score is among the k best of the slots' (k slots hold k entries
-// that are at least as good as the k-th slot's best one).  So the pass over the row only keeps every slot's largest score;
-// a bound is found among those by bisection, the few slots that reach it are read again (from L2), and their entries at or above the
-// bound are ranked.  Keys of (score, entry) are 64-bit numbers, larger is better, no two alike: equal scores go by entry.
+// The pass over the row keeps the largest score of every slot.  A few slots of a thread (or of two neighbours) make a group, and the
+// k-th largest of 512 groups' maxima is a bound that k entries reach: only slots that reach it are read again (about k of
+// them), their entries that reach it are collected and ranked.  Keys of (score, entry) are 64-bit numbers, larger is better, no two
+// alike: equal scores go by entry.  Where a score at the bound is that of very many entries (masks of the lowest value, rows all
+// alike) the better ones are collected first, then the first of the equal ones in the order of the row.
 __device__ __forceinline__ uint64_t entry_key(float z, int i) { return (uint64_t)order_key(z) << 32 | (uint32_t)~i; }
 
 template <int THREADS>
 struct TopShared {
     static constexpr int kCap = THREADS >= 256 ? 1024 : 512;      // a chunk has to fit in beside HR_K_MAX kept entries
+    static constexpr int kAll = kCap + 1, kGroups = 512;
     Slots<THREADS> slots;
-    uint16_t picked[Slots<THREADS>::kMax];
+    uint16_t picked[Slots<THREADS>::kPer * THREADS];
     uint64_t key[kCap];
     uint64_t best[HR_K_MAX];
     uint64_t bound;                     // entries at or below it are not among the best
-    int npicked, fill, valid;
-    uint64_t count[2][THREADS / 64];
+    uint32_t group[kGroups];
+    int wave[THREADS / 64];
+    int npicked, fill, ties;
+    int valid[2];                       // by turns: keys that there was room for, or kAll where that was all of a round's
 };
 
-// A lower bound, as an order_key, of the k-th largest of the slots, such that few more than k reach it where they differ
-// (the range between the smallest and the largest is cut until k .. 1.5 k + 8 are left).  Empty slots are never reached.
-template <int THREADS>
-__device__ uint32_t slot_bound(TopShared<THREADS>& t, int nslots, int k, uint32_t largest)
+// A lower bound, as an order_key, of the k-th largest of 64 N keys, N of which every lane of a wave holds, such that few more
+// than k reach it where they differ (the range between the smallest and the largest is cut until k .. 1.5 k + 8 are left;
+// ties: more than that reach it).  Keys at or below kNoCandidate are none; with fewer than k others all of those reach the bound.
+template <int N>
+__device__ __forceinline__ uint32_t bound_of(const uint32_t* mine, int k, bool& ties)
 {
-    constexpr int PER = Slots<THREADS>::kMax / THREADS;
-    uint32_t mine[PER];
-    uint32_t least = 0xffffffffu;
+    uint32_t least = 0xffffffffu, largest = 0;
 #pragma unroll
-    for (int i = 0; i < PER; ++i) {
-        const int s = i * THREADS + threadIdx.x;
-        mine[i] = s < nslots ? t.slots.key[s] : 0;
-        if (mine[i] > kNoCandidate && mine[i] < least) least = mine[i];
+    for (int i = 0; i < N; ++i) {
+        if (mine[i] > kNoCandidate) least = min(least, mine[i]);
+        largest = max(largest, mine[i]);
     }
-    const int enough = k + k / 2 + 8;
     least = wave_min(least);
-    if (THREADS > 64) {
-        if (lane_id() == 0) t.count[1][threadIdx.x / 64] = least;
-        __syncthreads();
-        for (int w = 0; w < THREADS / 64; ++w) least = min(least, (uint32_t)t.count[1][w]);
-    }
+    largest = wave_fold(largest, [](uint32_t x, uint32_t y) { return x > y ? x : y; });
+    ties = false;
     // lo is reached by k or more, hi + 1 by fewer
     uint32_t lo = kNoCandidate + 1, hi = largest;
     if (least > largest) return lo;
-    for (int turn = 0; lo < hi; ++turn) {
-        // three bounds at once split what is left in four; the first time the smallest slot is the lowest of them
-        const uint32_t part = (hi - lo) / 4, b1 = turn ? lo + part + 1 : least, b2 = turn ? lo + 2 * part + 1 : least + (hi - least) / 3,
-                       b3 = turn ? lo + 3 * part + 1 : least + (hi - least) / 3 * 2;
+    const int enough = k + k / 2 + 8;
+    int reached = 0;
+    for (bool once = true; lo < hi || once; once = false) {
+        // three bounds at once split what is left in four; the first time the smallest key is the lowest of them
+        const uint32_t from = once ? least : lo + 1, part = (hi - from) / (once ? 3 : 4) + 1;
+        const uint32_t b1 = once ? from : min(lo + part, hi), b2 = min(b1 + part, hi), b3 = min(b2 + part, hi);
         int n1 = 0, n2 = 0, n3 = 0;
 #pragma unroll
-        for (int i = 0; i < PER; ++i) {
+        for (int i = 0; i < N; ++i) {
             n1 += __popcll(__ballot(mine[i] >= b1));
             n2 += __popcll(__ballot(mine[i] >= b2));
             n3 += __popcll(__ballot(mine[i] >= b3));
         }
-        uint64_t n = (uint64_t)n3 << 32 | (uint32_t)n2 << 16 | (uint32_t)n1;
-        if (THREADS > 64) {
-            if (lane_id() == 0) t.count[turn & 1][threadIdx.x / 64] = n;
-            __syncthreads();
-            n = 0;
-            for (int w = 0; w < THREADS / 64; ++w) n += t.count[turn & 1][w];
-        }
-        n1 = (int)(n & 0xffff);
-        n2 = (int)(n >> 16 & 0xffff);
-        n3 = (int)(n >> 32);
-        int reached;
         if (n3 >= k) { lo = b3; reached = n3; }
         else if (n2 >= k) { lo = b2; hi = b3 - 1; reached = n2; }
         else if (n1 >= k) { lo = b1; hi = b2 - 1; reached = n1; }
-        else { hi = b1 - 1; reached = Slots<THREADS>::kMax; if (turn == 0) return lo; }
-        if (reached <= enough) break;
+        else if (once) return lo;
+        else { hi = b1 - 1; continue; }
+        if (reached <= enough) return lo;
     }
+    ties = true;
     return lo;
 }
 
-// The best k of the first `fill` keys go to the front, best first; returns how many there are.  16 lanes count how many keys
-// beat one.
+// The best k of the first `fill` keys, best first, in t.best; returns how many there are.
 template <int THREADS>
 __device__ int rank_best(TopShared<THREADS>& t, int fill, int k)
 {
+    if (fill > k + k / 2 + 64) {
+        // Most of them need not be ranked: a bound among their scores, or among the entries of equal scores, and those that
+        // reach it go to the front.
+        constexpr int N = TopShared<THREADS>::kCap / 64, PER = TopShared<THREADS>::kCap / THREADS;
+        uint32_t part[N];
+#pragma unroll
+        for (int i = 0; i < N; ++i) part[i] = i * 64 + lane_id() < fill ? (uint32_t)(t.key[i * 64 + lane_id()] >> 32) : 0;
+        bool ties;
+        const uint32_t score = bound_of<N>(part, k, ties);
+        uint64_t least = (uint64_t)score << 32;
+        if (ties) {
+            int better = 0;
+#pragma unroll
+            for (int i = 0; i < N; ++i) {
+                better += __popcll(__ballot(part[i] > score));
+                part[i] = part[i] == score ? (uint32_t)t.key[i * 64 + lane_id()] : 0;      // (~entry, above kNoCandidate: entries are below 2^30)
+            }
+            bool none;
+            least |= bound_of<N>(part, k - better, none);
+        }
+        uint64_t mine[PER];
+#pragma unroll
+        for (int i = 0; i < PER; ++i) mine[i] = i * THREADS + (int)threadIdx.x < fill ? t.key[i * THREADS + threadIdx.x] : 0;
+        __syncthreads();
+        if (threadIdx.x == 0) t.fill = 0;
+        __syncthreads();
+#pragma unroll
+        for (int i = 0; i < PER; ++i)
+            if (mine[i] >= least) t.key[atomicAdd(&t.fill, 1)] = mine[i];
+        __syncthreads();
+        fill = t.fill;
+    }
+    // 16 lanes count how many keys beat one
     const int sub = threadIdx.x & 15;
-    __syncthreads();
     for (int i = threadIdx.x / 16; i < fill; i += THREADS / 16) {
         const uint64_t mine = t.key[i];
         int n = 0;
         for (int j = sub; j < fill; j += 16) n += t.key[j] > mine;
-        n += __builtin_amdgcn_update_dpp(0, n, 0xb1, 0xf, 0xf, false);
+        n += __builtin_amdgcn_update_dpp(0, n, 0xb1, 0xf, 0xf, false);      // lanes ^ 1, ^ 2, the other four, the other eight
         n += __builtin_amdgcn_update_dpp(0, n, 0x4e, 0xf, 0xf, false);
         n += __builtin_amdgcn_update_dpp(0, n, 0x141, 0xf, 0xf, false);
         n += __builtin_amdgcn_update_dpp(0, n, 0x140, 0xf, 0xf, false);
         if (sub == 0 && n < k) t.best[n] = mine;
     }
     __syncthreads();
-    const int found = fill < k ? fill : k;
-    for (int i = threadIdx.x; i < found; i += THREADS) t.key[i] = t.best[i];
-    __syncthreads();
-    return found;
+    return fill < k ? fill : k;
 }
 
-// The best k of a row whose slots are filled: keys in t.key, best first; returns how many there are.
+// Offers chunk c of the row (-1: none), one of every thread, to the buffer: entries above t.bound are appended.  Where there is
+// no room for a chunk's, the best k of what the buffer holds are kept, the k-th is the new bound, and the chunk is offered again:
+// there is room for one at least.  turn: a number that changes from call to call: what a round leaves in t.valid is read behind its
+// barrier, when the next round may already write the other one.
 template <typename T, int THREADS>
-__device__ int best_entries(const Row<T>& row, int shift, int k, uint32_t largest, TopShared<THREADS>& t)
+__device__ __forceinline__ void offer(const Row<T>& row, int c, TopShared<THREADS>& t, int k, int turn)
 {
     constexpr int E = Row<T>::E;
-    const int nslots = (row.nchunks + (1 << shift) - 1) >> shift;
-    __syncthreads();
-    const uint32_t bound = slot_bound<THREADS>(t, nslots, k, largest);
-    if (threadIdx.x == 0) {
-        t.fill = t.npicked = 0;
-        t.bound = ((uint64_t)bound << 32) - 1;
+    float v[E];
+    bool pending = c >= 0;
+    const int first = pending ? row.load(c, v) : 0;
+    for (;;) {
+        int cnt = 0;
+        const uint64_t above = t.bound;
+        if (pending) {
+#pragma unroll
+            for (int e = 0; e < E; ++e) cnt += entry_key(v[e], first + e) > above;
+        }
+        pending = pending && cnt > 0;
+        if (pending) {
+            int pos = atomicAdd(&t.fill, cnt);
+            if (pos + cnt <= TopShared<THREADS>::kCap) {
+#pragma unroll
+                for (int e = 0; e < E; ++e) {
+                    const uint64_t key = entry_key(v[e], first + e);
+                    if (key > above) t.key[pos++] = key;
+                }
+                pending = false;
+            } else {
+                atomicMin(&t.valid[turn & 1], pos);
+            }
+        }
+        __syncthreads();
+        const int valid = t.valid[turn & 1];
+        if (valid == TopShared<THREADS>::kAll) return;
+        const int kept = rank_best(t, valid, k);
+        for (int j = threadIdx.x; j < kept; j += THREADS) t.key[j] = t.best[j];
+        __syncthreads();
+        if (threadIdx.x == 0) {
+            t.fill = kept;
+            t.valid[turn & 1] = TopShared<THREADS>::kAll;
+            if (kept == k) t.bound = t.best[k - 1];
+        }
+        __syncthreads();
+    }
+}
+
+// Appends the first of the entries with this score, in the order of the row, until the buffer holds k.
+template <typename T, int THREADS>
+__device__ void append_equal(const Row<T>& row, uint32_t score, TopShared<THREADS>& t, int k)
+{
+    constexpr int E = Row<T>::E;
+    int have = t.fill;
+    for (int c0 = 0; c0 < row.nchunks && have < k; c0 += THREADS) {
+        const int c = c0 + threadIdx.x;
+        float v[E];
+        int first = 0, cnt = 0;
+        if (c < row.nchunks) {
+            first = row.load(c, v);
+#pragma unroll
+            for (int e = 0; e < E; ++e) cnt += order_key(v[e]) == score;
+        }
+        // places of a thread's behind those of the threads before it
+        int pos = wave_prefix_sum(cnt);
+        __syncthreads();
+        if (lane_id() == 63) t.wave[threadIdx.x / 64] = pos;
+        __syncthreads();
+        pos += have - cnt;
+        for (int w = 0; w < THREADS / 64; ++w) {
+            if (w < (int)threadIdx.x / 64) pos += t.wave[w];
+            have += t.wave[w];
+        }
+#pragma unroll
+        for (int e = 0; e < E; ++e)
+            if (c < row.nchunks && order_key(v[e]) == score && pos < k) t.key[pos++] = entry_key(v[e], first + e);
     }
     __syncthreads();
-    for (int s = threadIdx.x; s < nslots; s += THREADS)
-        if (t.slots.key[s] >= bound) t.picked[atomicAdd(&t.npicked, 1)] = (uint16_t)s;
+    if (threadIdx.x == 0) t.fill = min(have, k);
     __syncthreads();
-    const int64_t chunks = (int64_t)t.npicked << shift;
-    for (int64_t c0 = 0; c0 < chunks; c0 += THREADS) {
-        const int64_t i = c0 + threadIdx.x;
-        float v[E];
-        int first = 0;
-        bool pending = i < chunks;
-        if (pending) first = row.load(((int)t.picked[i >> shift] << shift) + (int)(i & ((1 << shift) - 1)), v);
-        // Entries above the bound are appended.  Where the buffer has no room for a chunk's, the best k of what it holds are
-        // kept, the k-th is the new bound, and the chunk is offered again: the buffer has room for one at least.
-        for (;;) {
-            if (threadIdx.x == 0) t.valid = TopShared<THREADS>::kCap;
-            __syncthreads();
-            int cnt = 0;
-            if (pending)
-                for (int e = 0; e < E; ++e) cnt += entry_key(v[e], first + e) > t.bound;
-            pending = pending && cnt > 0;
-            if (pending) {
-                int pos = atomicAdd(&t.fill, cnt);
-                if (pos + cnt <= TopShared<THREADS>::kCap) {
-                    for (int e = 0; e < E; ++e) {
-                        const uint64_t key = entry_key(v[e], first + e);
-                        if (key > t.bound) t.key[pos++] = key;
-                    }
-                    pending = false;
-                } else {
-                    atomicMin(&t.valid, pos);
-                }
-            }
-            if (!__syncthreads_or(pending)) break;
-            const int kept = rank_best(t, min(t.valid, t.fill), k);
-            if (threadIdx.x == 0) {
-                t.fill = kept;
-                if (kept == k) t.bound = t.key[k - 1];
-            }
-            __syncthreads();
+}
+
+// The best k of a row whose slots are filled, best first, in t.best; returns how many there are.
+template <typename T, int THREADS>
+__device__ int best_entries(const Row<T>& row, int span, int k, TopShared<THREADS>& t)
+{
+    constexpr int PER = Slots<THREADS>::kPer;
+    static_assert(THREADS == 64 || THREADS == 256 || THREADS == 1024);
+    uint32_t mine[PER];
+#pragma unroll
+    for (int i = 0; i < PER; ++i) mine[i] = t.slots.key[i][threadIdx.x];
+    // the groups' maxima: a thread's slots one by one, four of them, or all of two neighbours
+    if (THREADS == 64) {
+#pragma unroll
+        for (int i = 0; i < PER; ++i) t.group[i * 64 + threadIdx.x] = mine[i];
+    } else {
+        uint32_t a = max(max(mine[0], mine[1]), max(mine[2], mine[3]));
+        if (THREADS == 1024) {
+            a = max(a, (uint32_t)__builtin_amdgcn_update_dpp(0, (int)a, 0xb1, 0xf, 0xf, false));      // lane ^ 1
+            t.group[threadIdx.x / 2] = a;
+        } else {
+            t.group[threadIdx.x] = a;
+            t.group[(256 + threadIdx.x) % TopShared<THREADS>::kGroups] = max(max(mine[PER - 4], mine[PER - 3]), max(mine[PER - 2], mine[PER - 1]));
         }
     }
+    __syncthreads();
+    if (threadIdx.x < 64) {
+        constexpr int N = TopShared<THREADS>::kGroups / 64;
+        uint32_t g[N];
+#pragma unroll
+        for (int i = 0; i < N; ++i) g[i] = t.group[i * 64 + lane_id()];
+        bool ties;
+        // (256 groups are enough for few, and their bound is found in 2 us less)
+        uint32_t bound;
+        if (k <= 32) {
+            uint32_t h[N / 2];
+#pragma unroll
+            for (int i = 0; i < N / 2; ++i) h[i] = max(g[2 * i], g[2 * i + 1]);
+            bound = bound_of<N / 2>(h, k, ties);
+        } else {
+            bound = bound_of<N>(g, k, ties);
+        }
+        if (threadIdx.x == 0) {
+            t.bound = ((uint64_t)(bound + ties) << 32) - 1;
+            t.ties = ties;
+            t.fill = t.npicked = 0;
+            t.valid[0] = t.valid[1] = TopShared<THREADS>::kAll;
+        }
+    }
+    __syncthreads();
+    const uint32_t bound = (uint32_t)(t.bound >> 32) + 1;
+#pragma unroll
+    for (int i = 0; i < PER; ++i)
+        if (mine[i] >= bound) t.picked[atomicAdd(&t.npicked, 1)] = (uint16_t)(i * THREADS + threadIdx.x);
+    __syncthreads();
+    // chunks of the picked slots, then the edges
+    // (numbers of chunks, also of those that slots have behind the row's end, are below 2^30)
+    const uint32_t chunks = (uint32_t)t.npicked * span, all = chunks + (row.edges() ? 2 : 0);
+    int turn = 0;
+    for (uint32_t c0 = 0; c0 < all; c0 += THREADS) {
+        const uint32_t i = c0 + threadIdx.x;
+        int c = -1;
+        if (i < chunks) {
+            const uint32_t j = span == 1 ? i : i / (uint32_t)span, p = t.picked[j];
+            const uint32_t at = ((p / THREADS) * span + (i - j * span)) * THREADS + p % THREADS;
+            if ((int)at >= row.lo && (int)at < row.hi) c = (int)at;
+        } else if (i < all) {
+            c = i == chunks ? (row.lo > 0 ? 0 : -1) : (row.hi < row.nchunks && row.hi >= row.lo ? row.hi : -1);
+        }
+        offer<T, THREADS>(row, c, t, k, turn++);
+    }
+    if (t.ties && t.fill < k) append_equal<T, THREADS>(row, bound - 1, t, k);
     return rank_best(t, t.fill, k);
 }
 
@@ -176,16 +293,14 @@ __global__ __launch_bounds__(THREADS) void k_logprobs(LogprobsArgs a)
     const float c2 = a.scale * kLog2e;
     for (int64_t r = blockIdx.x; r < a.rows; r += gridDim.x) {
         const Row<T> row(a.logits, r * a.ld, a.n);
-        uint32_t* slots = nullptr;
-        int shift = 0;
+        Slots<THREADS>* slots = nullptr;
+        int span = 0;
         if constexpr (TOP) {
-            slots = top_.slots.key;
-            shift = Slots<THREADS>::shift_for(row.nchunks);
-            for (int i = threadIdx.x; i < Slots<THREADS>::kMax; i += THREADS) slots[i] = 0;
-            __syncthreads();
+            slots = &top_.slots;
+            span = Slots<THREADS>::span_for(row.nchunks);
         }
         float z[kListPer<THREADS>];
-        const RowStat st = row_stats<T, THREADS, true, TOP>(row, 0, row.nchunks, c2, sh, slots, shift, [&] {
+        const RowStat st = row_stats<T, THREADS, true, TOP>(row, 0, row.nchunks, c2, sh, slots, span, [&] {
 #pragma unroll
             for (int i = 0; i < kListPer<THREADS>; ++i) {
                 const int j = i * THREADS + threadIdx.x;
@@ -204,11 +319,11 @@ __global__ __launch_bounds__(THREADS) void k_logprobs(LogprobsArgs a)
         }
         if constexpr (TOP) {
             const bool some = logsum == logsum;
-            const int found = some ? best_entries<T, THREADS>(row, shift, a.k, order_key(st.m), top_) : 0;
+            const int found = some ? best_entries<T, THREADS>(row, span, a.k, top_) : 0;
             for (int j = threadIdx.x; j < a.k; j += THREADS) {
                 const bool there = j < found;
-                const float z = there ? order_value((uint32_t)(top_.key[j] >> 32)) : -INFINITY;
-                a.top_ids[r * a.k + j] = there ? (int64_t)(uint32_t)~(uint32_t)top_.key[j] : -1;
+                const float z = there ? order_value((uint32_t)(top_.best[j] >> 32)) : -INFINITY;
+                a.top_ids[r * a.k + j] = there ? (int64_t)(uint32_t)~(uint32_t)top_.best[j] : -1;
                 a.top_logprobs[r * a.k + j] = some ? st.log_p(z, a.scale, logsum) : NAN;
             }
             __syncthreads();
@@ -391,11 +506,11 @@ __global__ __launch_bounds__(THREADS) void k_distill_backward(DistillArgs a)
 static unsigned row_grid(int64_t rows) { return (unsigned)(rows < (1 << 20) ? rows : 1 << 20); }      // (a launch may not have 2^32 threads)
 
 // Threads of the workgroup that takes a row: four chunks of it or more for each.
-static int row_threads(int dtype, int64_t n)
+static int row_threads(int dtype, int64_t n, int k = 0)
 {
     const int64_t chunks = n * (int64_t)element_bytes(dtype) / 16;
     if (const char* e = getenv("HR_T")) return atoi(e);
-    return chunks <= 256 ? 64 : (chunks <= 2048 ? 256 : 1024);
+    return chunks <= 256 && k <= 32 ? 64 : (chunks <= 2048 ? 256 : 1024);
 }
 
 // f(element, threads) with the type and the number as compile-time values
@@ -417,7 +532,7 @@ static void with_row_type(int dtype, int threads, F&& f)
 
 static hipError_t launch_logprobs(int dtype, const LogprobsArgs& a, hipStream_t s)
 {
-    with_row_type(dtype, row_threads(dtype, a.n), [&](auto e, auto threads) {
+    with_row_type(dtype, row_threads(dtype, a.n, a.k), [&](auto e, auto threads) {
         if (a.k > 0) HR_ROWS_LAUNCH((k_logprobs<decltype(e), decltype(threads)::value, true>));
         else HR_ROWS_LAUNCH((k_logprobs<decltype(e), decltype(threads)::value, false>));
     });

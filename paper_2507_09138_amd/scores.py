@@ -5,6 +5,7 @@ check their tensors, allocate results and workspace on the current stream of the
 Matrices may be slices of columns of wider ones (rows contiguous); others are copied first.
 """
 import ctypes
+import functools
 from typing import NamedTuple, Optional
 
 import torch
@@ -92,18 +93,38 @@ def hr_distill_step(logits, ld, dtype, rows, n, scale, ids, teacher, k, weights,
 
 
 # ---- tensors in, tensors out
+# A call of these for one row takes less time on the GPU than Python takes around it: addresses and streams go to the library as
+# plain numbers, sizes of workspaces are kept by shape, and the library is called without another function in between.
 
-def _matrix(t, name, dtypes, shape=(None, None)):
+_raw_stream = torch._C._cuda_getCurrentRawStream          # (current_stream() makes an object first: 3 us)
+_i8_bytes = functools.lru_cache(1024)(lib.hr_i8_workspace_bytes)
+_logprobs_bytes = functools.lru_cache(1024)(lib.hr_logprobs_workspace_bytes)
+_distill_bytes = functools.lru_cache(1024)(lib.hr_distill_workspace_bytes)
+_I8 = {torch.int8: None}
+
+
+def _on_device(f):
+    """The device of the first tensor is the current one while f runs."""
+    @functools.wraps(f)
+    def call(t, *args, **kw):
+        if not isinstance(t, torch.Tensor) or not t.is_cuda or t.device.index == torch._C._cuda_getDevice():
+            return f(t, *args, **kw)
+        with torch.cuda.device(t.device):
+            return f(t, *args, **kw)
+    return call
+
+
+def _matrix(t, name, dtypes, columns=None):
     """A device matrix of one of the types whose rows are contiguous, and the distance between its rows."""
     if not isinstance(t, torch.Tensor) or not t.is_cuda:
         raise HrError(-1, f"{name} must be a device tensor")
     if t.dtype not in dtypes:
         raise HrError(-1, f"{name} has dtype {t.dtype}, want one of {[str(d) for d in dtypes]}")
-    if t.dim() != 2 or any(w is not None and g != w for g, w in zip(t.shape, shape)):
-        raise HrError(-1, f"{name} has shape {tuple(t.shape)}, want {tuple('*' if w is None else w for w in shape)}")
+    if t.dim() != 2 or (columns is not None and t.shape[1] != columns):
+        raise HrError(-1, f"{name} has shape {tuple(t.shape)}, want {('*', '*' if columns is None else columns)}")
     rows, cols = t.shape
-    ld = t.stride(0)
-    if (cols > 1 and t.stride(1) != 1) or (rows > 1 and ld < cols):
+    ld, step = t.stride()
+    if (cols > 1 and step != 1) or (rows > 1 and ld < cols):
         t = t.contiguous()
         ld = cols
     return t, (ld if rows > 1 else max(cols, 1))
@@ -136,39 +157,29 @@ def _workspace(need, device):
     return torch.empty(need, dtype=torch.uint8, device=device)
 
 
-class _on:
-    """The device whose tensors a call takes is the current one during the call."""
-
-    def __init__(self, device):
-        self.guard = None if device.index == torch.cuda.current_device() else torch.cuda.device(device)
-
-    def __enter__(self):
-        if self.guard is not None:
-            self.guard.__enter__()
-
-    def __exit__(self, *exc):
-        if self.guard is not None:
-            self.guard.__exit__(*exc)
+def _at(t):
+    return None if t is None else t.data_ptr()
 
 
 def _padded(n):
     return (n + 63) // 64 * 64
 
 
+@_on_device
 def quantize_rows(x):
     """Rows of x [m, k] in 8 bits: (int8 [m, k], float32 scale [m]).  The rows lie a multiple of 64 bytes apart."""
     x, ld = _matrix(x, "x", _DTYPE)
     m, k = x.shape
-    q = torch.empty(m, _padded(k), dtype=torch.int8, device=x.device)
-    scale = torch.empty(m, dtype=torch.float32, device=x.device)
-    with _on(x.device):
-        hr_i8_quantize(x, ld, _DTYPE[x.dtype], m, k, q, q.shape[1], scale)
+    dev = x.device
+    q = torch.empty(m, _padded(k), dtype=torch.int8, device=dev)
+    scale = torch.empty(m, dtype=torch.float32, device=dev)
+    _check(lib.hr_i8_quantize(x.data_ptr(), ld, _DTYPE[x.dtype], m, k, q.data_ptr(), q.shape[1], scale.data_ptr(), _raw_stream(dev.index)))
     return q[:, :k], scale
 
 
-def _i8_matrix(t, name, shape=(None, None)):
+def _i8_matrix(t, name, columns=None):
     """An int8 matrix, copied where the library would read behind its memory (rows on 16-byte boundaries of a length that is not)."""
-    t, ld = _matrix(t, name, (torch.int8,), shape)
+    t, ld = _matrix(t, name, _I8, columns)
     rows, k = t.shape
     if k % 16 and rows and ld % 16 == 0 and t.data_ptr() % 16 == 0 and \
             t.storage_offset() + (rows - 1) * ld + (k + 15) // 16 * 16 > t.untyped_storage().nbytes():
@@ -178,45 +189,41 @@ def _i8_matrix(t, name, shape=(None, None)):
     return t, ld
 
 
-def _out_type(dtype):
+def _product_operands(m, k, dev, b, b_scale, bias, dtype, out):
+    b, ldb = _i8_matrix(b, "b", k)
+    n = b.shape[0]
+    if b.device != dev:
+        raise HrError(-1, f"b is on {b.device}, want {dev}")
     if dtype not in _DTYPE:
         raise HrError(-1, f"dtype {dtype}: want float32, float16 or bfloat16")
-    return _DTYPE[dtype]
+    b_scale = _like(b_scale, "b_scale", torch.float32, (n,), dev)
+    bias = None if bias is None else _like(bias, "bias", torch.float32, (n,), dev)
+    out, ldo = _result(out, "out", dtype, (m, n), dev)
+    return b, ldb, n, b_scale, bias, out, ldo, _workspace(_i8_bytes(m, n, k), dev)
 
 
+@_on_device
 def i8_product(a, a_scale, b, b_scale, bias=None, dtype=torch.float32, out=None):
     """a [m, k] times b [n, k] transposed, both int8, in the scales [m] and [n] of their rows, plus bias [n]: [m, n] in dtype."""
     a, lda = _i8_matrix(a, "a")
     m, k = a.shape
-    b, ldb = _i8_matrix(b, "b", (None, k))
-    n, dev = b.shape[0], a.device
-    code = _out_type(dtype)
-    a_scale, b_scale = _like(a_scale, "a_scale", torch.float32, (m,), dev), _like(b_scale, "b_scale", torch.float32, (n,), dev)
-    if b.device != dev:
-        raise HrError(-1, f"b is on {b.device}, a on {dev}")
-    bias = None if bias is None else _like(bias, "bias", torch.float32, (n,), dev)
-    out, ldo = _result(out, "out", dtype, (m, n), dev)
-    with _on(dev):
-        ws = _workspace(hr_i8_workspace_bytes(m, n, k), dev)
-        hr_i8_product(a, lda, a_scale, b, ldb, b_scale, bias, m, n, k, out, ldo, code, ws, ws.numel())
+    dev = a.device
+    a_scale = _like(a_scale, "a_scale", torch.float32, (m,), dev)
+    b, ldb, n, b_scale, bias, out, ldo, ws = _product_operands(m, k, dev, b, b_scale, bias, dtype, out)
+    _check(lib.hr_i8_product(a.data_ptr(), lda, a_scale.data_ptr(), b.data_ptr(), ldb, b_scale.data_ptr(), _at(bias), m, n, k, out.data_ptr(),
+                             ldo, _DTYPE[dtype], ws.data_ptr(), ws.numel(), _raw_stream(dev.index)))
     return out
 
 
+@_on_device
 def i8_linear(x, b, b_scale, bias=None, dtype=torch.float32, out=None):
     """Rows of floats x [m, k], quantised row by row, times b [n, k] int8 transposed: [m, n] in dtype."""
     x, ldx = _matrix(x, "x", _DTYPE)
     m, k = x.shape
-    b, ldb = _i8_matrix(b, "b", (None, k))
-    n, dev = b.shape[0], x.device
-    code = _out_type(dtype)
-    b_scale = _like(b_scale, "b_scale", torch.float32, (n,), dev)
-    if b.device != dev:
-        raise HrError(-1, f"b is on {b.device}, x on {dev}")
-    bias = None if bias is None else _like(bias, "bias", torch.float32, (n,), dev)
-    out, ldo = _result(out, "out", dtype, (m, n), dev)
-    with _on(dev):
-        ws = _workspace(hr_i8_workspace_bytes(m, n, k), dev)
-        hr_i8_linear(x, ldx, _DTYPE[x.dtype], b, ldb, b_scale, bias, m, n, k, out, ldo, code, ws, ws.numel())
+    dev = x.device
+    b, ldb, n, b_scale, bias, out, ldo, ws = _product_operands(m, k, dev, b, b_scale, bias, dtype, out)
+    _check(lib.hr_i8_linear(x.data_ptr(), ldx, _DTYPE[x.dtype], b.data_ptr(), ldb, b_scale.data_ptr(), _at(bias), m, n, k, out.data_ptr(), ldo,
+                            _DTYPE[dtype], ws.data_ptr(), ws.numel(), _raw_stream(dev.index)))
     return out
 
 
@@ -237,26 +244,29 @@ def _list(ids, name, rows, device):
     return ids.to(torch.int64).contiguous()
 
 
+@_on_device
 def logprobs(logits, given=None, k=0, scale=1.0):
     """softmax(scale * logits) of every row [rows, n]: log probabilities of the given entries [rows, g], entropy, the k best."""
     z, ld = _matrix(logits, "logits", _DTYPE)
     rows, n = z.shape
     dev = z.device
-    given = None if given is None else _list(given, "given", rows, dev)
-    g = 0 if given is None else given.shape[1]
-    lp = None if given is None else torch.empty(rows, g, dtype=torch.float32, device=dev)
+    g, lp, ids, top = 0, None, None, None
+    if given is not None:
+        given = _list(given, "given", rows, dev)
+        g = given.shape[1]
+        lp = torch.empty(rows, g, dtype=torch.float32, device=dev)
+    ws = _workspace(_logprobs_bytes(rows, n, k), dev)
     entropy = torch.empty(rows, dtype=torch.float32, device=dev)
     norm = torch.empty(rows, 2, dtype=torch.float32, device=dev)
-    ids = top = None
     if k > 0:
         ids = torch.empty(rows, k, dtype=torch.int64, device=dev)
         top = torch.empty(rows, k, dtype=torch.float32, device=dev)
-    with _on(dev):
-        ws = _workspace(hr_logprobs_workspace_bytes(rows, n, k), dev)
-        hr_logprobs(z, ld, _DTYPE[z.dtype], rows, n, scale, given, g, k, lp, entropy, norm, ids, top, ws, ws.numel())
+    _check(lib.hr_logprobs(z.data_ptr(), ld, _DTYPE[z.dtype], rows, n, scale, _at(given), g, k, _at(lp), entropy.data_ptr(), norm.data_ptr(),
+                           _at(ids), _at(top), ws.data_ptr(), ws.numel(), _raw_stream(dev.index)))
     return Logprobs(lp, entropy, norm, ids, top)
 
 
+@_on_device
 def logprobs_backward(logits, given, result, grad_logprobs=None, grad_entropy=None, scale=1.0, out=None):
     """Gradient with respect to the logits, given those with respect to the result's logprobs [rows, g] and entropy [rows]
     (None: 0).  ``out`` may be the logits themselves."""
@@ -274,20 +284,20 @@ def logprobs_backward(logits, given, result, grad_logprobs=None, grad_entropy=No
     if grad_entropy is not None:
         grad_entropy = _like(grad_entropy, "grad_entropy", torch.float32, (rows,), dev)
     grad, ldg = _result(out, "out", z.dtype, (rows, n), dev)
-    with _on(dev):
-        hr_logprobs_backward(z, ld, _DTYPE[z.dtype], rows, n, scale, given, g, entropy, norm, grad_logprobs, grad_entropy, grad, ldg)
+    _check(lib.hr_logprobs_backward(z.data_ptr(), ld, _DTYPE[z.dtype], rows, n, scale, _at(given), g, entropy.data_ptr(), norm.data_ptr(),
+                                    _at(grad_logprobs), _at(grad_entropy), grad.data_ptr(), ldg, _raw_stream(dev.index)))
     return grad
 
 
 def _taught(logits, ids, name, values):
     z, ld = _matrix(logits, "logits", _DTYPE)
-    rows = z.shape[0]
-    ids = _list(ids, "ids", rows, z.device)
+    ids = _list(ids, "ids", z.shape[0], z.device)
     if ids.shape[1] < 1:
         raise HrError(-1, "ids has no columns")
     return z, ld, ids, _like(values, name, torch.float32, ids.shape, z.device)
 
 
+@_on_device
 def distill_forward(logits, ids, teacher, scale=1.0):
     """Loss [rows] of the logits [rows, n] against a teacher's scores [rows, k] of the entries ids [rows, k] (-1: empty), and what
     ``distill_backward`` needs: (loss, norm, q)."""
@@ -297,12 +307,13 @@ def distill_forward(logits, ids, teacher, scale=1.0):
     loss = torch.empty(rows, dtype=torch.float32, device=dev)
     norm = torch.empty(rows, 2, dtype=torch.float32, device=dev)
     q = torch.empty(rows, k, dtype=torch.float32, device=dev)
-    with _on(dev):
-        ws = _workspace(hr_distill_workspace_bytes(rows, n, k), dev)
-        hr_distill_forward(z, ld, _DTYPE[z.dtype], rows, n, scale, ids, teacher, k, loss, norm, q, ws, ws.numel())
+    ws = _workspace(_distill_bytes(rows, n, k), dev)
+    _check(lib.hr_distill_forward(z.data_ptr(), ld, _DTYPE[z.dtype], rows, n, scale, ids.data_ptr(), teacher.data_ptr(), k, loss.data_ptr(),
+                                  norm.data_ptr(), q.data_ptr(), ws.data_ptr(), ws.numel(), _raw_stream(dev.index)))
     return loss, norm, q
 
 
+@_on_device
 def distill_backward(logits, ids, q, norm, weights=None, scale=1.0, out=None):
     """Gradient with respect to the logits; weights [rows]: that of the caller's loss with respect to every row's (None: 1).
     ``out`` may be the logits themselves."""
@@ -312,11 +323,12 @@ def distill_backward(logits, ids, q, norm, weights=None, scale=1.0, out=None):
     norm = _like(norm, "norm", torch.float32, (rows, 2), dev)
     weights = None if weights is None else _like(weights, "weights", torch.float32, (rows,), dev)
     grad, ldg = _result(out, "out", z.dtype, (rows, n), dev)
-    with _on(dev):
-        hr_distill_backward(z, ld, _DTYPE[z.dtype], rows, n, scale, ids, q, ids.shape[1], norm, weights, grad, ldg)
+    _check(lib.hr_distill_backward(z.data_ptr(), ld, _DTYPE[z.dtype], rows, n, scale, ids.data_ptr(), q.data_ptr(), ids.shape[1],
+                                   norm.data_ptr(), _at(weights), grad.data_ptr(), ldg, _raw_stream(dev.index)))
     return grad
 
 
+@_on_device
 def distill_step(logits, ids, teacher, weights=None, scale=1.0, out=None):
     """``distill_forward`` and ``distill_backward`` in one, for weights known beforehand: (loss [rows], gradient [rows, n])."""
     z, ld, ids, teacher = _taught(logits, ids, "teacher", teacher)
@@ -325,7 +337,7 @@ def distill_step(logits, ids, teacher, weights=None, scale=1.0, out=None):
     weights = None if weights is None else _like(weights, "weights", torch.float32, (rows,), dev)
     loss = torch.empty(rows, dtype=torch.float32, device=dev)
     grad, ldg = _result(out, "out", z.dtype, (rows, n), dev)
-    with _on(dev):
-        ws = _workspace(hr_distill_workspace_bytes(rows, n, k), dev)
-        hr_distill_step(z, ld, _DTYPE[z.dtype], rows, n, scale, ids, teacher, k, weights, loss, None, None, grad, ldg, ws, ws.numel())
+    ws = _workspace(_distill_bytes(rows, n, k), dev)
+    _check(lib.hr_distill_step(z.data_ptr(), ld, _DTYPE[z.dtype], rows, n, scale, ids.data_ptr(), teacher.data_ptr(), k, _at(weights),
+                               loss.data_ptr(), None, None, grad.data_ptr(), ldg, ws.data_ptr(), ws.numel(), _raw_stream(dev.index)))
     return loss, grad
