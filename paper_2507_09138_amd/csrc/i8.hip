@@ -1,4 +1,7 @@
 // Products in 8-bit integers with a scale for each row of both matrices, and the quantisation of rows (hr_scores.h).
+#include <algorithm>
+#include <type_traits>
+
 #include "entry.h"
 #include "row_math.h"
 
@@ -6,62 +9,170 @@ namespace hr {
 
 typedef int intx4 __attribute__((ext_vector_type(4)));
 
+constexpr int kStep = 64;                                // bytes of k that one matrix instruction takes
+constexpr int kStaticLds = 64 * 1024;                    // what a launch may ask for without saying so beforehand
+
 struct QuantizeArgs {
     const void* x; int64_t ldx, m; int k;
     int8_t* q; int64_t ldq; float* scale;
 };
 
-// A row's scale, from the largest magnitude in it and whether it holds a NaN or an infinity.
-__device__ __forceinline__ float quant_scale(float top, bool bad) { return bad ? NAN : top / 127.0f; }
-__device__ __forceinline__ int quant(float v, float scale) { return scale > 0.0f ? (int)rintf(v / scale) : 0; }
-
-template <typename T, int THREADS>
-__global__ __launch_bounds__(THREADS) void k_quantize(QuantizeArgs a)
+// ---- quantisation.  Rows are taken in pieces of 16 elements: 16 bytes of the result.
+template <typename T>
+__device__ __forceinline__ void load_piece(const T* row, int t, int k, float* v)        // zeros from element k on
 {
-    constexpr int E = Row<T>::E;
-    __shared__ RowShared<THREADS> sh;
-    for (int64_t r = blockIdx.x; r < a.m; r += gridDim.x) {
-        const Row<T> row(a.x, r * a.ldx, a.k);
-        float top = 0.0f;
-        bool bad = false;
-        for (int c = threadIdx.x; c < row.nchunks; c += THREADS) {
-            float v[E];
-            const int first = row.load(c, v);
-            for (int e = 0; e < E; ++e) {
-                const bool in = first + e >= 0 && first + e < a.k;
-                top = fmaxf(top, in ? fabsf(v[e]) : 0.0f);
-                bad |= in && !(fabsf(v[e]) <= FLT_MAX);
+    if (t + 16 <= k) {
+        T x[16];
+        __builtin_memcpy(x, row + t, sizeof x);          // (rows may start at any element)
+#pragma unroll
+        for (int e = 0; e < 16; ++e) v[e] = (float)x[e];
+    } else {
+#pragma unroll
+        for (int e = 0; e < 16; ++e) v[e] = t + e < k ? (float)row[t + e] : 0.0f;
+    }
+}
+// The largest magnitude of a piece as the bits of a float: in order, infinities and NaNs above all others.
+__device__ __forceinline__ uint32_t largest_bits(const float* v)
+{
+    uint32_t b = 0;
+#pragma unroll
+    for (int e = 0; e < 16; ++e) b = max(b, __builtin_bit_cast(uint32_t, v[e]) & 0x7fffffffu);
+    return b;
+}
+__device__ __forceinline__ float quant_scale(uint32_t largest) { return largest >= 0x7f800000u ? NAN : bits_float(largest) / 127.0f; }
+// The quotient rounded to float32, then to a whole number.  A product with the reciprocal is off by 2^-23 of itself, 1.5e-5 at most: only
+// where it lies that near to the middle of two whole numbers the quotient itself is needed.  (A scale that small has no reciprocal.)
+__device__ __forceinline__ u32x4 quant_piece(const float* v, float scale)
+{
+    if (!(scale > 0.0f)) return u32x4{0, 0, 0, 0};
+    const float inv = 1.0f / scale;
+    float q[16];
+    bool near = !(scale > 1e-37f);
+#pragma unroll
+    for (int e = 0; e < 16; ++e) {
+        const float y = v[e] * inv;
+        q[e] = rintf(y);
+        near |= fabsf(y - q[e]) > 0.5f - 0x1p-15f;
+    }
+    if (near) {
+#pragma unroll
+        for (int e = 0; e < 16; ++e) q[e] = rintf(v[e] / scale);
+    }
+    uint32_t w[4];
+#pragma unroll
+    for (int d = 0; d < 4; ++d) {
+        w[d] = 0;
+#pragma unroll
+        for (int e = 0; e < 4; ++e) w[d] |= ((uint32_t)(int)q[4 * d + e] & 0xffu) << (8 * e);
+    }
+    return u32x4{w[0], w[1], w[2], w[3]};
+}
+
+// A workgroup takes a row, or each of its waves one (THREADS 64, four rows to a workgroup).  Rows of up to PIECES pieces per
+// thread are held in registers between the search for the largest magnitude and the rounding, longer ones are read again.
+template <typename T, int THREADS>
+__global__ __launch_bounds__(256) void k_quantize(QuantizeArgs a)
+{
+    constexpr int PIECES = 2, ROWS = 256 / THREADS;
+    __shared__ uint32_t part[4];
+    const int t = threadIdx.x % THREADS;
+    const int npieces = (a.k + 15) / 16;
+    const int padded = (int)min((int64_t)(a.k + 63) / 64 * 64, a.ldq);
+    const bool whole = a.ldq % 16 == 0 && (uintptr_t)a.q % 16 == 0;
+    for (int64_t r0 = (int64_t)blockIdx.x * ROWS; r0 < a.m; r0 += (int64_t)gridDim.x * ROWS) {
+        const int64_t r = r0 + threadIdx.x / THREADS;
+        const bool in = r < a.m;
+        const T* row = (const T*)a.x + (in ? r : a.m - 1) * a.ldx;
+        float v[PIECES][16];
+        uint32_t largest = 0;
+        for (int p0 = 0; p0 < npieces; p0 += PIECES * THREADS) {
+#pragma unroll
+            for (int i = 0; i < PIECES; ++i) {
+                const int p = p0 + i * THREADS + t;
+                if (p < npieces) load_piece(row, p * 16, a.k, v[i]);
+            }
+#pragma unroll
+            for (int i = 0; i < PIECES; ++i)
+                if (p0 + i * THREADS + t < npieces) largest = max(largest, largest_bits(v[i]));
+        }
+        largest = wave_fold(largest, [](uint32_t x, uint32_t y) { return x > y ? x : y; });
+        if (THREADS > 64) {
+            __syncthreads();
+            if (lane_id() == 0) part[threadIdx.x / 64] = largest;
+            __syncthreads();
+            largest = max(max(part[0], part[1]), max(part[2], part[3]));
+        }
+        const float scale = quant_scale(largest);
+        if (in && t == 0) a.scale[r] = scale;
+        int8_t* q = a.q + r * a.ldq;
+        const bool held = npieces <= PIECES * THREADS;
+        for (int p0 = 0; p0 < npieces; p0 += PIECES * THREADS) {
+#pragma unroll
+            for (int i = 0; i < PIECES; ++i) {
+                const int p = p0 + i * THREADS + t;
+                if (!in || p >= npieces) continue;
+                if (!held) load_piece(row, p * 16, a.k, v[i]);
+                const u32x4 w = quant_piece(v[i], scale);
+                if (whole && p * 16 + 16 <= padded) {
+                    *(u32x4*)(q + p * 16) = w;
+                } else {
+                    for (int e = 0; e < 16; ++e)
+                        if (p * 16 + e < padded) q[p * 16 + e] = (int8_t)(w[e / 4] >> (8 * (e % 4)));
+                }
             }
         }
-        top = group_max<THREADS>(top, sh);
-        bad = __syncthreads_or(bad);
-        const float scale = quant_scale(top, bad);
-        if (threadIdx.x == 0) a.scale[r] = scale;
-        int8_t* q = a.q + r * a.ldq;
-        for (int c = threadIdx.x; c < row.nchunks; c += THREADS) {
-            float v[E];
-            const int first = row.load(c, v);
-            for (int e = 0; e < E; ++e)
-                if (first + e >= 0 && first + e < a.k) q[first + e] = (int8_t)quant(v[e], scale);
-        }
-        const int64_t padded = (a.k + 63LL) / 64 * 64, end = padded < a.ldq ? padded : a.ldq;
-        for (int64_t i = a.k + threadIdx.x; i < end; i += THREADS) q[i] = 0;
+        for (int b = npieces * 16 + t; in && b < padded; b += THREADS) q[b] = 0;
     }
 }
 
+// ---- products
 struct ProductArgs {
     const int8_t* a; int64_t lda; const float* a_scale;
     const int8_t* b; int64_t ldb; const float* b_scale;
     const float* bias;
     int64_t m, n; int k;
     void* out; int64_t ldo;
+    // more than one part: the parts of k, the bytes of each (a multiple of 128), and their sums [parts][m][n]
+    int parts, part_k; int* sums;
+    // k_i8_few: floats to be quantised in the place of a, or null; waves that share 16 rows of b
+    const void* x; int64_t ldx; int share;
 };
 
-// The value of an output: the exact sum, scaled and rounded once.
-__device__ __forceinline__ float scaled_sum(int sum, float sa, float sb, bool has_bias, float bias)
+// Matrix instructions take 16 bytes of a row per lane, lane l those of row l % 16 from byte 16 (l / 16) on of a step of 64: the
+// first operand's rows are the result's rows, four of them in the registers of lane l, 4 (l / 16) .. + 3, in column l % 16.  The rows
+// of b come first, so that a lane holds four neighbouring outputs of a row of a.
+
+// Four neighbouring outputs: the exact sums, scaled, with the bias, rounded once.
+template <typename O>
+__device__ __forceinline__ void store_outputs(const ProductArgs& p, int64_t row, int64_t col, intx4 sum, float sa, floatx4 sb, floatx4 bias)
 {
-    const float v = (float)sum * sa;
-    return has_bias ? fmaf(v, sb, bias) : v * sb;
+    typedef O out4 __attribute__((ext_vector_type(4)));
+    out4 o;
+#pragma unroll
+    for (int e = 0; e < 4; ++e) {
+        const float v = (float)sum[e] * sa;
+        o[e] = (O)(p.bias ? fmaf(v, sb[e], bias[e]) : v * sb[e]);
+    }
+    O* at = (O*)p.out + row * p.ldo + col;
+    if (col + 4 <= p.n) {
+        __builtin_memcpy(at, &o, sizeof o);
+    } else {
+#pragma unroll
+        for (int e = 0; e < 4; ++e)
+            if (col + e < p.n) at[e] = o[e];
+    }
+}
+__device__ __forceinline__ floatx4 load_four(const float* x, int64_t col, int64_t n)
+{
+    floatx4 v = {0, 0, 0, 0};
+    if (col + 4 <= n) {
+        __builtin_memcpy(&v, x + col, 16);
+    } else {
+#pragma unroll
+        for (int e = 0; e < 4; ++e)
+            if (col + e < n) v[e] = x[col + e];
+    }
+    return v;
 }
 
 // 16 bytes of a row from byte t on, zeros from byte k on; rows may start anywhere
@@ -79,7 +190,7 @@ __device__ __forceinline__ u32x4 load16(const int8_t* row, int t, int k)
     return v;
 }
 
-// Tiles of 64 x 64 outputs, four waves of 32 x 32, blocks of 64 bytes of k staged through registers: rows of any alignment.
+// ---- rows of any alignment: tiles of 64 x 64 outputs, four waves of 32 x 32, blocks of 64 bytes of k staged through registers
 template <typename O>
 __global__ __launch_bounds__(256) void k_i8_product_any(ProductArgs p)
 {
@@ -92,7 +203,7 @@ __global__ __launch_bounds__(256) void k_i8_product_any(ProductArgs p)
     const int8_t* ra = m0 + lr < p.m ? p.a + (m0 + lr) * p.lda : nullptr;
     const int8_t* rb = n0 + lr < p.n ? p.b + (n0 + lr) * p.ldb : nullptr;
     intx4 acc[2][2] = {};
-    for (int t = 0; t < p.k; t += 64) {
+    for (int t = 0; t < p.k; t += kStep) {
         const u32x4 zero = {0, 0, 0, 0};
         const u32x4 va = ra ? load16(ra, t + lc, p.k) : zero, vb = rb ? load16(rb, t + lc, p.k) : zero;
         __syncthreads();
@@ -107,38 +218,381 @@ __global__ __launch_bounds__(256) void k_i8_product_any(ProductArgs p)
         for (int i = 0; i < 2; ++i)
             for (int j = 0; j < 2; ++j) acc[i][j] = __builtin_amdgcn_mfma_i32_16x16x64_i8(fb[j], fa[i], acc[i][j], 0, 0, 0);
     }
-    for (int i = 0; i < 2; ++i) {
-        const int64_t row = m0 + wm + i * 16 + lane % 16;
-        if (row >= p.m) continue;
-        const float sa = p.a_scale[row];
-        for (int j = 0; j < 2; ++j)
-            for (int e = 0; e < 4; ++e) {
-                const int64_t col = n0 + wn + j * 16 + lane / 16 * 4 + e;
-                if (col < p.n) ((O*)p.out)[row * p.ldo + col] = (O)scaled_sum(acc[i][j][e], sa, p.b_scale[col], p.bias, p.bias ? p.bias[col] : 0.0f);
+    for (int j = 0; j < 2; ++j) {
+        const int64_t col = n0 + wn + j * 16 + lane / 16 * 4;
+        const floatx4 sb = load_four(p.b_scale, col, p.n), bias = p.bias ? load_four(p.bias, col, p.n) : floatx4{};
+        for (int i = 0; i < 2; ++i) {
+            const int64_t row = m0 + wm + i * 16 + lane % 16;
+            if (row < p.m) store_outputs<O>(p, row, col, acc[i][j], p.a_scale[row], sb, bias);
+        }
+    }
+}
+
+// ---- many rows on both sides: tiles of BM x BN outputs, a wave's share of them WM x WN
+// Blocks of 128 bytes of k of both sides go straight to LDS (no registers, all of a block asked for at once), the next one while this one is
+// multiplied; one barrier a block.  A wave's load brings 8 rows of 128 bytes; the 16-byte pieces of row r lie at place (piece ^ r % 8),
+// so that the 16 rows that a fragment is read from lie in different banks.
+template <typename O, int BM, int BN, int WM, int WN>
+__global__ __launch_bounds__(BM / WM * (BN / WN) * 64) void k_i8_product(ProductArgs p)
+{
+    constexpr int WAVES = BM / WM * (BN / WN), TM = WM / 16, TN = WN / 16, BK = 128, UNITS = (BM + BN) / 8 / WAVES, BUF = (BM + BN) * BK;
+    static_assert(BM / 8 % WAVES == 0 && BN / 8 % WAVES == 0);
+    extern __shared__ __align__(1024) int8_t lds[];
+    // Tiles that run at the same time on an XCD share its L2: each has a stretch of the tiles, and takes them in blocks of
+    // four rows of tiles.
+    const int64_t tiles_m = (p.m + BM - 1) / BM, tiles_n = (p.n + BN - 1) / BN, tiles = tiles_m * tiles_n;
+    const int64_t stretch = (tiles + 7) / 8, tile = (blockIdx.x % 8) * stretch + blockIdx.x / 8;
+    if (blockIdx.x / 8 >= stretch || tile >= tiles) return;
+    const int64_t g = tile / (4 * tiles_n), rest = tile - g * 4 * tiles_n, high = min((int64_t)4, tiles_m - g * 4);
+    const int64_t m0 = (g * 4 + rest % high) * BM, n0 = rest / high * BN;
+    const int lane = lane_id(), wave = __builtin_amdgcn_readfirstlane(threadIdx.x / 64);
+    const int wm = wave / (BN / WN) * WM, wn = wave % (BN / WN) * WN;
+    const int k_begin = blockIdx.y * p.part_k, k_end = min(p.k, k_begin + p.part_k);
+
+    const int piece = ((lane & 7) ^ (lane >> 3)) * 16;
+    uint32_t off[UNITS];                                // (rows of a tile lie within 2^31 bytes: the host sees to it)
+#pragma unroll
+    for (int i = 0; i < UNITS; ++i) {
+        const int row = (i * WAVES + wave) * 8 + lane / 8;
+        off[i] = (uint32_t)(i * WAVES * 8 < BM ? min((int64_t)row, p.m - 1 - m0) * p.lda : min((int64_t)row - BM, p.n - 1 - n0) * p.ldb) + piece;
+    }
+    const int8_t *ga = p.a + m0 * p.lda, *gb = p.b + n0 * p.ldb;
+    const uint32_t lds0 = lds_addr(lds);
+    auto request = [&](int k0, uint32_t buf) __attribute__((always_inline)) {
+        // (pieces behind the rows' end are the row's first one instead, and are multiplied by 0)
+        const uint32_t back = k0 + piece >= k_end ? piece : 0;
+#pragma unroll
+        for (int i = 0; i < UNITS; ++i)
+            lds_dma16((i * WAVES * 8 < BM ? ga : gb) + k0, off[i] - back, lds0 + buf + (i * WAVES + wave) * 1024);
+    };
+
+    intx4 acc[TM][TN] = {};
+    const int frag = (lane % 16) * BK + (((lane / 16) ^ (lane & 7)) * 16);
+    auto multiply = [&](int k0, uint32_t buf, auto last) __attribute__((always_inline)) {
+#pragma unroll
+        for (int ks = 0; ks < 2; ++ks) {
+            const int8_t* f = lds + ((frag ^ (ks * 64)) + buf);
+            intx4 fa[TM], fb[TN];
+#pragma unroll
+            for (int j = 0; j < TN; ++j) fb[j] = *(const intx4*)(f + (BM + wn + j * 16) * BK);
+#pragma unroll
+            for (int i = 0; i < TM; ++i) fa[i] = *(const intx4*)(f + (wm + i * 16) * BK);
+            if (decltype(last)::value) {
+                const int left = k_end - (k0 + ks * kStep + lane / 16 * 16);
+#pragma unroll
+                for (int w = 0; w < 4; ++w) {
+                    const int bytes = min(max(left - 4 * w, 0), 4);
+                    const int mask = bytes == 4 ? -1 : (1 << (8 * bytes)) - 1;
+#pragma unroll
+                    for (int j = 0; j < TN; ++j) fb[j][w] &= mask;
+                }
             }
+#pragma unroll
+            for (int j = 0; j < TN; ++j)
+#pragma unroll
+                for (int i = 0; i < TM; ++i) acc[i][j] = __builtin_amdgcn_mfma_i32_16x16x64_i8(fb[j], fa[i], acc[i][j], 0, 0, 0);
+        }
+    };
+
+    request(k_begin, 0);
+    uint32_t buf = 0;
+    int k0 = k_begin;
+    for (; k0 + BK < k_end; k0 += BK) {
+        wait_vmcnt<0>();
+        __syncthreads();                                // this block has landed, and nobody reads the other one any more
+        request(k0 + BK, buf ^ BUF);
+        multiply(k0, buf, std::false_type{});
+        buf ^= BUF;
+    }
+    wait_vmcnt<0>();
+    __syncthreads();
+    multiply(k0, buf, std::true_type{});
+
+#pragma unroll
+    for (int j = 0; j < TN; ++j) {
+        const int64_t col = n0 + wn + j * 16 + lane / 16 * 4;
+        if (p.parts > 1) {
+#pragma unroll
+            for (int i = 0; i < TM; ++i) {
+                const int64_t row = m0 + wm + i * 16 + lane % 16;
+                if (row < p.m)
+                    for (int e = 0; e < 4; ++e)
+                        if (col + e < p.n) p.sums[((int64_t)blockIdx.y * p.m + row) * p.n + col + e] = acc[i][j][e];
+            }
+            continue;
+        }
+        const floatx4 sb = load_four(p.b_scale, col, p.n), bias = p.bias ? load_four(p.bias, col, p.n) : floatx4{};
+#pragma unroll
+        for (int i = 0; i < TM; ++i) {
+            const int64_t row = m0 + wm + i * 16 + lane % 16;
+            if (row < p.m) store_outputs<O>(p, row, col, acc[i][j], p.a_scale[row], sb, bias);
+        }
+    }
+}
+
+// adds up the parts of k: whole numbers, in any order the same
+template <typename O>
+__global__ __launch_bounds__(256) void k_i8_join(ProductArgs p)
+{
+    const int64_t fours = (p.n + 3) / 4;
+    for (int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x; i < p.m * fours; i += (int64_t)gridDim.x * 256) {
+        const int64_t row = i / fours, col = i % fours * 4;
+        intx4 sum = {0, 0, 0, 0};
+        for (int s = 0; s < p.parts; ++s) {
+            const int* at = p.sums + ((int64_t)s * p.m + row) * p.n + col;
+#pragma unroll
+            for (int e = 0; e < 4; ++e)
+                if (col + e < p.n) sum[e] += at[e];
+        }
+        store_outputs<O>(p, row, col, sum, p.a_scale[row], load_four(p.b_scale, col, p.n), p.bias ? load_four(p.bias, col, p.n) : floatx4{});
+    }
+}
+
+// ---- few rows a (16 MT): bound by reading b
+// The rows of a lie in LDS as the fragments they are multiplied as; every wave streams RN * 16 rows of b through its registers, eight
+// fragments under way, no barrier.  p.share waves may take parts of k of the same rows, so that few rows of b keep the chip busy too.
+// With floats X in the place of int8 each workgroup quantises a itself: one launch less, from L2.
+template <typename O, typename X, int MT, int RN>
+__global__ __launch_bounds__(512) void k_i8_few(ProductArgs p)
+{
+    constexpr int WAVES = 8, D = RN == 1 ? 8 : 3;
+    extern __shared__ __align__(1024) int8_t lds[];
+    __shared__ float a_scale[MT * 16];
+    __shared__ uint32_t largest[MT * 16];
+    const int lane = lane_id(), wave = __builtin_amdgcn_readfirstlane(threadIdx.x / 64);
+    const int steps = (p.k + kStep - 1) / kStep, k16 = (p.k + 15) / 16 * 16;
+    const int sub = wave % p.share, first = steps * sub / p.share, cnt = steps * (sub + 1) / p.share - first;     // this wave's steps of every group
+    const int at_once = WAVES / p.share;
+    const int64_t groups = (p.n + RN * 16 - 1) / (RN * 16), stride = (int64_t)gridDim.x * at_once;
+    const int64_t g0 = (int64_t)blockIdx.x * at_once + wave / p.share;
+    const int rounds = (int)((groups - (int64_t)blockIdx.x * at_once + stride - 1) / stride);         // (of the workgroup: the same for all waves)
+
+    // where the next fragments come from
+    const int8_t* from[RN];
+    int64_t load_group = g0;
+    int load_step = 0;
+    auto aim = [&]() __attribute__((always_inline)) {
+#pragma unroll
+        for (int r = 0; r < RN; ++r) from[r] = p.b + min((load_group * RN + r) * 16 + lane % 16, p.n - 1) * p.ldb;
+    };
+    intx4 ring[D][RN];
+    auto request = [&](int u) __attribute__((always_inline)) {
+        const int t = (first + load_step) * kStep + lane / 16 * 16;
+#pragma unroll
+        for (int r = 0; r < RN; ++r) ring[u][r] = *(const intx4*)(from[r] + (t < k16 ? t : 0));     // (behind the rows' end: multiplied by 0)
+        if (++load_step == cnt) {
+            load_step = 0;
+            load_group += stride;
+            aim();
+        }
+    };
+    aim();
+#pragma unroll
+    for (int u = 0; u < D; ++u) request(u);
+
+    // rows of a: piece t of row r is lane (t % 4) * 16 + r % 16 of the fragment of step t / 4
+    const int pieces = steps * 4;
+    auto place = [&](int r, int t) { return lds + ((t / 4 * MT + r / 16) * 64 + t % 4 * 16 + r % 16) * 16; };
+    if constexpr (sizeof(X) == 1) {
+        for (int i = threadIdx.x; i < MT * 16 * pieces; i += 512) {
+            const int r = i / pieces, t = i - r * pieces;
+            *(u32x4*)place(r, t) = r < p.m ? load16(p.a + r * p.lda, t * 16, p.k) : u32x4{0, 0, 0, 0};
+        }
+        for (int r = threadIdx.x; r < MT * 16; r += 512) a_scale[r] = r < p.m ? p.a_scale[r] : 0.0f;
+    } else {
+        for (int r = threadIdx.x; r < MT * 16; r += 512) largest[r] = 0;
+        __syncthreads();
+        for (int i = threadIdx.x; i < (int)p.m * pieces; i += 512) {
+            const int r = i / pieces, t = i - r * pieces;
+            float v[16];
+            load_piece((const X*)p.x + r * p.ldx, t * 16, p.k, v);
+            atomicMax(&largest[r], largest_bits(v));
+        }
+        __syncthreads();
+        for (int i = threadIdx.x; i < MT * 16 * pieces; i += 512) {
+            const int r = i / pieces, t = i - r * pieces;
+            float v[16];
+            u32x4 w = {0, 0, 0, 0};
+            if (r < p.m) {
+                load_piece((const X*)p.x + r * p.ldx, t * 16, p.k, v);
+                w = quant_piece(v, quant_scale(largest[r]));
+            }
+            *(u32x4*)place(r, t) = w;
+        }
+        for (int r = threadIdx.x; r < MT * 16; r += 512) a_scale[r] = quant_scale(largest[r]);
+    }
+    __syncthreads();
+    int* const shared = (int*)(lds + pieces * MT * 256);        // sums of waves that share rows: [wave][MT][64][4]
+
+    int64_t group = g0;
+    int step = 0;
+    intx4 acc[RN][MT] = {};
+    for (int s0 = 0; s0 < rounds * cnt; s0 += D) {
+#pragma unroll
+        for (int u = 0; u < D; ++u) {
+            if (s0 + u >= rounds * cnt) continue;
+            const int8_t* fa = lds + ((first + step) * MT * 64 + lane) * 16;
+#pragma unroll
+            for (int i = 0; i < MT; ++i) {
+                const intx4 f = *(const intx4*)(fa + i * 1024);
+#pragma unroll
+                for (int r = 0; r < RN; ++r) acc[r][i] = __builtin_amdgcn_mfma_i32_16x16x64_i8(ring[u][r], f, acc[r][i], 0, 0, 0);
+            }
+            request(u);
+            if (++step < cnt) continue;
+            step = 0;
+            if (RN == 1 && p.share > 1) {
+                if (sub > 0) {
+#pragma unroll
+                    for (int i = 0; i < MT; ++i) *(intx4*)(shared + ((wave * MT + i) * 64 + lane) * 4) = acc[0][i];
+                }
+                __syncthreads();
+                if (sub == 0) {
+                    for (int w = 1; w < p.share; ++w)
+#pragma unroll
+                        for (int i = 0; i < MT; ++i) acc[0][i] += *(const intx4*)(shared + (((wave + w) * MT + i) * 64 + lane) * 4);
+                }
+                __syncthreads();
+            }
+            if (sub == 0 && group < groups) {
+#pragma unroll
+                for (int r = 0; r < RN; ++r) {
+                    const int64_t col = (group * RN + r) * 16 + lane / 16 * 4;
+                    const floatx4 sb = load_four(p.b_scale, col, p.n), bias = p.bias ? load_four(p.bias, col, p.n) : floatx4{};
+#pragma unroll
+                    for (int i = 0; i < MT; ++i) {
+                        const int row = i * 16 + lane % 16;
+                        if (row < p.m) store_outputs<O>(p, row, col, acc[r][i], a_scale[row], sb, bias);
+                    }
+                }
+            }
+#pragma unroll
+            for (int r = 0; r < RN; ++r)
+#pragma unroll
+                for (int i = 0; i < MT; ++i) acc[r][i] = intx4{0, 0, 0, 0};
+            group += stride;
+        }
+    }
+}
+
+// ---- which kernel
+constexpr int kCus = 256;
+constexpr int64_t kFewBytes = 64 * 1024;                // rows a that every workgroup quantises for itself
+
+// f(type) with the C++ type of a code
+template <typename F>
+static auto with_type(int dtype, F&& f)
+{
+    switch (dtype) {
+    case HR_F32: return f(float{});
+    case HR_F16: return f(_Float16{});
+    default: return f(__bf16{});
     }
 }
 
 static hipError_t launch_quantize(int dtype, const QuantizeArgs& a, hipStream_t s)
 {
-    const dim3 grid((unsigned)(a.m < (1 << 20) ? a.m : 1 << 20)), block(256);
-    switch (dtype) {
-    case HR_F32: hipLaunchKernelGGL((k_quantize<float, 256>), grid, block, 0, s, a); break;
-    case HR_F16: hipLaunchKernelGGL((k_quantize<_Float16, 256>), grid, block, 0, s, a); break;
-    default: hipLaunchKernelGGL((k_quantize<__bf16, 256>), grid, block, 0, s, a); break;
-    }
+    // a wave per row up to 2048 elements (what its registers hold), a workgroup beyond
+    const int rows = a.k <= 2048 && a.m >= 4 ? 4 : 1;
+    const int64_t want = (a.m + rows - 1) / rows;
+    const dim3 grid((unsigned)(want < (1 << 20) ? want : 1 << 20));
+    with_type(dtype, [&](auto t) {
+        if (rows == 4) hipLaunchKernelGGL((k_quantize<decltype(t), 64>), grid, dim3(256), 0, s, a);
+        else hipLaunchKernelGGL((k_quantize<decltype(t), 256>), grid, dim3(256), 0, s, a);
+    });
     return hipGetLastError();
 }
 
+// Few rows a: those that fit LDS as fragments, with room for the sums of waves that share rows of b.
+static int few_tiles(int64_t m, int64_t k)
+{
+    if (m > 64) return 0;
+    const int tiles = m <= 16 ? 1 : (m <= 32 ? 2 : 4);
+    return (k + 63) / 64 * 1024 * tiles + 8 * 1024 * tiles <= 150 * 1024 ? tiles : 0;
+}
+
+template <typename O, typename X>
+static hipError_t launch_few(int tiles, ProductArgs p, hipStream_t s)
+{
+    const int steps = (p.k + 63) / 64;
+    // With several tiles of a, waves take 64 rows of b where that leaves each of them one at least: a quarter of the reads from LDS,
+    // outputs in whole lines.
+    const bool wide = tiles > 1 && p.n >= 64 * 8 * kCus;
+    const int64_t groups = (p.n + (wide ? 63 : 15)) / (wide ? 64 : 16);
+    p.share = 1;
+    while (!wide && p.share < 8 && groups * p.share < 8 * kCus && steps >= 4 * p.share) p.share *= 2;
+    const size_t lds = (size_t)steps * 1024 * tiles + (p.share > 1 ? 8 * 1024 * tiles : 0);
+    const int64_t want = (groups + 8 / p.share - 1) / (8 / p.share), most = (lds <= 76 * 1024 ? 2 : 1) * kCus;
+    const dim3 grid((unsigned)(want < most ? want : most)), block(512);
+    hipError_t e = hipSuccess;
+    auto go = [&](auto kernel) {
+        if (lds > kStaticLds) e = hipFuncSetAttribute((const void*)kernel, hipFuncAttributeMaxDynamicSharedMemorySize, (int)lds);
+        if (e == hipSuccess) hipLaunchKernelGGL(kernel, grid, block, lds, s, p);
+    };
+    if (tiles == 1) go(k_i8_few<O, X, 1, 1>);
+    else if constexpr (sizeof(X) == 1) {
+        if (tiles == 2) wide ? go(k_i8_few<O, X, 2, 4>) : go(k_i8_few<O, X, 2, 1>);
+        else wide ? go(k_i8_few<O, X, 4, 4>) : go(k_i8_few<O, X, 4, 1>);
+    }
+    return e == hipSuccess ? hipGetLastError() : e;
+}
+
+// Tiles of 256 x 256 where they keep the chip busy, else of 128 x 128; in parts of k where those are few as well.
+struct Tiling { bool any, big; int parts, part_k; };
+static Tiling tiling_for(int64_t m, int64_t n, int64_t k)
+{
+    const int64_t big = (m + 255) / 256 * ((n + 255) / 256), small = (m + 127) / 128 * ((n + 127) / 128);
+    Tiling t{false, big >= kCus, 1, (int)k};
+    if (!t.big && small > 0 && small < kCus) {
+        const int64_t blocks = (k + 127) / 128;
+        int64_t parts = 2 * kCus / small;
+        parts = std::min(parts, blocks / 4);             // (four blocks of k at least)
+        if (parts > 1) {
+            t.part_k = (int)((blocks + parts - 1) / parts * 128);
+            t.parts = (int)((k + t.part_k - 1) / t.part_k);
+        }
+    }
+    return t;
+}
+static size_t sums_bytes(int64_t m, int64_t n, int64_t k)
+{
+    const Tiling t = tiling_for(m, n, k);
+    return t.parts > 1 ? (size_t)t.parts * m * n * 4 : 0;
+}
+
+template <typename O>
+static hipError_t launch_tiles(const Tiling& t, ProductArgs p, hipStream_t s)
+{
+    hipError_t e = hipSuccess;
+    auto go = [&](auto kernel, int side, int waves) {
+        const size_t lds = (size_t)side * 2 * 128 * 2;
+        const int64_t tiles = (p.m + side - 1) / side * ((p.n + side - 1) / side);
+        if (lds > kStaticLds) e = hipFuncSetAttribute((const void*)kernel, hipFuncAttributeMaxDynamicSharedMemorySize, (int)lds);
+        if (e == hipSuccess) hipLaunchKernelGGL(kernel, dim3((unsigned)((tiles + 7) / 8 * 8), t.parts), dim3(waves * 64), lds, s, p);
+    };
+    p.parts = t.parts;
+    p.part_k = t.part_k;
+    if (t.big) go(k_i8_product<O, 256, 256, 128, 64>, 256, 8);
+    else go(k_i8_product<O, 128, 128, 64, 64>, 128, 4);
+    if (e == hipSuccess && t.parts > 1) {
+        const int64_t want = (p.m * ((p.n + 3) / 4) + 255) / 256;
+        hipLaunchKernelGGL(k_i8_join<O>, dim3((unsigned)(want < (1 << 20) ? want : 1 << 20)), dim3(256), 0, s, p);
+    }
+    return e == hipSuccess ? hipGetLastError() : e;
+}
+
+static bool on_16(const void* p, int64_t ld) { return (uintptr_t)p % 16 == 0 && ld % 16 == 0; }
+
 static hipError_t launch_product(int dtype, const ProductArgs& p, hipStream_t s)
 {
-    const dim3 grid((unsigned)((p.m + 63) / 64 * ((p.n + 63) / 64))), block(256);
-    switch (dtype) {
-    case HR_F32: hipLaunchKernelGGL(k_i8_product_any<float>, grid, block, 0, s, p); break;
-    case HR_F16: hipLaunchKernelGGL(k_i8_product_any<_Float16>, grid, block, 0, s, p); break;
-    default: hipLaunchKernelGGL(k_i8_product_any<__bf16>, grid, block, 0, s, p); break;
-    }
-    return hipGetLastError();
+    return with_type(dtype, [&](auto o) -> hipError_t {
+        using O = decltype(o);
+        if (const int tiles = few_tiles(p.m, p.k); tiles && on_16(p.b, p.ldb)) return launch_few<O, int8_t>(tiles, p, s);
+        // (offsets inside a tile are 32-bit numbers)
+        if (on_16(p.a, p.lda) && on_16(p.b, p.ldb) && p.lda < (1 << 22) && p.ldb < (1 << 22)) return launch_tiles<O>(tiling_for(p.m, p.n, p.k), p, s);
+        hipLaunchKernelGGL(k_i8_product_any<O>, dim3((unsigned)((p.m + 63) / 64 * ((p.n + 63) / 64))), dim3(256), 0, s, p);
+        return hipGetLastError();
+    });
 }
 
 }  // namespace hr
@@ -166,9 +620,11 @@ static int check_shape(int64_t m, int64_t n, int64_t k)
     return HR_OK;
 }
 
-// workspace: the quantised rows of hr_i8_linear, then their scales
+// workspace: the quantised rows of hr_i8_linear, their scales, sums of the parts of k
 static int64_t padded_k(int64_t k) { return (k + 63) / 64 * 64; }
 static size_t aligned(size_t bytes) { return (bytes + HR_WORKSPACE_ALIGN - 1) / HR_WORKSPACE_ALIGN * HR_WORKSPACE_ALIGN; }
+static size_t rows_bytes(int64_t m, int64_t k) { return aligned((size_t)(m * padded_k(k))); }
+static size_t scales_bytes(int64_t m) { return aligned((size_t)m * 4); }
 
 extern "C" {
 
@@ -189,7 +645,10 @@ int hr_i8_quantize(const void* x, int64_t ldx, int32_t dtype, int64_t m, int64_t
 size_t hr_i8_workspace_bytes(int64_t m, int64_t n, int64_t k)
 {
     if (check_shape(m, n, k)) return 0;
-    return aligned((size_t)(m * padded_k(k))) + aligned((size_t)m * 4) + HR_WORKSPACE_ALIGN;
+    // (fewer rows may be cut in more parts: no more sums than two tiles of 128 x 128 for every compute unit have, with two rows of tiles)
+    size_t sums = 0;
+    for (int64_t rows = m; rows > 0; rows = rows > 128 ? (rows - 1) / 128 * 128 : 0) sums = std::max(sums, sums_bytes(rows, n, k));
+    return rows_bytes(m, k) + scales_bytes(m) + aligned(sums) + HR_WORKSPACE_ALIGN;
 }
 
 int hr_i8_product(const int8_t* a, int64_t lda, const float* a_scale, const int8_t* b, int64_t ldb, const float* b_scale,
@@ -205,6 +664,7 @@ int hr_i8_product(const int8_t* a, int64_t lda, const float* a_scale, const int8
     if (!a_scale || !b_scale) return fail(HR_ERR_ARG, "a_scale / b_scale is null");
     if (int rc = check_workspace(workspace, workspace_bytes, hr_i8_workspace_bytes(m, n, k))) return rc;
     ProductArgs p{a, lda, a_scale, b, ldb, b_scale, bias, m, n, (int)k, out, ldo};
+    p.sums = (int*)((char*)workspace + rows_bytes(m, k) + scales_bytes(m));
     HR_HIP(launch_product(out_dtype, p, (hipStream_t)stream));
     return HR_OK;
 }
@@ -223,10 +683,18 @@ int hr_i8_linear(const void* x, int64_t ldx, int32_t x_dtype, const int8_t* b, i
     if (!b_scale) return fail(HR_ERR_ARG, "b_scale is null");
     if (int rc = check_workspace(workspace, workspace_bytes, hr_i8_workspace_bytes(m, n, k))) return rc;
     int8_t* q = (int8_t*)workspace;
-    float* scale = (float*)(q + aligned((size_t)(m * padded_k(k))));
+    float* scale = (float*)(q + rows_bytes(m, k));
+    if (few_tiles(m, k) == 1 && on_16(b, ldb) && m * k * (int64_t)element_bytes(x_dtype) <= kFewBytes) {
+        ProductArgs p{nullptr, 0, nullptr, b, ldb, b_scale, bias, m, n, (int)k, out, ldo};
+        p.x = x;
+        p.ldx = ldx;
+        HR_HIP(with_type(out_dtype, [&](auto o) { return with_type(x_dtype, [&](auto e) { return launch_few<decltype(o), decltype(e)>(1, p, (hipStream_t)stream); }); }));
+        return HR_OK;
+    }
     QuantizeArgs qa{x, ldx, m, (int)k, q, padded_k(k), scale};
     HR_HIP(launch_quantize(x_dtype, qa, (hipStream_t)stream));
     ProductArgs p{q, padded_k(k), scale, b, ldb, b_scale, bias, m, n, (int)k, out, ldo};
+    p.sums = (int*)((char*)scale + scales_bytes(m));
     HR_HIP(launch_product(out_dtype, p, (hipStream_t)stream));
     return HR_OK;
 }

@@ -44,6 +44,7 @@ def test_workspace_of_fewer_rows_is_enough(hr):
         assert all(s > 0 and s % 256 == 0 for s in sizes) and sizes == sorted(sizes)
     sizes = [hr.hr_logprobs_workspace_bytes(8, 131072, k) for k in range(0, 129)]
     assert sizes == sorted(sizes)
+    assert hr.hr_i8_workspace_bytes(5, 0, 700) > 0 and hr.hr_i8_workspace_bytes(0, 5, 700) > 0          # (nothing to do, but no error)
     assert hr.hr_i8_workspace_bytes(1, 1, 0) == 0 and hr.hr_i8_workspace_bytes(-1, 1, 1) == 0 and hr.hr_i8_workspace_bytes(1, 1, 131072) == 0
     assert hr.hr_logprobs_workspace_bytes(1, 0, 1) == 0 and hr.hr_logprobs_workspace_bytes(1, 10, 129) == 0
     assert hr.hr_distill_workspace_bytes(1, 10, 0) == 0 and hr.hr_distill_workspace_bytes(1, 10, 513) == 0
