@@ -134,7 +134,7 @@ struct ProductArgs {
     void* out; int64_t ldo;
     // more than one part: the parts of k, the bytes of each (a multiple of 128), and their sums [parts][m][n]
     int parts, part_k; int* sums;
-    // k_i8_few: floats to be quantised in the place of a, or null; waves that share 16 rows of b
+    // k_i8_few: floats to be quantised in the place of a; waves that share 16 rows of b
     const void* x; int64_t ldx; int share;
 };
 
@@ -348,131 +348,127 @@ __global__ __launch_bounds__(256) void k_i8_join(ProductArgs p)
     }
 }
 
-// ---- few rows a (16 MT): bound by reading b
-// The rows of a lie in LDS as the fragments they are multiplied as; every wave streams RN * 16 rows of b through its registers, eight
-// fragments under way, no barrier.  p.share waves may take parts of k of the same rows, so that few rows of b keep the chip busy too.
-// With floats X in the place of int8 each workgroup quantises a itself: one launch less, from L2.
-template <typename O, typename X, int MT, int RN>
-__global__ __launch_bounds__(512) void k_i8_few(ProductArgs p)
+// ---- up to 16 rows a: bound by reading b
+// The rows of a lie in LDS.  Every wave takes 16 rows of b at a time and has four blocks of 128 bytes of them on their way to a ring of
+// its own in LDS (whole lines: 16 rows of 64 bytes straight to registers reached 4.8 TB/s where this reaches ); no barrier.
+// p.share waves may take parts of k of the same rows, so that few rows of b keep the chip busy too.  With floats X in the place of
+// int8 each workgroup quantises a itself: one launch less, from L2.
+constexpr int kFewWaves = 8, kRing = 4, kRingBytes = kFewWaves * kRing * 2048;
+constexpr int kFewLds = 90 * 1024;                       // most bytes of a
+// bytes between the rows of a in LDS: 16 rows in different banks, nothing behind a row that is not zero
+__host__ __device__ constexpr int few_stride(int k) { return (k + 127) / 128 * 128 + 16; }
+
+template <typename O, typename X>
+__global__ __launch_bounds__(kFewWaves * 64) void k_i8_few(ProductArgs p)
 {
-    constexpr int WAVES = 8, D = RN == 1 ? 8 : 3;
-    extern __shared__ __align__(1024) int8_t lds[];
-    __shared__ float a_scale[MT * 16];
-    __shared__ uint32_t largest[MT * 16];
+    constexpr int THREADS = kFewWaves * 64;
+    extern __shared__ __align__(1024) int8_t lds[];      // rings, rows of a, 16 zeros, sums of waves that share rows
+    __shared__ float a_scale[16];
+    __shared__ uint32_t largest[16];
     const int lane = lane_id(), wave = __builtin_amdgcn_readfirstlane(threadIdx.x / 64);
-    const int steps = (p.k + kStep - 1) / kStep, k16 = (p.k + 15) / 16 * 16;
-    const int sub = wave % p.share, first = steps * sub / p.share, cnt = steps * (sub + 1) / p.share - first;     // this wave's steps of every group
-    const int at_once = WAVES / p.share;
-    const int64_t groups = (p.n + RN * 16 - 1) / (RN * 16), stride = (int64_t)gridDim.x * at_once;
+    const int blocks = (p.k + 127) / 128, a_stride = few_stride(p.k), m = (int)p.m;
+    int8_t* const rows = lds + kRingBytes;
+    const int sub = wave % p.share, first = blocks * sub / p.share, cnt = blocks * (sub + 1) / p.share - first;     // this wave's blocks of every group
+    const int at_once = kFewWaves / p.share;
+    const int64_t groups = (p.n + 15) / 16, stride = (int64_t)gridDim.x * at_once;
     const int64_t g0 = (int64_t)blockIdx.x * at_once + wave / p.share;
     const int rounds = (int)((groups - (int64_t)blockIdx.x * at_once + stride - 1) / stride);         // (of the workgroup: the same for all waves)
 
-    // where the next fragments come from
-    const int8_t* from[RN];
+    // Where the next block comes from.  Lane l brings piece l % 8 ^ l / 8 of row l / 8 (and of row 8 + l / 8) to place l % 8 of that row.
+    const int piece = ((lane & 7) ^ (lane >> 3)) * 16;
+    const int8_t* from = p.b;
+    uint32_t off[2];
     int64_t load_group = g0;
-    int load_step = 0;
+    int load_block = 0;
     auto aim = [&]() __attribute__((always_inline)) {
+        const int64_t g = min(load_group, groups - 1);   // (requests behind the end bring the last rows again)
+        const int last = (int)min((int64_t)15, p.n - 1 - g * 16);
+        from = p.b + g * 16 * p.ldb;
 #pragma unroll
-        for (int r = 0; r < RN; ++r) from[r] = p.b + min((load_group * RN + r) * 16 + lane % 16, p.n - 1) * p.ldb;
+        for (int h = 0; h < 2; ++h) off[h] = (uint32_t)min(h * 8 + lane / 8, last) * (uint32_t)p.ldb + piece;
     };
-    intx4 ring[D][RN];
+    const uint32_t ring = lds_addr(lds) + wave * kRing * 2048;
     auto request = [&](int u) __attribute__((always_inline)) {
-        const int t = (first + load_step) * kStep + lane / 16 * 16;
+        const int k0 = (first + load_block) * 128;
+        const uint32_t back = k0 + piece >= p.k ? piece : 0;        // (behind the rows' end: multiplied by 0)
 #pragma unroll
-        for (int r = 0; r < RN; ++r) ring[u][r] = *(const intx4*)(from[r] + (t < k16 ? t : 0));     // (behind the rows' end: multiplied by 0)
-        if (++load_step == cnt) {
-            load_step = 0;
+        for (int h = 0; h < 2; ++h) lds_dma16(from + k0, off[h] - back, ring + u * 2048 + h * 1024);
+        if (++load_block == cnt) {
+            load_block = 0;
             load_group += stride;
             aim();
         }
     };
     aim();
 #pragma unroll
-    for (int u = 0; u < D; ++u) request(u);
+    for (int u = 0; u < kRing; ++u) request(u);
 
-    // rows of a: piece t of row r is lane (t % 4) * 16 + r % 16 of the fragment of step t / 4
-    const int pieces = steps * 4;
-    auto place = [&](int r, int t) { return lds + ((t / 4 * MT + r / 16) * 64 + t % 4 * 16 + r % 16) * 16; };
+    const int pieces = a_stride / 16;                    // (those behind the row are zeros)
     if constexpr (sizeof(X) == 1) {
-        for (int i = threadIdx.x; i < MT * 16 * pieces; i += 512) {
+        for (int i = threadIdx.x; i < m * pieces; i += THREADS) {
             const int r = i / pieces, t = i - r * pieces;
-            *(u32x4*)place(r, t) = r < p.m ? load16(p.a + r * p.lda, t * 16, p.k) : u32x4{0, 0, 0, 0};
+            *(u32x4*)(rows + i * 16) = load16(p.a + r * p.lda, t * 16, p.k);
         }
-        for (int r = threadIdx.x; r < MT * 16; r += 512) a_scale[r] = r < p.m ? p.a_scale[r] : 0.0f;
+        if ((int)threadIdx.x < m) a_scale[threadIdx.x] = p.a_scale[threadIdx.x];
     } else {
-        for (int r = threadIdx.x; r < MT * 16; r += 512) largest[r] = 0;
+        if (threadIdx.x < 16) largest[threadIdx.x] = 0;
         __syncthreads();
-        for (int i = threadIdx.x; i < (int)p.m * pieces; i += 512) {
+        for (int i = threadIdx.x; i < m * pieces; i += THREADS) {
             const int r = i / pieces, t = i - r * pieces;
             float v[16];
             load_piece((const X*)p.x + r * p.ldx, t * 16, p.k, v);
             atomicMax(&largest[r], largest_bits(v));
         }
         __syncthreads();
-        for (int i = threadIdx.x; i < MT * 16 * pieces; i += 512) {
+        for (int i = threadIdx.x; i < m * pieces; i += THREADS) {
             const int r = i / pieces, t = i - r * pieces;
             float v[16];
-            u32x4 w = {0, 0, 0, 0};
-            if (r < p.m) {
-                load_piece((const X*)p.x + r * p.ldx, t * 16, p.k, v);
-                w = quant_piece(v, quant_scale(largest[r]));
-            }
-            *(u32x4*)place(r, t) = w;
+            load_piece((const X*)p.x + r * p.ldx, t * 16, p.k, v);
+            *(u32x4*)(rows + i * 16) = quant_piece(v, quant_scale(largest[r]));
         }
-        for (int r = threadIdx.x; r < MT * 16; r += 512) a_scale[r] = quant_scale(largest[r]);
+        if ((int)threadIdx.x < m) a_scale[threadIdx.x] = quant_scale(largest[threadIdx.x]);
     }
+    if (threadIdx.x == 0) *(u32x4*)(rows + m * a_stride) = u32x4{0, 0, 0, 0};
     __syncthreads();
-    int* const shared = (int*)(lds + pieces * MT * 256);        // sums of waves that share rows: [wave][MT][64][4]
+    intx4* const sums = (intx4*)(rows + m * a_stride + 16);
 
+    const int row = lane % 16;
+    const int8_t* const fa = rows + (row < m ? row * a_stride + lane / 16 * 16 : m * a_stride);
+    const int fa_step = row < m ? kStep : 0;             // (rows that a has not got are the zeros)
+    const int fb = wave * kRing * 2048 + row * 128 + ((lane / 16) ^ (lane & 7)) * 16;
     int64_t group = g0;
-    int step = 0;
-    intx4 acc[RN][MT] = {};
-    for (int s0 = 0; s0 < rounds * cnt; s0 += D) {
+    int block = 0;
+    intx4 acc = {0, 0, 0, 0};
+    for (int s0 = 0; s0 < rounds * cnt; s0 += kRing) {
 #pragma unroll
-        for (int u = 0; u < D; ++u) {
+        for (int u = 0; u < kRing; ++u) {
             if (s0 + u >= rounds * cnt) continue;
-            const int8_t* fa = lds + ((first + step) * MT * 64 + lane) * 16;
-#pragma unroll
-            for (int i = 0; i < MT; ++i) {
-                const intx4 f = *(const intx4*)(fa + i * 1024);
-#pragma unroll
-                for (int r = 0; r < RN; ++r) acc[r][i] = __builtin_amdgcn_mfma_i32_16x16x64_i8(ring[u][r], f, acc[r][i], 0, 0, 0);
-            }
+            wait_vmcnt<2 * (kRing - 1)>();               // (stores in between only make it longer)
+            const int8_t* a = fa + (first + block) * 2 * fa_step;
+            const intx4 b0 = *(const intx4*)(lds + (fb + u * 2048)), b1 = *(const intx4*)(lds + ((fb ^ 64) + u * 2048));
+            acc = __builtin_amdgcn_mfma_i32_16x16x64_i8(b0, *(const intx4*)a, acc, 0, 0, 0);
+            acc = __builtin_amdgcn_mfma_i32_16x16x64_i8(b1, *(const intx4*)(a + fa_step), acc, 0, 0, 0);
+            asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");          // the block has been read: its place may be filled again
             request(u);
-            if (++step < cnt) continue;
-            step = 0;
-            if (RN == 1 && p.share > 1) {
-                if (sub > 0) {
-#pragma unroll
-                    for (int i = 0; i < MT; ++i) *(intx4*)(shared + ((wave * MT + i) * 64 + lane) * 4) = acc[0][i];
-                }
+            if (++block < cnt) continue;
+            block = 0;
+            if (p.share > 1) {
+                if (sub > 0) sums[wave * 64 + lane] = acc;
                 __syncthreads();
-                if (sub == 0) {
-                    for (int w = 1; w < p.share; ++w)
-#pragma unroll
-                        for (int i = 0; i < MT; ++i) acc[0][i] += *(const intx4*)(shared + (((wave + w) * MT + i) * 64 + lane) * 4);
-                }
+                if (sub == 0)
+                    for (int w = 1; w < p.share; ++w) acc += sums[(wave + w) * 64 + lane];
                 __syncthreads();
             }
-            if (sub == 0 && group < groups) {
-#pragma unroll
-                for (int r = 0; r < RN; ++r) {
-                    const int64_t col = (group * RN + r) * 16 + lane / 16 * 4;
-                    const floatx4 sb = load_four(p.b_scale, col, p.n), bias = p.bias ? load_four(p.bias, col, p.n) : floatx4{};
-#pragma unroll
-                    for (int i = 0; i < MT; ++i) {
-                        const int row = i * 16 + lane % 16;
-                        if (row < p.m) store_outputs<O>(p, row, col, acc[r][i], a_scale[row], sb, bias);
-                    }
-                }
+            if (sub == 0 && group < groups && row < m) {
+                const int64_t col = group * 16 + lane / 16 * 4;
+                const floatx4 sb = load_four(p.b_scale, col, p.n), bias = p.bias ? load_four(p.bias, col, p.n) : floatx4{};
+                store_outputs<O>(p, row, col, acc, a_scale[row], sb, bias);
             }
-#pragma unroll
-            for (int r = 0; r < RN; ++r)
-#pragma unroll
-                for (int i = 0; i < MT; ++i) acc[r][i] = intx4{0, 0, 0, 0};
+            acc = intx4{0, 0, 0, 0};
             group += stride;
         }
     }
+    wait_vmcnt<0>();                                     // (nothing may arrive in LDS that is no longer this workgroup's)
 }
 
 // ---- which kernel
@@ -503,50 +499,35 @@ static hipError_t launch_quantize(int dtype, const QuantizeArgs& a, hipStream_t 
     return hipGetLastError();
 }
 
-// Few rows a: those that fit LDS as fragments, with room for the sums of waves that share rows of b.
-static int few_tiles(int64_t m, int64_t k)
-{
-    if (m > 64) return 0;
-    const int tiles = m <= 16 ? 1 : (m <= 32 ? 2 : 4);
-    return (k + 63) / 64 * 1024 * tiles + 8 * 1024 * tiles <= 150 * 1024 ? tiles : 0;
-}
+static bool few_rows(int64_t m, int64_t k) { return m <= 16 && m * few_stride((int)k) <= kFewLds; }
 
 template <typename O, typename X>
-static hipError_t launch_few(int tiles, ProductArgs p, hipStream_t s)
+static hipError_t launch_few(ProductArgs p, hipStream_t s)
 {
-    const int steps = (p.k + 63) / 64;
-    // With several tiles of a, waves take 64 rows of b where that leaves each of them one at least: a quarter of the reads from LDS,
-    // outputs in whole lines.
-    const bool wide = tiles > 1 && p.n >= 64 * 8 * kCus;
-    const int64_t groups = (p.n + (wide ? 63 : 15)) / (wide ? 64 : 16);
+    const int blocks = (p.k + 127) / 128;
+    const int64_t groups = (p.n + 15) / 16;
     p.share = 1;
-    while (!wide && p.share < 8 && groups * p.share < 8 * kCus && steps >= 4 * p.share) p.share *= 2;
-    const size_t lds = (size_t)steps * 1024 * tiles + (p.share > 1 ? 8 * 1024 * tiles : 0);
-    const int64_t want = (groups + 8 / p.share - 1) / (8 / p.share), most = (lds <= 76 * 1024 ? 2 : 1) * kCus;
-    const dim3 grid((unsigned)(want < most ? want : most)), block(512);
-    hipError_t e = hipSuccess;
-    auto go = [&](auto kernel) {
-        if (lds > kStaticLds) e = hipFuncSetAttribute((const void*)kernel, hipFuncAttributeMaxDynamicSharedMemorySize, (int)lds);
-        if (e == hipSuccess) hipLaunchKernelGGL(kernel, grid, block, lds, s, p);
-    };
-    if (tiles == 1) go(k_i8_few<O, X, 1, 1>);
-    else if constexpr (sizeof(X) == 1) {
-        if (tiles == 2) wide ? go(k_i8_few<O, X, 2, 4>) : go(k_i8_few<O, X, 2, 1>);
-        else wide ? go(k_i8_few<O, X, 4, 4>) : go(k_i8_few<O, X, 4, 1>);
-    }
-    return e == hipSuccess ? hipGetLastError() : e;
+    while (p.share < kFewWaves && groups * p.share < 2 * kFewWaves * kCus && blocks >= 4 * p.share) p.share *= 2;
+    const size_t lds = kRingBytes + (size_t)p.m * few_stride(p.k) + 16 + (p.share > 1 ? kFewWaves * 1024 : 0);
+    const int at_once = kFewWaves / p.share;
+    const int64_t want = (groups + at_once - 1) / at_once, most = (lds <= 79 * 1024 ? 2 : 1) * kCus;
+    if (hipError_t e = hipFuncSetAttribute((const void*)k_i8_few<O, X>, hipFuncAttributeMaxDynamicSharedMemorySize, (int)lds)) return e;
+    hipLaunchKernelGGL((k_i8_few<O, X>), dim3((unsigned)(want < most ? want : most)), dim3(kFewWaves * 64), lds, s, p);
+    return hipGetLastError();
 }
 
-// Tiles of 256 x 256 where they keep the chip busy, else of 128 x 128; in parts of k where those are few as well.
-struct Tiling { bool any, big; int parts, part_k; };
+// Tiles (BM rows a, BN rows b): 256 x 256 where they keep the chip busy, else 128 x 128, or 64 x 256 for few rows a; in parts of k where
+// those are few as well.
+struct Tiling { int bm, bn, parts, part_k; };
 static Tiling tiling_for(int64_t m, int64_t n, int64_t k)
 {
-    const int64_t big = (m + 255) / 256 * ((n + 255) / 256), small = (m + 127) / 128 * ((n + 127) / 128);
-    Tiling t{false, big >= kCus, 1, (int)k};
-    if (!t.big && small > 0 && small < kCus) {
-        const int64_t blocks = (k + 127) / 128;
-        int64_t parts = 2 * kCus / small;
-        parts = std::min(parts, blocks / 4);             // (four blocks of k at least)
+    auto tiles = [&](int bm, int bn) { return (m + bm - 1) / bm * ((n + bn - 1) / bn); };
+    Tiling t{128, 128, 1, (int)k};
+    if (m <= 64) t.bm = 64, t.bn = 256;
+    else if (tiles(256, 256) >= kCus) t.bm = t.bn = 256;
+    const int64_t all = tiles(t.bm, t.bn);
+    if (all > 0 && all < kCus) {
+        const int64_t blocks = (k + 127) / 128, parts = std::min(2 * kCus / all, blocks / 4);        // (four blocks of k at least)
         if (parts > 1) {
             t.part_k = (int)((blocks + parts - 1) / parts * 128);
             t.parts = (int)((k + t.part_k - 1) / t.part_k);
@@ -564,16 +545,17 @@ template <typename O>
 static hipError_t launch_tiles(const Tiling& t, ProductArgs p, hipStream_t s)
 {
     hipError_t e = hipSuccess;
-    auto go = [&](auto kernel, int side, int waves) {
-        const size_t lds = (size_t)side * 2 * 128 * 2;
-        const int64_t tiles = (p.m + side - 1) / side * ((p.n + side - 1) / side);
+    auto go = [&](auto kernel, int waves) {
+        const size_t lds = (size_t)(t.bm + t.bn) * 128 * 2;
+        const int64_t tiles = (p.m + t.bm - 1) / t.bm * ((p.n + t.bn - 1) / t.bn);
         if (lds > kStaticLds) e = hipFuncSetAttribute((const void*)kernel, hipFuncAttributeMaxDynamicSharedMemorySize, (int)lds);
         if (e == hipSuccess) hipLaunchKernelGGL(kernel, dim3((unsigned)((tiles + 7) / 8 * 8), t.parts), dim3(waves * 64), lds, s, p);
     };
     p.parts = t.parts;
     p.part_k = t.part_k;
-    if (t.big) go(k_i8_product<O, 256, 256, 128, 64>, 256, 8);
-    else go(k_i8_product<O, 128, 128, 64, 64>, 128, 4);
+    if (t.bm == 256) go(k_i8_product<O, 256, 256, 128, 64>, 8);
+    else if (t.bm == 128) go(k_i8_product<O, 128, 128, 64, 64>, 4);
+    else go(k_i8_product<O, 64, 256, 64, 32>, 8);
     if (e == hipSuccess && t.parts > 1) {
         const int64_t want = (p.m * ((p.n + 3) / 4) + 255) / 256;
         hipLaunchKernelGGL(k_i8_join<O>, dim3((unsigned)(want < (1 << 20) ? want : 1 << 20)), dim3(256), 0, s, p);
@@ -581,15 +563,15 @@ static hipError_t launch_tiles(const Tiling& t, ProductArgs p, hipStream_t s)
     return e == hipSuccess ? hipGetLastError() : e;
 }
 
-static bool on_16(const void* p, int64_t ld) { return (uintptr_t)p % 16 == 0 && ld % 16 == 0; }
+// rows that requests of 16 bytes reach; offsets inside a tile are 32-bit numbers
+static bool in_tiles(const void* p, int64_t ld) { return (uintptr_t)p % 16 == 0 && ld % 16 == 0 && ld < (1 << 22); }
 
 static hipError_t launch_product(int dtype, const ProductArgs& p, hipStream_t s)
 {
     return with_type(dtype, [&](auto o) -> hipError_t {
         using O = decltype(o);
-        if (const int tiles = few_tiles(p.m, p.k); tiles && on_16(p.b, p.ldb)) return launch_few<O, int8_t>(tiles, p, s);
-        // (offsets inside a tile are 32-bit numbers)
-        if (on_16(p.a, p.lda) && on_16(p.b, p.ldb) && p.lda < (1 << 22) && p.ldb < (1 << 22)) return launch_tiles<O>(tiling_for(p.m, p.n, p.k), p, s);
+        if (few_rows(p.m, p.k) && in_tiles(p.b, p.ldb)) return launch_few<O, int8_t>(p, s);
+        if (in_tiles(p.a, p.lda) && in_tiles(p.b, p.ldb)) return launch_tiles<O>(tiling_for(p.m, p.n, p.k), p, s);
         hipLaunchKernelGGL(k_i8_product_any<O>, dim3((unsigned)((p.m + 63) / 64 * ((p.n + 63) / 64))), dim3(256), 0, s, p);
         return hipGetLastError();
     });
@@ -645,9 +627,11 @@ int hr_i8_quantize(const void* x, int64_t ldx, int32_t dtype, int64_t m, int64_t
 size_t hr_i8_workspace_bytes(int64_t m, int64_t n, int64_t k)
 {
     if (check_shape(m, n, k)) return 0;
-    // (fewer rows may be cut in more parts: no more sums than two tiles of 128 x 128 for every compute unit have, with two rows of tiles)
-    size_t sums = 0;
-    for (int64_t rows = m; rows > 0; rows = rows > 128 ? (rows - 1) / 128 * 128 : 0) sums = std::max(sums, sums_bytes(rows, n, k));
+    // (fewer rows may be cut in more parts; the most sums of rows in as many tiles are those of whole tiles.  Rows beyond 128 x 256 tiles
+    // are never cut)
+    size_t sums = sums_bytes(m, n, k);
+    for (int64_t rows = std::min(m - 1, (int64_t)128 * kCus) / 128 * 128; rows > 0; rows -= 128) sums = std::max(sums, sums_bytes(rows, n, k));
+    if (m > 64) sums = std::max(sums, sums_bytes(64, n, k));
     return rows_bytes(m, k) + scales_bytes(m) + aligned(sums) + HR_WORKSPACE_ALIGN;
 }
 
@@ -684,11 +668,11 @@ int hr_i8_linear(const void* x, int64_t ldx, int32_t x_dtype, const int8_t* b, i
     if (int rc = check_workspace(workspace, workspace_bytes, hr_i8_workspace_bytes(m, n, k))) return rc;
     int8_t* q = (int8_t*)workspace;
     float* scale = (float*)(q + rows_bytes(m, k));
-    if (few_tiles(m, k) == 1 && on_16(b, ldb) && m * k * (int64_t)element_bytes(x_dtype) <= kFewBytes) {
+    if (few_rows(m, k) && in_tiles(b, ldb) && m * k * (int64_t)element_bytes(x_dtype) <= kFewBytes) {
         ProductArgs p{nullptr, 0, nullptr, b, ldb, b_scale, bias, m, n, (int)k, out, ldo};
         p.x = x;
         p.ldx = ldx;
-        HR_HIP(with_type(out_dtype, [&](auto o) { return with_type(x_dtype, [&](auto e) { return launch_few<decltype(o), decltype(e)>(1, p, (hipStream_t)stream); }); }));
+        HR_HIP(with_type(out_dtype, [&](auto o) { return with_type(x_dtype, [&](auto e) { return launch_few<decltype(o), decltype(e)>(p, (hipStream_t)stream); }); }));
         return HR_OK;
     }
     QuantizeArgs qa{x, ldx, m, (int)k, q, padded_k(k), scale};
