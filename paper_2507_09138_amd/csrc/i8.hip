@@ -229,104 +229,153 @@ __global__ __launch_bounds__(256) void k_i8_product_any(ProductArgs p)
 }
 
 // ---- many rows on both sides: tiles of BM x BN outputs, a wave's share of them WM x WN
-// Blocks of 128 bytes of k of both sides go straight to LDS (no registers, all of a block asked for at once), the next one while this one is
-// multiplied; one barrier a block.  A wave's load brings 8 rows of 128 bytes; the 16-byte pieces of row r lie at place (piece ^ r % 8),
-// so that the 16 rows that a fragment is read from lie in different banks.
+// Blocks of 128 bytes of k of both sides go straight to LDS (no registers), into one of two buffers; rows of 64 bytes, in four smaller
+// buffers, halve the lines that the first-level cache keeps of every line it asks for: 8192 x 8192 x 8192 without any multiplication
+// took 356 us that way.  The fragments of a step of 64 are read while the step before is multiplied, and where those of a block's second
+// step have been read by all waves its buffer is filled again: one barrier a block, two steps for its loads to land.  A wave's load
+// brings 8 rows; the 16-byte pieces of row r lie at place piece ^ r % 8, so that the lanes of a read lie in different banks (a read
+// of 16 bytes a lane goes in turns of 16 lanes, rows 0 .. 3 and 12 .. 15 of one piece with rows 4 .. 11 of the next).
+// A workgroup takes tiles until there are none left, and asks for the next one's first blocks before it writes its outputs.
 template <typename O, int BM, int BN, int WM, int WN>
 __global__ __launch_bounds__(BM / WM * (BN / WN) * 64) void k_i8_product(ProductArgs p)
 {
     constexpr int WAVES = BM / WM * (BN / WN), TM = WM / 16, TN = WN / 16, BK = 128, UNITS = (BM + BN) / 8 / WAVES, BUF = (BM + BN) * BK;
     static_assert(BM / 8 % WAVES == 0 && BN / 8 % WAVES == 0);
     extern __shared__ __align__(1024) int8_t lds[];
+    const int lane = lane_id(), wave = __builtin_amdgcn_readfirstlane(threadIdx.x / 64);
+    const int wm = wave / (BN / WN) * WM, wn = wave % (BN / WN) * WN;
+    const int k_begin = blockIdx.y * p.part_k, k_end = min(p.k, k_begin + p.part_k), blocks = (k_end - k_begin + BK - 1) / BK;
+    const int piece = ((lane & 7) ^ (lane >> 3)) * 16;
+    const uint32_t lds0 = lds_addr(lds);
+
     // Tiles that run at the same time on an XCD share its L2: each has a stretch of the tiles, and takes them in blocks of
     // four rows of tiles.
     const int64_t tiles_m = (p.m + BM - 1) / BM, tiles_n = (p.n + BN - 1) / BN, tiles = tiles_m * tiles_n;
-    const int64_t stretch = (tiles + 7) / 8, tile = (blockIdx.x % 8) * stretch + blockIdx.x / 8;
-    if (blockIdx.x / 8 >= stretch || tile >= tiles) return;
-    const int64_t g = tile / (4 * tiles_n), rest = tile - g * 4 * tiles_n, high = min((int64_t)4, tiles_m - g * 4);
-    const int64_t m0 = (g * 4 + rest % high) * BM, n0 = rest / high * BN;
-    const int lane = lane_id(), wave = __builtin_amdgcn_readfirstlane(threadIdx.x / 64);
-    const int wm = wave / (BN / WN) * WM, wn = wave % (BN / WN) * WN;
-    const int k_begin = blockIdx.y * p.part_k, k_end = min(p.k, k_begin + p.part_k);
-
-    const int piece = ((lane & 7) ^ (lane >> 3)) * 16;
+    const int64_t stretch = (tiles + 7) / 8, tile0 = (blockIdx.x % 8) * stretch, end = min(stretch, tiles - tile0);
+    int64_t tile = blockIdx.x / 8;
+    int64_t m0 = 0, n0 = 0;
     uint32_t off[UNITS];                                // (rows of a tile lie within 2^31 bytes: the host sees to it)
+    const int8_t *ga = p.a, *gb = p.b;
+    auto aim = [&](int64_t t) __attribute__((always_inline)) {
+        t += tile0;
+        const int64_t g = t / (4 * tiles_n), rest = t - g * 4 * tiles_n, high = min((int64_t)4, tiles_m - g * 4);
+        m0 = (g * 4 + rest % high) * BM;
+        n0 = rest / high * BN;
+        ga = p.a + m0 * p.lda;
+        gb = p.b + n0 * p.ldb;
 #pragma unroll
-    for (int i = 0; i < UNITS; ++i) {
-        const int row = (i * WAVES + wave) * 8 + lane / 8;
-        off[i] = (uint32_t)(i * WAVES * 8 < BM ? min((int64_t)row, p.m - 1 - m0) * p.lda : min((int64_t)row - BM, p.n - 1 - n0) * p.ldb) + piece;
-    }
-    const int8_t *ga = p.a + m0 * p.lda, *gb = p.b + n0 * p.ldb;
-    const uint32_t lds0 = lds_addr(lds);
-    auto request = [&](int k0, uint32_t buf) __attribute__((always_inline)) {
-        // (pieces behind the rows' end are the row's first one instead, and are multiplied by 0)
+        for (int i = 0; i < UNITS; ++i) {
+            const int row = (i * WAVES + wave) * 8 + lane / 8;
+            off[i] = (i * WAVES * 8 < BM ? (uint32_t)min((int64_t)row, p.m - 1 - m0) * (uint32_t)p.lda
+                                         : (uint32_t)min((int64_t)row - BM, p.n - 1 - n0) * (uint32_t)p.ldb) + piece;
+        }
+    };
+    auto request = [&](int block) __attribute__((always_inline)) {
+        // (pieces behind the rows' end are the row's first one of the block instead, and are multiplied by 0)
+        const int k0 = k_begin + block * BK;
         const uint32_t back = k0 + piece >= k_end ? piece : 0;
 #pragma unroll
         for (int i = 0; i < UNITS; ++i)
-            lds_dma16((i * WAVES * 8 < BM ? ga : gb) + k0, off[i] - back, lds0 + buf + (i * WAVES + wave) * 1024);
+            lds_dma16((i * WAVES * 8 < BM ? ga : gb) + k0, off[i] - back, lds0 + (block & 1) * BUF + (i * WAVES + wave) * 1024);
     };
 
-    intx4 acc[TM][TN] = {};
-    const int frag = (lane % 16) * BK + (((lane / 16) ^ (lane & 7)) * 16);
-    auto multiply = [&](int k0, uint32_t buf, auto last) __attribute__((always_inline)) {
+    const int frag = (lane % 16) * BK + ((lane / 16) ^ (lane & 7)) * 16;
+    struct Fragments { intx4 a[TM], b[TN]; };
+    auto read = [&](Fragments& f, int block, int ks) __attribute__((always_inline)) {
+        const int8_t* at = lds + ((frag ^ (ks * 64)) + (block & 1) * BUF);
 #pragma unroll
-        for (int ks = 0; ks < 2; ++ks) {
-            const int8_t* f = lds + ((frag ^ (ks * 64)) + buf);
-            intx4 fa[TM], fb[TN];
+        for (int j = 0; j < TN; ++j) f.b[j] = *(const intx4*)(at + (BM + wn + j * 16) * BK);
 #pragma unroll
-            for (int j = 0; j < TN; ++j) fb[j] = *(const intx4*)(f + (BM + wn + j * 16) * BK);
+        for (int i = 0; i < TM; ++i) f.a[i] = *(const intx4*)(at + (wm + i * 16) * BK);
+        const int k0 = k_begin + block * BK + ks * kStep;
+        if (k_end - k0 < kStep) {                       // (uniform: the last block)
+            const int left = k_end - k0 - lane / 16 * 16;
 #pragma unroll
-            for (int i = 0; i < TM; ++i) fa[i] = *(const intx4*)(f + (wm + i * 16) * BK);
-            if (decltype(last)::value) {
-                const int left = k_end - (k0 + ks * kStep + lane / 16 * 16);
+            for (int w = 0; w < 4; ++w) {
+                const int bytes = min(max(left - 4 * w, 0), 4);
+                const int mask = bytes == 4 ? -1 : (1 << (8 * bytes)) - 1;
 #pragma unroll
-                for (int w = 0; w < 4; ++w) {
-                    const int bytes = min(max(left - 4 * w, 0), 4);
-                    const int mask = bytes == 4 ? -1 : (1 << (8 * bytes)) - 1;
-#pragma unroll
-                    for (int j = 0; j < TN; ++j) fb[j][w] &= mask;
-                }
+                for (int j = 0; j < TN; ++j) f.b[j][w] &= mask;
             }
-#pragma unroll
-            for (int j = 0; j < TN; ++j)
-#pragma unroll
-                for (int i = 0; i < TM; ++i) acc[i][j] = __builtin_amdgcn_mfma_i32_16x16x64_i8(fb[j], fa[i], acc[i][j], 0, 0, 0);
         }
     };
-
-    request(k_begin, 0);
-    uint32_t buf = 0;
-    int k0 = k_begin;
-    for (; k0 + BK < k_end; k0 += BK) {
-        wait_vmcnt<0>();
-        __syncthreads();                                // this block has landed, and nobody reads the other one any more
-        request(k0 + BK, buf ^ BUF);
-        multiply(k0, buf, std::false_type{});
-        buf ^= BUF;
-    }
-    wait_vmcnt<0>();
-    __syncthreads();
-    multiply(k0, buf, std::true_type{});
-
+    intx4 acc[TM][TN];
+    auto multiply = [&](const Fragments& f) __attribute__((always_inline)) {
 #pragma unroll
-    for (int j = 0; j < TN; ++j) {
-        const int64_t col = n0 + wn + j * 16 + lane / 16 * 4;
+        for (int j = 0; j < TN; ++j)
+#pragma unroll
+            for (int i = 0; i < TM; ++i) acc[i][j] = __builtin_amdgcn_mfma_i32_16x16x64_i8(f.b[j], f.a[i], acc[i][j], 0, 0, 0);
+    };
+    // everything asked for has landed, everything read is in registers: of all waves
+    auto meet = [&]() __attribute__((always_inline)) {
+        wait_vmcnt<0>();
+        asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
+        __builtin_amdgcn_s_barrier();
+        asm volatile("" ::: "memory");
+    };
+
+    if (tile >= end) return;
+    aim(tile);
+    request(0);
+    for (;;) {
+        Fragments f0, f1;
+        meet();
+        if (blocks > 1) request(1);
+        read(f0, 0, 0);
+#pragma unroll
+        for (int i = 0; i < TM; ++i)
+#pragma unroll
+            for (int j = 0; j < TN; ++j) acc[i][j] = intx4{0, 0, 0, 0};
+        for (int b = 0; b < blocks; ++b) {
+            read(f1, b, 1);
+            multiply(f0);
+            meet();                                     // (nobody reads this block's buffer any more, the next block has landed)
+            if (b + 2 < blocks) request(b + 2);
+            if (b + 1 < blocks) read(f0, b + 1, 0);
+            multiply(f1);
+        }
+        const int64_t mt = m0, nt = n0;
+        tile += gridDim.x / 8;
+        const bool more = tile < end;
+        if (more) {
+            aim(tile);
+            request(0);                                 // (both buffers are free since the last meeting)
+        }
+
         if (p.parts > 1) {
 #pragma unroll
             for (int i = 0; i < TM; ++i) {
-                const int64_t row = m0 + wm + i * 16 + lane % 16;
-                if (row < p.m)
-                    for (int e = 0; e < 4; ++e)
-                        if (col + e < p.n) p.sums[((int64_t)blockIdx.y * p.m + row) * p.n + col + e] = acc[i][j][e];
-            }
-            continue;
-        }
-        const floatx4 sb = load_four(p.b_scale, col, p.n), bias = p.bias ? load_four(p.bias, col, p.n) : floatx4{};
+                const int64_t row = mt + wm + i * 16 + lane % 16;
 #pragma unroll
-        for (int i = 0; i < TM; ++i) {
-            const int64_t row = m0 + wm + i * 16 + lane % 16;
-            if (row < p.m) store_outputs<O>(p, row, col, acc[i][j], p.a_scale[row], sb, bias);
+                for (int j = 0; j < TN; ++j) {
+                    const int64_t col = nt + wn + j * 16 + lane / 16 * 4;
+                    int* at = p.sums + ((int64_t)blockIdx.y * p.m + row) * p.n + col;
+                    if (row < p.m && col + 4 <= p.n) __builtin_memcpy(at, &acc[i][j], 16);
+                    else if (row < p.m)
+                        for (int e = 0; e < 4; ++e)
+                            if (col + e < p.n) at[e] = acc[i][j][e];
+                }
+            }
+        } else {
+            floatx4 sb[TN], bias[TN];
+            float sa[TM];
+#pragma unroll
+            for (int i = 0; i < TM; ++i) sa[i] = p.a_scale[min(mt + wm + i * 16 + lane % 16, p.m - 1)];
+#pragma unroll
+            for (int j = 0; j < TN; ++j) {
+                const int64_t col = nt + wn + j * 16 + lane / 16 * 4;
+                sb[j] = load_four(p.b_scale, col, p.n);
+                bias[j] = p.bias ? load_four(p.bias, col, p.n) : floatx4{};
+            }
+#pragma unroll
+            for (int i = 0; i < TM; ++i) {
+                const int64_t row = mt + wm + i * 16 + lane % 16;
+#pragma unroll
+                for (int j = 0; j < TN; ++j)
+                    if (row < p.m) store_outputs<O>(p, row, nt + wn + j * 16 + lane / 16 * 4, acc[i][j], sa[i], sb[j], bias[j]);
+            }
         }
+        if (!more) break;
     }
 }
 
@@ -549,7 +598,7 @@ static hipError_t launch_tiles(const Tiling& t, ProductArgs p, hipStream_t s)
         const size_t lds = (size_t)(t.bm + t.bn) * 128 * 2;
         const int64_t tiles = (p.m + t.bm - 1) / t.bm * ((p.n + t.bn - 1) / t.bn);
         if (lds > kStaticLds) e = hipFuncSetAttribute((const void*)kernel, hipFuncAttributeMaxDynamicSharedMemorySize, (int)lds);
-        if (e == hipSuccess) hipLaunchKernelGGL(kernel, dim3((unsigned)((tiles + 7) / 8 * 8), t.parts), dim3(waves * 64), lds, s, p);
+        if (e == hipSuccess) hipLaunchKernelGGL(kernel, dim3((unsigned)(std::min((tiles + 7) / 8, (int64_t)kCus / 8 * (lds <= 80 * 1024 ? 2 : 1)) * 8), t.parts), dim3(waves * 64), lds, s, p);
     };
     p.parts = t.parts;
     p.part_k = t.part_k;
