@@ -15,6 +15,7 @@ constexpr int kStaticLds = 64 * 1024;                    // what a launch may as
 struct QuantizeArgs {
     const void* x; int64_t ldx, m; int k;
     int8_t* q; int64_t ldq; float* scale;
+    int padded;                                          // places that a row has in q, those behind k to be zeros
 };
 
 // ---- quantisation.  Rows are taken in pieces of 16 elements: 16 bytes of the result.
@@ -77,7 +78,6 @@ __global__ __launch_bounds__(256) void k_quantize(QuantizeArgs a)
     __shared__ uint32_t part[4];
     const int t = threadIdx.x % THREADS;
     const int npieces = (a.k + 15) / 16;
-    const int padded = (int)min((int64_t)(a.k + 63) / 64 * 64, a.ldq);
     const bool whole = a.ldq % 16 == 0 && (uintptr_t)a.q % 16 == 0;
     for (int64_t r0 = (int64_t)blockIdx.x * ROWS; r0 < a.m; r0 += (int64_t)gridDim.x * ROWS) {
         const int64_t r = r0 + threadIdx.x / THREADS;
@@ -113,15 +113,15 @@ __global__ __launch_bounds__(256) void k_quantize(QuantizeArgs a)
                 if (!in || p >= npieces) continue;
                 if (!held) load_piece(row, p * 16, a.k, v[i]);
                 const u32x4 w = quant_piece(v[i], scale);
-                if (whole && p * 16 + 16 <= padded) {
+                if (whole && p * 16 + 16 <= a.padded) {
                     *(u32x4*)(q + p * 16) = w;
                 } else {
                     for (int e = 0; e < 16; ++e)
-                        if (p * 16 + e < padded) q[p * 16 + e] = (int8_t)(w[e / 4] >> (8 * (e % 4)));
+                        if (p * 16 + e < a.padded) q[p * 16 + e] = (int8_t)(w[e / 4] >> (8 * (e % 4)));
                 }
             }
         }
-        for (int b = npieces * 16 + t; in && b < padded; b += THREADS) q[b] = 0;
+        for (int b = npieces * 16 + t; in && b < a.padded; b += THREADS) q[b] = 0;
     }
 }
 
@@ -144,7 +144,7 @@ struct ProductArgs {
 
 // Four neighbouring outputs: the exact sums, scaled, with the bias, rounded once.
 template <typename O>
-__device__ __forceinline__ void store_outputs(const ProductArgs& p, int64_t row, int64_t col, intx4 sum, float sa, floatx4 sb, floatx4 bias)
+__device__ __forceinline__ void store_outputs(const ProductArgs& p, int64_t row, int64_t col, intx4 sum, float sa, floatx4 sb, floatx4 bias, bool whole = false)
 {
     typedef O out4 __attribute__((ext_vector_type(4)));
     out4 o;
@@ -154,7 +154,7 @@ __device__ __forceinline__ void store_outputs(const ProductArgs& p, int64_t row,
         o[e] = (O)(p.bias ? fmaf(v, sb[e], bias[e]) : v * sb[e]);
     }
     O* at = (O*)p.out + row * p.ldo + col;
-    if (col + 4 <= p.n) {
+    if (whole || col + 4 <= p.n) {
         __builtin_memcpy(at, &o, sizeof o);
     } else {
 #pragma unroll
@@ -188,6 +188,16 @@ __device__ __forceinline__ u32x4 load16(const int8_t* row, int t, int k)
         v = u32x4{w[0], w[1], w[2], w[3]};
     }
     return v;
+}
+
+// rows of a, copied with zeros behind them
+__global__ __launch_bounds__(256) void k_i8_pad(const int8_t* a, int64_t lda, int64_t m, int k, int8_t* q, int64_t ldq)
+{
+    const int64_t pieces = ldq / 16;
+    for (int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x; i < m * pieces; i += (int64_t)gridDim.x * 256) {
+        const int64_t r = i / pieces;
+        *(u32x4*)(q + i * 16) = load16(a + r * lda, (int)(i - r * pieces) * 16, k);
+    }
 }
 
 // ---- rows of any alignment: tiles of 64 x 64 outputs, four waves of 32 x 32, blocks of 64 bytes of k staged through registers
@@ -235,12 +245,18 @@ __global__ __launch_bounds__(256) void k_i8_product_any(ProductArgs p)
 // step have been read by all waves its buffer is filled again: one barrier a block, two steps for its loads to land.  A wave's load
 // brings 8 rows; the 16-byte pieces of row r lie at place piece ^ r % 8, so that the lanes of a read lie in different banks (a read
 // of 16 bytes a lane goes in turns of 16 lanes, rows 0 .. 3 and 12 .. 15 of one piece with rows 4 .. 11 of the next).
-// A workgroup takes tiles until there are none left, and asks for the next one's first blocks before it writes its outputs.
+// Rows of a are a multiple of 128 bytes long, with zeros behind k.
+// A workgroup takes tiles until there are none left.  It asks for the next one's first two blocks before it writes its outputs, and
+// waits for those blocks only: the outputs have two blocks' time to be written.  Scales and bias come to LDS with a tile's blocks
+// (SCALES; 64 x 256 leaves no room for them beside a second workgroup).
+// bytes of LDS for scales and bias
+__host__ __device__ constexpr int tile_scales(int bm, int bn) { return bm == 64 ? 0 : (bm + 2 * bn) * 4; }
 template <typename O, int BM, int BN, int WM, int WN>
 __global__ __launch_bounds__(BM / WM * (BN / WN) * 64) void k_i8_product(ProductArgs p)
 {
     constexpr int WAVES = BM / WM * (BN / WN), TM = WM / 16, TN = WN / 16, BK = 128, UNITS = (BM + BN) / 8 / WAVES, BUF = (BM + BN) * BK;
     static_assert(BM / 8 % WAVES == 0 && BN / 8 % WAVES == 0);
+    constexpr bool SCALES = tile_scales(BM, BN) > 0;
     extern __shared__ __align__(1024) int8_t lds[];
     const int lane = lane_id(), wave = __builtin_amdgcn_readfirstlane(threadIdx.x / 64);
     const int wm = wave / (BN / WN) * WM, wn = wave % (BN / WN) * WN;
@@ -250,129 +266,129 @@ __global__ __launch_bounds__(BM / WM * (BN / WN) * 64) void k_i8_product(Product
 
     // Tiles that run at the same time on an XCD share its L2: each has a stretch of the tiles, and takes them in blocks of
     // four rows of tiles.
-    const int64_t tiles_m = (p.m + BM - 1) / BM, tiles_n = (p.n + BN - 1) / BN, tiles = tiles_m * tiles_n;
-    const int64_t stretch = (tiles + 7) / 8, tile0 = (blockIdx.x % 8) * stretch, end = min(stretch, tiles - tile0);
-    int64_t tile = blockIdx.x / 8;
-    int64_t m0 = 0, n0 = 0;
+    const int m = (int)p.m, n = (int)p.n, tiles_m = (m + BM - 1) / BM, tiles_n = (n + BN - 1) / BN, tiles = tiles_m * tiles_n;
+    const int stretch = (tiles + 7) / 8, tile0 = (int)(blockIdx.x % 8) * stretch, end = min(stretch, tiles - tile0);
+    int tile = blockIdx.x / 8, m0 = 0, n0 = 0;
     uint32_t off[UNITS];                                // (rows of a tile lie within 2^31 bytes: the host sees to it)
     const int8_t *ga = p.a, *gb = p.b;
-    auto aim = [&](int64_t t) __attribute__((always_inline)) {
+    auto aim = [&](int t) __attribute__((always_inline)) {
         t += tile0;
-        const int64_t g = t / (4 * tiles_n), rest = t - g * 4 * tiles_n, high = min((int64_t)4, tiles_m - g * 4);
+        const int g = t / (4 * tiles_n), rest = t - g * 4 * tiles_n, high = min(4, tiles_m - g * 4);
         m0 = (g * 4 + rest % high) * BM;
         n0 = rest / high * BN;
-        ga = p.a + m0 * p.lda;
-        gb = p.b + n0 * p.ldb;
+        ga = p.a + (int64_t)m0 * p.lda;
+        gb = p.b + (int64_t)n0 * p.ldb;
 #pragma unroll
         for (int i = 0; i < UNITS; ++i) {
             const int row = (i * WAVES + wave) * 8 + lane / 8;
-            off[i] = (i * WAVES * 8 < BM ? (uint32_t)min((int64_t)row, p.m - 1 - m0) * (uint32_t)p.lda
-                                         : (uint32_t)min((int64_t)row - BM, p.n - 1 - n0) * (uint32_t)p.ldb) + piece;
+            off[i] = (i * WAVES * 8 < BM ? (uint32_t)min(row, m - 1 - m0) * (uint32_t)p.lda
+                                         : (uint32_t)min(row - BM, n - 1 - n0) * (uint32_t)p.ldb) + piece;
         }
     };
     auto request = [&](int block) __attribute__((always_inline)) {
-        // (pieces behind the rows' end are the row's first one of the block instead, and are multiplied by 0)
+        // (pieces of b behind the rows' end are the row's first one of the block instead: rows of a are zeros there)
         const int k0 = k_begin + block * BK;
         const uint32_t back = k0 + piece >= k_end ? piece : 0;
 #pragma unroll
         for (int i = 0; i < UNITS; ++i)
-            lds_dma16((i * WAVES * 8 < BM ? ga : gb) + k0, off[i] - back, lds0 + (block & 1) * BUF + (i * WAVES + wave) * 1024);
+            lds_dma16((i * WAVES * 8 < BM ? ga : gb) + k0, i * WAVES * 8 < BM ? off[i] : off[i] - back, lds0 + (block & 1) * BUF + (i * WAVES + wave) * 1024);
     };
 
     const int frag = (lane % 16) * BK + ((lane / 16) ^ (lane & 7)) * 16;
-    struct Fragments { intx4 a[TM], b[TN]; };
-    auto read = [&](Fragments& f, int block, int ks) __attribute__((always_inline)) {
-        const int8_t* at = lds + ((frag ^ (ks * 64)) + (block & 1) * BUF);
+    intx4 acc[TM][TN], a[TM], b0[TN], b1[TN];
+    auto place = [&](int block, int ks) __attribute__((always_inline)) { return lds + ((frag ^ (ks * 64)) + (block & 1) * BUF); };
+    auto read_b = [&](intx4* f, int block, int ks) __attribute__((always_inline)) {
+        const int8_t* at = place(block, ks) + (BM + wn) * BK;
 #pragma unroll
-        for (int j = 0; j < TN; ++j) f.b[j] = *(const intx4*)(at + (BM + wn + j * 16) * BK);
+        for (int j = 0; j < TN; ++j) f[j] = *(const intx4*)(at + j * 16 * BK);
+    };
+    // one step: fragments a and b; where a fragment of a has been used for the last time the next step's takes its registers
+    auto step = [&](const intx4* b, const int8_t* next) __attribute__((always_inline)) {
 #pragma unroll
-        for (int i = 0; i < TM; ++i) f.a[i] = *(const intx4*)(at + (wm + i * 16) * BK);
-        const int k0 = k_begin + block * BK + ks * kStep;
-        if (k_end - k0 < kStep) {                       // (uniform: the last block)
-            const int left = k_end - k0 - lane / 16 * 16;
+        for (int i = 0; i < TM; ++i) {
 #pragma unroll
-            for (int w = 0; w < 4; ++w) {
-                const int bytes = min(max(left - 4 * w, 0), 4);
-                const int mask = bytes == 4 ? -1 : (1 << (8 * bytes)) - 1;
-#pragma unroll
-                for (int j = 0; j < TN; ++j) f.b[j][w] &= mask;
-            }
+            for (int j = 0; j < TN; ++j) acc[i][j] = __builtin_amdgcn_mfma_i32_16x16x64_i8(b[j], a[i], acc[i][j], 0, 0, 0);
+            a[i] = *(const intx4*)(next + (wm + i * 16) * BK);
         }
     };
-    intx4 acc[TM][TN];
-    auto multiply = [&](const Fragments& f) __attribute__((always_inline)) {
-#pragma unroll
-        for (int j = 0; j < TN; ++j)
-#pragma unroll
-            for (int i = 0; i < TM; ++i) acc[i][j] = __builtin_amdgcn_mfma_i32_16x16x64_i8(f.b[j], f.a[i], acc[i][j], 0, 0, 0);
-    };
-    // everything asked for has landed, everything read is in registers: of all waves
-    auto meet = [&]() __attribute__((always_inline)) {
-        wait_vmcnt<0>();
+    // Everything asked for has landed, everything read is in registers: of all waves.  stores: but for the TM TN stores of a whole
+    // tile that were enqueued behind the blocks.
+    auto meet = [&](bool stores) __attribute__((always_inline)) {
+        if (stores) wait_vmcnt<TM * TN>();
+        else wait_vmcnt<0>();
         asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
         __builtin_amdgcn_s_barrier();
         asm volatile("" ::: "memory");
     };
 
+    float* const scales = (float*)(lds + 2 * BUF);      // of BM rows a, of BN rows b, BN of the bias
+    auto request_scales = [&]() __attribute__((always_inline)) {
+#pragma unroll
+        for (int i = 0; i < (BM + 2 * BN) / 64; i += WAVES) {
+            const int u = i + wave;                     // 64 numbers each
+            if (u >= (p.bias ? BM + 2 * BN : BM + BN) / 64) continue;
+            const bool of_a = u < BM / 64;
+            const int at = of_a ? m0 + u * 64 : n0 + (u - BM / 64) % (BN / 64) * 64, last = (of_a ? m : n) - 1;
+            const float* from = of_a ? p.a_scale : (u < (BM + BN) / 64 ? p.b_scale : p.bias);
+            const int first = min(at, last);
+            lds_dma4(from + first, (uint32_t)min(lane, last - first) * 4, lds0 + 2 * BUF + u * 256);
+        }
+    };
+
     if (tile >= end) return;
     aim(tile);
     request(0);
+    if (blocks > 1) request(1);
+    bool stores = false;
     for (;;) {
-        Fragments f0, f1;
-        meet();
-        if (blocks > 1) request(1);
-        read(f0, 0, 0);
+        meet(stores);
+        if (SCALES && p.parts == 1) request_scales();
+        read_b(b0, 0, 0);
+#pragma unroll
+        for (int i = 0; i < TM; ++i) a[i] = *(const intx4*)(place(0, 0) + (wm + i * 16) * BK);
 #pragma unroll
         for (int i = 0; i < TM; ++i)
 #pragma unroll
             for (int j = 0; j < TN; ++j) acc[i][j] = intx4{0, 0, 0, 0};
         for (int b = 0; b < blocks; ++b) {
-            read(f1, b, 1);
-            multiply(f0);
-            meet();                                     // (nobody reads this block's buffer any more, the next block has landed)
+            read_b(b1, b, 1);
+            step(b0, place(b, 1));
+            meet(stores && b == 0 && blocks > 2);       // (nobody reads this block's buffer any more, the next block has landed)
             if (b + 2 < blocks) request(b + 2);
-            if (b + 1 < blocks) read(f0, b + 1, 0);
-            multiply(f1);
+            read_b(b0, b + 1, 0);                       // (behind the last block: whatever the buffer holds, not multiplied)
+            step(b1, place(b + 1, 0));
         }
-        const int64_t mt = m0, nt = n0;
+        const int mt = m0, nt = n0;
         tile += gridDim.x / 8;
         const bool more = tile < end;
         if (more) {
             aim(tile);
             request(0);                                 // (both buffers are free since the last meeting)
+            if (blocks > 1) request(1);
         }
+        stores = mt + BM <= m && nt + BN <= n;
 
-        if (p.parts > 1) {
 #pragma unroll
-            for (int i = 0; i < TM; ++i) {
-                const int64_t row = mt + wm + i * 16 + lane % 16;
-#pragma unroll
-                for (int j = 0; j < TN; ++j) {
-                    const int64_t col = nt + wn + j * 16 + lane / 16 * 4;
-                    int* at = p.sums + ((int64_t)blockIdx.y * p.m + row) * p.n + col;
-                    if (row < p.m && col + 4 <= p.n) __builtin_memcpy(at, &acc[i][j], 16);
-                    else if (row < p.m)
-                        for (int e = 0; e < 4; ++e)
-                            if (col + e < p.n) at[e] = acc[i][j][e];
-                }
-            }
-        } else {
-            floatx4 sb[TN], bias[TN];
-            float sa[TM];
-#pragma unroll
-            for (int i = 0; i < TM; ++i) sa[i] = p.a_scale[min(mt + wm + i * 16 + lane % 16, p.m - 1)];
+        for (int i = 0; i < TM; ++i) {
+            const int row = mt + wm + i * 16 + lane % 16;
+            if (!stores && row >= m) continue;
+            float sa = 0.0f;
+            if (p.parts == 1) sa = SCALES ? scales[wm + i * 16 + lane % 16] : p.a_scale[row];
 #pragma unroll
             for (int j = 0; j < TN; ++j) {
-                const int64_t col = nt + wn + j * 16 + lane / 16 * 4;
-                sb[j] = load_four(p.b_scale, col, p.n);
-                bias[j] = p.bias ? load_four(p.bias, col, p.n) : floatx4{};
-            }
-#pragma unroll
-            for (int i = 0; i < TM; ++i) {
-                const int64_t row = mt + wm + i * 16 + lane % 16;
-#pragma unroll
-                for (int j = 0; j < TN; ++j)
-                    if (row < p.m) store_outputs<O>(p, row, nt + wn + j * 16 + lane / 16 * 4, acc[i][j], sa[i], sb[j], bias[j]);
+                const int col = nt + wn + j * 16 + lane / 16 * 4;
+                if (p.parts > 1) {
+                    int* at = p.sums + ((int64_t)blockIdx.y * m + row) * n + col;
+                    if (stores || col + 4 <= n) __builtin_memcpy(at, &acc[i][j], 16);
+                    else
+                        for (int e = 0; e < 4; ++e)
+                            if (col + e < n) at[e] = acc[i][j][e];
+                    continue;
+                }
+                const float* sb = scales + BM + wn + j * 16 + lane / 16 * 4;
+                const floatx4 sb4 = SCALES ? *(const floatx4*)sb : load_four(p.b_scale, col, p.n);
+                const floatx4 bias = !p.bias ? floatx4{} : (SCALES ? *(const floatx4*)(sb + BN) : load_four(p.bias, col, p.n));
+                store_outputs<O>(p, row, col, acc[i][j], sa, sb4, bias, stores);
             }
         }
         if (!more) break;
@@ -595,7 +611,7 @@ static hipError_t launch_tiles(const Tiling& t, ProductArgs p, hipStream_t s)
 {
     hipError_t e = hipSuccess;
     auto go = [&](auto kernel, int waves) {
-        const size_t lds = (size_t)(t.bm + t.bn) * 128 * 2;
+        const size_t lds = (size_t)(t.bm + t.bn) * 128 * 2 + tile_scales(t.bm, t.bn);
         const int64_t tiles = (p.m + t.bm - 1) / t.bm * ((p.n + t.bn - 1) / t.bn);
         if (lds > kStaticLds) e = hipFuncSetAttribute((const void*)kernel, hipFuncAttributeMaxDynamicSharedMemorySize, (int)lds);
         if (e == hipSuccess) hipLaunchKernelGGL(kernel, dim3((unsigned)(std::min((tiles + 7) / 8, (int64_t)kCus / 8 * (lds <= 80 * 1024 ? 2 : 1)) * 8), t.parts), dim3(waves * 64), lds, s, p);
@@ -615,12 +631,26 @@ static hipError_t launch_tiles(const Tiling& t, ProductArgs p, hipStream_t s)
 // rows that requests of 16 bytes reach; offsets inside a tile are 32-bit numbers
 static bool in_tiles(const void* p, int64_t ld) { return (uintptr_t)p % 16 == 0 && ld % 16 == 0 && ld < (1 << 22); }
 
-static hipError_t launch_product(int dtype, const ProductArgs& p, hipStream_t s)
+static int64_t padded_k(int64_t k) { return (k + 127) / 128 * 128; }
+
+// padded: room for the rows of a at multiples of 128 bytes (or those rows themselves)
+static hipError_t launch_product(int dtype, const ProductArgs& p, int8_t* padded, hipStream_t s)
 {
     return with_type(dtype, [&](auto o) -> hipError_t {
         using O = decltype(o);
         if (few_rows(p.m, p.k) && in_tiles(p.b, p.ldb)) return launch_few<O, int8_t>(p, s);
-        if (in_tiles(p.a, p.lda) && in_tiles(p.b, p.ldb)) return launch_tiles<O>(tiling_for(p.m, p.n, p.k), p, s);
+        if (in_tiles(p.b, p.ldb)) {
+            ProductArgs t = p;
+            if (p.k % 128 || !in_tiles(p.a, p.lda)) {
+                t.a = padded;
+                t.lda = padded_k(p.k);
+                if (t.a != p.a) {
+                    const int64_t want = (p.m * (t.lda / 16) + 255) / 256;
+                    hipLaunchKernelGGL(k_i8_pad, dim3((unsigned)(want < (1 << 20) ? want : 1 << 20)), dim3(256), 0, s, p.a, p.lda, p.m, p.k, padded, t.lda);
+                }
+            }
+            return launch_tiles<O>(tiling_for(p.m, p.n, p.k), t, s);
+        }
         hipLaunchKernelGGL(k_i8_product_any<O>, dim3((unsigned)((p.m + 63) / 64 * ((p.n + 63) / 64))), dim3(256), 0, s, p);
         return hipGetLastError();
     });
@@ -646,13 +676,12 @@ static int check_shape(int64_t m, int64_t n, int64_t k)
     if (m < 0 || m > (1 << 24)) return fail(HR_ERR_ARG, "m=%lld out of range", (long long)m);
     if (n < 0 || n > (1LL << 31) - 1) return fail(HR_ERR_ARG, "n=%lld out of range", (long long)n);
     if (k < 1 || k > HR_I8_K_MAX) return fail(HR_ERR_ARG, "k=%lld must be in 1..%d", (long long)k, HR_I8_K_MAX);
-    // (tiles of 64 x 64 outputs, and a launch may not have 2^32 threads)
-    if ((m + 63) / 64 * ((n + 63) / 64) >= (1LL << 24)) return fail(HR_ERR_UNSUPPORTED, "m=%lld x n=%lld: more outputs than one call takes", (long long)m, (long long)n);
+    // (tiles of 64 x 64 outputs, and a launch may not have 2^32 threads; numbers of rows and tiles fit 32 bits)
+    if (n > (1LL << 30) || (m + 63) / 64 * ((n + 63) / 64) >= (1LL << 24)) return fail(HR_ERR_UNSUPPORTED, "m=%lld x n=%lld: more outputs than one call takes", (long long)m, (long long)n);
     return HR_OK;
 }
 
-// workspace: the quantised rows of hr_i8_linear, their scales, sums of the parts of k
-static int64_t padded_k(int64_t k) { return (k + 63) / 64 * 64; }
+// workspace: rows a as the tiles want them (quantised ones, or copied ones), their scales, sums of the parts of k
 static size_t aligned(size_t bytes) { return (bytes + HR_WORKSPACE_ALIGN - 1) / HR_WORKSPACE_ALIGN * HR_WORKSPACE_ALIGN; }
 static size_t rows_bytes(int64_t m, int64_t k) { return aligned((size_t)(m * padded_k(k))); }
 static size_t scales_bytes(int64_t m) { return aligned((size_t)m * 4); }
@@ -668,7 +697,7 @@ int hr_i8_quantize(const void* x, int64_t ldx, int32_t dtype, int64_t m, int64_t
     if (int rc = check_matrix("q", q, m, k, ldq, 1)) return rc;
     if (m == 0) return HR_OK;
     if (!scale) return fail(HR_ERR_ARG, "scale is null");
-    QuantizeArgs a{x, ldx, m, (int)k, q, ldq, scale};
+    QuantizeArgs a{x, ldx, m, (int)k, q, ldq, scale, (int)std::min((k + 63) / 64 * 64, ldq)};
     HR_HIP(launch_quantize(dtype, a, (hipStream_t)stream));
     return HR_OK;
 }
@@ -698,7 +727,7 @@ int hr_i8_product(const int8_t* a, int64_t lda, const float* a_scale, const int8
     if (int rc = check_workspace(workspace, workspace_bytes, hr_i8_workspace_bytes(m, n, k))) return rc;
     ProductArgs p{a, lda, a_scale, b, ldb, b_scale, bias, m, n, (int)k, out, ldo};
     p.sums = (int*)((char*)workspace + rows_bytes(m, k) + scales_bytes(m));
-    HR_HIP(launch_product(out_dtype, p, (hipStream_t)stream));
+    HR_HIP(launch_product(out_dtype, p, (int8_t*)workspace, (hipStream_t)stream));
     return HR_OK;
 }
 
@@ -724,11 +753,11 @@ int hr_i8_linear(const void* x, int64_t ldx, int32_t x_dtype, const int8_t* b, i
         HR_HIP(with_type(out_dtype, [&](auto o) { return with_type(x_dtype, [&](auto e) { return launch_few<decltype(o), decltype(e)>(p, (hipStream_t)stream); }); }));
         return HR_OK;
     }
-    QuantizeArgs qa{x, ldx, m, (int)k, q, padded_k(k), scale};
+    QuantizeArgs qa{x, ldx, m, (int)k, q, padded_k(k), scale, (int)padded_k(k)};
     HR_HIP(launch_quantize(x_dtype, qa, (hipStream_t)stream));
     ProductArgs p{q, padded_k(k), scale, b, ldb, b_scale, bias, m, n, (int)k, out, ldo};
     p.sums = (int*)((char*)scale + scales_bytes(m));
-    HR_HIP(launch_product(out_dtype, p, (hipStream_t)stream));
+    HR_HIP(launch_product(out_dtype, p, q, (hipStream_t)stream));
     return HR_OK;
 }
 
