@@ -24,14 +24,15 @@ __device__ __forceinline__ uint64_t entry_key(float z, int i) { return (uint64_t
 
 template <int THREADS>
 struct TopShared {
-    static constexpr int kCap = THREADS >= 256 ? 1024 : 512;      // a chunk has to fit in beside HR_K_MAX kept entries
+    // (one wave takes up to 32 entries: as little LDS as lets 28 of them share a compute unit)
+    static constexpr int kMost = THREADS >= 256 ? HR_K_MAX : 32, kCap = THREADS >= 256 ? 1024 : 256;      // a chunk has to fit in beside kMost kept entries
     static constexpr int kAll = kCap + 1, kGroups = 512;
     Slots<THREADS> slots;
     uint16_t picked[Slots<THREADS>::kPer * THREADS];
     uint64_t key[kCap];
-    uint64_t best[HR_K_MAX];
+    uint64_t best[kMost];
     uint64_t bound;                     // entries at or below it are not among the best
-    uint32_t group[kGroups];
+    uint32_t group[THREADS == 64 ? 1 : kGroups];         // (with 64 threads every slot is a group)
     int wave[THREADS / 64];
     int npicked, fill, ties;
     int valid[2];                       // by turns: keys that there was room for, or kAll where that was all of a round's
@@ -222,10 +223,7 @@ __device__ int best_entries(const Row<T>& row, int span, int k, TopShared<THREAD
 #pragma unroll
     for (int i = 0; i < PER; ++i) mine[i] = t.slots.key[i][threadIdx.x];
     // the groups' maxima: a thread's slots one by one, four of them, or all of two neighbours
-    if (THREADS == 64) {
-#pragma unroll
-        for (int i = 0; i < PER; ++i) t.group[i * 64 + threadIdx.x] = mine[i];
-    } else {
+    if (THREADS > 64) {
         uint32_t a = max(max(mine[0], mine[1]), max(mine[2], mine[3]));
         if (THREADS == 1024) {
             a = max(a, (uint32_t)__builtin_amdgcn_update_dpp(0, (int)a, 0xb1, 0xf, 0xf, false));      // lane ^ 1
@@ -240,7 +238,7 @@ __device__ int best_entries(const Row<T>& row, int span, int k, TopShared<THREAD
         constexpr int N = TopShared<THREADS>::kGroups / 64;
         uint32_t g[N];
 #pragma unroll
-        for (int i = 0; i < N; ++i) g[i] = t.group[i * 64 + lane_id()];
+        for (int i = 0; i < N; ++i) g[i] = THREADS == 64 ? mine[i % PER] : t.group[i * 64 + lane_id()];
         bool ties;
         // (256 groups are enough for few, and their bound is found in 2 us less)
         uint32_t bound;
@@ -505,12 +503,17 @@ __global__ __launch_bounds__(THREADS) void k_distill_backward(DistillArgs a)
 // ---- launches
 static unsigned row_grid(int64_t rows) { return (unsigned)(rows < (1 << 20) ? rows : 1 << 20); }      // (a launch may not have 2^32 threads)
 
-// Threads of the workgroup that takes a row: four chunks of it or more for each.
-static int row_threads(int dtype, int64_t n, int k = 0)
+// Threads of the workgroup that takes a row (us a call with 64, 256, 1024 threads; 20 alternatives unless it says otherwise):
+//   64    rows of a few chunks a lane, or many short rows, where what a row takes besides its scores is least with one wave: 4096 rows of
+//         2000 float32 23, 36, 128, 2048 of 8192 23, 26, 68; 1024 of 8192 17.6, 15.6
+//   1024  few long rows: each has a compute unit for itself.  One row of 131072 float32 101, 27, 17.5, 64 rows 105, 29, 18; 256 of 32768 35, 14, 14
+//   256   the others: 1024 rows of 131072 139, 103, 120
+static int row_threads(int dtype, int64_t rows, int64_t n, int k)
 {
-    const int64_t chunks = n * (int64_t)element_bytes(dtype) / 16;
     if (const char* e = getenv("HR_T")) return atoi(e);
-    return chunks <= 256 && k <= 32 ? 64 : (chunks <= 2048 ? 256 : 1024);
+    const int64_t chunks = n * (int64_t)element_bytes(dtype) / 16;
+    if (k <= 32 && (chunks <= 256 || (chunks <= 2048 && rows >= 1536))) return 64;
+    return chunks >= 4096 && rows < 256 ? 1024 : 256;
 }
 
 // f(element, threads) with the type and the number as compile-time values
@@ -532,7 +535,7 @@ static void with_row_type(int dtype, int threads, F&& f)
 
 static hipError_t launch_logprobs(int dtype, const LogprobsArgs& a, hipStream_t s)
 {
-    with_row_type(dtype, row_threads(dtype, a.n, a.k), [&](auto e, auto threads) {
+    with_row_type(dtype, row_threads(dtype, a.rows, a.n, a.k), [&](auto e, auto threads) {
         if (a.k > 0) HR_ROWS_LAUNCH((k_logprobs<decltype(e), decltype(threads)::value, true>));
         else HR_ROWS_LAUNCH((k_logprobs<decltype(e), decltype(threads)::value, false>));
     });
@@ -540,22 +543,22 @@ static hipError_t launch_logprobs(int dtype, const LogprobsArgs& a, hipStream_t 
 }
 static hipError_t launch_logprobs_backward(int dtype, const LogprobsBackwardArgs& a, hipStream_t s)
 {
-    with_row_type(dtype, row_threads(dtype, a.n), [&](auto e, auto threads) { HR_ROWS_LAUNCH((k_logprobs_backward<decltype(e), decltype(threads)::value>)); });
+    with_row_type(dtype, row_threads(dtype, a.rows, a.n, 0), [&](auto e, auto threads) { HR_ROWS_LAUNCH((k_logprobs_backward<decltype(e), decltype(threads)::value>)); });
     return hipGetLastError();
 }
 static hipError_t launch_distill(int dtype, const DistillArgs& a, hipStream_t s)
 {
-    with_row_type(dtype, row_threads(dtype, a.n), [&](auto e, auto threads) { HR_ROWS_LAUNCH((k_distill<decltype(e), decltype(threads)::value, false>)); });
+    with_row_type(dtype, row_threads(dtype, a.rows, a.n, 0), [&](auto e, auto threads) { HR_ROWS_LAUNCH((k_distill<decltype(e), decltype(threads)::value, false>)); });
     return hipGetLastError();
 }
 static hipError_t launch_distill_step(int dtype, const DistillArgs& a, hipStream_t s)
 {
-    with_row_type(dtype, row_threads(dtype, a.n), [&](auto e, auto threads) { HR_ROWS_LAUNCH((k_distill<decltype(e), decltype(threads)::value, true>)); });
+    with_row_type(dtype, row_threads(dtype, a.rows, a.n, 0), [&](auto e, auto threads) { HR_ROWS_LAUNCH((k_distill<decltype(e), decltype(threads)::value, true>)); });
     return hipGetLastError();
 }
 static hipError_t launch_distill_backward(int dtype, const DistillArgs& a, hipStream_t s)
 {
-    with_row_type(dtype, row_threads(dtype, a.n), [&](auto e, auto threads) { HR_ROWS_LAUNCH((k_distill_backward<decltype(e), decltype(threads)::value>)); });
+    with_row_type(dtype, row_threads(dtype, a.rows, a.n, 0), [&](auto e, auto threads) { HR_ROWS_LAUNCH((k_distill_backward<decltype(e), decltype(threads)::value>)); });
     return hipGetLastError();
 }
 
