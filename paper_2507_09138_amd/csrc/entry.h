@@ -21,6 +21,7 @@ inline int check_workspace(const void* ws, size_t bytes, size_t need)
     return HR_OK;
 }
 
+inline size_t aligned(size_t bytes) { return (bytes + HR_WORKSPACE_ALIGN - 1) / HR_WORKSPACE_ALIGN * HR_WORKSPACE_ALIGN; }
 inline size_t element_bytes(int32_t dtype) { return dtype == HR_F32 ? 4 : 2; }
 
 }  // namespace hr

@@ -7,7 +7,6 @@
 
 namespace hr {
 
-typedef int intx4 __attribute__((ext_vector_type(4)));
 
 constexpr int kStep = 64;                                // bytes of k that one matrix instruction takes
 constexpr int kStaticLds = 64 * 1024;                    // what a launch may ask for without saying so beforehand
@@ -682,7 +681,6 @@ static int check_shape(int64_t m, int64_t n, int64_t k)
 }
 
 // workspace: rows a as the tiles want them (quantised ones, or copied ones), their scales, sums of the parts of k
-static size_t aligned(size_t bytes) { return (bytes + HR_WORKSPACE_ALIGN - 1) / HR_WORKSPACE_ALIGN * HR_WORKSPACE_ALIGN; }
 static size_t rows_bytes(int64_t m, int64_t k) { return aligned((size_t)(m * padded_k(k))); }
 static size_t scales_bytes(int64_t m) { return aligned((size_t)m * 4); }
 

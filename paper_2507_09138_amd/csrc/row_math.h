@@ -9,6 +9,8 @@
 
 namespace hr {
 
+typedef int intx4 __attribute__((ext_vector_type(4)));
+
 constexpr float kLog2e = 1.4426950408889634f, kLn2 = 0.6931471805599453f;
 constexpr float kLowest2 = -2000.0f;                 // 2^kLowest2 is 0, and products with it stay finite
 
@@ -74,19 +76,25 @@ struct Row {
     __device__ __forceinline__ float at(int64_t i) const { return i >= 0 && i < n ? (float)z[i] : -INFINITY; }
 };
 
+// What a thread holds of a row while it goes over it: two requests of U chunks.  Afterwards the last ones: a those of `at`, b the U behind.
+template <int U, typename T>
+struct Held {
+    typename Row<T>::V a[U], b[U];
+    int at;
+};
+
 // f(raw chunk, c, in) for the chunks of begin .. end-1 (begin a multiple of 16) that are the row's throughout, U at a time for
 // every thread, all threads alike: in is false for a thread that has none.  The next U chunks are asked for before the last ones
-// are worked on; what is asked for behind the row's end is its last chunk, again.
-// first() is called once, behind the first request.
-template <int U, int THREADS, typename T, typename F, typename G>
-__device__ __forceinline__ void for_chunks(const Row<T>& row, int begin, int end, F&& f, G&& first)
+// are worked on; what is asked for behind the row's end is its last chunk, again.  first() is called once, behind the first request.
+template <int THREADS, int U, typename T, typename F, typename G>
+__device__ __forceinline__ void for_chunks(const Row<T>& row, int begin, int end, Held<U, T>& h, F&& f, G&& first)
 {
     const int stop = min(end, row.hi);
+    h.at = begin;
     if (stop <= max(begin, row.lo)) {
         first();
         return;
     }
-    typename Row<T>::V a[U], b[U];
     auto load = [&](typename Row<T>::V* r, int c0) __attribute__((always_inline)) {
 #pragma unroll
         for (int u = 0; u < U; ++u) r[u] = row.raw(c0 + u * THREADS + (int)threadIdx.x);
@@ -98,13 +106,28 @@ __device__ __forceinline__ void for_chunks(const Row<T>& row, int begin, int end
             if (c0 + u * THREADS < stop) f(r[u], c, c >= row.lo && c < stop);
         }
     };
-    load(a, begin);
+    load(h.a, begin);
     first();
-    for (int c0 = begin; c0 < stop; c0 += 2 * U * THREADS) {
-        load(b, c0 + U * THREADS);
-        work(a, c0);
-        load(a, c0 + 2 * U * THREADS);
-        work(b, c0 + U * THREADS);
+    for (int c0 = begin;; c0 += 2 * U * THREADS) {
+        load(h.b, c0 + U * THREADS);
+        work(h.a, c0);
+        h.at = c0;
+        const bool more = c0 + 2 * U * THREADS < stop;
+        if (more) load(h.a, c0 + 2 * U * THREADS);
+        work(h.b, c0 + U * THREADS);
+        if (!more) return;
+    }
+}
+// f for the chunks that are still held (of begin .. end-1 as before); those before h.at are not among them
+template <int THREADS, int U, typename T, typename F>
+__device__ __forceinline__ void for_held(const Row<T>& row, int begin, int end, const Held<U, T>& h, F&& f)
+{
+    const int stop = min(end, row.hi);
+    if (stop <= max(begin, row.lo)) return;
+#pragma unroll
+    for (int u = 0; u < 2 * U; ++u) {
+        const int c = h.at + u * THREADS + (int)threadIdx.x;
+        if (h.at + u * THREADS < stop) f(u < U ? h.a[u % U] : h.b[u % U], c, c >= row.lo && c < stop);
     }
 }
 
@@ -125,8 +148,10 @@ struct RowShared {
     float part[3][kWaves];
 };
 struct ListShared {
-    int id[HR_LIST_MAX];
+    __align__(16) int id[HR_LIST_MAX];
     float c[HR_LIST_MAX], z[HR_LIST_MAX];
+    float loss;
+    bool some;
 };
 
 // Folds over the lanes of a wave and over a workgroup, to all of them, in the same order every time.
@@ -233,7 +258,7 @@ struct Slots {
 // Maximum and sums of chunks begin .. end-1 of a row (begin a multiple of 16; the edges if begin is 0), to all threads of a workgroup.
 // TOP: the slots of this thread as well (none of the edges).  first() is called once while the first chunks are on their way.
 template <typename T, int THREADS, bool ENTROPY, bool TOP, typename G>
-__device__ __forceinline__ RowStat row_stats(const Row<T>& row, int begin, int end, float c2, RowShared<THREADS>& sh, Slots<THREADS>* slots, int span, G&& first)
+__device__ __forceinline__ RowStat row_stats(const Row<T>& row, int begin, int end, float c2, RowShared<THREADS>& sh, Slots<THREADS>* slots, int span, Held<4, T>& held, G&& first)
 {
     constexpr int E = Row<T>::E;
     RowStat st;
@@ -244,7 +269,7 @@ __device__ __forceinline__ RowStat row_stats(const Row<T>& row, int begin, int e
 #pragma unroll
         for (int i = 0; i < Slots<THREADS>::kPer; ++i) slots->key[i][threadIdx.x] = 0;
     }
-    for_chunks<4, THREADS>(row, begin, end, [&](const typename Row<T>::V& raw, int c, bool in) __attribute__((always_inline)) {
+    for_chunks<THREADS>(row, begin, end, held, [&](const typename Row<T>::V& raw, int c, bool in) __attribute__((always_inline)) {
         float v[E];
 #pragma unroll
         for (int e = 0; e < E; ++e) v[e] = (float)raw[e];
@@ -273,16 +298,40 @@ __device__ __forceinline__ RowStat row_stats(const Row<T>& row, int begin, int e
     return st;
 }
 
+// Few long rows are cut in parts, a workgroup of kPartThreads each, whose sums and slots a second launch puts together.
+constexpr int kPartThreads = 256, kMostParts = 16;
+struct Parts {
+    int n, len;                         // parts of a row (0: whole rows), chunks of each: a multiple of kPartThreads
+    float* stats;                       // [rows][n][4]: m, S0, S1
+    uint32_t* slots;                    // [rows][n][kPartThreads]: the largest score that each thread has seen
+};
+
+// the parts' sums together, to all threads of a wave
+__device__ __forceinline__ RowStat joined_stats(const Parts& parts, int64_t r, float c2)
+{
+    RowStat st;
+    st.clear();
+    const int i = lane_id();
+    if (i < parts.n) {
+        const floatx4 v = *(const floatx4*)(parts.stats + (r * parts.n + i) * 4);
+        st.m = v[0]; st.s0 = v[1]; st.s1 = v[2];
+    }
+    st.fold_lanes(c2);
+    return st;
+}
+
 struct LogprobsArgs {
     const void* logits; int64_t ld, rows; int n; float scale;
     const int64_t* given; int ngiven, k;
     float *logprobs, *entropy, *norm; int64_t* top_ids; float* top_logprobs;
+    Parts parts;
 };
 struct LogprobsBackwardArgs {
     const void* logits; int64_t ld, rows; int n; float scale;
     const int64_t* given; int ngiven;
     const float *entropy, *norm, *grad_logprobs, *grad_entropy;
     void* grad; int64_t ldg;
+    int slice;                          // chunks of a row that a workgroup takes
 };
 struct DistillArgs {
     const void* logits; int64_t ld, rows; int n; float scale;
@@ -290,6 +339,8 @@ struct DistillArgs {
     const float* weights;
     float *loss, *norm, *q;
     void* grad; int64_t ldg;
+    Parts parts;
+    int slice;
 };
 
 }  // namespace hr

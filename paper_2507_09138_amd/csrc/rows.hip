@@ -5,7 +5,9 @@
 //   ln p_i = s (z_i - m) - ln S0,      entropy = ln S0 - S1 / S0  (two terms that are not negative: nothing cancels).
 // Every thread keeps m, S0, S1 of the chunks it has seen (float32; a larger maximum rescales the sums) and the threads' are
 // merged in a fixed order at the end.  Exponents are counted in base 2: one multiplication by s / ln 2 serves scale and base.
-#include <stdlib.h>
+#include <algorithm>
+#include <type_traits>
+
 #include "entry.h"
 #include "row_math.h"
 
@@ -213,15 +215,16 @@ __device__ void append_equal(const Row<T>& row, uint32_t score, TopShared<THREAD
     __syncthreads();
 }
 
-// The best k of a row whose slots are filled, best first, in t.best; returns how many there are.
-template <typename T, int THREADS>
+// The best k of a row whose slots are filled, best first, in t.best; returns how many there are.  Slot s: the chunks that thread
+// s % WIDTH of WIDTH threads has read in its steps from s / WIDTH * span on.
+template <typename T, int THREADS, int WIDTH>
 __device__ int best_entries(const Row<T>& row, int span, int k, TopShared<THREADS>& t)
 {
     constexpr int PER = Slots<THREADS>::kPer;
     static_assert(THREADS == 64 || THREADS == 256 || THREADS == 1024);
     uint32_t mine[PER];
 #pragma unroll
-    for (int i = 0; i < PER; ++i) mine[i] = t.slots.key[i][threadIdx.x];
+    for (int i = 0; i < PER; ++i) mine[i] = t.slots.key[i][threadIdx.x];          // slot i THREADS + this thread
     // the groups' maxima: a thread's slots one by one, four of them, or all of two neighbours
     if (THREADS > 64) {
         uint32_t a = max(max(mine[0], mine[1]), max(mine[2], mine[3]));
@@ -272,7 +275,7 @@ __device__ int best_entries(const Row<T>& row, int span, int k, TopShared<THREAD
         int c = -1;
         if (i < chunks) {
             const uint32_t j = span == 1 ? i : i / (uint32_t)span, p = t.picked[j];
-            const uint32_t at = ((p / THREADS) * span + (i - j * span)) * THREADS + p % THREADS;
+            const uint32_t at = ((p / WIDTH) * span + (i - j * span)) * WIDTH + p % WIDTH;
             if ((int)at >= row.lo && (int)at < row.hi) c = (int)at;
         } else if (i < all) {
             c = i == chunks ? (row.lo > 0 ? 0 : -1) : (row.hi < row.nchunks && row.hi >= row.lo ? row.hi : -1);
@@ -283,7 +286,26 @@ __device__ int best_entries(const Row<T>& row, int span, int k, TopShared<THREAD
     return rank_best(t, t.fill, k);
 }
 
-template <typename T, int THREADS, bool TOP>
+// Sums (and with SLOTS the largest score that each thread has seen) of part blockIdx.x of row blockIdx.y.
+template <typename T, bool ENTROPY, bool SLOTS>
+__global__ __launch_bounds__(kPartThreads) void k_row_parts(const void* logits, int64_t ld, int n, float scale, Parts parts)
+{
+    constexpr int THREADS = kPartThreads;
+    __shared__ RowShared<THREADS> sh;
+    __shared__ std::conditional_t<SLOTS, Slots<THREADS>, char> slots;
+    const int64_t r = blockIdx.y, part = r * parts.n + blockIdx.x;
+    const Row<T> row(logits, r * ld, n);
+    const int begin = (int)blockIdx.x * parts.len, end = blockIdx.x + 1 == gridDim.x ? row.nchunks : begin + parts.len;
+    Held<4, T> held;
+    Slots<THREADS>* mine = nullptr;
+    if constexpr (SLOTS) mine = &slots;
+    const RowStat st = row_stats<T, THREADS, ENTROPY, SLOTS>(row, begin, end, scale * kLog2e, sh, mine, 1 << 30, held, [] {});
+    if (threadIdx.x == 0) *(floatx4*)(parts.stats + part * 4) = floatx4{st.m, st.s0, st.s1, 0.0f};
+    if constexpr (SLOTS) parts.slots[part * THREADS + threadIdx.x] = slots.key[0][threadIdx.x];
+}
+
+// PARTS: the sums and slots come from k_row_parts
+template <typename T, int THREADS, bool TOP, bool PARTS>
 __global__ __launch_bounds__(THREADS) void k_logprobs(LogprobsArgs a)
 {
     __shared__ RowShared<THREADS> sh;
@@ -298,13 +320,29 @@ __global__ __launch_bounds__(THREADS) void k_logprobs(LogprobsArgs a)
             span = Slots<THREADS>::span_for(row.nchunks);
         }
         float z[kListPer<THREADS>];
-        const RowStat st = row_stats<T, THREADS, true, TOP>(row, 0, row.nchunks, c2, sh, slots, span, [&] {
+        auto read_given = [&] {
 #pragma unroll
             for (int i = 0; i < kListPer<THREADS>; ++i) {
                 const int j = i * THREADS + threadIdx.x;
                 if (i * THREADS < a.ngiven) z[i] = j < a.ngiven ? row.at(a.given[r * a.ngiven + j]) : 0.0f;
             }
-        });
+        };
+        RowStat st;
+        if constexpr (PARTS) {
+            read_given();
+            if constexpr (TOP) {
+                span = a.parts.len / kPartThreads;
+#pragma unroll
+                for (int i = 0; i < Slots<THREADS>::kPer; ++i) {
+                    const int s = i * THREADS + threadIdx.x;
+                    slots->key[i][threadIdx.x] = s < a.parts.n * kPartThreads ? a.parts.slots[r * a.parts.n * kPartThreads + s] : 0;
+                }
+            }
+            st = joined_stats(a.parts, r, c2);
+        } else {
+            Held<4, T> held;
+            st = row_stats<T, THREADS, true, TOP>(row, 0, row.nchunks, c2, sh, slots, span, held, read_given);
+        }
         const float logsum = st.log_sum();
         if (threadIdx.x == 0) {
             if (a.norm) { a.norm[2 * r] = st.top(); a.norm[2 * r + 1] = logsum; }
@@ -317,7 +355,7 @@ __global__ __launch_bounds__(THREADS) void k_logprobs(LogprobsArgs a)
         }
         if constexpr (TOP) {
             const bool some = logsum == logsum;
-            const int found = some ? best_entries<T, THREADS>(row, span, a.k, top_) : 0;
+            const int found = some ? best_entries<T, THREADS, PARTS ? kPartThreads : THREADS>(row, span, a.k, top_) : 0;
             for (int j = threadIdx.x; j < a.k; j += THREADS) {
                 const bool there = j < found;
                 const float z = there ? order_value((uint32_t)(top_.best[j] >> 32)) : -INFINITY;
@@ -330,42 +368,94 @@ __global__ __launch_bounds__(THREADS) void k_logprobs(LogprobsArgs a)
 }
 
 // ---- gradients:  g_i = p_i (A + B ln p_i) + sum of the list's c_j with id_j = i
-// list.id, list.c, list.z: entries (-1: none), coefficients and scores, read before this: the gradient may take the place of the scores.
-template <typename T, int THREADS, bool ENTROPY>
-__device__ __forceinline__ void row_gradient(const Row<T>& row, int begin, int end, T* out, float m, float logsum, float scale, float A, float B, bool zero, int count,
-                             ListShared& list)
-{
-    __syncthreads();
-    // The exponential instruction gives 0 below 2^-126, but p times ln p and the coefficients may be above that: it is taken of x + 32
-    // (p is 0 from 2^-158 on) and the product brought back.
-    const float c2 = scale * kLog2e, l2 = logsum * kLog2e - 32.0f, b2 = B * kLn2, a2 = A - 32.0f * b2;
-    auto grad = [&](float z) {
+// The exponential instruction gives 0 below 2^-126, but p times ln p and the coefficients may be above that: it is taken of x + 32
+// (p is 0 from 2^-158 on), the coefficients are divided by 2^32: exactly, unless they are so small that nothing of this shows.
+struct Coefficients {
+    float m, l2, c2, a1, a2, b2;
+    bool zero;                          // the row takes no part
+
+    __device__ __forceinline__ void set(float m_, float logsum, float scale, float A, float B, bool zero_)
+    {
+        const float shift = fmaxf(fabsf(A), fabsf(B)) > 0x1p-90f ? 32.0f : 0.0f, unit = __builtin_amdgcn_exp2f(-shift);
+        m = m_;
+        c2 = scale * kLog2e;
+        l2 = logsum * kLog2e - shift;
+        b2 = B * kLn2 * unit;
+        a1 = A * unit;
+        a2 = (A - shift * (B * kLn2)) * unit;
+        zero = zero_;
+    }
+    template <bool ENTROPY>
+    __device__ __forceinline__ float grad(float z) const
+    {
         const float x = fmaf(z - m, c2, -l2), p = __builtin_amdgcn_exp2f(x);
-        return ENTROPY ? p * fmaf(b2, fmaxf(x, kLowest2), a2) * 0x1p-32f : p * A * 0x1p-32f;
-    };
+        return ENTROPY ? p * fmaf(b2, fmaxf(x, kLowest2), a2) : p * a1;
+    }
+};
+
+// held: chunks of the row that the thread has already, from held->at on (null: none).  first() is called once while the first
+// chunks are on their way: it fills k (Coefficients) and the list: entries (-1: none), coefficients, scores, which have to be read before anything is
+// written (the gradient may take the place of the scores), with a barrier at its end.
+template <typename T, int THREADS, bool ENTROPY, typename G>
+__device__ __forceinline__ void row_gradient(const Row<T>& row, int begin, int end, T* out, const Coefficients& k, int count, ListShared& list, const Held<4, T>* held, G&& first)
+{
     constexpr int E = Row<T>::E;
-    for_chunks<4, THREADS>(row, begin, end, [&](const typename Row<T>::V& raw, int c, bool in) __attribute__((always_inline)) {
+    auto chunk = [&](const typename Row<T>::V& raw, int c, bool in) __attribute__((always_inline)) {
         float v[E];
 #pragma unroll
-        for (int e = 0; e < E; ++e) v[e] = zero ? 0.0f : grad((float)raw[e]);
+        for (int e = 0; e < E; ++e) v[e] = k.zero ? 0.0f : k.template grad<ENTROPY>((float)raw[e]);
         if (in) store_chunk<T>(out + row.first(c), v);
-    }, [] {});
+    };
+    Held<4, T> rest;
+    if (held) {
+        first();
+        for_held<THREADS>(row, begin, end, *held, chunk);
+        const int left = min(held->at, end);
+        if (left > begin) for_chunks<THREADS>(row, begin, left, rest, chunk, [] {});
+    } else {
+        for_chunks<THREADS>(row, begin, end, rest, chunk, first);
+    }
     if (begin == 0 && row.edges()) {
         const int i = row.edge(threadIdx.x);
-        if (i >= 0) out[i] = (T)(zero ? 0.0f : grad((float)row.z[i]));
+        if (i >= 0) out[i] = (T)(k.zero ? 0.0f : k.template grad<ENTROPY>((float)row.z[i]));
     }
-    if (zero) return;
+    if (k.zero) return;
     __syncthreads();
     for (int j = threadIdx.x; j < count; j += THREADS) {
         const int id = list.id[j];
         if (id < 0) continue;
+        // (an entry may be listed more than once: the first of them writes the sum)
         float c = list.c[j];
-        bool first = true;
-        for (int i = 0; i < count; ++i)
-            if (i != j && list.id[i] == id) { c += list.c[i]; first &= i > j; }
-        if (first) out[id] = (T)(list.z[j] == -INFINITY ? 0.0f : grad(list.z[j]) + c);
+        bool leads = true;
+        for (int i = 0; i < count; i += 4) {
+            const intx4 other = *(const intx4*)(list.id + i);         // (behind the last one: -1)
+#pragma unroll
+            for (int e = 0; e < 4; ++e)
+                if (other[e] == id && i + e != j) {
+                    c += list.c[i + e];
+                    leads &= i + e > j;
+                }
+        }
+        if (leads) out[id] = (T)(list.z[j] == -INFINITY ? 0.0f : k.template grad<ENTROPY>(list.z[j]) + c);
     }
 }
+
+// Chunks that workgroup blockIdx.y of a row takes: the first has the edges too, wherever they are.
+template <typename T>
+struct Slice {
+    int begin, end;
+    __device__ __forceinline__ Slice(const Row<T>& row, int len)
+    {
+        begin = (int)blockIdx.y * len;
+        end = min(begin + len, row.nchunks);
+    }
+    __device__ __forceinline__ bool has(const Row<T>& row, int64_t id) const
+    {
+        if (id < 0 || id >= row.n) return false;
+        const int c = (int)((id + row.before) / Row<T>::E);
+        return c < row.lo || c >= row.hi ? begin == 0 : c >= begin && c < end;
+    }
+};
 
 template <typename T, int THREADS>
 __global__ __launch_bounds__(THREADS) void k_logprobs_backward(LogprobsBackwardArgs a)
@@ -374,23 +464,29 @@ __global__ __launch_bounds__(THREADS) void k_logprobs_backward(LogprobsBackwardA
     __shared__ ListShared list;
     for (int64_t r = blockIdx.x; r < a.rows; r += gridDim.x) {
         const Row<T> row(a.logits, r * a.ld, a.n);
-        __syncthreads();
-        float sum = 0.0f;
-        for (int j = threadIdx.x; j < a.ngiven; j += THREADS) {
-            const int64_t id = a.given[r * a.ngiven + j];
-            const float z = row.at(id);
-            const bool there = z != -INFINITY;
-            const float g = there ? a.grad_logprobs[r * a.ngiven + j] : 0.0f;
-            list.id[j] = there ? (int)id : -1;
-            list.c[j] = g * a.scale;
-            list.z[j] = z;
-            sum += g;
-        }
-        sum = group_sum<THREADS>(sum, sh);
-        const float gh = a.grad_entropy ? a.grad_entropy[r] : 0.0f;
-        const float A = -a.scale * (sum + (gh != 0.0f ? gh * a.entropy[r] : 0.0f));
-        const float m = a.norm[2 * r];
-        row_gradient<T, THREADS, true>(row, 0, row.nchunks, (T*)a.grad + r * a.ldg, m, a.norm[2 * r + 1], a.scale, A, -a.scale * gh, m == -INFINITY, a.ngiven, list);
+        const Slice<T> slice(row, a.slice);
+        const float m = a.norm[2 * r], logsum = a.norm[2 * r + 1], gh = a.grad_entropy ? a.grad_entropy[r] : 0.0f;
+        const float entropy = gh != 0.0f ? a.entropy[r] : 0.0f;
+        Coefficients k;
+        row_gradient<T, THREADS, true>(row, slice.begin, slice.end, (T*)a.grad + r * a.ldg, k, a.ngiven, list, nullptr, [&] {
+            __syncthreads();                            // (the list of the row before is no longer read)
+            float sum = 0.0f;
+            for (int j = threadIdx.x; j < (a.ngiven + 3) / 4 * 4; j += THREADS) {
+                const int64_t id = j < a.ngiven ? a.given[r * a.ngiven + j] : -1;
+                const float z = row.at(id);
+                const bool there = z != -INFINITY;
+                const float g = there ? a.grad_logprobs[r * a.ngiven + j] : 0.0f;
+                list.id[j] = there && slice.has(row, id) ? (int)id : -1;
+                list.c[j] = g * a.scale;
+                list.z[j] = z;
+                sum += g;
+            }
+            if (a.ngiven > 0) {
+                sum = group_sum<THREADS>(sum, sh);
+                __syncthreads();
+            }
+            k.set(m, logsum, a.scale, -a.scale * (sum + gh * entropy), -a.scale * gh, m == -INFINITY);
+        });
     }
 }
 
@@ -417,9 +513,14 @@ struct Teacher {
             }
         }
     }
-    // q of the entries that count into list.c, their entries and scores into list.id, list.z (0, -1 for the others); the loss
-    __device__ __forceinline__ float finish(int k, float scale, const RowStat& st, float logsum, ListShared& list, RowShared<THREADS>& sh, bool& some)
+    // q of the entries that count into list.c, their entries and scores into list.id, list.z (0, -1 for the others), the loss and
+    // whether any counts into list.loss, list.some: for all to read behind a barrier.  A list of 64 entries is the first wave's alone.
+    __device__ __forceinline__ void finish(int k, float scale, const RowStat& st, float logsum, ListShared& list, RowShared<THREADS>& sh)
     {
+        const bool one = k <= 64;
+        if (one && threadIdx.x >= 64) return;
+        auto all_max = [&](float v) { return one ? lanes_max(v) : group_max<THREADS>(v, sh); };
+        auto all_sum = [&](float v) { return one ? lanes_sum(v) : group_sum<THREADS>(v, sh); };
         float top = -INFINITY;
 #pragma unroll
         for (int i = 0; i < PER; ++i) {
@@ -427,15 +528,14 @@ struct Teacher {
             // (a NaN counts, and makes the loss NaN)
             if (id[i] >= 0) top = fmaxf(top, t[i] == t[i] ? t[i] : -FLT_MAX);
         }
-        top = group_max<THREADS>(top, sh);
-        some = top != -INFINITY;
+        top = all_max(top);
         float sum = 0.0f, e[PER];
 #pragma unroll
         for (int i = 0; i < PER; ++i) {
             e[i] = id[i] >= 0 ? expf((t[i] - top) * scale) : 0.0f;
             sum += e[i];
         }
-        sum = group_sum<THREADS>(sum, sh);
+        sum = all_sum(sum);
         const float logq = logf(sum);
         float loss = 0.0f;
 #pragma unroll
@@ -444,13 +544,17 @@ struct Teacher {
             const float q = id[i] >= 0 ? e[i] / sum : 0.0f;
             // q (ln q - ln p), the part of ln p that may not fit float32 multiplied by q first (a student's mask of the lowest value)
             if (q != 0.0f) loss += fmaf(q * scale, st.m - z[i], q * ((t[i] - top) * scale - logq + logsum));
-            if (j < k) { list.id[j] = id[i]; list.c[j] = q; list.z[j] = z[i]; }
+            if (j < (k + 3) / 4 * 4) { list.id[j] = id[i]; list.c[j] = q; list.z[j] = z[i]; }
         }
-        return group_sum<THREADS>(loss, sh);
+        loss = all_sum(loss);
+        if (threadIdx.x == 0) {
+            list.loss = loss;
+            list.some = top != -INFINITY;
+        }
     }
 };
 
-template <typename T, int THREADS, bool STEP>
+template <typename T, int THREADS, bool STEP, bool PARTS>
 __global__ __launch_bounds__(THREADS) void k_distill(DistillArgs a)
 {
     __shared__ RowShared<THREADS> sh;
@@ -458,21 +562,31 @@ __global__ __launch_bounds__(THREADS) void k_distill(DistillArgs a)
     for (int64_t r = blockIdx.x; r < a.rows; r += gridDim.x) {
         const Row<T> row(a.logits, r * a.ld, a.n);
         Teacher<T, THREADS> teacher;
-        const RowStat st = row_stats<T, THREADS, false, false>(row, 0, row.nchunks, a.scale * kLog2e, sh, nullptr, 0,
-                                                              [&] { teacher.read(row, a.ids + r * a.k, a.teacher + r * a.k, a.k); });
+        auto read_teacher = [&] { teacher.read(row, a.ids + r * a.k, a.teacher + r * a.k, a.k); };
+        Held<4, T> held;
+        RowStat st;
+        if constexpr (PARTS) {
+            read_teacher();
+            st = joined_stats(a.parts, r, a.scale * kLog2e);
+        } else {
+            st = row_stats<T, THREADS, false, false>(row, 0, row.nchunks, a.scale * kLog2e, sh, nullptr, 0, held, read_teacher);
+        }
         const float logsum = st.log_sum();
-        bool some;
         __syncthreads();                                 // (the list of the row before is no longer read)
-        const float loss = teacher.finish(a.k, a.scale, st, logsum, list, sh, some);
+        teacher.finish(a.k, a.scale, st, logsum, list, sh);
+        __syncthreads();
         if (threadIdx.x == 0) {
-            a.loss[r] = loss;
+            a.loss[r] = list.loss;
             if (a.norm) { a.norm[2 * r] = st.top(); a.norm[2 * r + 1] = logsum; }
         }
         for (int j = threadIdx.x; a.q && j < a.k; j += THREADS) a.q[r * a.k + j] = list.c[j];
         if (STEP) {
             const float w = (a.weights ? a.weights[r] : 1.0f) * a.scale;
+            Coefficients k;
+            k.set(st.top(), logsum, a.scale, w, 0.0f, !list.some || w == 0.0f);
+            // (a thread scales its own entries, which are read behind the next barrier)
             for (int j = threadIdx.x; j < a.k; j += THREADS) list.c[j] *= -w;
-            row_gradient<T, THREADS, false>(row, 0, row.nchunks, (T*)a.grad + r * a.ldg, st.top(), logsum, a.scale, w, 0.0f, !some || w == 0.0f, a.k, list);
+            row_gradient<T, THREADS, false>(row, 0, row.nchunks, (T*)a.grad + r * a.ldg, k, a.k, list, &held, [] {});
         }
     }
 }
@@ -483,20 +597,24 @@ __global__ __launch_bounds__(THREADS) void k_distill_backward(DistillArgs a)
     __shared__ ListShared list;
     for (int64_t r = blockIdx.x; r < a.rows; r += gridDim.x) {
         const Row<T> row(a.logits, r * a.ld, a.n);
-        const float w = (a.weights ? a.weights[r] : 1.0f) * a.scale;
-        __syncthreads();
-        int some = 0;
-        for (int j = threadIdx.x; j < a.k; j += THREADS) {
-            const float q = a.q[r * a.k + j];
-            const int64_t id = a.ids[r * a.k + j];
-            const bool counts = q != 0.0f && id >= 0 && id < a.n;
-            list.id[j] = counts ? (int)id : -1;
-            list.c[j] = -w * q;
-            list.z[j] = row.at(id);
-            some |= counts;
-        }
-        some = __syncthreads_or(some);
-        row_gradient<T, THREADS, false>(row, 0, row.nchunks, (T*)a.grad + r * a.ldg, a.norm[2 * r], a.norm[2 * r + 1], a.scale, w, 0.0f, !some || w == 0.0f, a.k, list);
+        const Slice<T> slice(row, a.slice);
+        const float m = a.norm[2 * r], logsum = a.norm[2 * r + 1], w = (a.weights ? a.weights[r] : 1.0f) * a.scale;
+        Coefficients k;
+        row_gradient<T, THREADS, false>(row, slice.begin, slice.end, (T*)a.grad + r * a.ldg, k, a.k, list, nullptr, [&] {
+            __syncthreads();                            // (the list of the row before is no longer read)
+            int some = 0;
+            for (int j = threadIdx.x; j < (a.k + 3) / 4 * 4; j += THREADS) {
+                const float q = j < a.k ? a.q[r * a.k + j] : 0.0f;
+                const int64_t id = j < a.k ? a.ids[r * a.k + j] : -1;
+                const bool counts = q != 0.0f && id >= 0 && id < a.n, mine = counts && slice.has(row, id);
+                list.id[j] = mine ? (int)id : -1;
+                list.c[j] = -w * q;
+                list.z[j] = mine ? (float)row.z[id] : 0.0f;             // (other slices' scores may be gradients by now)
+                some |= counts;
+            }
+            some = __syncthreads_or(some);
+            k.set(m, logsum, a.scale, w, 0.0f, !some || w == 0.0f);
+        });
     }
 }
 
@@ -510,7 +628,6 @@ static unsigned row_grid(int64_t rows) { return (unsigned)(rows < (1 << 20) ? ro
 //   256   the others: 1024 rows of 131072 139, 103, 120
 static int row_threads(int dtype, int64_t rows, int64_t n, int k)
 {
-    if (const char* e = getenv("HR_T")) return atoi(e);
     const int64_t chunks = n * (int64_t)element_bytes(dtype) / 16;
     if (k <= 32 && (chunks <= 256 || (chunks <= 2048 && rows >= 1536))) return 64;
     return chunks >= 4096 && rows < 256 ? 1024 : 256;
@@ -532,33 +649,100 @@ static void with_row_type(int dtype, int threads, F&& f)
 }
 
 #define HR_ROWS_LAUNCH(kernel) hipLaunchKernelGGL(kernel, dim3(row_grid(a.rows)), dim3(decltype(threads)::value), 0, s, a)
+#define HR_SLICES_LAUNCH(kernel) hipLaunchKernelGGL(kernel, dim3(row_grid(a.rows), slices), dim3(decltype(threads)::value), 0, s, a)
+
+static int64_t row_chunks(int dtype, int64_t n) { return (n * (int64_t)element_bytes(dtype) + 15) / 16 + 1; }        // (at most)
+
+// Parts of few long rows: 16, 1024 in all, of 1024 chunks at least, for rows of 192 KB (us a call, whole rows and in parts: one row of 131072
+// bfloat16 with 20 alternatives 16.4, 10.9, gradient 15.2, 7.2, 65 rows of 600001 52, ; 64 rows of 32768 float32, 128 KB, 11.7, 11.4, a step 12.4, 14.4).
+constexpr int64_t kPartsInAll = 1024, kPartRow = 12288, kPartRows = 255;
+static Parts row_parts(int dtype, int64_t rows, int64_t n)
+{
+    const int64_t chunks = row_chunks(dtype, n);
+    Parts p{0, 0, nullptr, nullptr};
+    if (rows < 1 || rows > kPartRows || chunks < kPartRow) return p;
+    const int64_t parts = std::min({(int64_t)kMostParts, kPartsInAll / rows, chunks / 1024});
+    p.len = (int)((chunks + parts * kPartThreads - 1) / (parts * kPartThreads) * kPartThreads);
+    p.n = (int)((chunks + p.len - 1) / p.len);
+    return p;
+}
+// places for the parts of any number of rows up to this one
+static int64_t part_places(int64_t rows) { return std::min(rows * kMostParts, kPartsInAll); }
+static size_t stats_bytes(int64_t rows) { return (size_t)part_places(rows) * 16; }
+static size_t slots_bytes(int64_t rows) { return (size_t)part_places(rows) * kPartThreads * 4; }
+
+// Slices of a row that workgroups write the gradient of, 1024 in all or rows with at least 1024 chunks each.
+static int gradient_slices(int dtype, int64_t rows, int64_t n, int threads, int& slice)
+{
+    const int64_t chunks = row_chunks(dtype, n), want = std::max((int64_t)1, std::min((int64_t)1024 / rows, chunks / 1024));
+    slice = (int)((chunks + want - 1) / want + threads - 1) / threads * threads;
+    return (int)((chunks + slice - 1) / slice);
+}
+
+template <bool ENTROPY>
+static void launch_parts(int dtype, const void* logits, int64_t ld, int64_t rows, int n, float scale, const Parts& parts, hipStream_t s)
+{
+    with_row_type(dtype, kPartThreads, [&](auto e, auto) {
+        using T = decltype(e);
+        const dim3 grid(parts.n, (unsigned)rows), block(kPartThreads);
+        if (ENTROPY && parts.slots) hipLaunchKernelGGL((k_row_parts<T, ENTROPY, ENTROPY>), grid, block, 0, s, logits, ld, n, scale, parts);
+        else hipLaunchKernelGGL((k_row_parts<T, ENTROPY, false>), grid, block, 0, s, logits, ld, n, scale, parts);
+    });
+}
 
 static hipError_t launch_logprobs(int dtype, const LogprobsArgs& a, hipStream_t s)
 {
+    if (a.parts.n > 1) {
+        launch_parts<true>(dtype, a.logits, a.ld, a.rows, a.n, a.scale, a.parts, s);
+        with_row_type(dtype, 1024, [&](auto e, auto) {
+            const std::integral_constant<int, 1024> threads;
+            if (a.k > 0) HR_ROWS_LAUNCH((k_logprobs<decltype(e), 1024, true, true>));
+            else HR_ROWS_LAUNCH((k_logprobs<decltype(e), 1024, false, true>));
+        });
+        return hipGetLastError();
+    }
     with_row_type(dtype, row_threads(dtype, a.rows, a.n, a.k), [&](auto e, auto threads) {
-        if (a.k > 0) HR_ROWS_LAUNCH((k_logprobs<decltype(e), decltype(threads)::value, true>));
-        else HR_ROWS_LAUNCH((k_logprobs<decltype(e), decltype(threads)::value, false>));
+        if (a.k > 0) HR_ROWS_LAUNCH((k_logprobs<decltype(e), decltype(threads)::value, true, false>));
+        else HR_ROWS_LAUNCH((k_logprobs<decltype(e), decltype(threads)::value, false, false>));
     });
     return hipGetLastError();
 }
-static hipError_t launch_logprobs_backward(int dtype, const LogprobsBackwardArgs& a, hipStream_t s)
+static hipError_t launch_logprobs_backward(int dtype, LogprobsBackwardArgs a, hipStream_t s)
 {
-    with_row_type(dtype, row_threads(dtype, a.rows, a.n, 0), [&](auto e, auto threads) { HR_ROWS_LAUNCH((k_logprobs_backward<decltype(e), decltype(threads)::value>)); });
+    // In the place of the scores a row has one workgroup: each looks at the scores of all given entries.
+    const int few = row_threads(dtype, a.rows, a.n, 0), chosen = a.grad == a.logits ? few : std::min(few, 256);
+    int slices = 1;
+    if (a.grad == a.logits) a.slice = (int)row_chunks(dtype, a.n);
+    else slices = gradient_slices(dtype, a.rows, a.n, chosen, a.slice);
+    with_row_type(dtype, chosen, [&](auto e, auto threads) { HR_SLICES_LAUNCH((k_logprobs_backward<decltype(e), decltype(threads)::value>)); });
     return hipGetLastError();
 }
 static hipError_t launch_distill(int dtype, const DistillArgs& a, hipStream_t s)
 {
-    with_row_type(dtype, row_threads(dtype, a.rows, a.n, 0), [&](auto e, auto threads) { HR_ROWS_LAUNCH((k_distill<decltype(e), decltype(threads)::value, false>)); });
+    if (a.parts.n > 1) {
+        launch_parts<false>(dtype, a.logits, a.ld, a.rows, a.n, a.scale, a.parts, s);
+        with_row_type(dtype, 256, [&](auto e, auto) {
+            const std::integral_constant<int, 256> threads;
+            HR_ROWS_LAUNCH((k_distill<decltype(e), 256, false, true>));
+        });
+        return hipGetLastError();
+    }
+    with_row_type(dtype, row_threads(dtype, a.rows, a.n, 0), [&](auto e, auto threads) { HR_ROWS_LAUNCH((k_distill<decltype(e), decltype(threads)::value, false, false>)); });
+    return hipGetLastError();
+}
+static hipError_t launch_distill_backward(int dtype, DistillArgs a, hipStream_t s)
+{
+    const int chosen = std::min(row_threads(dtype, a.rows, a.n, 0), 256), slices = gradient_slices(dtype, a.rows, a.n, chosen, a.slice);
+    with_row_type(dtype, chosen, [&](auto e, auto threads) { HR_SLICES_LAUNCH((k_distill_backward<decltype(e), decltype(threads)::value>)); });
     return hipGetLastError();
 }
 static hipError_t launch_distill_step(int dtype, const DistillArgs& a, hipStream_t s)
 {
-    with_row_type(dtype, row_threads(dtype, a.rows, a.n, 0), [&](auto e, auto threads) { HR_ROWS_LAUNCH((k_distill<decltype(e), decltype(threads)::value, true>)); });
-    return hipGetLastError();
-}
-static hipError_t launch_distill_backward(int dtype, const DistillArgs& a, hipStream_t s)
-{
-    with_row_type(dtype, row_threads(dtype, a.rows, a.n, 0), [&](auto e, auto threads) { HR_ROWS_LAUNCH((k_distill_backward<decltype(e), decltype(threads)::value>)); });
+    if (a.parts.n > 1) {
+        if (hipError_t e = launch_distill(dtype, a, s)) return e;
+        return launch_distill_backward(dtype, a, s);
+    }
+    with_row_type(dtype, row_threads(dtype, a.rows, a.n, 0), [&](auto e, auto threads) { HR_ROWS_LAUNCH((k_distill<decltype(e), decltype(threads)::value, true, false>)); });
     return hipGetLastError();
 }
 
@@ -596,7 +780,9 @@ size_t hr_logprobs_workspace_bytes(int64_t rows, int64_t n, int32_t k)
         fail(HR_ERR_ARG, "rows=%lld, n=%lld or k=%d out of range", (long long)rows, (long long)n, k);
         return 0;
     }
-    return HR_WORKSPACE_ALIGN;
+    // (float32 has the most chunks; without alternatives no slots)
+    if (row_chunks(HR_F32, n) < kPartRow) return HR_WORKSPACE_ALIGN;
+    return aligned(stats_bytes(rows)) + (k > 0 ? slots_bytes(rows) : 0) + HR_WORKSPACE_ALIGN;
 }
 
 int hr_logprobs(const void* logits, int64_t ld, int32_t dtype, int64_t rows, int64_t n, float scale, const int64_t* given,
@@ -610,7 +796,9 @@ int hr_logprobs(const void* logits, int64_t ld, int32_t dtype, int64_t rows, int
     if (ngiven > 0 && (!given || !out_logprobs)) return fail(HR_ERR_ARG, "given / out_logprobs is null");
     if (k > 0 && (!out_top_ids || !out_top_logprobs)) return fail(HR_ERR_ARG, "out_top_ids / out_top_logprobs is null");
     if (int rc = check_workspace(workspace, workspace_bytes, hr_logprobs_workspace_bytes(rows, n, k))) return rc;
-    LogprobsArgs a{logits, ld, rows, (int)n, scale, given, ngiven, k, out_logprobs, out_entropy, out_norm, out_top_ids, out_top_logprobs};
+    LogprobsArgs a{logits, ld, rows, (int)n, scale, given, ngiven, k, out_logprobs, out_entropy, out_norm, out_top_ids, out_top_logprobs, row_parts(dtype, rows, n)};
+    a.parts.stats = (float*)workspace;
+    if (k > 0) a.parts.slots = (uint32_t*)((char*)workspace + aligned(stats_bytes(rows)));
     HR_HIP(launch_logprobs(dtype, a, (hipStream_t)stream));
     return HR_OK;
 }
@@ -626,7 +814,7 @@ int hr_logprobs_backward(const void* logits, int64_t ld, int32_t dtype, int64_t 
     if (!norm) return fail(HR_ERR_ARG, "norm is null");
     if (grad_logprobs && ngiven > 0 && !given) return fail(HR_ERR_ARG, "given is null");
     if (grad_entropy && !entropy) return fail(HR_ERR_ARG, "entropy is null");
-    LogprobsBackwardArgs a{logits, ld, rows, (int)n, scale, given, grad_logprobs ? ngiven : 0, entropy, norm, grad_logprobs, grad_entropy, grad_logits, ldg};
+    LogprobsBackwardArgs a{logits, ld, rows, (int)n, scale, given, grad_logprobs ? ngiven : 0, entropy, norm, grad_logprobs, grad_entropy, grad_logits, ldg, 0};
     HR_HIP(launch_logprobs_backward(dtype, a, (hipStream_t)stream));
     return HR_OK;
 }
@@ -637,7 +825,10 @@ size_t hr_distill_workspace_bytes(int64_t rows, int64_t n, int32_t k)
         fail(HR_ERR_ARG, "rows=%lld, n=%lld or k=%d out of range", (long long)rows, (long long)n, k);
         return 0;
     }
-    return HR_WORKSPACE_ALIGN;
+    if (row_chunks(HR_F32, n) < kPartRow) return HR_WORKSPACE_ALIGN;
+    // (with rows in parts a step keeps what the backward call needs: there are few of them)
+    const int64_t few = std::min(rows, kPartRows);
+    return aligned(stats_bytes(rows)) + aligned((size_t)few * 8) + aligned((size_t)few * k * 4) + HR_WORKSPACE_ALIGN;
 }
 
 int hr_distill_forward(const void* logits, int64_t ld, int32_t dtype, int64_t rows, int64_t n, float scale, const int64_t* ids,
@@ -649,7 +840,8 @@ int hr_distill_forward(const void* logits, int64_t ld, int32_t dtype, int64_t ro
     if (rows == 0) return HR_OK;
     if (!ids || !teacher || !out_loss) return fail(HR_ERR_ARG, "ids / teacher / out_loss is null");
     if (int rc = check_workspace(workspace, workspace_bytes, hr_distill_workspace_bytes(rows, n, k))) return rc;
-    DistillArgs a{logits, ld, rows, (int)n, scale, ids, teacher, k, nullptr, out_loss, out_norm, out_q, nullptr, 0};
+    DistillArgs a{logits, ld, rows, (int)n, scale, ids, teacher, k, nullptr, out_loss, out_norm, out_q, nullptr, 0, row_parts(dtype, rows, n), 0};
+    a.parts.stats = (float*)workspace;
     HR_HIP(launch_distill(dtype, a, (hipStream_t)stream));
     return HR_OK;
 }
@@ -662,7 +854,7 @@ int hr_distill_backward(const void* logits, int64_t ld, int32_t dtype, int64_t r
     if (rows == 0) return HR_OK;
     if (!ids || !q || !norm) return fail(HR_ERR_ARG, "ids / q / norm is null");
     if (int rc = check_gradient(logits, ld, dtype, n, grad_logits, ldg)) return rc;
-    DistillArgs a{logits, ld, rows, (int)n, scale, ids, nullptr, k, weights, nullptr, (float*)norm, (float*)q, grad_logits, ldg};
+    DistillArgs a{logits, ld, rows, (int)n, scale, ids, nullptr, k, weights, nullptr, (float*)norm, (float*)q, grad_logits, ldg, {0, 0, nullptr, nullptr}, 0};
     HR_HIP(launch_distill_backward(dtype, a, (hipStream_t)stream));
     return HR_OK;
 }
@@ -677,7 +869,13 @@ int hr_distill_step(const void* logits, int64_t ld, int32_t dtype, int64_t rows,
     if (!ids || !teacher || !out_loss) return fail(HR_ERR_ARG, "ids / teacher / out_loss is null");
     if (int rc = check_gradient(logits, ld, dtype, n, grad_logits, ldg)) return rc;
     if (int rc = check_workspace(workspace, workspace_bytes, hr_distill_workspace_bytes(rows, n, k))) return rc;
-    DistillArgs a{logits, ld, rows, (int)n, scale, ids, teacher, k, weights, out_loss, out_norm, out_q, grad_logits, ldg};
+    DistillArgs a{logits, ld, rows, (int)n, scale, ids, teacher, k, weights, out_loss, out_norm, out_q, grad_logits, ldg, row_parts(dtype, rows, n), 0};
+    a.parts.stats = (float*)workspace;
+    if (a.parts.n > 1) {
+        char* room = (char*)workspace + aligned(stats_bytes(rows));
+        if (!a.norm) a.norm = (float*)room;
+        if (!a.q) a.q = (float*)(room + aligned((size_t)rows * 8));
+    }
     HR_HIP(launch_distill_step(dtype, a, (hipStream_t)stream));
     return HR_OK;
 }
