@@ -141,23 +141,23 @@ struct ProductArgs {
 // first operand's rows are the result's rows, four of them in the registers of lane l, 4 (l / 16) .. + 3, in column l % 16.  The rows
 // of b come first, so that a lane holds four neighbouring outputs of a row of a.
 
-// Four neighbouring outputs: the exact sums, scaled, with the bias, rounded once.
-template <typename O>
-__device__ __forceinline__ void store_outputs(const ProductArgs& p, int64_t row, int64_t col, intx4 sum, float sa, floatx4 sb, floatx4 bias, bool whole = false)
+// 4 P neighbouring outputs: the exact sums, scaled, with the bias, rounded once.  whole: all of them are there.
+template <typename O, int P = 1>
+__device__ __forceinline__ void store_outputs(const ProductArgs& p, int64_t row, int64_t col, const intx4* sum, float sa, const floatx4* sb, const floatx4* bias, bool whole = false)
 {
-    typedef O out4 __attribute__((ext_vector_type(4)));
-    out4 o;
+    typedef O outs __attribute__((ext_vector_type(4 * P)));
+    outs o;
 #pragma unroll
-    for (int e = 0; e < 4; ++e) {
-        const float v = (float)sum[e] * sa;
-        o[e] = (O)(p.bias ? fmaf(v, sb[e], bias[e]) : v * sb[e]);
+    for (int e = 0; e < 4 * P; ++e) {
+        const float v = (float)sum[e / 4][e % 4] * sa;
+        o[e] = (O)(p.bias ? fmaf(v, sb[e / 4][e % 4], bias[e / 4][e % 4]) : v * sb[e / 4][e % 4]);
     }
     O* at = (O*)p.out + row * p.ldo + col;
-    if (whole || col + 4 <= p.n) {
+    if (whole || col + 4 * P <= p.n) {
         __builtin_memcpy(at, &o, sizeof o);
     } else {
 #pragma unroll
-        for (int e = 0; e < 4; ++e)
+        for (int e = 0; e < 4 * P; ++e)
             if (col + e < p.n) at[e] = o[e];
     }
 }
@@ -232,7 +232,7 @@ __global__ __launch_bounds__(256) void k_i8_product_any(ProductArgs p)
         const floatx4 sb = load_four(p.b_scale, col, p.n), bias = p.bias ? load_four(p.bias, col, p.n) : floatx4{};
         for (int i = 0; i < 2; ++i) {
             const int64_t row = m0 + wm + i * 16 + lane % 16;
-            if (row < p.m) store_outputs<O>(p, row, col, acc[i][j], p.a_scale[row], sb, bias);
+            if (row < p.m) store_outputs<O>(p, row, col, &acc[i][j], p.a_scale[row], &sb, &bias);
         }
     }
 }
@@ -255,6 +255,8 @@ __global__ __launch_bounds__(BM / WM * (BN / WN) * 64) void k_i8_product(Product
 {
     constexpr int WAVES = BM / WM * (BN / WN), TM = WM / 16, TN = WN / 16, BK = 128, UNITS = (BM + BN) / 8 / WAVES, BUF = (BM + BN) * BK;
     static_assert(BM / 8 % WAVES == 0 && BN / 8 % WAVES == 0);
+    // Outputs of 16 bits: a lane holds eight neighbouring ones, four of each of two tiles of 16 (see row_of).
+    constexpr int P = sizeof(O) == 2 ? 2 : 1;
     constexpr bool SCALES = tile_scales(BM, BN) > 0;
     extern __shared__ __align__(1024) int8_t lds[];
     const int lane = lane_id(), wave = __builtin_amdgcn_readfirstlane(threadIdx.x / 64);
@@ -270,6 +272,9 @@ __global__ __launch_bounds__(BM / WM * (BN / WN) * 64) void k_i8_product(Product
     int tile = blockIdx.x / 8, m0 = 0, n0 = 0;
     uint32_t off[UNITS];                                // (rows of a tile lie within 2^31 bytes: the host sees to it)
     const int8_t *ga = p.a, *gb = p.b;
+    // The row of b that lies in row r of its part of a buffer: with pairs of tiles, rows 0 .. 15 and 16 .. 31 of 32 are four of each eight, so
+    // that lanes store 16 bytes and four of them 64 that lie together (8 and 32: 64 queries against 1 M rows 214 us, now ).
+    auto row_of = [&](int r) __attribute__((always_inline)) { return P == 1 ? r : (r & ~31) | (r & 12) << 1 | (r & 16) >> 2 | (r & 3); };
     auto aim = [&](int t) __attribute__((always_inline)) {
         t += tile0;
         const int g = t / (4 * tiles_n), rest = t - g * 4 * tiles_n, high = min(4, tiles_m - g * 4);
@@ -281,7 +286,7 @@ __global__ __launch_bounds__(BM / WM * (BN / WN) * 64) void k_i8_product(Product
         for (int i = 0; i < UNITS; ++i) {
             const int row = (i * WAVES + wave) * 8 + lane / 8;
             off[i] = (i * WAVES * 8 < BM ? (uint32_t)min(row, m - 1 - m0) * (uint32_t)p.lda
-                                         : (uint32_t)min(row - BM, n - 1 - n0) * (uint32_t)p.ldb) + piece;
+                                         : (uint32_t)min(row_of(row - BM), n - 1 - n0) * (uint32_t)p.ldb) + piece;
         }
     };
     auto request = [&](int block) __attribute__((always_inline)) {
@@ -310,10 +315,10 @@ __global__ __launch_bounds__(BM / WM * (BN / WN) * 64) void k_i8_product(Product
             a[i] = *(const intx4*)(next + (wm + i * 16) * BK);
         }
     };
-    // Everything asked for has landed, everything read is in registers: of all waves.  stores: but for the TM TN stores of a whole
+    // Everything asked for has landed, everything read is in registers: of all waves.  stores: but for the TM TN / P stores of a whole
     // tile that were enqueued behind the blocks.
     auto meet = [&](bool stores) __attribute__((always_inline)) {
-        if (stores) wait_vmcnt<TM * TN>();
+        if (stores) wait_vmcnt<TM * TN / P>();
         else wait_vmcnt<0>();
         asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
         __builtin_amdgcn_s_barrier();
@@ -374,20 +379,27 @@ __global__ __launch_bounds__(BM / WM * (BN / WN) * 64) void k_i8_product(Product
             float sa = 0.0f;
             if (p.parts == 1) sa = SCALES ? scales[wm + i * 16 + lane % 16] : p.a_scale[row];
 #pragma unroll
-            for (int j = 0; j < TN; ++j) {
-                const int col = nt + wn + j * 16 + lane / 16 * 4;
+            for (int j = 0; j < TN; j += P) {
+                const int first = wn + j * 16 + lane / 16 * 4 * P, col = nt + first;
                 if (p.parts > 1) {
                     int* at = p.sums + ((int64_t)blockIdx.y * m + row) * n + col;
-                    if (stores || col + 4 <= n) __builtin_memcpy(at, &acc[i][j], 16);
-                    else
-                        for (int e = 0; e < 4; ++e)
-                            if (col + e < n) at[e] = acc[i][j][e];
+#pragma unroll
+                    for (int e = 0; e < 4 * P; e += 4) {
+                        if (stores || col + e + 4 <= n) __builtin_memcpy(at + e, &acc[i][j + e / 4], 16);
+                        else
+                            for (int f = 0; f < 4; ++f)
+                                if (col + e + f < n) at[e + f] = acc[i][j + e / 4][f];
+                    }
                     continue;
                 }
-                const float* sb = scales + BM + wn + j * 16 + lane / 16 * 4;
-                const floatx4 sb4 = SCALES ? *(const floatx4*)sb : load_four(p.b_scale, col, p.n);
-                const floatx4 bias = !p.bias ? floatx4{} : (SCALES ? *(const floatx4*)(sb + BN) : load_four(p.bias, col, p.n));
-                store_outputs<O>(p, row, col, acc[i][j], sa, sb4, bias, stores);
+                floatx4 sb[P], bias[P];
+#pragma unroll
+                for (int e = 0; e < P; ++e) {
+                    const float* at = scales + BM + first + 4 * e;
+                    sb[e] = SCALES ? *(const floatx4*)at : load_four(p.b_scale, col + 4 * e, p.n);
+                    bias[e] = !p.bias ? floatx4{} : (SCALES ? *(const floatx4*)(at + BN) : load_four(p.bias, col + 4 * e, p.n));
+                }
+                store_outputs<O, P>(p, row, col, &acc[i][j], sa, sb, bias, stores);
             }
         }
         if (!more) break;
@@ -408,7 +420,8 @@ __global__ __launch_bounds__(256) void k_i8_join(ProductArgs p)
             for (int e = 0; e < 4; ++e)
                 if (col + e < p.n) sum[e] += at[e];
         }
-        store_outputs<O>(p, row, col, sum, p.a_scale[row], load_four(p.b_scale, col, p.n), p.bias ? load_four(p.bias, col, p.n) : floatx4{});
+        const floatx4 sb = load_four(p.b_scale, col, p.n), bias = p.bias ? load_four(p.bias, col, p.n) : floatx4{};
+        store_outputs<O>(p, row, col, &sum, p.a_scale[row], &sb, &bias);
     }
 }
 
@@ -526,7 +539,7 @@ __global__ __launch_bounds__(kFewWaves * 64) void k_i8_few(ProductArgs p)
             if (sub == 0 && group < groups && row < m) {
                 const int64_t col = group * 16 + lane / 16 * 4;
                 const floatx4 sb = load_four(p.b_scale, col, p.n), bias = p.bias ? load_four(p.bias, col, p.n) : floatx4{};
-                store_outputs<O>(p, row, col, acc, a_scale[row], sb, bias);
+                store_outputs<O>(p, row, col, &acc, a_scale[row], &sb, &bias);
             }
             acc = intx4{0, 0, 0, 0};
             group += stride;
@@ -591,7 +604,7 @@ static Tiling tiling_for(int64_t m, int64_t n, int64_t k)
     else if (tiles(256, 256) >= kCus) t.bm = t.bn = 256;
     const int64_t all = tiles(t.bm, t.bn);
     if (all > 0 && all < kCus) {
-        const int64_t blocks = (k + 127) / 128, parts = std::min(2 * kCus / all, blocks / 4);        // (four blocks of k at least)
+        const int64_t blocks = (k + 127) / 128, parts = std::min(kCus / all, blocks / 4);        // (four blocks of k at least)
         if (parts > 1) {
             t.part_k = (int)((blocks + parts - 1) / parts * 128);
             t.parts = (int)((k + t.part_k - 1) / t.part_k);
