@@ -13,6 +13,7 @@ import torch
 from .binding import _DTYPE, _addr, _check, _stream, HR_K_MAX, HrError, hr_last_error, lib
 
 HR_I8_K_MAX, HR_LIST_MAX, HR_ROW_MAX = 131071, 512, 1 << 30
+HR_WORKSPACE_ALIGN = 256
 
 _c, _p = ctypes, ctypes.c_void_p
 _i32, _i64, _f32, _size = _c.c_int32, _c.c_int64, _c.c_float, _c.c_size_t
@@ -151,10 +152,19 @@ def _result(out, name, dtype, shape, device):
     return out, (ld if shape[0] > 1 else max(shape[1], 1))
 
 
+_unused = {}
+
+
 def _workspace(need, device):
+    """Of this many bytes; where a call wants none but has to be given one, always the same, which nothing reads or writes."""
+    if need > HR_WORKSPACE_ALIGN:
+        return torch.empty(need, dtype=torch.uint8, device=device)
     if need == 0:
         raise HrError(-1, hr_last_error())
-    return torch.empty(need, dtype=torch.uint8, device=device)
+    ws = _unused.get(device)
+    if ws is None:
+        ws = _unused[device] = torch.empty(HR_WORKSPACE_ALIGN, dtype=torch.uint8, device=device)
+    return ws
 
 
 def _at(t):
@@ -241,7 +251,7 @@ def _list(ids, name, rows, device):
         raise HrError(-1, f"{name} must be an integer tensor")
     if ids.device != device or ids.dim() != 2 or ids.shape[0] != rows or ids.shape[1] > HR_LIST_MAX:
         raise HrError(-1, f"{name} must be a [{rows}, 0..{HR_LIST_MAX}] tensor on {device}")
-    return ids.to(torch.int64).contiguous()
+    return (ids if ids.dtype == torch.int64 else ids.to(torch.int64)).contiguous()
 
 
 @_on_device

@@ -120,6 +120,30 @@ def test_products_of_every_type(m, n, k, dtype, bias):
     _check_product(m, n, k, dtype, bias, "padded", seed=1)
 
 
+@pytest.mark.parametrize("k", [70, 128, 200, 256, 300, 385, 513])
+@pytest.mark.parametrize("m,n", [(4101, 4099), (3001, 2999), (40, 140003), (16, 70001), (64, 66000), (129, 60000), (4352, 4096)])
+def test_products_of_many_tiles(m, n, k):
+    """More tiles than workgroups, of every size, whole ones and ragged ones in turn, with one block of k and with several."""
+    _say("many tiles", m, n, k)
+    hr = _hr()
+    dtype = TYPES[(m + k) % 3]
+    a, b = _i8(m, k, m + k), _i8(n, k, n + k)
+    sa = torch.rand(m, generator=_gen(m), device="cuda") * 0.01
+    sb = torch.rand(n, generator=_gen(n), device="cuda") * 0.01
+    bs = torch.randn(n, generator=_gen(n + 1), device="cuda") if k % 2 else None
+    a, b = _strided(a, 0, -k % 64, 99)[0], _strided(b, 0, -k % 64, -128)[0]
+    # (whole numbers below 2^53 in 64 bits: exact; blocks of rows keep the reference small)
+    got = hr.i8_product(a, sa, b, sb, bias=bs, dtype=dtype)
+    for lo in range(0, m, 1024):
+        v = (a[lo:lo + 1024].double() @ b.double().T.contiguous()) * sa[lo:lo + 1024].double()[:, None] * sb.double()
+        tol = 4 * ref.U * v.abs()
+        if bs is not None:
+            v, tol = v + bs.double(), tol + 4 * ref.U * bs.double().abs()
+        off = (got[lo:lo + 1024].double() - v).abs() - tol * (1 + 2 * ref.EPS[dtype]) - ref.EPS[dtype] * v.abs() - ref.TINY[dtype]
+        assert float(off.max()) <= 0, (lo, float(off.max()))
+    assert torch.equal(hr.i8_product(a, sa, b, sb, bias=bs, dtype=dtype), got)
+
+
 @pytest.mark.parametrize("m,n,k", [(1, 5, 131071), (3, 40, 131071), (70, 90, 131071), (300, 300, 70000)])
 def test_sums_are_exact_up_to_the_longest_rows(m, n, k):
     """Whole numbers: -128 x -128 throughout reaches 2^31 - 2^14; float32 of the exact sum is what comes back."""
@@ -197,7 +221,7 @@ def _scores(kind, rows, n, dtype, seed):
 
 
 ROW_SIZES = [(1, 1), (3, 2), (2, 7), (5, 8), (4, 9), (3, 63), (9, 64), (2, 65), (5, 127), (3, 130), (7, 1000), (3, 1025), (4, 4096), (5, 4099),
-             (3, 16385), (2, 32003), (300, 333), (2, 131072), (1, 300001), (2, 1100003), (70, 9001), (1100, 2050)]
+             (3, 16385), (2, 32003), (300, 333), (2, 131072), (1, 300001), (2, 1100003), (70, 9001), (1100, 2050), (1700, 3001), (40, 20011), (260, 52001), (200, 100003)]
 KINDS = ["plain", "ties", "rising", "falling", "masked", "lowest", "wide", "zeros"]
 
 
@@ -406,6 +430,54 @@ def test_distillation_of_rows_that_take_no_part():
 
 
 # ---- where the calls run
+
+def test_nothing_is_written_behind_a_workspace():
+    """Exactly the bytes asked for, between guards: what lies around them stays, and the results are those of any workspace."""
+    hr = _hr()
+    guard = 4096
+
+    def room(need):
+        t = torch.full((need + 2 * guard,), 0xA5, dtype=torch.uint8, device="cuda")
+        assert t.data_ptr() % 256 == 0
+        return t, t[guard:]
+
+    def check(t, need):
+        torch.cuda.synchronize()
+        assert (t[:guard] == 0xA5).all() and (t[guard + need:] == 0xA5).all()
+
+    for m, n, k in ((1, 1000, 768), (17, 300, 4096), (64, 256, 8192), (100, 200, 3333), (300, 100, 1000)):
+        x = torch.randn(m, k, generator=_gen(1), device="cuda")
+        w, ws = hr.quantize_rows(torch.randn(n, k, generator=_gen(2), device="cuda"))
+        need = hr.hr_i8_workspace_bytes(m, n, k)
+        t, at = room(need)
+        out = torch.empty(m, n, device="cuda")
+        hr.hr_i8_linear(x, k, hr.HR_F32, w, w.stride(0), ws, None, m, n, k, out, n, hr.HR_F32, at, need)
+        check(t, need)
+        assert torch.equal(out, hr.i8_linear(x, w, ws))
+        q, s = hr.quantize_rows(x)
+        hr.hr_i8_product(q, q.stride(0), s, w, w.stride(0), ws, None, m, n, k, out, n, hr.HR_F32, at, need)
+        check(t, need)
+        assert torch.equal(out, hr.i8_linear(x, w, ws))
+    for rows, n, k in ((1, 100, 5), (1, 200001, 20), (60, 60000, 3), (64, 131072, 128), (255, 50000, 10), (300, 50000, 0)):
+        z = _scores("plain", rows, n, torch.float32, n)
+        need = hr.hr_logprobs_workspace_bytes(rows, n, k)
+        t, at = room(need)
+        entropy, norm = torch.empty(rows, device="cuda"), torch.empty(rows, 2, device="cuda")
+        ids, top = torch.empty(rows, k, dtype=torch.int64, device="cuda"), torch.empty(rows, k, device="cuda")
+        hr.hr_logprobs(z, n, hr.HR_F32, rows, n, 1.0, None, 0, k, None, entropy, norm, ids, top, at, need)
+        check(t, need)
+        r = hr.logprobs(z, k=k)
+        assert torch.equal(entropy, r.entropy) and (k == 0 or torch.equal(ids, r.top_ids))
+        kk = max(k, 1)
+        want, teacher, weights = _teacher(z, kk, 3)
+        need = hr.hr_distill_workspace_bytes(rows, n, kk)
+        t, at = room(need)
+        loss, g = torch.empty(rows, device="cuda"), torch.empty_like(z)
+        hr.hr_distill_step(z, n, hr.HR_F32, rows, n, 1.0, want, teacher, kk, weights, loss, None, None, g, n, at, need)
+        check(t, need)
+        a, b = hr.distill_step(z, want, teacher, weights)
+        assert torch.equal(a, loss) and torch.equal(b, g)
+
 
 def test_rows_beyond_32_bits():
     """Rows more than 2^31 elements apart: offsets of rows are 64-bit numbers."""
