@@ -595,3 +595,15 @@ def test_what_is_refused():
     with pytest.raises(hr.HrError) as e:
         hr.hr_logprobs(z, 10, hr.HR_F32, 3, 10, 1.0, None, 0, 0, None, r.entropy, None, None, None, ws_small, 16)
     assert e.value.code == -3
+
+
+def test_the_example_teaches_its_encoder(capsys):
+    """examples/teach_query_encoder.py, small: search, product in 8 bits, distillation and log probabilities together."""
+    import importlib.util
+    import os
+    path = os.path.join(os.path.dirname(os.path.dirname(os.path.abspath(__file__))), "examples", "teach_query_encoder.py")
+    spec = importlib.util.spec_from_file_location("teach_query_encoder", path)
+    example = importlib.util.module_from_spec(spec)
+    spec.loader.exec_module(example)
+    before, after, losses = example.main(passages=8192, d=128, nlist=64, batch=128, k=16, probes=8, steps=30)
+    assert losses[-1] < 0.8 * losses[0] and after > before
