@@ -621,15 +621,15 @@ __global__ __launch_bounds__(THREADS) void k_distill_backward(DistillArgs a)
 // ---- launches
 static unsigned row_grid(int64_t rows) { return (unsigned)(rows < (1 << 20) ? rows : 1 << 20); }      // (a launch may not have 2^32 threads)
 
-// Threads of the workgroup that takes a row (us a call with 64, 256, 1024 threads; 20 alternatives unless it says otherwise):
-//   64    rows of a few chunks a lane, or many short rows, where what a row takes besides its scores is least with one wave: 4096 rows of
-//         2000 float32 23, 36, 128, 2048 of 8192 23, 26, 68; 1024 of 8192 17.6, 15.6
+// Threads of the workgroup that takes a row (us a call with 64, 256, 1024 threads, 20 alternatives):
+//   64    many short rows: what a row takes besides its scores is least with one wave.  4096 rows of 2000 float32 23, 36, 128, 2048 of 8192
+//         23, 26, 68, but 1024 of 2000 13.0, 12.2, 34, one row of 2000 11.0, 8.1, 8.6
 //   1024  few long rows: each has a compute unit for itself.  One row of 131072 float32 101, 27, 17.5, 64 rows 105, 29, 18; 256 of 32768 35, 14, 14
 //   256   the others: 1024 rows of 131072 139, 103, 120
 static int row_threads(int dtype, int64_t rows, int64_t n, int k)
 {
     const int64_t chunks = n * (int64_t)element_bytes(dtype) / 16;
-    if (k <= 32 && (chunks <= 256 || (chunks <= 2048 && rows >= 1536))) return 64;
+    if (k <= TopShared<64>::kMost && chunks <= 2048 && rows >= 1536) return 64;
     return chunks >= 4096 && rows < 256 ? 1024 : 256;
 }
 
@@ -742,7 +742,18 @@ static hipError_t launch_distill_step(int dtype, const DistillArgs& a, hipStream
         if (hipError_t e = launch_distill(dtype, a, s)) return e;
         return launch_distill_backward(dtype, a, s);
     }
-    with_row_type(dtype, row_threads(dtype, a.rows, a.n, 0), [&](auto e, auto threads) { HR_ROWS_LAUNCH((k_distill<decltype(e), decltype(threads)::value, true, false>)); });
+    int chosen = row_threads(dtype, a.rows, a.n, 0);
+    // Rows of 128 KB and more are read twice, but for the eight chunks that each thread still holds: with twice the threads half as many
+    // rows are under way, and of each twice as much is held (4096 rows of 131072 bfloat16 522, with 512 threads 496, with 1024 535; 2048 rows 273, 240,
+    // 253; 1024 rows of 65536 float32 137, 128, 124; 2048 rows of 65537 binary16 132, 133, 155).
+    if (chosen == 256 && row_chunks(dtype, a.n) >= 12288) {
+        with_row_type(dtype, 256, [&](auto e, auto) {
+            const std::integral_constant<int, 512> threads;
+            HR_ROWS_LAUNCH((k_distill<decltype(e), 512, true, false>));
+        });
+        return hipGetLastError();
+    }
+    with_row_type(dtype, chosen, [&](auto e, auto threads) { HR_ROWS_LAUNCH((k_distill<decltype(e), decltype(threads)::value, true, false>)); });
     return hipGetLastError();
 }
 
