@@ -244,13 +244,14 @@ __global__ __launch_bounds__(256) void k_i8_product_any(ProductArgs p)
 // step have been read by all waves its buffer is filled again: one barrier a block, two steps for its loads to land.  A wave's load
 // brings 8 rows; the 16-byte pieces of row r lie at place piece ^ r % 8, so that the lanes of a read lie in different banks (a read
 // of 16 bytes a lane goes in turns of 16 lanes, rows 0 .. 3 and 12 .. 15 of one piece with rows 4 .. 11 of the next).
+// Where there is no more than a tile for every compute unit nothing else hides the time that loads take: NB buffers, all but one on their way.
 // Rows of a are a multiple of 128 bytes long, with zeros behind k.
 // A workgroup takes tiles until there are none left.  It asks for the next one's first two blocks before it writes its outputs, and
 // waits for those blocks only: the outputs have two blocks' time to be written.  Scales and bias come to LDS with a tile's blocks
 // (SCALES; 64 x 256 leaves no room for them beside a second workgroup).
 // bytes of LDS for scales and bias
 __host__ __device__ constexpr int tile_scales(int bm, int bn) { return bm == 64 ? 0 : (bm + 2 * bn) * 4; }
-template <typename O, int BM, int BN, int WM, int WN>
+template <typename O, int BM, int BN, int WM, int WN, int NB = 2>
 __global__ __launch_bounds__(BM / WM * (BN / WN) * 64) void k_i8_product(ProductArgs p)
 {
     constexpr int WAVES = BM / WM * (BN / WN), TM = WM / 16, TN = WN / 16, BK = 128, UNITS = (BM + BN) / 8 / WAVES, BUF = (BM + BN) * BK;
@@ -295,12 +296,12 @@ __global__ __launch_bounds__(BM / WM * (BN / WN) * 64) void k_i8_product(Product
         const uint32_t back = k0 + piece >= k_end ? piece : 0;
 #pragma unroll
         for (int i = 0; i < UNITS; ++i)
-            lds_dma16((i * WAVES * 8 < BM ? ga : gb) + k0, i * WAVES * 8 < BM ? off[i] : off[i] - back, lds0 + (block & 1) * BUF + (i * WAVES + wave) * 1024);
+            lds_dma16((i * WAVES * 8 < BM ? ga : gb) + k0, i * WAVES * 8 < BM ? off[i] : off[i] - back, lds0 + (uint32_t)block % NB * BUF + (i * WAVES + wave) * 1024);
     };
 
     const int frag = (lane % 16) * BK + ((lane / 16) ^ (lane & 7)) * 16;
     intx4 acc[TM][TN], a[TM], b0[TN], b1[TN];
-    auto place = [&](int block, int ks) __attribute__((always_inline)) { return lds + ((frag ^ (ks * 64)) + (block & 1) * BUF); };
+    auto place = [&](int block, int ks) __attribute__((always_inline)) { return lds + ((frag ^ (ks * 64)) + (uint32_t)block % NB * BUF); };
     auto read_b = [&](intx4* f, int block, int ks) __attribute__((always_inline)) {
         const int8_t* at = place(block, ks) + (BM + wn) * BK;
 #pragma unroll
@@ -315,17 +316,20 @@ __global__ __launch_bounds__(BM / WM * (BN / WN) * 64) void k_i8_product(Product
             a[i] = *(const intx4*)(next + (wm + i * 16) * BK);
         }
     };
-    // Everything asked for has landed, everything read is in registers: of all waves.  stores: but for the TM TN / P stores of a whole
-    // tile that were enqueued behind the blocks.
-    auto meet = [&](bool stores) __attribute__((always_inline)) {
-        if (stores) wait_vmcnt<TM * TN / P>();
+    // Everything asked for has landed, but for `behind` blocks that were asked for last, everything read is in registers: of all waves.
+    // stores: but for the TM TN / P stores of a whole tile that were enqueued behind the blocks.
+    auto meet = [&](bool stores, int behind) __attribute__((always_inline)) {
+        if (NB > 2 && behind >= 2) wait_vmcnt<2 * UNITS>();
+        else if (NB > 2 && behind == 1) wait_vmcnt<UNITS>();
+        else if (stores) wait_vmcnt<TM * TN / P>();
         else wait_vmcnt<0>();
         asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
         __builtin_amdgcn_s_barrier();
         asm volatile("" ::: "memory");
     };
 
-    float* const scales = (float*)(lds + 2 * BUF);      // of BM rows a, of BN rows b, BN of the bias
+    static_assert(NB >= 2 && NB <= 4);
+    float* const scales = (float*)(lds + NB * BUF);      // of BM rows a, of BN rows b, BN of the bias
     auto request_scales = [&]() __attribute__((always_inline)) {
 #pragma unroll
         for (int i = 0; i < (BM + 2 * BN) / 64; i += WAVES) {
@@ -335,18 +339,20 @@ __global__ __launch_bounds__(BM / WM * (BN / WN) * 64) void k_i8_product(Product
             const int at = of_a ? m0 + u * 64 : n0 + (u - BM / 64) % (BN / 64) * 64, last = (of_a ? m : n) - 1;
             const float* from = of_a ? p.a_scale : (u < (BM + BN) / 64 ? p.b_scale : p.bias);
             const int first = min(at, last);
-            lds_dma4(from + first, (uint32_t)min(lane, last - first) * 4, lds0 + 2 * BUF + u * 256);
+            lds_dma4(from + first, (uint32_t)min(lane, last - first) * 4, lds0 + NB * BUF + u * 256);
         }
     };
 
     if (tile >= end) return;
     aim(tile);
-    request(0);
-    if (blocks > 1) request(1);
+    if (NB > 2 && SCALES && p.parts == 1) request_scales();
+#pragma unroll
+    for (int b = 0; b < NB; ++b)
+        if (b < blocks) request(b);
     bool stores = false;
     for (;;) {
-        meet(stores);
-        if (SCALES && p.parts == 1) request_scales();
+        meet(stores, min(blocks, NB) - 1);
+        if (NB == 2 && SCALES && p.parts == 1) request_scales();
         read_b(b0, 0, 0);
 #pragma unroll
         for (int i = 0; i < TM; ++i) a[i] = *(const intx4*)(place(0, 0) + (wm + i * 16) * BK);
@@ -357,14 +363,14 @@ __global__ __launch_bounds__(BM / WM * (BN / WN) * 64) void k_i8_product(Product
         for (int b = 0; b < blocks; ++b) {
             read_b(b1, b, 1);
             step(b0, place(b, 1));
-            meet(stores && b == 0 && blocks > 2);       // (nobody reads this block's buffer any more, the next block has landed)
-            if (b + 2 < blocks) request(b + 2);
+            meet(stores && b == 0 && blocks > 2, min(blocks - 2 - b, NB - 2));          // (nobody reads this block's buffer any more, the next block has landed)
+            if (b + NB < blocks) request(b + NB);
             read_b(b0, b + 1, 0);                       // (behind the last block: whatever the buffer holds, not multiplied)
             step(b1, place(b + 1, 0));
         }
         const int mt = m0, nt = n0;
         tile += gridDim.x / 8;
-        const bool more = tile < end;
+        const bool more = NB == 2 && tile < end;        // (with more buffers the host launches a workgroup for every tile)
         if (more) {
             aim(tile);
             request(0);                                 // (both buffers are free since the last meeting)
@@ -622,17 +628,18 @@ template <typename O>
 static hipError_t launch_tiles(const Tiling& t, ProductArgs p, hipStream_t s)
 {
     hipError_t e = hipSuccess;
-    auto go = [&](auto kernel, int waves) {
-        const size_t lds = (size_t)(t.bm + t.bn) * 128 * 2 + tile_scales(t.bm, t.bn);
-        const int64_t tiles = (p.m + t.bm - 1) / t.bm * ((p.n + t.bn - 1) / t.bn);
+    const int64_t tiles = (p.m + t.bm - 1) / t.bm * ((p.n + t.bn - 1) / t.bn);
+    const bool deep = t.bm < 256 && tiles * t.parts <= kCus;
+    auto go = [&](auto kernel, int waves, int buffers) {
+        const size_t lds = (size_t)(t.bm + t.bn) * 128 * buffers + tile_scales(t.bm, t.bn);
         if (lds > kStaticLds) e = hipFuncSetAttribute((const void*)kernel, hipFuncAttributeMaxDynamicSharedMemorySize, (int)lds);
         if (e == hipSuccess) hipLaunchKernelGGL(kernel, dim3((unsigned)(std::min((tiles + 7) / 8, (int64_t)kCus / 8 * (lds <= 80 * 1024 ? 2 : 1)) * 8), t.parts), dim3(waves * 64), lds, s, p);
     };
     p.parts = t.parts;
     p.part_k = t.part_k;
-    if (t.bm == 256) go(k_i8_product<O, 256, 256, 128, 64>, 8);
-    else if (t.bm == 128) go(k_i8_product<O, 128, 128, 64, 64>, 4);
-    else go(k_i8_product<O, 64, 256, 64, 32>, 8);
+    if (t.bm == 256) go(k_i8_product<O, 256, 256, 128, 64>, 8, 2);
+    else if (t.bm == 128) deep ? go(k_i8_product<O, 128, 128, 64, 32, 4>, 8, 4) : go(k_i8_product<O, 128, 128, 64, 32>, 8, 2);
+    else deep ? go(k_i8_product<O, 64, 256, 64, 32, 3>, 8, 3) : go(k_i8_product<O, 64, 256, 64, 32>, 8, 2);
     if (e == hipSuccess && t.parts > 1) {
         const int64_t want = (p.m * ((p.n + 3) / 4) + 255) / 256;
         hipLaunchKernelGGL(k_i8_join<O>, dim3((unsigned)(want < (1 << 20) ? want : 1 << 20)), dim3(256), 0, s, p);
