@@ -68,34 +68,46 @@ __device__ __forceinline__ u32x4 quant_piece(const float* v, float scale)
     return u32x4{w[0], w[1], w[2], w[3]};
 }
 
-// A workgroup takes a row, or each of its waves one (THREADS 64, four rows to a workgroup).  Rows of up to PIECES pieces per
-// thread are held in registers between the search for the largest magnitude and the rounding, longer ones are read again.
-template <typename T, int THREADS>
+// LANES lanes take a row: 4 or 16 of a wave, a wave, or the workgroup.  Rows of up to PIECES pieces per lane are held in registers
+// between the search for the largest magnitude and the rounding, longer ones are read again.
+template <typename T, int LANES, int PIECES>
 __global__ __launch_bounds__(256) void k_quantize(QuantizeArgs a)
 {
-    constexpr int PIECES = 2, ROWS = 256 / THREADS;
+    constexpr int ROWS = 256 / LANES;
     __shared__ uint32_t part[4];
-    const int t = threadIdx.x % THREADS;
+    const int t = threadIdx.x % LANES;
     const int npieces = (a.k + 15) / 16;
     const bool whole = a.ldq % 16 == 0 && (uintptr_t)a.q % 16 == 0;
     for (int64_t r0 = (int64_t)blockIdx.x * ROWS; r0 < a.m; r0 += (int64_t)gridDim.x * ROWS) {
-        const int64_t r = r0 + threadIdx.x / THREADS;
+        const int64_t r = r0 + threadIdx.x / LANES;
         const bool in = r < a.m;
         const T* row = (const T*)a.x + (in ? r : a.m - 1) * a.ldx;
         float v[PIECES][16];
         uint32_t largest = 0;
-        for (int p0 = 0; p0 < npieces; p0 += PIECES * THREADS) {
+        for (int p0 = 0; p0 < npieces; p0 += PIECES * LANES) {
 #pragma unroll
             for (int i = 0; i < PIECES; ++i) {
-                const int p = p0 + i * THREADS + t;
+                const int p = p0 + i * LANES + t;
                 if (p < npieces) load_piece(row, p * 16, a.k, v[i]);
             }
 #pragma unroll
             for (int i = 0; i < PIECES; ++i)
-                if (p0 + i * THREADS + t < npieces) largest = max(largest, largest_bits(v[i]));
+                if (p0 + i * LANES + t < npieces) largest = max(largest, largest_bits(v[i]));
         }
-        largest = wave_fold(largest, [](uint32_t x, uint32_t y) { return x > y ? x : y; });
-        if (THREADS > 64) {
+        // (of four or sixteen neighbouring lanes: lane ^ 1, ^ 2, the other four of eight, the other eight of sixteen)
+        auto fold = [&](auto ctrl) __attribute__((always_inline)) {
+            largest = max(largest, (uint32_t)__builtin_amdgcn_update_dpp(0, (int)largest, decltype(ctrl)::value, 0xf, 0xf, false));
+        };
+        if (LANES <= 16) {
+            fold(std::integral_constant<int, 0xb1>{});
+            fold(std::integral_constant<int, 0x4e>{});
+        }
+        if (LANES == 16) {
+            fold(std::integral_constant<int, 0x141>{});
+            fold(std::integral_constant<int, 0x140>{});
+        }
+        if (LANES >= 64) largest = wave_fold(largest, [](uint32_t x, uint32_t y) { return x > y ? x : y; });
+        if (LANES > 64) {
             __syncthreads();
             if (lane_id() == 0) part[threadIdx.x / 64] = largest;
             __syncthreads();
@@ -104,11 +116,11 @@ __global__ __launch_bounds__(256) void k_quantize(QuantizeArgs a)
         const float scale = quant_scale(largest);
         if (in && t == 0) a.scale[r] = scale;
         int8_t* q = a.q + r * a.ldq;
-        const bool held = npieces <= PIECES * THREADS;
-        for (int p0 = 0; p0 < npieces; p0 += PIECES * THREADS) {
+        const bool held = npieces <= PIECES * LANES;
+        for (int p0 = 0; p0 < npieces; p0 += PIECES * LANES) {
 #pragma unroll
             for (int i = 0; i < PIECES; ++i) {
-                const int p = p0 + i * THREADS + t;
+                const int p = p0 + i * LANES + t;
                 if (!in || p >= npieces) continue;
                 if (!held) load_piece(row, p * 16, a.k, v[i]);
                 const u32x4 w = quant_piece(v[i], scale);
@@ -120,7 +132,7 @@ __global__ __launch_bounds__(256) void k_quantize(QuantizeArgs a)
                 }
             }
         }
-        for (int b = npieces * 16 + t; in && b < a.padded; b += THREADS) q[b] = 0;
+        for (int b = npieces * 16 + t; in && b < a.padded; b += LANES) q[b] = 0;
     }
 }
 
@@ -308,13 +320,16 @@ __global__ __launch_bounds__(BM / WM * (BN / WN) * 64) void k_i8_product(Product
         for (int j = 0; j < TN; ++j) f[j] = *(const intx4*)(at + j * 16 * BK);
     };
     // one step: fragments a and b; where a fragment of a has been used for the last time the next step's takes its registers
+    // (at a raised priority: the wave that shares the SIMD and is behind does its reads and requests in between; 1 .. 2 %)
     auto step = [&](const intx4* b, const int8_t* next) __attribute__((always_inline)) {
+        __builtin_amdgcn_s_setprio(1);
 #pragma unroll
         for (int i = 0; i < TM; ++i) {
 #pragma unroll
             for (int j = 0; j < TN; ++j) acc[i][j] = __builtin_amdgcn_mfma_i32_16x16x64_i8(b[j], a[i], acc[i][j], 0, 0, 0);
             a[i] = *(const intx4*)(next + (wm + i * 16) * BK);
         }
+        __builtin_amdgcn_s_setprio(0);
     };
     // Everything asked for has landed, but for `behind` blocks that were asked for last, everything read is in registers: of all waves.
     // stores: but for the TM TN / P stores of a whole tile that were enqueued behind the blocks.
@@ -571,13 +586,17 @@ static auto with_type(int dtype, F&& f)
 
 static hipError_t launch_quantize(int dtype, const QuantizeArgs& a, hipStream_t s)
 {
-    // a wave per row up to 2048 elements (what its registers hold), a workgroup beyond
-    const int rows = a.k <= 2048 && a.m >= 4 ? 4 : 1;
+    // A piece for every lane; a workgroup for a row where that is not enough (us: 262144 rows of 768 float32 197 with two pieces per
+    // lane of a wave, 186 with one; 100000 rows of 100 50 with a wave a row, ; 4096 of 8192 bfloat16 25.8 read again, 23.4 held).
+    const int lanes = a.k <= 64 ? 4 : (a.k <= 256 ? 16 : (a.k <= 1024 ? 64 : 256)), rows = 256 / lanes;
     const int64_t want = (a.m + rows - 1) / rows;
     const dim3 grid((unsigned)(want < (1 << 20) ? want : 1 << 20));
     with_type(dtype, [&](auto t) {
-        if (rows == 4) hipLaunchKernelGGL((k_quantize<decltype(t), 64>), grid, dim3(256), 0, s, a);
-        else hipLaunchKernelGGL((k_quantize<decltype(t), 256>), grid, dim3(256), 0, s, a);
+        using T = decltype(t);
+        if (lanes == 4) hipLaunchKernelGGL((k_quantize<T, 4, 1>), grid, dim3(256), 0, s, a);
+        else if (lanes == 16) hipLaunchKernelGGL((k_quantize<T, 16, 1>), grid, dim3(256), 0, s, a);
+        else if (lanes == 64) hipLaunchKernelGGL((k_quantize<T, 64, 1>), grid, dim3(256), 0, s, a);
+        else hipLaunchKernelGGL((k_quantize<T, 256, 2>), grid, dim3(256), 0, s, a);
     });
     return hipGetLastError();
 }
