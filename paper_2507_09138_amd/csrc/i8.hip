@@ -509,19 +509,36 @@ __global__ __launch_bounds__(kFewWaves * 64) void k_i8_few(ProductArgs p)
         }
         if ((int)threadIdx.x < m) a_scale[threadIdx.x] = p.a_scale[threadIdx.x];
     } else {
+        // (two pieces of every thread are held between the search for the largest and the rounding, others read again)
+        float held[2][16];
         if (threadIdx.x < 16) largest[threadIdx.x] = 0;
+#pragma unroll
+        for (int h = 0; h < 2; ++h) {
+            const int i = h * THREADS + threadIdx.x, r = i / pieces;
+            if (i < m * pieces) load_piece((const X*)p.x + r * p.ldx, (i - r * pieces) * 16, p.k, held[h]);
+        }
         __syncthreads();
-        for (int i = threadIdx.x; i < m * pieces; i += THREADS) {
-            const int r = i / pieces, t = i - r * pieces;
+#pragma unroll
+        for (int h = 0; h < 2; ++h) {
+            const int i = h * THREADS + threadIdx.x;
+            if (i < m * pieces) atomicMax(&largest[i / pieces], largest_bits(held[h]));
+        }
+        for (int i = 2 * THREADS + threadIdx.x; i < m * pieces; i += THREADS) {
+            const int r = i / pieces;
             float v[16];
-            load_piece((const X*)p.x + r * p.ldx, t * 16, p.k, v);
+            load_piece((const X*)p.x + r * p.ldx, (i - r * pieces) * 16, p.k, v);
             atomicMax(&largest[r], largest_bits(v));
         }
         __syncthreads();
-        for (int i = threadIdx.x; i < m * pieces; i += THREADS) {
-            const int r = i / pieces, t = i - r * pieces;
+#pragma unroll
+        for (int h = 0; h < 2; ++h) {
+            const int i = h * THREADS + threadIdx.x;
+            if (i < m * pieces) *(u32x4*)(rows + i * 16) = quant_piece(held[h], quant_scale(largest[i / pieces]));
+        }
+        for (int i = 2 * THREADS + threadIdx.x; i < m * pieces; i += THREADS) {
+            const int r = i / pieces;
             float v[16];
-            load_piece((const X*)p.x + r * p.ldx, t * 16, p.k, v);
+            load_piece((const X*)p.x + r * p.ldx, (i - r * pieces) * 16, p.k, v);
             *(u32x4*)(rows + i * 16) = quant_piece(v, quant_scale(largest[r]));
         }
         if ((int)threadIdx.x < m) a_scale[threadIdx.x] = quant_scale(largest[threadIdx.x]);
@@ -551,10 +568,10 @@ __global__ __launch_bounds__(kFewWaves * 64) void k_i8_few(ProductArgs p)
             if (++block < cnt) continue;
             block = 0;
             if (p.share > 1) {
-                if (sub > 0) sums[wave * 64 + lane] = acc;
+                if (sub > 0) sums[(wave - 1) * 64 + lane] = acc;
                 __syncthreads();
                 if (sub == 0)
-                    for (int w = 1; w < p.share; ++w) acc += sums[(wave + w) * 64 + lane];
+                    for (int w = 1; w < p.share; ++w) acc += sums[(wave + w - 1) * 64 + lane];
                 __syncthreads();
             }
             if (sub == 0 && group < groups && row < m) {
@@ -610,7 +627,7 @@ static hipError_t launch_few(ProductArgs p, hipStream_t s)
     const int64_t groups = (p.n + 15) / 16;
     p.share = 1;
     while (p.share < kFewWaves && groups * p.share < 2 * kFewWaves * kCus && blocks >= 4 * p.share) p.share *= 2;
-    const size_t lds = kRingBytes + (size_t)p.m * few_stride(p.k) + 16 + (p.share > 1 ? kFewWaves * 1024 : 0);
+    const size_t lds = kRingBytes + (size_t)p.m * few_stride(p.k) + 16 + (p.share > 1 ? (kFewWaves - 1) * 1024 : 0);
     const int at_once = kFewWaves / p.share;
     const int64_t want = (groups + at_once - 1) / at_once, most = (lds <= 79 * 1024 ? 2 : 1) * kCus;
     if (hipError_t e = hipFuncSetAttribute((const void*)k_i8_few<O, X>, hipFuncAttributeMaxDynamicSharedMemorySize, (int)lds)) return e;
