@@ -103,8 +103,8 @@ int hr_logprobs_backward(const void* logits, int64_t ld, int32_t dtype, int64_t 
  *   out_loss DEV [rows] float32 (not weighted).   out_norm DEV [rows, 2], out_q DEV [rows, k] float32: what the backward call needs.
  *   weights DEV [rows] float32 or NULL (1): the gradient of the caller's loss with respect to every row's.
  *   grad_logits as in hr_logprobs_backward (may be logits itself).
- * hr_distill_step is both calls in one, for a caller who knows the weights beforehand (a mean, masked rows): the scores of
- * all but the longest rows come from HBM once.  out_norm and out_q may be NULL there.
+ * hr_distill_step is both calls in one, for a caller who knows the weights beforehand (a mean, masked rows): a row's scores are
+ * read again while they are in registers and caches.  out_norm and out_q may be NULL there.
  */
 size_t hr_distill_workspace_bytes(int64_t rows, int64_t n, int32_t k);    /* 0 on invalid arguments; enough for fewer rows and k as well */
 int hr_distill_forward(const void* logits, int64_t ld, int32_t dtype, int64_t rows, int64_t n, float scale, const int64_t* ids,

@@ -243,7 +243,7 @@ __device__ int best_entries(const Row<T>& row, int span, int k, TopShared<THREAD
 #pragma unroll
         for (int i = 0; i < N; ++i) g[i] = THREADS == 64 ? mine[i % PER] : t.group[i * 64 + lane_id()];
         bool ties;
-        // (256 groups are enough for few, and their bound is found in 2 us less)
+        // (256 groups are enough for few)
         uint32_t bound;
         if (k <= 32) {
             uint32_t h[N / 2];
@@ -654,7 +654,7 @@ static void with_row_type(int dtype, int threads, F&& f)
 static int64_t row_chunks(int dtype, int64_t n) { return (n * (int64_t)element_bytes(dtype) + 15) / 16 + 1; }        // (at most)
 
 // Parts of few long rows: 16, 1024 in all, of 1024 chunks at least, for rows of 192 KB (us a call, whole rows and in parts: one row of 131072
-// bfloat16 with 20 alternatives 16.4, 10.9, gradient 15.2, 7.2, 65 rows of 600001 52, ; 64 rows of 32768 float32, 128 KB, 11.7, 11.4, a step 12.4, 14.4).
+// bfloat16 with 20 alternatives 16.4, 10.9, gradient 15.2, 7.2, 65 rows of 600001 44, 21 without alternatives; 64 rows of 32768 float32, 128 KB, 11.7, 11.4, a step 12.4, 14.4).
 constexpr int64_t kPartsInAll = 1024, kPartRow = 12288, kPartRows = 255;
 static Parts row_parts(int dtype, int64_t rows, int64_t n)
 {
