@@ -60,7 +60,7 @@ int hr_i8_linear(const void* x, int64_t ldx, int32_t x_dtype, const int8_t* b, i
                  void* workspace, size_t workspace_bytes, void* stream);
 
 /*
- * hr_logprobs — rows of scores z read as distributions p = softmax(scale * z), scale > 0 (the inverse temperature).
+ * hr_logprobs — rows of scores z read as distributions p = softmax(scale * z), 0 < scale <= 1e30 (the inverse temperature).
  *   logits   DEV [rows, n] in `dtype`, 1 <= n <= HR_ROW_MAX.  A score of -inf is no candidate: probability 0.  (The lowest finite value
  *            of the type is a candidate like any other: a row of nothing else is uniform.)
  *   given    DEV [rows, ngiven] int64 entries of the row, 0 <= ngiven <= HR_LIST_MAX (NULL if 0); outside 0..n-1 (-1): none.

@@ -3,8 +3,8 @@
 //
 // Mathematics.  With s the scale, m the largest score of a row and t_i = exp(s (z_i - m)):  S0 = sum t_i >= 1,  S1 = sum s (z_i - m) t_i <= 0,
 //   ln p_i = s (z_i - m) - ln S0,      entropy = ln S0 - S1 / S0  (two terms that are not negative: nothing cancels).
-// Every thread keeps m, S0, S1 of the chunks it has seen (float32; a larger maximum rescales the sums) and the threads' are
-// merged in a fixed order at the end.  Exponents are counted in base 2: one multiplication by s / ln 2 serves scale and base.
+// Every thread keeps such sums of the chunks it has seen (float32) and the threads' are brought to the largest maximum and added
+// in a fixed order at the end.  Exponents are counted in base 2: one multiplication by s / ln 2 serves scale and base.
 #include <algorithm>
 #include <type_traits>
 
@@ -768,7 +768,7 @@ static int check_rows(const void* logits, int64_t ld, int32_t dtype, int64_t row
     if (rows < 0 || rows > (1 << 24)) return fail(HR_ERR_ARG, "rows=%lld out of range", (long long)rows);
     if (n < 1 || n > HR_ROW_MAX) return fail(HR_ERR_ARG, "n=%lld must be in 1..%d", (long long)n, HR_ROW_MAX);
     if (ld < n || ld > (1LL << 40)) return fail(HR_ERR_ARG, "ld=%lld: rows of %lld scores overlap or are too far apart", (long long)ld, (long long)n);
-    if (!(scale > 0.0f) || scale > FLT_MAX) return fail(HR_ERR_ARG, "scale=%g must be positive and finite", (double)scale);
+    if (!(scale > 0.0f) || scale > 1e30f) return fail(HR_ERR_ARG, "scale=%g must be positive, at most 1e30", (double)scale);
     if (rows > 0 && !logits) return fail(HR_ERR_ARG, "logits is null");
     if ((uintptr_t)logits % element_bytes(dtype)) return fail(HR_ERR_ARG, "logits is not aligned to its elements");
     return HR_OK;

@@ -310,6 +310,64 @@ def test_a_lowest_value_row_is_uniform():
             ref.close(g, want.expand(2, -1), 1e-6 * scale, dtype)
 
 
+@pytest.mark.parametrize("rows,n", [(3, 300), (2000, 3001), (2, 140001)])
+def test_an_offset_changes_nothing(rows, n):
+    hr = _hr()
+    _say("offsets", rows, n)
+    g = torch.Generator(device="cuda").manual_seed(n)
+    z = torch.randint(-40, 1, (rows, n), generator=g, device="cuda").float()
+    given = torch.randint(n, (rows, 3), generator=g, device="cuda")
+    want = hr.logprobs(z, given, k=4)
+    logp, p, _, _ = ref.parts(z, 1.0)
+    ref.close(want.entropy, ref.entropy(logp, p), 1e-5, torch.float32)
+    # whole numbers that float32 holds, and their products with log2(e) on both sides of 2^23 and 2^24
+    for offset in (4096, 2**22, 5814500, 5814540, 2**23, 11629060, 11629100, 2**24 - 40):
+        for sign in (1, -1):
+            r = hr.logprobs(z + sign * offset, given, k=4)
+            ref.close(r.logprobs, want.logprobs, 2e-5, torch.float32)
+            ref.close(r.entropy, want.entropy, 2e-5, torch.float32)
+            assert torch.equal(r.norm[:, 0] - sign * offset, want.norm[:, 0]) and torch.equal(r.top_ids, want.top_ids)
+    # a row with scores of both kinds: what lies below adds nothing
+    for low in (-(2.0**25), -(2.0**23), -(2.0**22), torch.finfo(torch.float32).min):
+        for top in (0.0, -(2.0**21), -5814520.0, -(2.0**22)):
+            mixed = torch.cat([torch.full((rows, n), low, device="cuda"), z + top, torch.full((rows, 77), low, device="cuda")], 1)
+            r = hr.logprobs(mixed, given + n, k=4)
+            if low < top - 200:
+                ref.close(r.logprobs, want.logprobs, 2e-5, torch.float32)
+                ref.close(r.entropy, want.entropy, 2e-5, torch.float32)
+                assert torch.equal(r.top_ids, want.top_ids + n)
+
+
+@pytest.mark.parametrize("rows,n", [(3, 300), (2000, 3001), (2, 140001)])
+def test_scores_whose_products_with_the_scale_do_not_fit(rows, n):
+    hr = _hr()
+    _say("large", rows, n)
+    g = torch.Generator(device="cuda").manual_seed(n)
+    step = torch.randint(-1000, 1000, (rows, n), generator=g, device="cuda").float()
+    best = torch.randint(n, (rows, 2), generator=g, device="cuda")
+    # two entries share all of p; whole numbers of 2^100 and a scale of 2^30, and the same below 0, beyond the other way
+    for offset in (1001.0, 1001.0 - 2**14):
+        z = step
+        z = z.scatter(1, best, 1000.0) + offset
+        z *= 2.0 ** 100
+        r = hr.logprobs(z, best, k=1, scale=2.0 ** 30)
+        twins = (best[:, :1] != best[:, 1:]).double()                  # (ln 2 where they are two)
+        ref.close(r.entropy, math.log(2) * twins[:, 0], 1e-6, torch.float32)
+        ref.close(r.logprobs, (-math.log(2) * twins).expand(-1, 2), 1e-6, torch.float32)
+        assert torch.equal(r.norm[:, 0], z.amax(1)) and torch.equal(r.top_ids[:, 0], best.amin(1))
+    # the largest scale that there is: two entries 2^-99 apart are a factor exp(-1e30 / 2^99) = exp(-1.577) apart
+    z = (step - 2000.0).scatter(1, best[:, :1], 0.0)
+    other = (best[:, :1] + 1) % n
+    z = z.scatter(1, other, -(2.0 ** -99))
+    r = hr.logprobs(z, torch.cat([best[:, :1], other], 1), scale=1e30)
+    d = float(torch.tensor(1e30, dtype=torch.float32)) * 2.0 ** -99
+    want = torch.tensor([0.0, -d], dtype=torch.float64) - math.log1p(math.exp(-d))
+    ref.close(r.logprobs, want.expand(rows, 2), 4e-6, torch.float32)
+    ref.close(r.entropy, -(want.exp() * want).sum().expand(rows), 4e-6, torch.float32)
+    with pytest.raises(hr.HrError):
+        hr.logprobs(z, scale=1.1e30)
+
+
 @pytest.mark.parametrize("kind", ["plain", "ties", "masked", "lowest", "wide"])
 @pytest.mark.parametrize("rows,n", [(1, 1), (2, 7), (5, 64), (3, 65), (7, 1000), (4, 4099), (2, 32003), (300, 333), (2, 131073), (1100, 2050), (1, 600001)])
 def test_gradient_of_logprobs_and_entropy(rows, n, kind):
