@@ -26,8 +26,8 @@ __device__ __forceinline__ uint64_t entry_key(float z, int i) { return (uint64_t
 
 template <int THREADS>
 struct TopShared {
-    // (one wave takes up to 32 entries: as little LDS as lets 28 of them share a compute unit)
-    static constexpr int kMost = THREADS >= 256 ? HR_K_MAX : 32, kCap = THREADS >= 256 ? 1024 : 256;      // a chunk has to fit in beside kMost kept entries
+    // (one wave has 7 KB, 22 of them share a compute unit; a chunk has to fit in beside kMost kept entries)
+    static constexpr int kMost = HR_K_MAX, kCap = THREADS >= 256 ? 1024 : 384;
     static constexpr int kAll = kCap + 1, kGroups = 512;
     Slots<THREADS> slots;
     uint16_t picked[Slots<THREADS>::kPer * THREADS];
@@ -118,17 +118,54 @@ __device__ int rank_best(TopShared<THREADS>& t, int fill, int k)
         __syncthreads();
         fill = t.fill;
     }
-    // 16 lanes count how many keys beat one
-    const int sub = threadIdx.x & 15;
-    for (int i = threadIdx.x / 16; i < fill; i += THREADS / 16) {
-        const uint64_t mine = t.key[i];
-        int n = 0;
-        for (int j = sub; j < fill; j += 16) n += t.key[j] > mine;
-        n += __builtin_amdgcn_update_dpp(0, n, 0xb1, 0xf, 0xf, false);      // lanes ^ 1, ^ 2, the other four, the other eight
-        n += __builtin_amdgcn_update_dpp(0, n, 0x4e, 0xf, 0xf, false);
-        n += __builtin_amdgcn_update_dpp(0, n, 0x141, 0xf, 0xf, false);
-        n += __builtin_amdgcn_update_dpp(0, n, 0x140, 0xf, 0xf, false);
-        if (sub == 0 && n < k) t.best[n] = mine;
+    // Up to 256 threads: each has a key (one wave's up to four) and counts how many beat it, all lanes reading the same four of them at a
+    // time.  With 1024 sixteen lanes count for a key, one round for 64 of them.  (That way with fewer threads 16 times as much LDS is read
+    // for a key: 4096 rows of 4096 float32 k 32 28.8 us, 24.7 now, k 64 44.8 and 32.8; 2048 of 32000 bfloat16 k 128 70 and 56; one row of 32003
+    // with 1024 threads k 32 11.0, and 11.7 this way.)
+    if constexpr (THREADS <= 256) {
+        constexpr int kWays = THREADS == 64 ? 4 : 1;
+        static_assert(HR_K_MAX + HR_K_MAX / 2 + 64 <= kWays * THREADS && HR_K_MAX + HR_K_MAX / 2 + 68 <= TopShared<THREADS>::kCap);
+        if (threadIdx.x < 4) t.key[fill + threadIdx.x] = 0;
+        __syncthreads();
+        auto rank = [&](auto ways) __attribute__((always_inline)) {
+            constexpr int N = decltype(ways)::value;
+            uint64_t mine[N];
+            int beaten[N] = {};
+#pragma unroll
+            for (int i = 0; i < N; ++i) mine[i] = i * THREADS + (int)threadIdx.x < fill ? t.key[i * THREADS + threadIdx.x] : 0;
+            for (int j = 0; j < fill; j += 4) {
+                uint64_t other[4];
+#pragma unroll
+                for (int e = 0; e < 4; ++e) other[e] = t.key[j + e];
+#pragma unroll
+                for (int e = 0; e < 4; ++e)
+#pragma unroll
+                    for (int i = 0; i < N; ++i) beaten[i] += other[e] > mine[i];
+            }
+#pragma unroll
+            for (int i = 0; i < N; ++i)
+                if (i * THREADS + (int)threadIdx.x < fill && beaten[i] < k) t.best[beaten[i]] = mine[i];
+        };
+        using std::integral_constant;
+        if (THREADS > 64 || fill <= 64) {
+            if ((int)threadIdx.x / 64 * 64 < fill) rank(integral_constant<int, 1>{});
+        } else if (fill <= 128) {
+            rank(integral_constant<int, 2>{});
+        } else {
+            rank(integral_constant<int, kWays>{});
+        }
+    } else {
+        const int sub = threadIdx.x & 15;
+        for (int i = threadIdx.x / 16; i < fill; i += THREADS / 16) {
+            const uint64_t mine = t.key[i];
+            int n = 0;
+            for (int j = sub; j < fill; j += 16) n += t.key[j] > mine;
+            n += __builtin_amdgcn_update_dpp(0, n, 0xb1, 0xf, 0xf, false);      // lanes ^ 1, ^ 2, the other four, the other eight
+            n += __builtin_amdgcn_update_dpp(0, n, 0x4e, 0xf, 0xf, false);
+            n += __builtin_amdgcn_update_dpp(0, n, 0x141, 0xf, 0xf, false);
+            n += __builtin_amdgcn_update_dpp(0, n, 0x140, 0xf, 0xf, false);
+            if (sub == 0 && n < k) t.best[n] = mine;
+        }
     }
     __syncthreads();
     return fill < k ? fill : k;
@@ -621,15 +658,17 @@ __global__ __launch_bounds__(THREADS) void k_distill_backward(DistillArgs a)
 // ---- launches
 static unsigned row_grid(int64_t rows) { return (unsigned)(rows < (1 << 20) ? rows : 1 << 20); }      // (a launch may not have 2^32 threads)
 
-// Threads of the workgroup that takes a row (us a call with 64, 256, 1024 threads, 20 alternatives):
-//   64    many short rows: what a row takes besides its scores is least with one wave.  4096 rows of 2000 float32 23, 36, 128, 2048 of 8192
-//         23, 26, 68, but 1024 of 2000 13.0, 12.2, 34, one row of 2000 11.0, 8.1, 8.6
-//   1024  few long rows: each has a compute unit for itself.  One row of 131072 float32 101, 27, 17.5, 64 rows 105, 29, 18; 256 of 32768 35, 14, 14
+// Threads of the workgroup that takes a row (us a call with 64, 256, 1024 threads):
+//   64    many short rows: what a row takes besides its scores is least with one wave, and with 256 threads the alternatives leave room for
+//         1024 rows at a time.  float32, 10 alternatives: 4096 rows of 4096 21.5, 40, -, 1400 of 4000 13.0, 19.4, -, 1024 of 4000 12.1, 12.6, -;
+//         128 of them: 4096 of 4096 51, 73, -, 2000 of 8000 49, 42, -
+//   1024  few long rows: each has a compute unit for itself.  20 alternatives: one row of 131072 float32 101, 27, 17.5, 64 rows 105, 29, 18; 256
+//         of 32768 35, 14, 14
 //   256   the others: 1024 rows of 131072 139, 103, 120
-static int row_threads(int dtype, int64_t rows, int64_t n, int k)
+static int row_threads(int dtype, int64_t rows, int64_t n)
 {
     const int64_t chunks = n * (int64_t)element_bytes(dtype) / 16;
-    if (k <= TopShared<64>::kMost && chunks <= 2048 && rows >= 1536) return 64;
+    if (chunks <= 2048 && rows > 1024) return 64;
     return chunks >= 4096 && rows < 256 ? 1024 : 256;
 }
 
@@ -701,7 +740,7 @@ static hipError_t launch_logprobs(int dtype, const LogprobsArgs& a, hipStream_t 
         });
         return hipGetLastError();
     }
-    with_row_type(dtype, row_threads(dtype, a.rows, a.n, a.k), [&](auto e, auto threads) {
+    with_row_type(dtype, row_threads(dtype, a.rows, a.n), [&](auto e, auto threads) {
         if (a.k > 0) HR_ROWS_LAUNCH((k_logprobs<decltype(e), decltype(threads)::value, true, false>));
         else HR_ROWS_LAUNCH((k_logprobs<decltype(e), decltype(threads)::value, false, false>));
     });
@@ -710,7 +749,7 @@ static hipError_t launch_logprobs(int dtype, const LogprobsArgs& a, hipStream_t 
 static hipError_t launch_logprobs_backward(int dtype, LogprobsBackwardArgs a, hipStream_t s)
 {
     // In the place of the scores a row has one workgroup: each looks at the scores of all given entries.
-    const int few = row_threads(dtype, a.rows, a.n, 0), chosen = a.grad == a.logits ? few : std::min(few, 256);
+    const int few = row_threads(dtype, a.rows, a.n), chosen = a.grad == a.logits ? few : std::min(few, 256);
     int slices = 1;
     if (a.grad == a.logits) a.slice = (int)row_chunks(dtype, a.n);
     else slices = gradient_slices(dtype, a.rows, a.n, chosen, a.slice);
@@ -727,12 +766,12 @@ static hipError_t launch_distill(int dtype, const DistillArgs& a, hipStream_t s)
         });
         return hipGetLastError();
     }
-    with_row_type(dtype, row_threads(dtype, a.rows, a.n, 0), [&](auto e, auto threads) { HR_ROWS_LAUNCH((k_distill<decltype(e), decltype(threads)::value, false, false>)); });
+    with_row_type(dtype, row_threads(dtype, a.rows, a.n), [&](auto e, auto threads) { HR_ROWS_LAUNCH((k_distill<decltype(e), decltype(threads)::value, false, false>)); });
     return hipGetLastError();
 }
 static hipError_t launch_distill_backward(int dtype, DistillArgs a, hipStream_t s)
 {
-    const int chosen = std::min(row_threads(dtype, a.rows, a.n, 0), 256), slices = gradient_slices(dtype, a.rows, a.n, chosen, a.slice);
+    const int chosen = std::min(row_threads(dtype, a.rows, a.n), 256), slices = gradient_slices(dtype, a.rows, a.n, chosen, a.slice);
     with_row_type(dtype, chosen, [&](auto e, auto threads) { HR_SLICES_LAUNCH((k_distill_backward<decltype(e), decltype(threads)::value>)); });
     return hipGetLastError();
 }
@@ -742,7 +781,7 @@ static hipError_t launch_distill_step(int dtype, const DistillArgs& a, hipStream
         if (hipError_t e = launch_distill(dtype, a, s)) return e;
         return launch_distill_backward(dtype, a, s);
     }
-    int chosen = row_threads(dtype, a.rows, a.n, 0);
+    int chosen = row_threads(dtype, a.rows, a.n);
     // Rows of 128 KB and more are read twice, but for the eight chunks that each thread still holds: with twice the threads half as many
     // rows are under way, and of each twice as much is held (4096 rows of 131072 bfloat16 522, with 512 threads 496, with 1024 535; 2048 rows 273, 240,
     // 253; 1024 rows of 65536 float32 137, 128, 124; 2048 rows of 65537 binary16 132, 133, 155).

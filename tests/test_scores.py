@@ -272,6 +272,15 @@ def test_alternatives_of_every_number(rows, n, kind, k):
     _check_logprobs(z, k, 1.0, None)
 
 
+@pytest.mark.parametrize("k", [1, 15, 32, 33, 64, 65, 100, 128])
+@pytest.mark.parametrize("kind", ["plain", "ties", "rising", "falling", "masked", "lowest", "zeros"])
+@pytest.mark.parametrize("rows,n", [(1025, 130), (1100, 2003), (1030, 8192)])
+def test_alternatives_of_many_rows(rows, n, kind, k):
+    _say("alternatives", rows, n, kind, k)
+    z = _scores(kind, rows, n, TYPES[k % 3], n + k)
+    _check_logprobs(z, k, 1.0, None)
+
+
 @pytest.mark.parametrize("dtype", TYPES)
 def test_rows_with_nan_or_infinity(dtype):
     hr = _hr()
