@@ -635,15 +635,17 @@ static hipError_t launch_few(ProductArgs p, hipStream_t s)
     return hipGetLastError();
 }
 
-// Tiles (BM rows a, BN rows b): 256 x 256 where they keep the chip busy, else 128 x 128, or 64 x 256 for few rows a; in parts of k where
-// those are few as well.
+// Tiles (BM rows a, BN rows b): 256 x 256 or 128 x 128, whichever takes less time, or 64 x 256 for few rows a; in parts of k where
+// the tiles are few.  Large tiles come in rounds of one for every compute unit, a round taking as long as about 780 small ones, two at a
+// time on a compute unit; k 4096, float32 outputs, us with large and small ones: 2048 x 6400 (200 large tiles, 800 small ones) 58,
+// 72, 3500 x 3000 (168, 672) 55, 55, 4096 x 4352 (272, 1088) 110, 88, 4096 x 6144 (384, 1536) 120, 122, 4096 x 8192 (512, 2048) 135, 153.
 struct Tiling { int bm, bn, parts, part_k; };
 static Tiling tiling_for(int64_t m, int64_t n, int64_t k)
 {
     auto tiles = [&](int bm, int bn) { return (m + bm - 1) / bm * ((n + bn - 1) / bn); };
     Tiling t{128, 128, 1, (int)k};
     if (m <= 64) t.bm = 64, t.bn = 256;
-    else if (tiles(256, 256) >= kCus) t.bm = t.bn = 256;
+    else if (tiles(128, 128) >= (tiles(256, 256) + kCus - 1) / kCus * 780) t.bm = t.bn = 256;
     const int64_t all = tiles(t.bm, t.bn);
     if (all > 0 && all < kCus) {
         const int64_t blocks = (k + 127) / 128, parts = std::min(kCus / all, blocks / 4);        // (four blocks of k at least)

@@ -144,6 +144,13 @@ def test_products_of_many_tiles(m, n, k):
     assert torch.equal(hr.i8_product(a, sa, b, sb, bias=bs, dtype=dtype), got)
 
 
+@pytest.mark.parametrize("k", [128, 200, 385, 513])
+@pytest.mark.parametrize("m,n", [(3001, 3800), (3329, 3585), (4001, 7777), (8195, 6401)])
+def test_products_of_rounds_of_tiles(m, n, k):
+    """On both sides of the choice between large and small tiles, with less than a tile for every workgroup, two and four."""
+    test_products_of_many_tiles(m, n, k)
+
+
 @pytest.mark.parametrize("m,n,k", [(1, 5, 131071), (3, 40, 131071), (70, 90, 131071), (300, 300, 70000)])
 def test_sums_are_exact_up_to_the_longest_rows(m, n, k):
     """Whole numbers: -128 x -128 throughout reaches 2^31 - 2^14; float32 of the exact sum is what comes back."""
