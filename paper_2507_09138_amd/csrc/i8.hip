@@ -3,6 +3,7 @@
 #include <type_traits>
 
 #include "entry.h"
+#include "i8_few.h"
 #include "row_math.h"
 
 namespace hr {
@@ -451,21 +452,16 @@ __global__ __launch_bounds__(256) void k_i8_join(ProductArgs p)
 // its own in LDS (whole lines: 16 rows of 64 bytes straight to registers reached 4.8 TB/s for 1 M rows of 768, this reaches 5.7); no barrier.
 // p.share waves may take parts of k of the same rows, so that few rows of b keep the chip busy too.  With floats X in the place of
 // int8 each workgroup quantises a itself: one launch less, from L2.
-constexpr int kFewWaves = 8, kRing = 4, kRingBytes = kFewWaves * kRing * 2048;
-constexpr int kFewLds = 90 * 1024;                       // most bytes of a
-// bytes between the rows of a in LDS: 16 rows in different banks, nothing behind a row that is not zero
-__host__ __device__ constexpr int few_stride(int k) { return (k + 127) / 128 * 128 + 16; }
-
 template <typename O, typename X>
 __global__ __launch_bounds__(kFewWaves * 64) void k_i8_few(ProductArgs p)
 {
     constexpr int THREADS = kFewWaves * 64;
-    extern __shared__ __align__(1024) int8_t lds[];      // rings, rows of a, 16 zeros, sums of waves that share rows
-    __shared__ float a_scale[16];
-    __shared__ uint32_t largest[16];
+    extern __shared__ __align__(1024) int8_t lds[];      // as i8_few.h has it
     const int lane = lane_id(), wave = __builtin_amdgcn_readfirstlane(threadIdx.x / 64);
     const int blocks = (p.k + 127) / 128, a_stride = few_stride(p.k), m = (int)p.m;
     int8_t* const rows = lds + kRingBytes;
+    float* const a_scale = (float*)(lds + few_scales(m, p.k));
+    uint32_t* const largest = (uint32_t*)a_scale + kFewRows;
     const int sub = wave % p.share, first = blocks * sub / p.share, cnt = blocks * (sub + 1) / p.share - first;     // this wave's blocks of every group
     const int at_once = kFewWaves / p.share;
     const int64_t groups = (p.n + 15) / 16, stride = (int64_t)gridDim.x * at_once;
@@ -543,9 +539,9 @@ __global__ __launch_bounds__(kFewWaves * 64) void k_i8_few(ProductArgs p)
         }
         if ((int)threadIdx.x < m) a_scale[threadIdx.x] = quant_scale(largest[threadIdx.x]);
     }
-    if (threadIdx.x == 0) *(u32x4*)(rows + m * a_stride) = u32x4{0, 0, 0, 0};
+    if (threadIdx.x == 0) *(u32x4*)(lds + few_zeros(m, p.k)) = u32x4{0, 0, 0, 0};
     __syncthreads();
-    intx4* const sums = (intx4*)(rows + m * a_stride + 16);
+    intx4* const sums = (intx4*)(lds + few_sums(m, p.k));
 
     const int row = lane % 16;
     const int8_t* const fa = rows + (row < m ? row * a_stride + lane / 16 * 16 : m * a_stride);
@@ -587,7 +583,6 @@ __global__ __launch_bounds__(kFewWaves * 64) void k_i8_few(ProductArgs p)
 }
 
 // ---- which kernel
-constexpr int kCus = 256;
 constexpr int64_t kFewBytes = 64 * 1024;                // rows a that every workgroup quantises for itself
 
 // f(type) with the C++ type of a code
@@ -618,19 +613,13 @@ static hipError_t launch_quantize(int dtype, const QuantizeArgs& a, hipStream_t 
     return hipGetLastError();
 }
 
-static bool few_rows(int64_t m, int64_t k) { return m <= 16 && m * few_stride((int)k) <= kFewLds; }
-
 template <typename O, typename X>
 static hipError_t launch_few(ProductArgs p, hipStream_t s)
 {
-    const int blocks = (p.k + 127) / 128;
-    const int64_t groups = (p.n + 15) / 16;
-    p.share = 1;
-    while (p.share < kFewWaves && groups * p.share < 2 * kFewWaves * kCus && blocks >= 4 * p.share) p.share *= 2;
-    const size_t lds = kRingBytes + (size_t)p.m * few_stride(p.k) + 16 + (p.share > 1 ? (kFewWaves - 1) * 1024 : 0);
-    const int at_once = kFewWaves / p.share;
-    const int64_t want = (groups + at_once - 1) / at_once, most = (lds <= 79 * 1024 ? 2 : 1) * kCus;
-    if (hipError_t e = hipFuncSetAttribute((const void*)k_i8_few<O, X>, hipFuncAttributeMaxDynamicSharedMemorySize, (int)lds)) return e;
+    p.share = few_share(p.n, p.k);
+    const int lds = few_lds((int)p.m, p.k, p.share), at_once = kFewWaves / p.share;
+    const int64_t groups = (p.n + 15) / 16, want = (groups + at_once - 1) / at_once, most = (lds <= kWorkgroupLds / 2 ? 2 : 1) * kCus;
+    if (hipError_t e = hipFuncSetAttribute((const void*)k_i8_few<O, X>, hipFuncAttributeMaxDynamicSharedMemorySize, lds)) return e;
     hipLaunchKernelGGL((k_i8_few<O, X>), dim3((unsigned)(want < most ? want : most)), dim3(kFewWaves * 64), lds, s, p);
     return hipGetLastError();
 }
@@ -695,7 +684,7 @@ static hipError_t launch_product(int dtype, const ProductArgs& p, int8_t* padded
 {
     return with_type(dtype, [&](auto o) -> hipError_t {
         using O = decltype(o);
-        if (few_rows(p.m, p.k) && in_tiles(p.b, p.ldb)) return launch_few<O, int8_t>(p, s);
+        if (few_rows(p.m, p.n, p.k) && in_tiles(p.b, p.ldb)) return launch_few<O, int8_t>(p, s);
         if (in_tiles(p.b, p.ldb)) {
             ProductArgs t = p;
             if (p.k % 128 || !in_tiles(p.a, p.lda)) {
@@ -802,7 +791,7 @@ int hr_i8_linear(const void* x, int64_t ldx, int32_t x_dtype, const int8_t* b, i
     if (int rc = check_workspace(workspace, workspace_bytes, hr_i8_workspace_bytes(m, n, k))) return rc;
     int8_t* q = (int8_t*)workspace;
     float* scale = (float*)(q + rows_bytes(m, k));
-    if (few_rows(m, k) && in_tiles(b, ldb) && m * k * (int64_t)element_bytes(x_dtype) <= kFewBytes) {
+    if (few_rows(m, n, k) && in_tiles(b, ldb) && m * k * (int64_t)element_bytes(x_dtype) <= kFewBytes) {
         ProductArgs p{nullptr, 0, nullptr, b, ldb, b_scale, bias, m, n, (int)k, out, ldo};
         p.x = x;
         p.ldx = ldx;
