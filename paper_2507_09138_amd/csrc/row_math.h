@@ -240,7 +240,8 @@ struct RowStat {
         return raised(any(flags));
     }
     __device__ __forceinline__ float top() const { return s0 == 0.0f ? -INFINITY : m; }
-    __device__ __forceinline__ float log_sum() const { return s0 == 0.0f ? 0.0f : logf(s0); }
+    // (the largest score's term is 1: a sum below is its rounding, and would make ln p of that score positive)
+    __device__ __forceinline__ float log_sum() const { return s0 == 0.0f ? 0.0f : logf(s0 < 1.0f ? 1.0f : s0); }
     // (rounding may leave a sharp row a little below 0)
     __device__ __forceinline__ float entropy(float logsum) const
     {
