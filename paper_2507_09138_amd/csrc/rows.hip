@@ -405,28 +405,59 @@ __global__ __launch_bounds__(THREADS) void k_logprobs(LogprobsArgs a)
 }
 
 // ---- gradients:  g_i = p_i (A + B ln p_i) + sum of the list's c_j with id_j = i
-// The exponential instruction gives 0 below 2^-126, but p times ln p and the coefficients may be above that: it is taken of x + 32
-// (p is 0 from 2^-158 on), the coefficients are divided by 2^32: exactly, unless they are so small that nothing of this shows.
+// With x = log2 p_i = (z_i - m) s / ln 2 - log2 S0 rounded as it is: a likely entry's is near 0, and A + B ln p_i, which cancels for a row that is sure of
+// an entry, keeps all of its bits.  The exponential instruction gives 0 below 2^-126, where p times a large coefficient, or p in float32
+// itself, is not 0 yet: an entry with x < -126 takes the square of 2^(x / 2), of which only one factor meets the coefficient before the other (products
+// with p down to 2^-252; what is lost beyond is below 2^-124 whatever the coefficient).
 struct Coefficients {
-    float m, l2, c2, a1, a2, b2;
+    float m, l2, c2, a, b2;
     bool zero;                          // the row takes no part
+    static constexpr float kNormal = -126.0f;
 
     __device__ __forceinline__ void set(float m_, float logsum, float scale, float A, float B, bool zero_)
     {
-        const float shift = fmaxf(fabsf(A), fabsf(B)) > 0x1p-90f ? 32.0f : 0.0f, unit = __builtin_amdgcn_exp2f(-shift);
         m = m_;
         c2 = scale * kLog2e;
-        l2 = logsum * kLog2e - shift;
-        b2 = B * kLn2 * unit;
-        a1 = A * unit;
-        a2 = (A - shift * (B * kLn2)) * unit;
+        l2 = logsum * kLog2e;
+        a = A;
+        b2 = B * kLn2;
         zero = zero_;
     }
+    __device__ __forceinline__ float exponent(float z) const { return fmaf(z - m, c2, -l2); }
+    // of an exponent that is not below kNormal
     template <bool ENTROPY>
-    __device__ __forceinline__ float grad(float z) const
+    __device__ __forceinline__ float near(float x) const
     {
-        const float x = fmaf(z - m, c2, -l2), p = __builtin_amdgcn_exp2f(x);
-        return ENTROPY ? p * fmaf(b2, fmaxf(x, kLowest2), a2) : p * a1;
+        const float p = __builtin_amdgcn_exp2f(x);
+        return ENTROPY ? p * fmaf(b2, x, a) : p * a;
+    }
+    // of any: where it is not, the same bits
+    template <bool ENTROPY>
+    __device__ __forceinline__ float any(float x) const
+    {
+        const bool low = x < kNormal;
+        const float e = __builtin_amdgcn_exp2f(low ? 0.5f * x : x), g = ENTROPY ? e * fmaf(b2, fmaxf(x, kLowest2), a) : e * a;
+        return low ? (e == 0.0f ? 0.0f : e * g) : g;
+    }
+    template <bool ENTROPY>
+    __device__ __forceinline__ float grad(float z) const { return any<ENTROPY>(exponent(z)); }
+    // of a chunk: few have entries that low
+    template <bool ENTROPY, int E, typename V>
+    __device__ __forceinline__ void grads(const V& z, float* v) const
+    {
+        float least = 0.0f;
+#pragma unroll
+        for (int e = 0; e < E; ++e) {
+            v[e] = exponent((float)z[e]);
+            least = fminf(least, v[e]);
+        }
+        if (least >= kNormal) {
+#pragma unroll
+            for (int e = 0; e < E; ++e) v[e] = near<ENTROPY>(v[e]);
+        } else {
+#pragma unroll
+            for (int e = 0; e < E; ++e) v[e] = any<ENTROPY>(v[e]);
+        }
     }
 };
 
@@ -439,8 +470,12 @@ __device__ __forceinline__ void row_gradient(const Row<T>& row, int begin, int e
     constexpr int E = Row<T>::E;
     auto chunk = [&](const typename Row<T>::V& raw, int c, bool in) __attribute__((always_inline)) {
         float v[E];
+        if (k.zero) {
 #pragma unroll
-        for (int e = 0; e < E; ++e) v[e] = k.zero ? 0.0f : k.template grad<ENTROPY>((float)raw[e]);
+            for (int e = 0; e < E; ++e) v[e] = 0.0f;
+        } else {
+            k.template grads<ENTROPY, E>(raw, v);
+        }
         if (in) store_chunk<T>(out + row.first(c), v);
     };
     Held<4, T> rest;
