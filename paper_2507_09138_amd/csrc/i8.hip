@@ -42,7 +42,8 @@ __device__ __forceinline__ uint32_t largest_bits(const float* v)
 }
 __device__ __forceinline__ float quant_scale(uint32_t largest) { return largest >= 0x7f800000u ? NAN : bits_float(largest) / 127.0f; }
 // The quotient rounded to float32, then to a whole number.  A product with the reciprocal is off by 2^-23 of itself, 1.5e-5 at most: only
-// where it lies that near to the middle of two whole numbers the quotient itself is needed.  (A scale that small has no reciprocal.)
+// where it lies that near to the middle of two whole numbers the quotient itself is needed.  A scale that small has no reciprocal, and where it is
+// below 2^-126 few bits: the largest quotients may be up to 190, and are limited to 127.
 __device__ __forceinline__ u32x4 quant_piece(const float* v, float scale)
 {
     if (!(scale > 0.0f)) return u32x4{0, 0, 0, 0};
@@ -57,7 +58,7 @@ __device__ __forceinline__ u32x4 quant_piece(const float* v, float scale)
     }
     if (near) {
 #pragma unroll
-        for (int e = 0; e < 16; ++e) q[e] = rintf(v[e] / scale);
+        for (int e = 0; e < 16; ++e) q[e] = fminf(fmaxf(rintf(v[e] / scale), -127.0f), 127.0f);
     }
     uint32_t w[4];
 #pragma unroll
