@@ -6,6 +6,7 @@ Matrices may be slices of columns of wider ones (rows contiguous); others are co
 """
 import ctypes
 import functools
+import inspect
 from typing import NamedTuple, Optional
 
 import torch
@@ -105,13 +106,16 @@ _I8 = {torch.int8: None}
 
 
 def _on_device(f):
-    """The device of the first tensor is the current one while f runs."""
+    """The device of f's first argument is the current one while f runs."""
+    name = next(iter(inspect.signature(f).parameters))
+
     @functools.wraps(f)
-    def call(t, *args, **kw):
+    def call(*args, **kw):
+        t = args[0] if args else kw.get(name)
         if not isinstance(t, torch.Tensor) or not t.is_cuda or t.device.index == torch._C._cuda_getDevice():
-            return f(t, *args, **kw)
+            return f(*args, **kw)
         with torch.cuda.device(t.device):
-            return f(t, *args, **kw)
+            return f(*args, **kw)
     return call
 
 

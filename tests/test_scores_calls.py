@@ -1,0 +1,35 @@
+"""How the functions of scores.py are called: by keyword, wrongly more than once, on tensors that autograd follows."""
+import inspect
+
+import pytest
+import torch
+
+import test_scores as scores
+
+FUNCTIONS = ["quantize_rows", "i8_product", "i8_linear", "logprobs", "logprobs_backward", "distill_forward", "distill_backward", "distill_step"]
+
+
+@pytest.mark.parametrize("name", FUNCTIONS)
+def test_arguments_go_by_their_names(name):
+    """Every argument by keyword reaches the function's own checks (host tensors are refused); what is missing is named."""
+    hr = scores._hr()
+    f = getattr(hr, name)
+    names = [p.name for p in inspect.signature(f).parameters.values() if p.default is p.empty]
+    with pytest.raises(hr.HrError) as e:
+        f(**{n: torch.zeros(3, 8) for n in names})
+    assert f"{names[0]} must be a device tensor" in str(e.value)
+    with pytest.raises(TypeError, match=repr(names[0])):
+        f()
+
+
+@pytest.mark.gpu
+def test_keyword_calls_give_the_same():
+    hr = scores._hr()
+    z = torch.randn(3, 50, device="cuda")
+    ids, t = torch.zeros(3, 2, dtype=torch.int64, device="cuda"), torch.zeros(3, 2, device="cuda")
+    r = hr.logprobs(given=ids, logits=z, k=2)
+    assert all(torch.equal(a, b) for a, b in zip(r, hr.logprobs(z, ids, 2)))
+    assert torch.equal(hr.logprobs_backward(grad_logprobs=t + 1, result=r, given=ids, logits=z), hr.logprobs_backward(z, ids, r, t + 1))
+    assert torch.equal(hr.distill_step(teacher=t, ids=ids, logits=z)[1], hr.distill_step(z, ids, t)[1])
+    w, ws = hr.quantize_rows(x=z)
+    assert torch.equal(hr.i8_linear(x=z, b=w, b_scale=ws), hr.i8_product(b_scale=ws, b=w, a_scale=ws, a=w))
