@@ -99,9 +99,22 @@ def hr_distill_step(logits, ld, dtype, rows, n, scale, ids, teacher, k, weights,
 # plain numbers, sizes of workspaces are kept by shape, and the library is called without another function in between.
 
 _raw_stream = torch._C._cuda_getCurrentRawStream          # (current_stream() makes an object first: 3 us)
-_i8_bytes = functools.lru_cache(1024)(lib.hr_i8_workspace_bytes)
-_logprobs_bytes = functools.lru_cache(1024)(lib.hr_logprobs_workspace_bytes)
-_distill_bytes = functools.lru_cache(1024)(lib.hr_distill_workspace_bytes)
+
+
+def _kept(f):
+    """Sizes that f gives, kept by shape; 0, a refusal, is raised and not kept: its message is that of the call that made it."""
+    @functools.lru_cache(1024)
+    def need(*shape):
+        size = f(*shape)
+        if size == 0:
+            raise HrError(-1, hr_last_error())
+        return size
+    return need
+
+
+_i8_bytes = _kept(lib.hr_i8_workspace_bytes)
+_logprobs_bytes = _kept(lib.hr_logprobs_workspace_bytes)
+_distill_bytes = _kept(lib.hr_distill_workspace_bytes)
 _I8 = {torch.int8: None}
 
 
@@ -163,8 +176,6 @@ def _workspace(need, device):
     """Of this many bytes; where a call wants none but has to be given one, always the same, which nothing reads or writes."""
     if need > HR_WORKSPACE_ALIGN:
         return torch.empty(need, dtype=torch.uint8, device=device)
-    if need == 0:
-        raise HrError(-1, hr_last_error())
     ws = _unused.get(device)
     if ws is None:
         ws = _unused[device] = torch.empty(HR_WORKSPACE_ALIGN, dtype=torch.uint8, device=device)

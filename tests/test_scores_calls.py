@@ -33,3 +33,29 @@ def test_keyword_calls_give_the_same():
     assert torch.equal(hr.distill_step(teacher=t, ids=ids, logits=z)[1], hr.distill_step(z, ids, t)[1])
     w, ws = hr.quantize_rows(x=z)
     assert torch.equal(hr.i8_linear(x=z, b=w, b_scale=ws), hr.i8_product(b_scale=ws, b=w, a_scale=ws, a=w))
+
+
+def test_a_refusal_says_why_every_time():
+    """Sizes of workspaces are kept from call to call, refusals are not: the same wrong call has the same message after another's."""
+    hr = scores._hr()
+    from paper_2507_09138_amd import scores as layer
+    for need, bad, other, text in ((layer._i8_bytes, (3, 4, 0), (3, 4, 131072), "k=0 "), (layer._logprobs_bytes, (3, 10, 129), (3, 10, -1), "k=129 "),
+                                   (layer._distill_bytes, (3, 10, 513), (3, 0, 5), "k=513 ")):
+        for _ in range(2):
+            with pytest.raises(hr.HrError, match=text):
+                need(*bad)
+            with pytest.raises(hr.HrError) as e:
+                need(*other)
+            assert text not in str(e.value)
+        assert need(3, 10, 5) == need(3, 10, 5) > 0
+
+
+@pytest.mark.gpu
+def test_a_refused_call_says_why_every_time():
+    hr = scores._hr()
+    z = torch.randn(3, 10, device="cuda")
+    for _ in range(2):
+        with pytest.raises(hr.HrError, match="k=129 "):
+            hr.logprobs(z, k=129)
+        with pytest.raises(hr.HrError, match="scale="):
+            hr.logprobs(z, scale=-1.0)
