@@ -3,6 +3,10 @@
 As in ``binding``: functions with the names of the C entry points take tensors (or raw addresses) and sizes; the others
 check their tensors, allocate results and workspace on the current stream of the tensors' device, and call those.
 Matrices may be slices of columns of wider ones (rows contiguous); others are copied first.
+
+Nothing here is recorded by autograd: results require no gradient, whatever their operands do.  A training step hands the gradient
+that ``distill_step`` or a ``..._backward`` call returns to ``scores.backward(gradient)``.  ``out=`` counts as a change in place of that
+tensor: where a recorded operation still needs its values, its backward pass says so.
 """
 import ctypes
 import functools
@@ -169,6 +173,13 @@ def _result(out, name, dtype, shape, device):
     return out, (ld if shape[0] > 1 else max(shape[1], 1))
 
 
+def _written(out, result):
+    """The result; where it lies in a tensor of the caller's (out), autograd learns that this has changed."""
+    if out is not None:
+        torch.autograd.graph.increment_version(out)
+    return result
+
+
 _unused = {}
 
 
@@ -223,33 +234,35 @@ def _product_operands(m, k, dev, b, b_scale, bias, dtype, out):
         raise HrError(-1, f"dtype {dtype}: want float32, float16 or bfloat16")
     b_scale = _like(b_scale, "b_scale", torch.float32, (n,), dev)
     bias = None if bias is None else _like(bias, "bias", torch.float32, (n,), dev)
-    out, ldo = _result(out, "out", dtype, (m, n), dev)
-    return b, ldb, n, b_scale, bias, out, ldo, _workspace(_i8_bytes(m, n, k), dev)
+    result, ldo = _result(out, "out", dtype, (m, n), dev)
+    return b, ldb, n, b_scale, bias, result, ldo, _workspace(_i8_bytes(m, n, k), dev)
 
 
 @_on_device
 def i8_product(a, a_scale, b, b_scale, bias=None, dtype=torch.float32, out=None):
-    """a [m, k] times b [n, k] transposed, both int8, in the scales [m] and [n] of their rows, plus bias [n]: [m, n] in dtype."""
+    """a [m, k] times b [n, k] transposed, both int8, in the scales [m] and [n] of their rows, plus bias [n]: [m, n] in dtype.
+    Not recorded by autograd."""
     a, lda = _i8_matrix(a, "a")
     m, k = a.shape
     dev = a.device
     a_scale = _like(a_scale, "a_scale", torch.float32, (m,), dev)
-    b, ldb, n, b_scale, bias, out, ldo, ws = _product_operands(m, k, dev, b, b_scale, bias, dtype, out)
-    _check(lib.hr_i8_product(a.data_ptr(), lda, a_scale.data_ptr(), b.data_ptr(), ldb, b_scale.data_ptr(), _at(bias), m, n, k, out.data_ptr(),
+    b, ldb, n, b_scale, bias, result, ldo, ws = _product_operands(m, k, dev, b, b_scale, bias, dtype, out)
+    _check(lib.hr_i8_product(a.data_ptr(), lda, a_scale.data_ptr(), b.data_ptr(), ldb, b_scale.data_ptr(), _at(bias), m, n, k, result.data_ptr(),
                              ldo, _DTYPE[dtype], ws.data_ptr(), ws.numel(), _raw_stream(dev.index)))
-    return out
+    return _written(out, result)
 
 
 @_on_device
 def i8_linear(x, b, b_scale, bias=None, dtype=torch.float32, out=None):
-    """Rows of floats x [m, k], quantised row by row, times b [n, k] int8 transposed: [m, n] in dtype."""
+    """Rows of floats x [m, k], quantised row by row, times b [n, k] int8 transposed: [m, n] in dtype.
+    Not recorded by autograd."""
     x, ldx = _matrix(x, "x", _DTYPE)
     m, k = x.shape
     dev = x.device
-    b, ldb, n, b_scale, bias, out, ldo, ws = _product_operands(m, k, dev, b, b_scale, bias, dtype, out)
-    _check(lib.hr_i8_linear(x.data_ptr(), ldx, _DTYPE[x.dtype], b.data_ptr(), ldb, b_scale.data_ptr(), _at(bias), m, n, k, out.data_ptr(), ldo,
+    b, ldb, n, b_scale, bias, result, ldo, ws = _product_operands(m, k, dev, b, b_scale, bias, dtype, out)
+    _check(lib.hr_i8_linear(x.data_ptr(), ldx, _DTYPE[x.dtype], b.data_ptr(), ldb, b_scale.data_ptr(), _at(bias), m, n, k, result.data_ptr(), ldo,
                             _DTYPE[dtype], ws.data_ptr(), ws.numel(), _raw_stream(dev.index)))
-    return out
+    return _written(out, result)
 
 
 class Logprobs(NamedTuple):
@@ -271,7 +284,8 @@ def _list(ids, name, rows, device):
 
 @_on_device
 def logprobs(logits, given=None, k=0, scale=1.0):
-    """softmax(scale * logits) of every row [rows, n]: log probabilities of the given entries [rows, g], entropy, the k best."""
+    """softmax(scale * logits) of every row [rows, n]: log probabilities of the given entries [rows, g], entropy, the k best.
+    Not recorded by autograd: the gradient is ``logprobs_backward``."""
     z, ld = _matrix(logits, "logits", _DTYPE)
     rows, n = z.shape
     dev = z.device
@@ -311,7 +325,7 @@ def logprobs_backward(logits, given, result, grad_logprobs=None, grad_entropy=No
     grad, ldg = _result(out, "out", z.dtype, (rows, n), dev)
     _check(lib.hr_logprobs_backward(z.data_ptr(), ld, _DTYPE[z.dtype], rows, n, scale, _at(given), g, entropy.data_ptr(), norm.data_ptr(),
                                     _at(grad_logprobs), _at(grad_entropy), grad.data_ptr(), ldg, _raw_stream(dev.index)))
-    return grad
+    return _written(out, grad)
 
 
 def _taught(logits, ids, name, values):
@@ -325,7 +339,7 @@ def _taught(logits, ids, name, values):
 @_on_device
 def distill_forward(logits, ids, teacher, scale=1.0):
     """Loss [rows] of the logits [rows, n] against a teacher's scores [rows, k] of the entries ids [rows, k] (-1: empty), and what
-    ``distill_backward`` needs: (loss, norm, q)."""
+    ``distill_backward`` needs: (loss, norm, q).  Not recorded by autograd."""
     z, ld, ids, teacher = _taught(logits, ids, "teacher", teacher)
     rows, n = z.shape
     k, dev = ids.shape[1], z.device
@@ -350,12 +364,13 @@ def distill_backward(logits, ids, q, norm, weights=None, scale=1.0, out=None):
     grad, ldg = _result(out, "out", z.dtype, (rows, n), dev)
     _check(lib.hr_distill_backward(z.data_ptr(), ld, _DTYPE[z.dtype], rows, n, scale, ids.data_ptr(), q.data_ptr(), ids.shape[1],
                                    norm.data_ptr(), _at(weights), grad.data_ptr(), ldg, _raw_stream(dev.index)))
-    return grad
+    return _written(out, grad)
 
 
 @_on_device
 def distill_step(logits, ids, teacher, weights=None, scale=1.0, out=None):
-    """``distill_forward`` and ``distill_backward`` in one, for weights known beforehand: (loss [rows], gradient [rows, n])."""
+    """``distill_forward`` and ``distill_backward`` in one, for weights known beforehand: (loss [rows], gradient [rows, n]).
+    Not recorded by autograd: the gradient goes to ``logits.backward``.  ``out`` may be the logits themselves."""
     z, ld, ids, teacher = _taught(logits, ids, "teacher", teacher)
     rows, n = z.shape
     k, dev = ids.shape[1], z.device
@@ -365,4 +380,4 @@ def distill_step(logits, ids, teacher, weights=None, scale=1.0, out=None):
     ws = _workspace(_distill_bytes(rows, n, k), dev)
     _check(lib.hr_distill_step(z.data_ptr(), ld, _DTYPE[z.dtype], rows, n, scale, ids.data_ptr(), teacher.data_ptr(), k, _at(weights),
                                loss.data_ptr(), None, None, grad.data_ptr(), ldg, ws.data_ptr(), ws.numel(), _raw_stream(dev.index)))
-    return loss, grad
+    return loss, _written(out, grad)

@@ -59,3 +59,41 @@ def test_a_refused_call_says_why_every_time():
             hr.logprobs(z, k=129)
         with pytest.raises(hr.HrError, match="scale="):
             hr.logprobs(z, scale=-1.0)
+
+
+@pytest.mark.gpu
+def test_what_is_written_over_is_known_to_autograd():
+    """Results are not recorded; a result in the place of a tensor that a backward pass needs is an error there, not a wrong gradient."""
+    hr = scores._hr()
+    ids, t = torch.zeros(3, 2, dtype=torch.int64, device="cuda"), torch.zeros(3, 2, device="cuda")
+    w, ws = hr.quantize_rows(torch.randn(10, 64, device="cuda"))
+
+    def written(call):
+        x = torch.randn(3, 10, device="cuda", requires_grad=True)
+        y = torch.exp(x)                                   # (its backward pass needs y)
+        before = y._version
+        call(y)
+        assert y._version > before
+        with pytest.raises(RuntimeError, match="modified by an inplace operation"):
+            y.sum().backward()
+
+    def norm_q(y):
+        return hr.distill_forward(y, ids, t)[:0:-1]
+
+    written(lambda y: hr.distill_step(y, ids, t, out=y.detach()))
+    written(lambda y: hr.distill_step(y, ids, t, out=y))
+    written(lambda y: hr.distill_backward(y, ids, *norm_q(y), out=y))
+    written(lambda y: hr.logprobs_backward(y, ids, hr.logprobs(y, ids), t, out=y))
+    written(lambda y: hr.i8_linear(torch.randn(3, 64, device="cuda"), w, ws, out=y))
+    written(lambda y: hr.i8_product(w[:3], ws[:3], w, ws, out=y))
+    # scores that a model made, their gradient in their place: what a training step does with it
+    x = torch.randn(3, 10, device="cuda", requires_grad=True)
+    y = 2 * x
+    want = hr.distill_step(y, ids, t)[1]
+    assert not want.requires_grad and not hr.logprobs(y, ids).logprobs.requires_grad
+    grad = hr.distill_step(y, ids, t, out=y)[1].detach()
+    y.backward(grad)
+    assert torch.equal(x.grad, 2 * want)
+    with torch.inference_mode():
+        z = torch.randn(3, 10, device="cuda")
+        assert hr.distill_step(z, ids, t, out=z)[1] is z
