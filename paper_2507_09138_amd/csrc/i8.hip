@@ -620,7 +620,8 @@ static hipError_t launch_few(ProductArgs p, hipStream_t s)
     p.share = few_share(p.n, p.k);
     const int lds = few_lds((int)p.m, p.k, p.share), at_once = kFewWaves / p.share;
     const int64_t groups = (p.n + 15) / 16, want = (groups + at_once - 1) / at_once, most = (lds <= kWorkgroupLds / 2 ? 2 : 1) * kCus;
-    if (hipError_t e = hipFuncSetAttribute((const void*)k_i8_few<O, X>, hipFuncAttributeMaxDynamicSharedMemorySize, lds)) return e;
+    // (the most that any launch of it takes, not this one's: the attribute is the process's, and another thread may be between setting it and its launch)
+    if (hipError_t e = hipFuncSetAttribute((const void*)k_i8_few<O, X>, hipFuncAttributeMaxDynamicSharedMemorySize, kWorkgroupLds)) return e;
     hipLaunchKernelGGL((k_i8_few<O, X>), dim3((unsigned)(want < most ? want : most)), dim3(kFewWaves * 64), lds, s, p);
     return hipGetLastError();
 }

@@ -1,6 +1,7 @@
 """Products of up to 16 rows a: whether a shape fits the LDS of a workgroup (host arithmetic, no GPU), and products on both sides of that."""
 import ctypes
 import os
+import re
 import subprocess
 
 import pytest
@@ -58,6 +59,13 @@ def test_the_kernel_has_no_other_lds():
     assert [ln for ln in body.splitlines() if "__shared__" in ln and "extern __shared__" not in ln] == []
 
 
+def test_the_limit_that_a_launch_sets_is_the_same_for_all():
+    """The attribute belongs to the process: a launch that set its own size would take room from one of another thread."""
+    text = open(os.path.join(ROOT, "paper_2507_09138_amd", "csrc", "i8.hip")).read()
+    body = text[text.index("static hipError_t launch_few("):text.index("struct Tiling")]
+    assert re.findall(r"MaxDynamicSharedMemorySize, ([^)]*)\)", body) == ["kWorkgroupLds"]
+
+
 @pytest.mark.gpu
 @pytest.mark.parametrize("m,n,k", [(16, 64, 5504), (16, 64, 5632), (16, 300, 5633), (16, 70000, 5632), (15, 100, 6016), (13, 100, 7040), (11, 300, 8192), (8, 200, 11392),
                                    (8, 100, 11008), (4, 50, 22400), (2, 40, 45000), (1, 33, 90000), (1, 33, 92032)])
@@ -80,3 +88,35 @@ def test_linear_where_rows_no_longer_fit(m, n, k, dtype):
     assert scores.torch.equal(got, hr.i8_product(q, s, w, ws, dtype=dtype))
     rq, rs = scores.ref.quantize(x)
     scores.ref.close(got, *scores.ref.product(rq, rs, w.cpu(), ws.cpu(), None), dtype)
+
+
+@pytest.mark.gpu
+def test_threads_with_launches_of_different_sizes():
+    """Two threads whose launches of the same kernel want little and much of LDS: neither's takes room from the other's."""
+    import threading
+    hr, torch = scores._hr(), scores.torch
+    ins, want, failed = [], [], []
+    for m, k in ((1, 256), (16, 5504)):
+        x = torch.randn(m, k, generator=scores._gen(m), device="cuda").half()
+        w, ws = hr.quantize_rows(torch.randn(100, k, generator=scores._gen(k), device="cuda"))
+        q, s = hr.quantize_rows(x)
+        ins.append((q, s, w, ws))
+        want.append(hr.i8_product(*ins[-1]))
+    torch.cuda.synchronize()
+
+    def work(i):
+        try:
+            with torch.cuda.stream(torch.cuda.Stream()):
+                got = [hr.i8_product(*ins[i]) for _ in range(500)]
+            torch.cuda.synchronize()
+            if not all(torch.equal(g, want[i]) for g in got):
+                failed.append((i, "other values"))
+        except Exception as e:                             # (said below, not in the thread)
+            failed.append((i, e))
+
+    threads = [threading.Thread(target=work, args=(i,)) for i in (0, 1)]
+    for t in threads:
+        t.start()
+    for t in threads:
+        t.join()
+    assert not failed
