@@ -213,7 +213,9 @@ __global__ __launch_bounds__(256) void k_i8_pad(const int8_t* a, int64_t lda, in
     }
 }
 
-// ---- rows of any alignment: tiles of 64 x 64 outputs, four waves of 32 x 32, blocks of 64 bytes of k staged through registers
+// ---- rows of any alignment: tiles of 64 x 64 outputs, four waves of 32 x 32, blocks of 64 bytes of k staged through registers.  Bound by the
+// wait for each block, one at a time between two barriers (us here, and with b where the other kernels can read it: 1 x 65536 x 768 14.5, 13.6,
+// 777 x 10007 x 1000 46, 26.5, 4096 x 4096 x 4096 194, 63, 11 x 4096 x 8192 73, 17): for matrices that a caller cannot lay out otherwise.
 template <typename O>
 __global__ __launch_bounds__(256) void k_i8_product_any(ProductArgs p)
 {
@@ -630,6 +632,7 @@ static hipError_t launch_few(ProductArgs p, hipStream_t s)
 // the tiles are few.  Large tiles come in rounds of one for every compute unit, a round taking as long as about 780 small ones, two at a
 // time on a compute unit; k 4096, float32 outputs, us with large and small ones: 2048 x 6400 (200 large tiles, 800 small ones) 58,
 // 72, 3500 x 3000 (168, 672) 55, 55, 4096 x 4352 (272, 1088) 110, 88, 4096 x 6144 (384, 1536) 120, 122, 4096 x 8192 (512, 2048) 135, 153.
+// (The 780 are of these: with other k, what a tile costs besides its steps weighs otherwise, and where both take as long they prove nothing.)
 struct Tiling { int bm, bn, parts, part_k; };
 static Tiling tiling_for(int64_t m, int64_t n, int64_t k)
 {

@@ -696,7 +696,8 @@ static unsigned row_grid(int64_t rows) { return (unsigned)(rows < (1 << 20) ? ro
 // Threads of the workgroup that takes a row (us a call with 64, 256, 1024 threads):
 //   64    many short rows: what a row takes besides its scores is least with one wave, and with 256 threads the alternatives leave room for
 //         1024 rows at a time.  float32, 10 alternatives: 4096 rows of 4096 21.5, 40, -, 1400 of 4000 13.0, 19.4, -, 1024 of 4000 12.1, 12.6, -;
-//         128 of them: 4096 of 4096 51, 73, -, 2000 of 8000 49, 42, -
+//         128 of them: 4096 of 4096 51, 73, -, 2000 of 8000 49, 42, -  (the rule does not know how many are wanted: with that many, such rows
+//         would be quicker with 256)
 //   1024  few long rows: each has a compute unit for itself.  20 alternatives: one row of 131072 float32 101, 27, 17.5, 64 rows 105, 29, 18; 256
 //         of 32768 35, 14, 14
 //   256   the others: 1024 rows of 131072 139, 103, 120
@@ -727,8 +728,8 @@ static void with_row_type(int dtype, int threads, F&& f)
 
 static int64_t row_chunks(int dtype, int64_t n) { return (n * (int64_t)element_bytes(dtype) + 15) / 16 + 1; }        // (at most)
 
-// Parts of few long rows: 16, 1024 in all, of 1024 chunks at least, for rows of 192 KB (us a call, whole rows and in parts: one row of 131072
-// bfloat16 with 20 alternatives 16.4, 10.9, gradient 15.2, 7.2, 65 rows of 600001 44, 21 without alternatives; 64 rows of 32768 float32, 128 KB, 11.7, 11.4, a step 12.4, 14.4).
+// Parts of few long rows: 16, 1024 in all, of 1024 chunks at least, for rows of 192 KB and more (us a call, whole rows and in parts: one row of 131072
+// bfloat16 with 20 alternatives 16.4, 10.9, gradient 15.2, 7.2, 65 rows of 600001 44, 21 without alternatives; 64 rows of 32768 float32, 128 KB, 11.7, 11.4, a step 12.4, 14.4: where one row of such a length or shorter would start to gain has not been measured).
 constexpr int64_t kPartsInAll = 1024, kPartRow = 12288, kPartRows = 255;
 static Parts row_parts(int dtype, int64_t rows, int64_t n)
 {
@@ -817,9 +818,9 @@ static hipError_t launch_distill_step(int dtype, const DistillArgs& a, hipStream
         return launch_distill_backward(dtype, a, s);
     }
     int chosen = row_threads(dtype, a.rows, a.n);
-    // Rows of 128 KB and more are read twice, but for the eight chunks that each thread still holds: with twice the threads half as many
-    // rows are under way, and of each twice as much is held (4096 rows of 131072 bfloat16 522, with 512 threads 496, with 1024 535; 2048 rows 273, 240,
-    // 253; 1024 rows of 65536 float32 137, 128, 124; 2048 rows of 65537 binary16 132, 133, 155).
+    // Rows are read again but for the eight chunks that each thread still holds, 32 KB of a row with 256 threads.  From 192 KB on twice as many
+    // take it: half as many rows are under way, and of each twice as much is held (4096 rows of 131072 bfloat16 522, with 512 threads 496, with 1024 535;
+    // 2048 rows 273, 240, 253; 1024 rows of 65536 float32 137, 128, 124; shorter ones, 2048 rows of 65537 binary16, 132, 133, 155).
     if (chosen == 256 && row_chunks(dtype, a.n) >= 12288) {
         with_row_type(dtype, 256, [&](auto e, auto) {
             const std::integral_constant<int, 512> threads;
