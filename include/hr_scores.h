@@ -32,8 +32,8 @@ extern "C" {
  * hr_i8_quantize — rows of x as 8-bit integers with a scale for each row:
  *   scale[i] = max_t |x[i, t]| / 127,   q[i, t] = x[i, t] / scale[i] rounded to the nearest whole number (even on ties),
  * both quotients rounded to float32 first, the whole number limited to -127 .. 127 (a scale below the smallest normal number has few
- * bits: of a row with magnitudes below 2.3e-41 the largest may be cut off, by a third at most).  A row whose scale is 0 becomes zeros; a row with a NaN or an infinity becomes
- * zeros with scale NaN, so that every score of it is NaN.
+ * bits: of a row with magnitudes below 2.3e-41 the largest may be cut off, by a third at most).  A row whose scale is 0 becomes zeros; a
+ * row with a NaN or an infinity becomes zeros with scale NaN, so that every score of it is NaN.
  *   x  DEV [m, k] in `dtype`;   q  DEV [m, k] int8, ldq >= k: the bytes behind a row, up to the next multiple of 64 or to the next
  *   row, are set to zero (ldq a multiple of 64 makes products fast);   scale  DEV [m] float32.
  */
