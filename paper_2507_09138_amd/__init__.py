@@ -1,10 +1,10 @@
-"""MI355X-native batched IVF-Flat search and operators around matrices of scores: thin Python binding over the C ABI of
-``hr_ivf.h`` and ``hr_scores.h``.
+"""MI355X-native batched IVF-Flat search, operators around matrices of scores, and layers of the models around them: thin Python
+binding over the C ABI of ``hr_ivf.h``, ``hr_scores.h`` and ``hr_layers.h``.
 
 Argument marshalling only; every step runs in the HIP kernels of
 ``libhr_ivf.so``.  PyTorch supplies device memory and streams.
 
-The names of ``binding`` and ``scores`` are resolved on first use (so that ``python -m
+The names of ``binding``, ``scores`` and ``layers`` are resolved on first use (so that ``python -m
 paper_2507_09138_amd.build`` can run before the library exists); using any of them
 without a built library raises ImportError.
 """
@@ -18,7 +18,12 @@ _SCORES = ["hr_i8_quantize", "hr_i8_workspace_bytes", "hr_i8_product", "hr_i8_li
            "hr_logprobs_backward", "hr_distill_workspace_bytes", "hr_distill_forward", "hr_distill_backward", "hr_distill_step",
            "quantize_rows", "i8_product", "i8_linear", "Logprobs", "logprobs", "logprobs_backward", "distill_forward",
            "distill_backward", "distill_step", "HR_I8_K_MAX", "HR_LIST_MAX", "HR_ROW_MAX"]
-__all__ = _NAMES + _SCORES
+# hr_layers.h: what an encoder or a reader is made of and taught with
+_LAYERS = ["hr_layer_norm", "hr_layer_norm_workspace_bytes", "hr_layer_norm_backward", "hr_gated_workspace_bytes", "hr_gated",
+           "hr_gated_backward_workspace_bytes", "hr_gated_backward", "hr_adamw", "hr_adamw_moments", "hr_adamw_tensor",
+           "LayerNorm", "LayerNormGrads", "layer_norm", "layer_norm_backward", "Gated", "GatedGrads", "gated", "gated_backward", "adamw_state",
+           "adamw", "adamw_moments", "HR_SILU", "HR_GELU", "HR_GELU_TANH", "HR_GATED_MAX", "HR_ADAMW_BLOCK"]
+__all__ = _NAMES + _SCORES + _LAYERS
 
 
 def __getattr__(name):
@@ -28,4 +33,7 @@ def __getattr__(name):
     if name in _SCORES:
         from . import scores
         return getattr(scores, name)
+    if name in _LAYERS:
+        from . import layers
+        return getattr(layers, name)
     raise AttributeError(name)

@@ -21,7 +21,28 @@ inline int check_workspace(const void* ws, size_t bytes, size_t need)
     return HR_OK;
 }
 
+inline bool known_type(int32_t dtype) { return dtype == HR_F32 || dtype == HR_F16 || dtype == HR_BF16; }
+
+inline int check_matrix(const char* name, const void* p, int64_t rows, int64_t k, int64_t ld, size_t es)
+{
+    if (rows > 0 && !p) return fail(HR_ERR_ARG, "%s is null", name);
+    if (ld < k || ld > (1LL << 40)) return fail(HR_ERR_ARG, "rows of %s: %lld elements, %lld apart", name, (long long)k, (long long)ld);
+    if ((uintptr_t)p % es) return fail(HR_ERR_ARG, "%s is not aligned to its elements", name);
+    return HR_OK;
+}
+
 inline size_t aligned(size_t bytes) { return (bytes + HR_WORKSPACE_ALIGN - 1) / HR_WORKSPACE_ALIGN * HR_WORKSPACE_ALIGN; }
 inline size_t element_bytes(int32_t dtype) { return dtype == HR_F32 ? 4 : 2; }
+
+// f(type) with the C++ type of a code
+template <typename F>
+inline auto with_type(int dtype, F&& f)
+{
+    switch (dtype) {
+    case HR_F32: return f(float{});
+    case HR_F16: return f(_Float16{});
+    default: return f(__bf16{});
+    }
+}
 
 }  // namespace hr

@@ -588,17 +588,6 @@ __global__ __launch_bounds__(kFewWaves * 64) void k_i8_few(ProductArgs p)
 // ---- which kernel
 constexpr int64_t kFewBytes = 64 * 1024;                // rows a that every workgroup quantises for itself
 
-// f(type) with the C++ type of a code
-template <typename F>
-static auto with_type(int dtype, F&& f)
-{
-    switch (dtype) {
-    case HR_F32: return f(float{});
-    case HR_F16: return f(_Float16{});
-    default: return f(__bf16{});
-    }
-}
-
 static hipError_t launch_quantize(int dtype, const QuantizeArgs& a, hipStream_t s)
 {
     // A piece for every lane; a workgroup for a row where that is not enough (us: 262144 rows of 768 float32 197 with two pieces per
@@ -711,16 +700,6 @@ static hipError_t launch_product(int dtype, const ProductArgs& p, int8_t* padded
 
 // ---- C entry points
 using namespace hr;
-
-static bool known_type(int32_t dtype) { return dtype == HR_F32 || dtype == HR_F16 || dtype == HR_BF16; }
-
-static int check_matrix(const char* name, const void* p, int64_t rows, int64_t k, int64_t ld, size_t es)
-{
-    if (rows > 0 && !p) return fail(HR_ERR_ARG, "%s is null", name);
-    if (ld < k || ld > (1LL << 40)) return fail(HR_ERR_ARG, "rows of %s: %lld elements, %lld apart", name, (long long)k, (long long)ld);
-    if ((uintptr_t)p % es) return fail(HR_ERR_ARG, "%s is not aligned to its elements", name);
-    return HR_OK;
-}
 
 static int check_shape(int64_t m, int64_t n, int64_t k)
 {
