@@ -1,113 +1,262 @@
-// The gated half of a feed-forward block, act(x w_gate') * (x w_up'), and its gradients (hr_layers.h).
+// The gated half of a feed-forward block, act(x w_gate') * (x w_up'), and its gradients (hr_layers.h): which kernels, and all but the tiles.
 #include <algorithm>
 #include <cmath>
 #include <type_traits>
 
 #include "entry.h"
-#include "hr_layers.h"
-#include "wave.h"
+#include "tile.h"
 
 namespace hr {
 
-// ---- activations: the value and the slope
-constexpr float kSqrtHalf = 0.7071067811865476f, kSqrt2OverPi = 0.7978845608028654f, kOverSqrt2Pi = 0.3989422804014327f;
+template <typename T> constexpr int kE = 16 / (int)sizeof(T);            // elements of 16 bytes
 
-__device__ __forceinline__ float act_value(float z, int act, float& slope)
+// 16 bytes of a row from element t on, zeros from element n on; rows may begin at any element
+template <typename T>
+__device__ __forceinline__ u32x4 load16(const T* row, int t, int n)
 {
-    if (act == HR_SILU) {
-        const float p = 1.0f / (1.0f + expf(-z));
-        slope = p * (1.0f + z * (1.0f - p));
-        return z * p;
+    u32x4 v = {0, 0, 0, 0};
+    if (t + kE<T> <= n) {
+        __builtin_memcpy(&v, row + t, 16);
+    } else if (t < n) {
+        T x[kE<T>];
+#pragma unroll
+        for (int e = 0; e < kE<T>; ++e) x[e] = t + e < n ? row[t + e] : (T)0.0f;
+        __builtin_memcpy(&v, x, 16);
     }
-    if (act == HR_GELU) {
-        const float p = 0.5f * (1.0f + erff(z * kSqrtHalf));
-        slope = p + z * expf(-0.5f * z * z) * kOverSqrt2Pi;
-        return z * p;
-    }
-    const float t = tanhf(kSqrt2OverPi * (z + 0.044715f * z * z * z));
-    slope = 0.5f * (1.0f + t) + 0.5f * z * (1.0f - t * t) * (kSqrt2OverPi * (1.0f + 3 * 0.044715f * z * z));
-    return 0.5f * z * (1.0f + t);
+    return v;
 }
 
-// 16 bytes of k a lane: one matrix instruction of 16 bits, four of 32 bits (k in another order, the same for both operands).
-// The first operand's rows are the result's rows, four of them in the registers of a lane, 4 (lane / 16) .. + 3, in column lane % 16.
-template <typename T> using Frag = T __attribute__((ext_vector_type(16 / sizeof(T))));
-__device__ __forceinline__ floatx4 multiply(Frag<_Float16> a, Frag<_Float16> b, floatx4 c) { return __builtin_amdgcn_mfma_f32_16x16x32_f16(a, b, c, 0, 0, 0); }
-__device__ __forceinline__ floatx4 multiply(Frag<__bf16> a, Frag<__bf16> b, floatx4 c) { return __builtin_amdgcn_mfma_f32_16x16x32_bf16(a, b, c, 0, 0, 0); }
-__device__ __forceinline__ floatx4 multiply(Frag<float> a, Frag<float> b, floatx4 c)
+// ---- rows that tiles cannot take as they are, copied with zeros behind them to multiples of 128 bytes
+template <typename T>
+__global__ __launch_bounds__(256) void k_pad(const T* x, int64_t ldx, int64_t rows, int n, char* out, int64_t ldo)
+{
+    const int64_t pieces = ldo / 16;
+    for (int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x; i < rows * pieces; i += (int64_t)gridDim.x * 256) {
+        const int64_t r = i / pieces;
+        *(u32x4*)(out + i * 16) = load16(x + r * ldx, (int)(i - r * pieces) * kE<T>, n);
+    }
+}
+
+// ---- 64 x 64 elements turned in LDS: rows of 64 elements and one word, so that the elements of a column lie in different banks
+template <typename T> constexpr int kTurn = 64 + 4 / (int)sizeof(T);
+template <typename T>
+__device__ __forceinline__ void turn_in(T* tile, int r, int c, u32x4 v)           // 16 bytes of row r from column c on
 {
 #pragma unroll
-    for (int e = 0; e < 4; ++e) c = __builtin_amdgcn_mfma_f32_16x16x4f32(a[e], b[e], c, 0, 0, 0);
-    return c;
+    for (int e = 0; e < 4; ++e) *(uint32_t*)(tile + r * kTurn<T> + c + e * (4 / (int)sizeof(T))) = v[e];
 }
-
-// out[i, j] = sum_t a[i, t] b[j, t] over one or two stretches of t, any strides
-struct Operand { const void* at; int64_t row, step; };
-struct ProductArgs {
-    Operand a[2], b[2];
-    int stretches;
-    int64_t m, n, k;
-    void *out, *out2; int64_t ldo, ldo2, split;          // rows from `split` on go to out2
-    float* pre; int act;                                 // GATED: b[0] is the gate's matrix, b[1] up's
-};
-template <typename T, bool GATED>
-__global__ __launch_bounds__(256) void k_product(ProductArgs p)
-{
-    constexpr int E = 16 / sizeof(T), K = 4 * E, S = K + E;
-    __shared__ __align__(16) T ta[64 * S], tb[64 * S];
-    constexpr int COLS = GATED ? 32 : 64;
-    const int64_t m0 = (int64_t)blockIdx.x * 64, n0 = (int64_t)blockIdx.y * COLS;
-    const int lane = lane_id(), wave = threadIdx.x / 64;
-    floatx4 acc[4] = {};
-    for (int s = 0; s < (GATED ? 1 : p.stretches); ++s)
-        for (int64_t t0 = 0; t0 < p.k; t0 += K) {
-            __syncthreads();
-            for (int i = threadIdx.x; i < 64 * K; i += 256) {
-                const int r = i / K, t = i % K;
-                const Operand &oa = p.a[s], &ob = p.b[GATED ? r / 32 : s];
-                const int64_t row = m0 + r, col = n0 + (GATED ? r % 32 : r);
-                ta[r * S + t] = row < p.m && t0 + t < p.k ? ((const T*)oa.at)[row * oa.row + (t0 + t) * oa.step] : (T)0.0f;
-                tb[r * S + t] = col < p.n && t0 + t < p.k ? ((const T*)ob.at)[col * ob.row + (t0 + t) * ob.step] : (T)0.0f;
-            }
-            __syncthreads();
-            const Frag<T> fa = *(const Frag<T>*)(ta + (wave * 16 + lane % 16) * S + lane / 16 * E);
-            for (int j = 0; j < 4; ++j) acc[j] = multiply(*(const Frag<T>*)(tb + (j * 16 + lane % 16) * S + lane / 16 * E), fa, acc[j]);
-        }
-    const int64_t row = m0 + wave * 16 + lane % 16;
-    if (row >= p.m) return;
-    for (int j = 0; j < (GATED ? 2 : 4); ++j)
-        for (int e = 0; e < 4; ++e) {
-            const int64_t col = n0 + j * 16 + lane / 16 * 4 + e;
-            if (col >= p.n) continue;
-            if (GATED) {
-                float slope;
-                const float g = acc[j][e], u = acc[j + 2][e];
-                ((T*)p.out)[row * p.ldo + col] = (T)(act_value(g, p.act, slope) * u);
-                if (p.pre) {
-                    p.pre[row * 2 * p.n + col] = g;
-                    p.pre[(row * 2 + 1) * p.n + col] = u;
-                }
-            } else if (row < p.split) {
-                ((T*)p.out)[row * p.ldo + col] = (T)acc[j][e];
-            } else {
-                ((T*)p.out2)[(row - p.split) * p.ldo2 + col] = (T)acc[j][e];
-            }
-        }
-}
-
-// gradients of gate and up, [m][2][f] in T
 template <typename T>
-__global__ __launch_bounds__(256) void k_gated_slopes(const float* pre, const void* dh, int64_t ldh, int64_t m, int64_t f, int act, void* out)
+__device__ __forceinline__ u32x4 turn_out(const T* tile, int c, int r)            // 16 bytes of column c from row r on
 {
-    for (int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x; i < m * f; i += (int64_t)gridDim.x * 256) {
-        const int64_t r = i / f, j = i - r * f;
-        const float g = pre[r * 2 * f + j], u = pre[(r * 2 + 1) * f + j], d = (float)((const T*)dh)[r * ldh + j];
-        float slope;
-        const float a = act_value(g, act, slope);
-        ((T*)out)[r * 2 * f + j] = (T)(d * u * slope);
-        ((T*)out)[(r * 2 + 1) * f + j] = (T)(d * a);
+    T x[kE<T>];
+#pragma unroll
+    for (int e = 0; e < kE<T>; ++e) x[e] = tile[(r + e) * kTurn<T> + c];
+    u32x4 v;
+    __builtin_memcpy(&v, x, 16);
+    return v;
+}
+
+// out[c, r] = x[r, c], rows of `out` filled up with zeros to whole blocks of 64 rows of x (as far as ldo, in elements, goes)
+template <typename T>
+__global__ __launch_bounds__(256) void k_turn(const T* x, int64_t ldx, int rows, int cols, T* out, int64_t ldo, int padded)
+{
+    __shared__ __align__(16) T tile[64 * kTurn<T>];
+    constexpr int E = kE<T>, PER = 64 / E;
+    const int r0 = blockIdx.y * 64, c0 = blockIdx.x * 64;
+    for (int i = threadIdx.x; i < 64 * PER; i += 256) {
+        const int r = i / PER, c = i % PER * E;
+        turn_in(tile, r, c, r0 + r < rows ? load16(x + (int64_t)(r0 + r) * ldx, c0 + c, cols) : u32x4{0, 0, 0, 0});
+    }
+    __syncthreads();
+    for (int i = threadIdx.x; i < 64 * PER; i += 256) {
+        const int c = i / PER, r = i % PER * E;
+        if (c0 + c < cols && r0 + r < padded) *(u32x4*)(out + (int64_t)(c0 + c) * ldo + r0 + r) = turn_out(tile, c, r);
     }
 }
+
+// ---- gradients of gate and up in T, as rows [m][2 fp] (gate's, then up's, zeros behind each) and as columns [2 f][mp] (zeros behind them):
+// 64 x 64 of both a workgroup.  Either may be left out.
+template <typename T>
+__global__ __launch_bounds__(256) void k_gated_slopes(const float* pre, const T* dh, int64_t ldh, int m, int f, int act, T* rows, int fp, T* cols, int mp)
+{
+    __shared__ __align__(16) T tiles[2][64 * kTurn<T>];
+    constexpr int E = kE<T>, PER = 64 / E;
+    const int r0 = blockIdx.y * 64, c0 = blockIdx.x * 64;
+    for (int i = threadIdx.x; i < 64 * PER; i += 256) {
+        const int r = i / PER, c = i % PER * E;
+        T dg[E], du[E];
+        T d[E];
+        const bool in = r0 + r < m;
+        const u32x4 raw = in ? load16(dh + (int64_t)(r0 + r) * ldh, c0 + c, f) : u32x4{0, 0, 0, 0};
+        __builtin_memcpy(d, &raw, 16);
+        const float* at = pre + (int64_t)(r0 + r) * 2 * f + c0 + c;
+#pragma unroll
+        for (int e = 0; e < E; ++e) {
+            dg[e] = du[e] = (T)0.0f;
+            if (!in || c0 + c + e >= f) continue;
+            float slope;
+            const float a = act_value(at[e], act, slope);
+            dg[e] = (T)((float)d[e] * at[f + e] * slope);
+            du[e] = (T)((float)d[e] * a);
+        }
+        u32x4 g, u;
+        __builtin_memcpy(&g, dg, 16);
+        __builtin_memcpy(&u, du, 16);
+        if (rows && in && c0 + c < fp) {
+            *(u32x4*)(rows + (int64_t)(r0 + r) * 2 * fp + c0 + c) = g;
+            *(u32x4*)(rows + (int64_t)(r0 + r) * 2 * fp + fp + c0 + c) = u;
+        }
+        turn_in(tiles[0], r, c, g);
+        turn_in(tiles[1], r, c, u);
+    }
+    if (!cols) return;
+    __syncthreads();
+    for (int i = threadIdx.x; i < 2 * 64 * PER; i += 256) {
+        const int up = i / (64 * PER), c = i / PER % 64, r = i % PER * E;
+        if (c0 + c < f && r0 + r < mp) *(u32x4*)(cols + ((int64_t)up * f + c0 + c) * mp + r0 + r) = turn_out(tiles[up], c, r);
+    }
+}
+
+template <typename T>
+__global__ __launch_bounds__(256) void k_clear(T* x, int64_t ld, int64_t rows, int64_t n)
+{
+    for (int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x; i < rows * n; i += (int64_t)gridDim.x * 256) x[i / n * ld + i % n] = (T)0.0f;
+}
+
+// ---- up to 16 MT rows x: bound by reading the matrices, straight to registers, once.  A workgroup takes eight columns of the result, its waves
+// parts of k; the first operand of a matrix instruction is eight rows of each matrix.  Rows may begin anywhere.
+template <typename T, int MT>
+__global__ __launch_bounds__(1024) void k_gated_few(const T* x, int64_t ldx, const T* gate, int64_t ldg, const T* up, int64_t ldu, int m, int k, int f, int act, T* out,
+                                                    int64_t ldo, float* pre)
+{
+    constexpr int K = 4 * kE<T>, U = 8;
+    __shared__ floatx4 sums[16][MT][64];
+    const int lane = lane_id(), wave = threadIdx.x / 64, share = blockDim.x / 64, row = lane % 16, first = blockIdx.x * 8;
+    const int steps = (k + K - 1) / K, begin = steps * wave / share, end = steps * (wave + 1) / share;
+    const int col = min(first + row % 8, f - 1), t0 = lane / 16 * kE<T>;
+    const T* w = row < 8 ? gate + (int64_t)col * ldg : up + (int64_t)col * ldu;
+    const T* xr[MT];
+#pragma unroll
+    for (int i = 0; i < MT; ++i) xr[i] = x + (int64_t)min(row + 16 * i, m - 1) * ldx;
+    floatx4 acc[MT] = {};
+    int s = begin;
+    for (; s + U <= end && (s + U) * K <= k; s += U) {
+        u32x4 b[U], a[U][MT];
+#pragma unroll
+        for (int u = 0; u < U; ++u) {
+            __builtin_memcpy(&b[u], w + (s + u) * K + t0, 16);
+#pragma unroll
+            for (int i = 0; i < MT; ++i) __builtin_memcpy(&a[u][i], xr[i] + (s + u) * K + t0, 16);
+        }
+#pragma unroll
+        for (int u = 0; u < U; ++u)
+#pragma unroll
+            for (int i = 0; i < MT; ++i) acc[i] = multiply(T{}, b[u], a[u][i], acc[i]);
+    }
+    for (; s < end; ++s) {
+        const u32x4 b = load16(w, s * K + t0, k);
+#pragma unroll
+        for (int i = 0; i < MT; ++i) acc[i] = multiply(T{}, b, load16(xr[i], s * K + t0, k), acc[i]);
+    }
+#pragma unroll
+    for (int i = 0; i < MT; ++i) sums[wave][i][lane] = acc[i];
+    __syncthreads();
+    if (wave >= MT) return;
+    for (int i = wave; i < MT; i += share) {
+        floatx4 v = sums[0][i][lane];
+        for (int q = 1; q < share; ++q) v += sums[q][i][lane];
+        float u[4];
+#pragma unroll
+        for (int e = 0; e < 4; ++e) u[e] = __shfl(v[e], lane ^ 32);         // (lanes 32 .. 63 hold up's sums)
+        const int r = row + 16 * i, c = first + lane / 16 * 4;
+        if (lane >= 32 || r >= m) continue;
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+            if (c + e >= f) continue;
+            float slope;
+            out[r * ldo + c + e] = (T)(act_value(v[e], act, slope) * u[e]);
+            if (pre) {
+                pre[(int64_t)r * 2 * f + c + e] = v[e];
+                pre[((int64_t)r * 2 + 1) * f + c + e] = u[e];
+            }
+        }
+    }
+}
+
+// ---- rows of any alignment, or further apart than tiles reach, that are not copied: tiles of 64 rows and 32 columns of the result, staged through
+// registers, one block of 64 bytes of k at a time
+template <typename T>
+__global__ __launch_bounds__(256) void k_gated_any(const T* x, int64_t ldx, const T* gate, int64_t ldg, const T* up, int64_t ldu, int m, int k, int f, int act, T* out,
+                                                   int64_t ldo, float* pre)
+{
+    constexpr int E = kE<T>, K = 4 * E, S = K + E;
+    __shared__ __align__(16) T ta[64 * S], tb[64 * S];
+    const int m0 = blockIdx.x * 64, n0 = blockIdx.y * 32;
+    const int lane = lane_id(), wave = threadIdx.x / 64, r = threadIdx.x / 4, t = threadIdx.x % 4 * E;
+    const T* ra = x + (int64_t)min(m0 + r, m - 1) * ldx;
+    const T* rb = r < 32 ? gate + (int64_t)min(n0 + r, f - 1) * ldg : up + (int64_t)min(n0 + r - 32, f - 1) * ldu;
+    floatx4 acc[4] = {};
+    for (int k0 = 0; k0 < k; k0 += K) {
+        const u32x4 va = load16(ra, k0 + t, k), vb = load16(rb, k0 + t, k);
+        __syncthreads();
+        *(u32x4*)(ta + r * S + t) = va;
+        *(u32x4*)(tb + r * S + t) = vb;
+        __syncthreads();
+        const u32x4 fa = *(const u32x4*)(ta + (wave * 16 + lane % 16) * S + lane / 16 * E);
+#pragma unroll
+        for (int j = 0; j < 4; ++j) acc[j] = multiply(T{}, *(const u32x4*)(tb + (j * 16 + lane % 16) * S + lane / 16 * E), fa, acc[j]);
+    }
+    const int row = m0 + wave * 16 + lane % 16;
+    if (row >= m) return;
+#pragma unroll
+    for (int j = 0; j < 2; ++j)
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+            const int col = n0 + j * 16 + lane / 16 * 4 + e;
+            if (col >= f) continue;
+            float slope;
+            const float g = acc[j][e], u = acc[j + 2][e];
+            out[(int64_t)row * ldo + col] = (T)(act_value(g, act, slope) * u);
+            if (pre) {
+                pre[(int64_t)row * 2 * f + col] = g;
+                pre[((int64_t)row * 2 + 1) * f + col] = u;
+            }
+        }
+}
+
+// ---- which kernel
+
+// Tiles (rows x columns): 256 x 256 or 128 x 128, whichever takes less time, or 64 x 256 for few rows; in parts of k where the tiles are
+// few.  Large tiles come in rounds of one for every compute unit, a round taking as long as about 780 small ones.  k_bytes: of a row.
+Tiling tiling_for(bool gated, int64_t m, int64_t n, int64_t k_bytes)
+{
+    auto tiles = [&](int bm, int bn) { return (m + bm - 1) / bm * ((n + bn / (gated ? 2 : 1) - 1) / (bn / (gated ? 2 : 1))); };
+    Tiling t{128, 128, 1, (int)k_bytes};
+    if (m <= 64) t.bm = 64, t.bn = 256;
+    else if (tiles(128, 128) >= (tiles(256, 256) + kComputeUnits - 1) / kComputeUnits * 780) t.bm = t.bn = 256;
+    const int64_t all = tiles(t.bm, t.bn);
+    if (all < kComputeUnits) {
+        const int64_t blocks = k_bytes / 128, parts = std::min(kComputeUnits / all, blocks / 4);        // (four blocks of k at least)
+        if (parts > 1) {
+            t.part_k = (int)((blocks + parts - 1) / parts * 128);
+            t.parts = (int)((k_bytes + t.part_k - 1) / t.part_k);
+        }
+    }
+    return t;
+}
+// Room for the sums of parts of k of a product with m rows or fewer: tiles times parts are never more than the compute units, and a tile is
+// 128 x 128 or 64 x 256 sums.
+static size_t sums_bytes(int64_t m, int64_t columns, int64_t k_bytes)
+{
+    const int64_t most = std::max<int64_t>(1, k_bytes / 128 / 4);
+    if (most == 1) return 0;
+    return aligned((size_t)(std::min<int64_t>((int64_t)kComputeUnits * 128 * 128, most * ((m + 63) / 64 * 64) * columns) * 4));
+}
+
+static int64_t padded(int64_t n, size_t es) { return (n * (int64_t)es + 127) / 128 * 128; }             // bytes of a row
+// rows that requests of 16 bytes reach; offsets inside a tile are 32-bit numbers
+static bool in_tiles(const void* p, int64_t ld, size_t es) { return (uintptr_t)p % 16 == 0 && ld * es % 16 == 0 && ld * es <= (1 << 22); }
+constexpr int kFewRows = 32;
 
 static int check_gated(int64_t m, int64_t k, int64_t f, int32_t dtype, int32_t activation)
 {
@@ -119,10 +268,107 @@ static int check_gated(int64_t m, int64_t k, int64_t f, int32_t dtype, int32_t a
     return HR_OK;
 }
 
-template <typename T, bool GATED>
-static void launch(const ProductArgs& p, hipStream_t s)
+template <typename T>
+static hipError_t launch_pad(const void* x, int64_t ldx, int64_t rows, int64_t n, void* out, hipStream_t s)
 {
-    hipLaunchKernelGGL((k_product<T, GATED>), dim3((unsigned)((p.m + 63) / 64), (unsigned)((p.n + (GATED ? 31 : 63)) / (GATED ? 32 : 64))), dim3(256), 0, s, p);
+    const int64_t ldo = padded(n, sizeof(T));
+    hipLaunchKernelGGL(k_pad<T>, dim3((unsigned)std::min<int64_t>((rows * (ldo / 16) + 255) / 256, 1 << 20)), dim3(256), 0, s, (const T*)x, ldx, rows, (int)n, (char*)out, ldo);
+    return hipGetLastError();
+}
+
+// waves that take parts of k of the same eight columns: enough for the chip to be busy, four steps each at least
+static int few_share(int64_t f, int64_t k_bytes)
+{
+    int share = 1;
+    while (share < 16 && (f + 7) / 8 * share < 4096 && k_bytes / 64 >= 8 * share) share *= 2;
+    return share;
+}
+
+struct GatedArgs {
+    const void* x; int64_t ldx;
+    const void* gate; int64_t ldg;
+    const void* up; int64_t ldu;
+    int64_t m, k, f; int act;
+    void* out; int64_t ldo; float* pre;
+};
+
+// workspace: x and both matrices with padded rows, where rows of k elements are not whole blocks; sums of the parts of k
+static size_t x_bytes(int64_t m, int64_t k, size_t es) { return k * es % 128 ? aligned((size_t)(m * padded(k, es))) : 0; }
+static size_t w_bytes(int64_t k, int64_t f, size_t es) { return k * es % 128 ? aligned((size_t)(2 * f * padded(k, es))) : 0; }
+
+template <typename T>
+static hipError_t launch_gated(const GatedArgs& g, char* ws, hipStream_t s)
+{
+    constexpr size_t es = sizeof(T);
+    if (g.m <= kFewRows) {
+        const int share = few_share(g.f, g.k * es);
+        auto go = [&](auto kernel) {
+            hipLaunchKernelGGL(kernel, dim3((unsigned)((g.f + 7) / 8)), dim3(64 * share), 0, s, (const T*)g.x, g.ldx, (const T*)g.gate, g.ldg, (const T*)g.up, g.ldu, (int)g.m, (int)g.k,
+                               (int)g.f, g.act, (T*)g.out, g.ldo, g.pre);
+        };
+        if (g.m <= 16) go(k_gated_few<T, 1>);
+        else go(k_gated_few<T, 2>);
+        return hipGetLastError();
+    }
+    TileArgs p{};
+    p.k = (int)padded(g.k, es);
+    if (g.k * es % 128) {
+        char *px = ws, *pw = ws + x_bytes(g.m, g.k, es);
+        if (hipError_t e = launch_pad<T>(g.x, g.ldx, g.m, g.k, px, s)) return e;
+        if (hipError_t e = launch_pad<T>(g.gate, g.ldg, g.f, g.k, pw, s)) return e;
+        if (hipError_t e = launch_pad<T>(g.up, g.ldu, g.f, g.k, pw + g.f * p.k, s)) return e;
+        p.a = px;
+        p.b = pw;
+        p.up = pw + g.f * p.k;
+        p.lda = p.ldb = p.ldup = p.k;
+    } else if (in_tiles(g.x, g.ldx, es) && in_tiles(g.gate, g.ldg, es) && in_tiles(g.up, g.ldu, es)) {
+        p.a = (const char*)g.x;
+        p.b = (const char*)g.gate;
+        p.up = (const char*)g.up;
+        p.lda = g.ldx * es;
+        p.ldb = g.ldg * es;
+        p.ldup = g.ldu * es;
+    } else {
+        hipLaunchKernelGGL(k_gated_any<T>, dim3((unsigned)((g.m + 63) / 64), (unsigned)((g.f + 31) / 32)), dim3(256), 0, s, (const T*)g.x, g.ldx, (const T*)g.gate, g.ldg,
+                           (const T*)g.up, g.ldu, (int)g.m, (int)g.k, (int)g.f, g.act, (T*)g.out, g.ldo, g.pre);
+        return hipGetLastError();
+    }
+    p.m = g.m;
+    p.n = g.f;
+    p.out = g.out;
+    p.ldo = g.ldo;
+    p.pre = g.pre;
+    p.act = g.act;
+    p.sums = (float*)(ws + x_bytes(g.m, g.k, es) + w_bytes(g.k, g.f, es));
+    return launch_tiles<T, true>(tiling_for(true, g.m, g.f, p.k), p, s);
+}
+
+// workspace of the gradients: those of gate and up as rows, [m][2 fp], and as columns, [2 f][mp]; both matrices turned, [k][2 fp]; x turned, [k][mp];
+// sums of the parts of the products' k.  fp, mp: whole blocks.
+struct BackwardPlan {
+    int64_t fp, mp;                                      // elements
+    size_t rows, cols, w, x, sums, all;                  // where each begins, and the end
+};
+static BackwardPlan backward_plan(int64_t m, int64_t k, int64_t f, size_t es)
+{
+    BackwardPlan p;
+    const int64_t fb = padded(f, es), mb = padded(m, es);
+    p.fp = fb / es;
+    p.mp = mb / es;
+    p.rows = 0;
+    p.cols = p.rows + aligned((size_t)(m * 2 * fb));
+    p.w = p.cols + aligned((size_t)(2 * f * mb));
+    p.x = p.w + aligned((size_t)(k * 2 * fb));
+    p.sums = p.x + aligned((size_t)(k * mb));
+    p.all = p.sums + std::max(sums_bytes(m, k, 2 * fb), sums_bytes(2 * f, k, mb)) + HR_WORKSPACE_ALIGN;
+    return p;
+}
+
+template <typename T>
+static hipError_t launch_turn(const void* x, int64_t ldx, int64_t rows, int64_t cols, void* out, int64_t ldo, int64_t padded, hipStream_t s)
+{
+    hipLaunchKernelGGL(k_turn<T>, dim3((unsigned)((cols + 63) / 64), (unsigned)((padded + 63) / 64)), dim3(256), 0, s, (const T*)x, ldx, (int)rows, (int)cols, (T*)out, ldo, (int)padded);
+    return hipGetLastError();
 }
 
 }  // namespace hr
@@ -135,7 +381,9 @@ extern "C" {
 size_t hr_gated_workspace_bytes(int64_t m, int64_t k, int64_t f, int32_t dtype)
 {
     if (check_gated(m, k, f, dtype, HR_SILU)) return 0;
-    return HR_WORKSPACE_ALIGN;
+    const size_t es = element_bytes(dtype);
+    if (m <= kFewRows) return HR_WORKSPACE_ALIGN;
+    return x_bytes(m, k, es) + w_bytes(k, f, es) + sums_bytes(m, 2 * f, padded(k, es)) + HR_WORKSPACE_ALIGN;
 }
 
 int hr_gated(const void* x, int64_t ldx, const void* w_gate, int64_t ldwg, const void* w_up, int64_t ldwu, int32_t dtype, int64_t m, int64_t k,
@@ -150,26 +398,15 @@ int hr_gated(const void* x, int64_t ldx, const void* w_gate, int64_t ldwg, const
     if ((uintptr_t)out_pre % 4) return fail(HR_ERR_ARG, "out_pre is not aligned to its elements");
     if (m == 0) return HR_OK;
     if (int rc = check_workspace(workspace, workspace_bytes, hr_gated_workspace_bytes(m, k, f, dtype))) return rc;
-    ProductArgs p{};
-    p.a[0] = {x, ldx, 1};
-    p.b[0] = {w_gate, ldwg, 1};
-    p.b[1] = {w_up, ldwu, 1};
-    p.m = m;
-    p.n = f;
-    p.k = k;
-    p.out = out;
-    p.ldo = ldo;
-    p.pre = out_pre;
-    p.act = activation;
-    with_type(dtype, [&](auto t) { launch<decltype(t), true>(p, (hipStream_t)stream); });
-    HR_HIP(hipGetLastError());
+    const GatedArgs g{x, ldx, w_gate, ldwg, w_up, ldwu, m, k, f, activation, out, ldo, out_pre};
+    HR_HIP(with_type(dtype, [&](auto t) { return launch_gated<decltype(t)>(g, (char*)workspace, (hipStream_t)stream); }));
     return HR_OK;
 }
 
 size_t hr_gated_backward_workspace_bytes(int64_t m, int64_t k, int64_t f, int32_t dtype)
 {
     if (check_gated(m, k, f, dtype, HR_SILU)) return 0;
-    return aligned((size_t)(m * 2 * f) * element_bytes(dtype)) + HR_WORKSPACE_ALIGN;
+    return backward_plan(m, k, f, element_bytes(dtype)).all;
 }
 
 int hr_gated_backward(const void* x, int64_t ldx, const void* w_gate, int64_t ldwg, const void* w_up, int64_t ldwu, int32_t dtype, int64_t m,
@@ -194,42 +431,49 @@ int hr_gated_backward(const void* x, int64_t ldx, const void* w_gate, int64_t ld
     }
     if (int rc = check_workspace(workspace, workspace_bytes, hr_gated_backward_workspace_bytes(m, k, f, dtype))) return rc;
     hipStream_t s = (hipStream_t)stream;
-    char* d = (char*)workspace;
-    with_type(dtype, [&](auto t) {
+    const BackwardPlan plan = backward_plan(m, k, f, es);
+    char *rows = (char*)workspace + plan.rows, *cols = (char*)workspace + plan.cols, *turned_w = (char*)workspace + plan.w, *turned_x = (char*)workspace + plan.x;
+    HR_HIP(with_type(dtype, [&](auto t) -> hipError_t {
         using T = decltype(t);
-        if (m > 0) hipLaunchKernelGGL(k_gated_slopes<T>, dim3((unsigned)std::min<int64_t>((m * f + 255) / 256, 1 << 20)), dim3(256), 0, s, pre, grad_out, ldgo, m, f, activation, d);
-        if (grad_x && m > 0) {
-            ProductArgs p{};
-            p.a[0] = {d, 2 * f, 1};
-            p.a[1] = {d + f * es, 2 * f, 1};
-            p.b[0] = {w_gate, 1, ldwg};
-            p.b[1] = {w_up, 1, ldwu};
-            p.stretches = 2;
-            p.m = m;
+        if (m == 0) {                                    // (sums over no rows)
+            if (!grad_w_gate) return hipSuccess;
+            const unsigned blocks = (unsigned)std::min<int64_t>((f * k + 255) / 256, 1 << 20);
+            hipLaunchKernelGGL(k_clear<T>, dim3(blocks), dim3(256), 0, s, (T*)grad_w_gate, ldgg, f, k);
+            hipLaunchKernelGGL(k_clear<T>, dim3(blocks), dim3(256), 0, s, (T*)grad_w_up, ldgu, f, k);
+            return hipGetLastError();
+        }
+        hipLaunchKernelGGL(k_gated_slopes<T>, dim3((unsigned)((plan.fp + 63) / 64), (unsigned)((plan.mp + 63) / 64)), dim3(256), 0, s, pre, (const T*)grad_out, ldgo, (int)m, (int)f,
+                           activation, grad_x ? (T*)rows : nullptr, (int)plan.fp, grad_w_gate ? (T*)cols : nullptr, (int)plan.mp);
+        TileArgs p{};
+        p.sums = (float*)((char*)workspace + plan.sums);
+        if (grad_x) {
+            if (hipError_t e = launch_turn<T>(w_gate, ldwg, f, k, turned_w, 2 * plan.fp, plan.fp, s)) return e;
+            if (hipError_t e = launch_turn<T>(w_up, ldwu, f, k, (T*)turned_w + plan.fp, 2 * plan.fp, plan.fp, s)) return e;
+            p.a = rows;
+            p.b = turned_w;
+            p.lda = p.ldb = p.k = (int)(2 * plan.fp * sizeof(T));
+            p.m = p.split = m;
             p.n = k;
-            p.k = f;
             p.out = grad_x;
             p.ldo = ldgx;
-            p.split = m;
-            launch<T, false>(p, s);
+            if (hipError_t e = launch_tiles<T, false>(tiling_for(false, p.m, p.n, p.k), p, s)) return e;
         }
         if (grad_w_gate) {
-            ProductArgs p{};
-            p.a[0] = {d, 1, 2 * f};
-            p.b[0] = {x, 1, ldx};
-            p.stretches = 1;
+            if (hipError_t e = launch_turn<T>(x, ldx, m, k, turned_x, plan.mp, plan.mp, s)) return e;
+            p.a = cols;
+            p.b = turned_x;
+            p.lda = p.ldb = p.k = (int)(plan.mp * sizeof(T));
             p.m = 2 * f;
+            p.split = f;
             p.n = k;
-            p.k = m;
             p.out = grad_w_gate;
             p.out2 = grad_w_up;
             p.ldo = ldgg;
             p.ldo2 = ldgu;
-            p.split = f;
-            launch<T, false>(p, s);
+            if (hipError_t e = launch_tiles<T, false>(tiling_for(false, p.m, p.n, p.k), p, s)) return e;
         }
-    });
-    HR_HIP(hipGetLastError());
+        return hipGetLastError();
+    }));
     return HR_OK;
 }
 

@@ -1,0 +1,7 @@
+// Tiles of float32 products (see tile.h).
+#include "tile_launch.h"
+
+namespace hr {
+template hipError_t launch_tiles<float, false>(const Tiling&, TileArgs, hipStream_t);
+template hipError_t launch_tiles<float, true>(const Tiling&, TileArgs, hipStream_t);
+}  // namespace hr

@@ -1,0 +1,264 @@
+// Products of floating point matrices in tiles (16-bit types and float32), and the gated block's arithmetic: what gated*.hip share.
+#pragma once
+#include "common.h"
+#include "hr_layers.h"
+#include "wave.h"
+
+namespace hr {
+
+// ---- activations: the value and the slope
+constexpr float kSqrtHalf = 0.7071067811865476f, kSqrt2OverPi = 0.7978845608028654f, kOverSqrt2Pi = 0.3989422804014327f;
+
+__device__ __forceinline__ float act_value(float z, int act, float& slope)
+{
+    if (act == HR_SILU) {
+        const float p = 1.0f / (1.0f + expf(-z));
+        slope = p * (1.0f + z * (1.0f - p));
+        return z * p;
+    }
+    if (act == HR_GELU) {
+        const float p = 0.5f * (1.0f + erff(z * kSqrtHalf));
+        slope = p + z * expf(-0.5f * z * z) * kOverSqrt2Pi;
+        return z * p;
+    }
+    const float t = tanhf(kSqrt2OverPi * (z + 0.044715f * z * z * z));
+    slope = 0.5f * (1.0f + t) + 0.5f * z * (1.0f - t * t) * (kSqrt2OverPi * (1.0f + 3 * 0.044715f * z * z));
+    return 0.5f * z * (1.0f + t);
+}
+
+// 16 bytes of k a lane, lane l those of row l % 16 from byte 16 (l / 16) on of a step of 64: one matrix instruction of 16 bits, four of 32 (the
+// k of a step in another order, the same for both operands).  The first operand's rows are the result's rows, four of them in the registers of
+// lane l, 4 (l / 16) .. + 3, in column l % 16: with the rows of b first a lane holds four neighbouring outputs of a row of a.
+__device__ __forceinline__ floatx4 multiply(_Float16, u32x4 b, u32x4 a, floatx4 c)
+{
+    return __builtin_amdgcn_mfma_f32_16x16x32_f16(__builtin_bit_cast(half8, b), __builtin_bit_cast(half8, a), c, 0, 0, 0);
+}
+__device__ __forceinline__ floatx4 multiply(__bf16, u32x4 b, u32x4 a, floatx4 c)
+{
+    return __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, b), __builtin_bit_cast(bf16x8, a), c, 0, 0, 0);
+}
+__device__ __forceinline__ floatx4 multiply(float, u32x4 b, u32x4 a, floatx4 c)
+{
+#pragma unroll
+    for (int e = 0; e < 4; ++e) c = __builtin_amdgcn_mfma_f32_16x16x4f32(__builtin_bit_cast(float, (uint32_t)b[e]), __builtin_bit_cast(float, (uint32_t)a[e]), c, 0, 0, 0);
+    return c;
+}
+
+// What tiles take: out[i, j] = sum_t a[i, t] b[j, t], all distances in bytes.  Rows begin at multiples of 16 bytes, `k` is a multiple of 128.
+struct TileArgs {
+    const char* a; int64_t lda;
+    const char* b; int64_t ldb;                          // gated: the gate's matrix
+    const char* up; int64_t ldup;                        // gated: up's
+    int64_t m, n; int k;                                 // n: columns of the result
+    int parts, part_k;                                   // parts of k (part_k bytes each, a multiple of 128), and where there are more than one
+    float* sums;                                         // their sums, [parts][m][n], gated [parts][m][2][n]
+    void* out; int64_t ldo;                              // elements apart
+    void* out2; int64_t ldo2, split;                     // rows from `split` on go to out2
+    float* pre; int act;                                 // gated
+};
+
+// eight neighbouring outputs of a row, as far as they are there
+template <typename O>
+__device__ __forceinline__ void store_eight(O* at, int64_t col, int64_t n, const float* v)
+{
+    typedef O outs __attribute__((ext_vector_type(8)));
+    outs o;
+#pragma unroll
+    for (int e = 0; e < 8; ++e) o[e] = (O)v[e];
+    if (col + 8 <= n) {
+        __builtin_memcpy(at + col, &o, sizeof o);
+    } else {
+#pragma unroll
+        for (int e = 0; e < 8; ++e)
+            if (col + e < n) at[col + e] = o[e];
+    }
+}
+
+// Eight neighbouring results of row `row`: of both matrices where the block is gated.
+template <typename T, bool GATED>
+__device__ __forceinline__ void finish(const TileArgs& p, int64_t row, int64_t col, const float* v, const float* up)
+{
+    if constexpr (GATED) {
+        float h[8], slope;
+#pragma unroll
+        for (int e = 0; e < 8; ++e) h[e] = act_value(v[e], p.act, slope) * up[e];
+        store_eight((T*)p.out + row * p.ldo, col, p.n, h);
+        if (p.pre) {
+            store_eight(p.pre + row * 2 * p.n, col, p.n, v);
+            store_eight(p.pre + (row * 2 + 1) * p.n, col, p.n, up);
+        }
+    } else {
+        store_eight(row < p.split ? (T*)p.out + row * p.ldo : (T*)p.out2 + (row - p.split) * p.ldo2, col, p.n, v);
+    }
+}
+
+// ---- tiles of BM x BN, a wave's share of them WM x 64.  Gated: the tile's BN rows b are BN / 2 of each matrix.
+// Blocks of 128 bytes of k of both sides go straight to LDS, into one of NB buffers; rows of 128 bytes, whole lines.  A wave's load
+// brings 8 rows; the 16-byte pieces of row r lie at place piece ^ r % 8, so that the lanes of a read lie in different banks.  The fragments of a
+// step of 64 bytes are read while the step before is multiplied; where those of a block's second step have been read by all waves its buffer is
+// filled again: one barrier a block.  Where there is no more than a tile for every compute unit nothing else hides the time that loads take: NB
+// buffers, all but one on their way.  Else a workgroup goes from tile to tile and asks for the next one's first blocks before it writes its outputs.
+template <typename T, bool GATED, int BM, int BN, int WM, int NB>
+__global__ __launch_bounds__(BM / WM * (BN / 64) * 64) void k_tiles(TileArgs p)
+{
+    constexpr int WN = 64, WAVES = BM / WM * (BN / WN), TM = WM / 16, TN = 4, BK = 128, UNITS = (BM + BN) / 8 / WAVES, BUF = (BM + BN) * BK;
+    constexpr int COLS = GATED ? BN / 2 : BN;            // of the result
+    static_assert(BM / 8 % WAVES == 0 && BN / 8 % WAVES == 0 && NB >= 2 && NB <= 4);
+    extern __shared__ __align__(1024) char lds[];
+    const int lane = lane_id(), wave = __builtin_amdgcn_readfirstlane(threadIdx.x / 64);
+    const int wm = wave / (BN / WN) * WM, wn = wave % (BN / WN) * WN;
+    const int k_begin = blockIdx.y * p.part_k, k_end = min(p.k, k_begin + p.part_k), blocks = (k_end - k_begin) / BK;
+    const int piece = ((lane & 7) ^ (lane >> 3)) * 16;
+    const uint32_t lds0 = lds_addr(lds);
+
+    // Tiles that run at the same time on an XCD share its L2: each has a stretch of the tiles, and takes them in blocks of four rows of tiles.
+    const int m = (int)p.m, n = (int)p.n, tiles_m = (m + BM - 1) / BM, tiles_n = (n + COLS - 1) / COLS, tiles = tiles_m * tiles_n;
+    const int stretch = (tiles + 7) / 8, tile0 = (int)(blockIdx.x % 8) * stretch, end = min(stretch, tiles - tile0);
+    int tile = blockIdx.x / 8, m0 = 0, n0 = 0;
+    uint32_t off[UNITS];                                 // (rows of a tile lie within 2^31 bytes: the host sees to it)
+    const char *ga = p.a, *gb = p.b, *gu = p.up;
+    // What lies in row r of b's part of a buffer.  Rows 0 .. 15 and 16 .. 31 of 32 are four of each eight columns, so that a lane has eight neighbouring
+    // outputs in two fragments; gated: 32 rows of the gate, then the same 32 of up.
+    auto column_of = [&](int r) __attribute__((always_inline)) {
+        const int c = (r & 12) << 1 | (r & 16) >> 2 | (r & 3);
+        return GATED ? r / 64 * 32 + c : (r & ~31) | c;
+    };
+    auto is_up = [&](int i) __attribute__((always_inline)) { return GATED && (((i * WAVES + wave) * 8 - BM) & 32) != 0; };       // (of a load: the same for its 8 rows)
+    auto aim = [&](int t) __attribute__((always_inline)) {
+        t += tile0;
+        const int g = t / (4 * tiles_n), rest = t - g * 4 * tiles_n, high = min(4, tiles_m - g * 4);
+        m0 = (g * 4 + rest % high) * BM;
+        n0 = rest / high * COLS;
+        ga = p.a + (int64_t)m0 * p.lda;
+        gb = p.b + (int64_t)n0 * p.ldb;
+        if (GATED) gu = p.up + (int64_t)n0 * p.ldup;
+#pragma unroll
+        for (int i = 0; i < UNITS; ++i) {
+            const int row = (i * WAVES + wave) * 8 + lane / 8;
+            off[i] = (i * WAVES * 8 < BM ? (uint32_t)min(row, m - 1 - m0) * (uint32_t)p.lda
+                                         : (uint32_t)min(column_of(row - BM), n - 1 - n0) * (uint32_t)(is_up(i) ? p.ldup : p.ldb)) + piece;
+        }
+    };
+    auto request = [&](int block) __attribute__((always_inline)) {
+        const int k0 = k_begin + block * BK;
+#pragma unroll
+        for (int i = 0; i < UNITS; ++i)
+            lds_dma16((i * WAVES * 8 < BM ? ga : (is_up(i) ? gu : gb)) + k0, off[i], lds0 + (uint32_t)block % NB * BUF + (i * WAVES + wave) * 1024);
+    };
+
+    const int frag = (lane % 16) * BK + ((lane / 16) ^ (lane & 7)) * 16;
+    floatx4 acc[TM][TN];
+    u32x4 a[TM], b0[TN], b1[TN];
+    auto place = [&](int block, int ks) __attribute__((always_inline)) { return lds + ((frag ^ (ks * 64)) + (uint32_t)block % NB * BUF); };
+    auto read_b = [&](u32x4* f, int block, int ks) __attribute__((always_inline)) {
+        const char* at = place(block, ks) + (BM + wn) * BK;
+#pragma unroll
+        for (int j = 0; j < TN; ++j) f[j] = *(const u32x4*)(at + j * 16 * BK);
+    };
+    // one step: fragments a and b; where a fragment of a has been used for the last time the next step's takes its registers
+    // (at a raised priority: the wave that shares the SIMD and is behind does its reads and requests in between)
+    auto step = [&](const u32x4* b, const char* next) __attribute__((always_inline)) {
+        __builtin_amdgcn_s_setprio(1);
+#pragma unroll
+        for (int i = 0; i < TM; ++i) {
+#pragma unroll
+            for (int j = 0; j < TN; ++j) acc[i][j] = multiply(T{}, b[j], a[i], acc[i][j]);
+            a[i] = *(const u32x4*)(next + (wm + i * 16) * BK);
+        }
+        __builtin_amdgcn_s_setprio(0);
+    };
+    // Everything asked for has landed, but for `behind` blocks that were asked for last, everything read is in registers: of all waves.
+    auto meet = [&](int behind) __attribute__((always_inline)) {
+        if (NB > 2 && behind >= 2) wait_vmcnt<2 * UNITS>();
+        else if (NB > 2 && behind == 1) wait_vmcnt<UNITS>();
+        else wait_vmcnt<0>();
+        asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
+        __builtin_amdgcn_s_barrier();
+        asm volatile("" ::: "memory");
+    };
+
+    if (tile >= end) return;
+    aim(tile);
+#pragma unroll
+    for (int b = 0; b < NB; ++b)
+        if (b < blocks) request(b);
+    for (;;) {
+        meet(min(blocks, NB) - 1);
+        read_b(b0, 0, 0);
+#pragma unroll
+        for (int i = 0; i < TM; ++i) a[i] = *(const u32x4*)(place(0, 0) + (wm + i * 16) * BK);
+#pragma unroll
+        for (int i = 0; i < TM; ++i)
+#pragma unroll
+            for (int j = 0; j < TN; ++j) acc[i][j] = floatx4{0, 0, 0, 0};
+        for (int b = 0; b < blocks; ++b) {
+            read_b(b1, b, 1);
+            step(b0, place(b, 1));
+            meet(min(blocks - 2 - b, NB - 2));           // (nobody reads this block's buffer any more, the next block has landed)
+            if (b + NB < blocks) request(b + NB);
+            read_b(b0, b + 1, 0);                        // (behind the last block: whatever the buffer holds, not multiplied)
+            step(b1, place(b + 1, 0));
+        }
+        const int mt = m0, nt = n0;
+        tile += gridDim.x / 8;
+        const bool more = NB == 2 && tile < end;         // (with more buffers the host launches a workgroup for every tile)
+        if (more) {
+            aim(tile);
+            request(0);                                  // (both buffers are free since the last meeting)
+            if (blocks > 1) request(1);
+        }
+#pragma unroll
+        for (int i = 0; i < TM; ++i) {
+            const int64_t row = mt + wm + i * 16 + lane % 16;
+            if (row >= m) continue;
+#pragma unroll
+            for (int j = 0; j < TN; j += GATED ? 4 : 2) {
+                const int64_t col = nt + (GATED ? wn / 2 : wn + j * 16) + lane / 16 * 8;
+                float v[8], up[8];
+#pragma unroll
+                for (int e = 0; e < 8; ++e) {
+                    v[e] = acc[i][j + e / 4][e % 4];
+                    if (GATED) up[e] = acc[i][(j + 2 + e / 4) % TN][e % 4];
+                }
+                if (p.parts > 1) {
+                    float* at = p.sums + ((int64_t)blockIdx.y * m + row) * (GATED ? 2 : 1) * n;
+                    store_eight(at, col, n, v);
+                    if (GATED) store_eight(at + n, col, n, up);
+                } else {
+                    finish<T, GATED>(p, row, col, v, up);
+                }
+            }
+        }
+        if (!more) break;
+    }
+}
+
+// adds up the parts of k, in their order
+template <typename T, bool GATED>
+__global__ __launch_bounds__(256) void k_tiles_join(TileArgs p)
+{
+    const int64_t eights = (p.n + 7) / 8, stride = p.m * p.n * (GATED ? 2 : 1);
+    for (int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x; i < p.m * eights; i += (int64_t)gridDim.x * 256) {
+        const int64_t row = i / eights, col = (i - row * eights) * 8;
+        const float* at = p.sums + row * (GATED ? 2 : 1) * p.n;
+        float v[8] = {}, up[8] = {};
+        for (int s = 0; s < p.parts; ++s, at += stride) {
+#pragma unroll
+            for (int e = 0; e < 8; ++e) {
+                const int64_t c = min(col + e, p.n - 1);
+                v[e] += at[c];
+                if (GATED) up[e] += at[p.n + c];
+            }
+        }
+        finish<T, GATED>(p, row, col, v, up);
+    }
+}
+
+// ---- which tiles (host): see gated.hip
+constexpr int kComputeUnits = 256;
+struct Tiling { int bm, bn, parts, part_k; };
+Tiling tiling_for(bool gated, int64_t m, int64_t n, int64_t k_bytes);
+template <typename T, bool GATED>
+hipError_t launch_tiles(const Tiling& t, TileArgs p, hipStream_t s);
+
+}  // namespace hr
