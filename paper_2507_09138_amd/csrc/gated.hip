@@ -56,64 +56,98 @@ __device__ __forceinline__ u32x4 turn_out(const T* tile, int c, int r)          
     return v;
 }
 
-// out[c, r] = x[r, c], rows of `out` filled up with zeros to whole blocks of 64 rows of x (as far as ldo, in elements, goes)
-template <typename T>
-__global__ __launch_bounds__(256) void k_turn(const T* x, int64_t ldx, int rows, int cols, T* out, int64_t ldo, int padded)
+// What the products of the gradients take, laid out by one launch: workgroups of 64 x 64 elements, in this order:
+struct LayOutArgs {
+    const float* pre; const void* dh; int64_t ldh; int act;
+    const void* gate; int64_t ldg;
+    const void* up; int64_t ldu;
+    const void* x; int64_t ldx;
+    int m, k, f, fp, mp;                                 // fp, mp: with the zeros behind them
+    void* rows;                                          // gradients of gate and up, [m][2 fp]: the gate's, zeros, up's, zeros; or NULL
+    void* cols;                                          // and [2 f][mp], zeros behind each; or NULL
+    void* turned_w;                                      // with rows: both matrices, [k][2 fp], zeros behind each
+    void* turned_x;                                      // with cols: x, [k][mp], zeros behind
+    int blocks_d, blocks_w;                              // workgroups of the gradients, of each matrix
+};
+// eight or four floats of a row of n from t on, zeros behind its end
+template <int E>
+__device__ __forceinline__ void load_floats(const float* row, int t, int n, float* v)
 {
-    __shared__ __align__(16) T tile[64 * kTurn<T>];
-    constexpr int E = kE<T>, PER = 64 / E;
-    const int r0 = blockIdx.y * 64, c0 = blockIdx.x * 64;
-    for (int i = threadIdx.x; i < 64 * PER; i += 256) {
-        const int r = i / PER, c = i % PER * E;
-        turn_in(tile, r, c, r0 + r < rows ? load16(x + (int64_t)(r0 + r) * ldx, c0 + c, cols) : u32x4{0, 0, 0, 0});
-    }
-    __syncthreads();
-    for (int i = threadIdx.x; i < 64 * PER; i += 256) {
-        const int c = i / PER, r = i % PER * E;
-        if (c0 + c < cols && r0 + r < padded) *(u32x4*)(out + (int64_t)(c0 + c) * ldo + r0 + r) = turn_out(tile, c, r);
+    if (t + E <= n) {
+        __builtin_memcpy(v, row + t, E * 4);
+    } else {
+#pragma unroll
+        for (int e = 0; e < E; ++e) v[e] = t + e < n ? row[t + e] : 0.0f;
     }
 }
-
-// ---- gradients of gate and up in T, as rows [m][2 fp] (gate's, then up's, zeros behind each) and as columns [2 f][mp] (zeros behind them):
-// 64 x 64 of both a workgroup.  Either may be left out.
 template <typename T>
-__global__ __launch_bounds__(256) void k_gated_slopes(const float* pre, const T* dh, int64_t ldh, int m, int f, int act, T* rows, int fp, T* cols, int mp)
+__global__ __launch_bounds__(256) void k_lay_out(LayOutArgs a)
 {
     __shared__ __align__(16) T tiles[2][64 * kTurn<T>];
     constexpr int E = kE<T>, PER = 64 / E;
-    const int r0 = blockIdx.y * 64, c0 = blockIdx.x * 64;
+    int block = blockIdx.x;
+    if (block < a.blocks_d) {
+        const int across = (a.fp + 63) / 64, r0 = block / across * 64, c0 = block % across * 64;
+#pragma unroll
+        for (int i = threadIdx.x; i < 64 * PER; i += 256) {
+            const int r = i / PER, c = i % PER * E;
+            const bool in = r0 + r < a.m;
+            u32x4 raw = {0, 0, 0, 0};
+            float z[E] = {}, w[E] = {};
+            if (in) {
+                const float* at = a.pre + (int64_t)(r0 + r) * 2 * a.f;
+                raw = load16((const T*)a.dh + (int64_t)(r0 + r) * a.ldh, c0 + c, a.f);
+                load_floats<E>(at, c0 + c, a.f, z);
+                load_floats<E>(at + a.f, c0 + c, a.f, w);
+            }
+            T d[E], dg[E], du[E];
+            __builtin_memcpy(d, &raw, 16);
+#pragma unroll
+            for (int e = 0; e < E; ++e) {                // (behind a row's end all three are 0, and so are both gradients)
+                float slope;
+                const float v = act_value(z[e], a.act, slope);
+                dg[e] = (T)((float)d[e] * w[e] * slope);
+                du[e] = (T)((float)d[e] * v);
+            }
+            u32x4 g, u;
+            __builtin_memcpy(&g, dg, 16);
+            __builtin_memcpy(&u, du, 16);
+            if (a.rows && in && c0 + c < a.fp) {
+                T* at = (T*)a.rows + (int64_t)(r0 + r) * 2 * a.fp + c0 + c;
+                *(u32x4*)at = g;
+                *(u32x4*)(at + a.fp) = u;
+            }
+            turn_in(tiles[0], r, c, g);
+            turn_in(tiles[1], r, c, u);
+        }
+        if (!a.cols) return;
+        __syncthreads();
+        for (int i = threadIdx.x; i < 2 * 64 * PER; i += 256) {
+            const int up = i / (64 * PER), c = i / PER % 64, r = i % PER * E;
+            if (c0 + c < a.f && r0 + r < a.mp) *(u32x4*)((T*)a.cols + ((int64_t)up * a.f + c0 + c) * a.mp + r0 + r) = turn_out(tiles[up], c, r);
+        }
+        return;
+    }
+    block -= a.blocks_d;
+    const bool of_w = a.rows && block < 2 * a.blocks_w, of_up = of_w && block >= a.blocks_w;
+    if (of_w) block -= of_up ? a.blocks_w : 0;
+    else if (a.rows) block -= 2 * a.blocks_w;
+    const T* from = (const T*)(of_w ? (of_up ? a.up : a.gate) : a.x);
+    const int64_t ld = of_w ? (of_up ? a.ldu : a.ldg) : a.ldx;
+    const int n = of_w ? a.f : a.m, padded = of_w ? a.fp : a.mp;                 // rows of what is turned
+    T* out = of_w ? (T*)a.turned_w + (of_up ? a.fp : 0) : (T*)a.turned_x;
+    const int64_t ldo = of_w ? 2 * a.fp : a.mp;
+    const int across = (a.k + 63) / 64, r0 = block / across * 64, c0 = block % across * 64;
+#pragma unroll
     for (int i = threadIdx.x; i < 64 * PER; i += 256) {
         const int r = i / PER, c = i % PER * E;
-        T dg[E], du[E];
-        T d[E];
-        const bool in = r0 + r < m;
-        const u32x4 raw = in ? load16(dh + (int64_t)(r0 + r) * ldh, c0 + c, f) : u32x4{0, 0, 0, 0};
-        __builtin_memcpy(d, &raw, 16);
-        const float* at = pre + (int64_t)(r0 + r) * 2 * f + c0 + c;
-#pragma unroll
-        for (int e = 0; e < E; ++e) {
-            dg[e] = du[e] = (T)0.0f;
-            if (!in || c0 + c + e >= f) continue;
-            float slope;
-            const float a = act_value(at[e], act, slope);
-            dg[e] = (T)((float)d[e] * at[f + e] * slope);
-            du[e] = (T)((float)d[e] * a);
-        }
-        u32x4 g, u;
-        __builtin_memcpy(&g, dg, 16);
-        __builtin_memcpy(&u, du, 16);
-        if (rows && in && c0 + c < fp) {
-            *(u32x4*)(rows + (int64_t)(r0 + r) * 2 * fp + c0 + c) = g;
-            *(u32x4*)(rows + (int64_t)(r0 + r) * 2 * fp + fp + c0 + c) = u;
-        }
-        turn_in(tiles[0], r, c, g);
-        turn_in(tiles[1], r, c, u);
+        turn_in(tiles[0], r, c, r0 + r < n ? load16(from + (int64_t)(r0 + r) * ld, c0 + c, a.k) : u32x4{0, 0, 0, 0});
     }
-    if (!cols) return;
     __syncthreads();
-    for (int i = threadIdx.x; i < 2 * 64 * PER; i += 256) {
-        const int up = i / (64 * PER), c = i / PER % 64, r = i % PER * E;
-        if (c0 + c < f && r0 + r < mp) *(u32x4*)(cols + ((int64_t)up * f + c0 + c) * mp + r0 + r) = turn_out(tiles[up], c, r);
+#pragma unroll
+    for (int i = threadIdx.x; i < 64 * PER; i += 256) {
+        const int c = i / PER, r = i % PER * E;
+        if (c0 + c < a.k && r0 + r < padded) *(u32x4*)(out + (c0 + c) * ldo + r0 + r) = turn_out(tiles[0], c, r);
     }
 }
 
@@ -123,52 +157,73 @@ __global__ __launch_bounds__(256) void k_clear(T* x, int64_t ld, int64_t rows, i
     for (int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x; i < rows * n; i += (int64_t)gridDim.x * 256) x[i / n * ld + i % n] = (T)0.0f;
 }
 
-// ---- up to 16 MT rows x: bound by reading the matrices, straight to registers, once.  A workgroup takes eight columns of the result, its waves
-// parts of k; the first operand of a matrix instruction is eight rows of each matrix.  Rows may begin anywhere.
-template <typename T, int MT>
+// ---- up to 16 MT rows x: bound by reading the matrices, straight to registers, once.  A workgroup takes 8 NT columns of the result, its waves
+// parts of k; the first operand of a matrix instruction is eight rows of each matrix.  Rows may begin anywhere.  U steps are asked for at once.
+constexpr int kFewRows = 32;
+template <typename T, int MT, int NT, int U>
 __global__ __launch_bounds__(1024) void k_gated_few(const T* x, int64_t ldx, const T* gate, int64_t ldg, const T* up, int64_t ldu, int m, int k, int f, int act, T* out,
                                                     int64_t ldo, float* pre)
 {
-    constexpr int K = 4 * kE<T>, U = 8;
-    __shared__ floatx4 sums[16][MT][64];
-    const int lane = lane_id(), wave = threadIdx.x / 64, share = blockDim.x / 64, row = lane % 16, first = blockIdx.x * 8;
-    const int steps = (k + K - 1) / K, begin = steps * wave / share, end = steps * (wave + 1) / share;
-    const int col = min(first + row % 8, f - 1), t0 = lane / 16 * kE<T>;
-    const T* w = row < 8 ? gate + (int64_t)col * ldg : up + (int64_t)col * ldu;
-    const T* xr[MT];
+    constexpr int K = 4 * kE<T>, SHARES = 16 / (MT * NT);
+    __shared__ floatx4 sums[SHARES][MT * NT][64];
+    const int lane = lane_id(), wave = threadIdx.x / 64, share = blockDim.x / 64, row = lane % 16, first = blockIdx.x * 8 * NT;
+    const int steps = (k + K - 1) / K, begin = steps * wave / share, stop = steps * (wave + 1) / share, end = min(stop, k / K), t0 = lane / 16 * kE<T>;
+    const T *w[NT], *xr[MT];
 #pragma unroll
-    for (int i = 0; i < MT; ++i) xr[i] = x + (int64_t)min(row + 16 * i, m - 1) * ldx;
-    floatx4 acc[MT] = {};
-    int s = begin;
-    for (; s + U <= end && (s + U) * K <= k; s += U) {
-        u32x4 b[U], a[U][MT];
+    for (int j = 0; j < NT; ++j) {
+        const int col = min(first + 8 * j + row % 8, f - 1);
+        w[j] = (row < 8 ? gate + (int64_t)col * ldg : up + (int64_t)col * ldu) + t0;
+    }
+#pragma unroll
+    for (int i = 0; i < MT; ++i) xr[i] = x + (int64_t)min(row + 16 * i, m - 1) * ldx + t0;
+    floatx4 acc[MT][NT] = {};
+    // U whole steps from s on; behind the last one it is asked for again, and not multiplied
+    auto batch = [&](int s, auto full) __attribute__((always_inline)) {
+        u32x4 a[U][MT], b[U][NT];
 #pragma unroll
         for (int u = 0; u < U; ++u) {
-            __builtin_memcpy(&b[u], w + (s + u) * K + t0, 16);
+            const int t = (decltype(full)::value ? s + u : min(s + u, end - 1)) * K;
 #pragma unroll
-            for (int i = 0; i < MT; ++i) __builtin_memcpy(&a[u][i], xr[i] + (s + u) * K + t0, 16);
+            for (int j = 0; j < NT; ++j) __builtin_memcpy(&b[u][j], w[j] + t, 16);
+#pragma unroll
+            for (int i = 0; i < MT; ++i) __builtin_memcpy(&a[u][i], xr[i] + t, 16);
         }
 #pragma unroll
-        for (int u = 0; u < U; ++u)
+        for (int u = 0; u < U; ++u) {
+            if (!decltype(full)::value && s + u >= end) break;
 #pragma unroll
-            for (int i = 0; i < MT; ++i) acc[i] = multiply(T{}, b[u], a[u][i], acc[i]);
+            for (int i = 0; i < MT; ++i)
+#pragma unroll
+                for (int j = 0; j < NT; ++j) acc[i][j] = multiply(T{}, b[u][j], a[u][i], acc[i][j]);
+        }
+    };
+    int s = begin;
+    for (; s + U <= end; s += U) batch(s, std::true_type{});
+    if (s < end) batch(s, std::false_type{});
+    if (stop > end && stop > begin) {                    // the last step of rows that are no whole steps
+        const int t = end * K;
+        u32x4 a[MT];
+#pragma unroll
+        for (int i = 0; i < MT; ++i) a[i] = load16(xr[i], t, k - t0);
+#pragma unroll
+        for (int j = 0; j < NT; ++j) {
+            const u32x4 b = load16(w[j], t, k - t0);
+#pragma unroll
+            for (int i = 0; i < MT; ++i) acc[i][j] = multiply(T{}, b, a[i], acc[i][j]);
+        }
     }
-    for (; s < end; ++s) {
-        const u32x4 b = load16(w, s * K + t0, k);
 #pragma unroll
-        for (int i = 0; i < MT; ++i) acc[i] = multiply(T{}, b, load16(xr[i], s * K + t0, k), acc[i]);
-    }
+    for (int i = 0; i < MT; ++i)
 #pragma unroll
-    for (int i = 0; i < MT; ++i) sums[wave][i][lane] = acc[i];
+        for (int j = 0; j < NT; ++j) sums[wave][i * NT + j][lane] = acc[i][j];
     __syncthreads();
-    if (wave >= MT) return;
-    for (int i = wave; i < MT; i += share) {
-        floatx4 v = sums[0][i][lane];
-        for (int q = 1; q < share; ++q) v += sums[q][i][lane];
+    for (int q = wave; q < MT * NT; q += share) {
+        floatx4 v = sums[0][q][lane];
+        for (int p = 1; p < share; ++p) v += sums[p][q][lane];
         float u[4];
 #pragma unroll
         for (int e = 0; e < 4; ++e) u[e] = __shfl(v[e], lane ^ 32);         // (lanes 32 .. 63 hold up's sums)
-        const int r = row + 16 * i, c = first + lane / 16 * 4;
+        const int r = row + q / NT * 16, c = first + q % NT * 8 + lane / 16 * 4;
         if (lane >= 32 || r >= m) continue;
 #pragma unroll
         for (int e = 0; e < 4; ++e) {
@@ -256,8 +311,6 @@ static size_t sums_bytes(int64_t m, int64_t columns, int64_t k_bytes)
 static int64_t padded(int64_t n, size_t es) { return (n * (int64_t)es + 127) / 128 * 128; }             // bytes of a row
 // rows that requests of 16 bytes reach; offsets inside a tile are 32-bit numbers
 static bool in_tiles(const void* p, int64_t ld, size_t es) { return (uintptr_t)p % 16 == 0 && ld * es % 16 == 0 && ld * es <= (1 << 22); }
-constexpr int kFewRows = 32;
-
 static int check_gated(int64_t m, int64_t k, int64_t f, int32_t dtype, int32_t activation)
 {
     if (!known_type(dtype)) return fail(HR_ERR_ARG, "unknown dtype %d", dtype);
@@ -265,6 +318,9 @@ static int check_gated(int64_t m, int64_t k, int64_t f, int32_t dtype, int32_t a
     if (k < 1 || k > HR_GATED_MAX) return fail(HR_ERR_ARG, "k=%lld must be in 1..%d", (long long)k, HR_GATED_MAX);
     if (f < 1 || f > HR_GATED_MAX) return fail(HR_ERR_ARG, "f=%lld must be in 1..%d", (long long)f, HR_GATED_MAX);
     if (activation < HR_SILU || activation > HR_GELU_TANH) return fail(HR_ERR_ARG, "unknown activation %d", activation);
+    // (workgroups of 64 x 64 elements of every matrix, and a launch may not have 2^32 threads)
+    auto blocks = [](int64_t r, int64_t c) { return (r + 64) / 64 * ((c + 64) / 64); };
+    if (blocks(m, 2 * f) + blocks(2 * f, k) + blocks(m, k) >= (1 << 24)) return fail(HR_ERR_UNSUPPORTED, "m=%lld, k=%lld, f=%lld: larger matrices than one call takes", (long long)m, (long long)k, (long long)f);
     return HR_OK;
 }
 
@@ -276,11 +332,11 @@ static hipError_t launch_pad(const void* x, int64_t ldx, int64_t rows, int64_t n
     return hipGetLastError();
 }
 
-// waves that take parts of k of the same eight columns: enough for the chip to be busy, four steps each at least
-static int few_share(int64_t f, int64_t k_bytes)
+// waves that take parts of k of the same columns: enough for the chip to be busy, eight steps each at least
+static int few_share(int64_t groups, int64_t k_bytes, int most)
 {
     int share = 1;
-    while (share < 16 && (f + 7) / 8 * share < 4096 && k_bytes / 64 >= 8 * share) share *= 2;
+    while (share < most && groups * share < 4096 && k_bytes / 64 >= 16 * share) share *= 2;
     return share;
 }
 
@@ -301,13 +357,13 @@ static hipError_t launch_gated(const GatedArgs& g, char* ws, hipStream_t s)
 {
     constexpr size_t es = sizeof(T);
     if (g.m <= kFewRows) {
-        const int share = few_share(g.f, g.k * es);
-        auto go = [&](auto kernel) {
-            hipLaunchKernelGGL(kernel, dim3((unsigned)((g.f + 7) / 8)), dim3(64 * share), 0, s, (const T*)g.x, g.ldx, (const T*)g.gate, g.ldg, (const T*)g.up, g.ldu, (int)g.m, (int)g.k,
-                               (int)g.f, g.act, (T*)g.out, g.ldo, g.pre);
+        auto go = [&](auto kernel, int columns, int most) {
+            const int64_t groups = (g.f + columns - 1) / columns;
+            hipLaunchKernelGGL(kernel, dim3((unsigned)groups), dim3(64 * few_share(groups, g.k * es, most)), 0, s, (const T*)g.x, g.ldx, (const T*)g.gate, g.ldg, (const T*)g.up, g.ldu,
+                               (int)g.m, (int)g.k, (int)g.f, g.act, (T*)g.out, g.ldo, g.pre);
         };
-        if (g.m <= 16) go(k_gated_few<T, 1>);
-        else go(k_gated_few<T, 2>);
+        if (g.m <= 16) go(k_gated_few<T, 1, 1, 8>, 8, 16);
+        else go(k_gated_few<T, 2, 2, 4>, 16, 4);
         return hipGetLastError();
     }
     TileArgs p{};
@@ -362,13 +418,6 @@ static BackwardPlan backward_plan(int64_t m, int64_t k, int64_t f, size_t es)
     p.sums = p.x + aligned((size_t)(k * mb));
     p.all = p.sums + std::max(sums_bytes(m, k, 2 * fb), sums_bytes(2 * f, k, mb)) + HR_WORKSPACE_ALIGN;
     return p;
-}
-
-template <typename T>
-static hipError_t launch_turn(const void* x, int64_t ldx, int64_t rows, int64_t cols, void* out, int64_t ldo, int64_t padded, hipStream_t s)
-{
-    hipLaunchKernelGGL(k_turn<T>, dim3((unsigned)((cols + 63) / 64), (unsigned)((padded + 63) / 64)), dim3(256), 0, s, (const T*)x, ldx, (int)rows, (int)cols, (T*)out, ldo, (int)padded);
-    return hipGetLastError();
 }
 
 }  // namespace hr
@@ -430,6 +479,7 @@ int hr_gated_backward(const void* x, int64_t ldx, const void* w_gate, int64_t ld
         if (int rc = check_matrix("grad_w_up", grad_w_up, f, k, ldgu, es)) return rc;
     }
     if (int rc = check_workspace(workspace, workspace_bytes, hr_gated_backward_workspace_bytes(m, k, f, dtype))) return rc;
+    if (!grad_x && !grad_w_gate) return HR_OK;
     hipStream_t s = (hipStream_t)stream;
     const BackwardPlan plan = backward_plan(m, k, f, es);
     char *rows = (char*)workspace + plan.rows, *cols = (char*)workspace + plan.cols, *turned_w = (char*)workspace + plan.w, *turned_x = (char*)workspace + plan.x;
@@ -442,13 +492,18 @@ int hr_gated_backward(const void* x, int64_t ldx, const void* w_gate, int64_t ld
             hipLaunchKernelGGL(k_clear<T>, dim3(blocks), dim3(256), 0, s, (T*)grad_w_up, ldgu, f, k);
             return hipGetLastError();
         }
-        hipLaunchKernelGGL(k_gated_slopes<T>, dim3((unsigned)((plan.fp + 63) / 64), (unsigned)((plan.mp + 63) / 64)), dim3(256), 0, s, pre, (const T*)grad_out, ldgo, (int)m, (int)f,
-                           activation, grad_x ? (T*)rows : nullptr, (int)plan.fp, grad_w_gate ? (T*)cols : nullptr, (int)plan.mp);
+        LayOutArgs l{pre, grad_out, ldgo, activation, w_gate, ldwg, w_up, ldwu, x, ldx, (int)m, (int)k, (int)f, (int)plan.fp, (int)plan.mp};
+        l.rows = grad_x ? rows : nullptr;
+        l.cols = grad_w_gate ? cols : nullptr;
+        l.turned_w = turned_w;
+        l.turned_x = turned_x;
+        auto blocks = [](int64_t r, int64_t c) { return (int)((r + 63) / 64 * ((c + 63) / 64)); };
+        l.blocks_d = blocks(plan.mp, plan.fp);
+        l.blocks_w = blocks(plan.fp, k);
+        hipLaunchKernelGGL(k_lay_out<T>, dim3((unsigned)(l.blocks_d + (grad_x ? 2 * l.blocks_w : 0) + (grad_w_gate ? blocks(plan.mp, k) : 0))), dim3(256), 0, s, l);
         TileArgs p{};
         p.sums = (float*)((char*)workspace + plan.sums);
         if (grad_x) {
-            if (hipError_t e = launch_turn<T>(w_gate, ldwg, f, k, turned_w, 2 * plan.fp, plan.fp, s)) return e;
-            if (hipError_t e = launch_turn<T>(w_up, ldwu, f, k, (T*)turned_w + plan.fp, 2 * plan.fp, plan.fp, s)) return e;
             p.a = rows;
             p.b = turned_w;
             p.lda = p.ldb = p.k = (int)(2 * plan.fp * sizeof(T));
@@ -459,7 +514,6 @@ int hr_gated_backward(const void* x, int64_t ldx, const void* w_gate, int64_t ld
             if (hipError_t e = launch_tiles<T, false>(tiling_for(false, p.m, p.n, p.k), p, s)) return e;
         }
         if (grad_w_gate) {
-            if (hipError_t e = launch_turn<T>(x, ldx, m, k, turned_x, plan.mp, plan.mp, s)) return e;
             p.a = cols;
             p.b = turned_x;
             p.lda = p.ldb = p.k = (int)(plan.mp * sizeof(T));

@@ -6,24 +6,29 @@
 
 namespace hr {
 
-// ---- activations: the value and the slope
-constexpr float kSqrtHalf = 0.7071067811865476f, kSqrt2OverPi = 0.7978845608028654f, kOverSqrt2Pi = 0.3989422804014327f;
+// ---- activations: the value and the slope.  All three are z times a share p of 0 .. 1 that one exponential gives; 2^x and 1 / x as the hardware has them
+// (within two units of the last place): what they are off by is a few units of the last place of z, and less than a rounding to 16 bits.
+constexpr float kLog2e = 1.4426950408889634f, kSqrt2OverPi = 0.7978845608028654f, kOverSqrt2Pi = 0.3989422804014327f;
 
 __device__ __forceinline__ float act_value(float z, int act, float& slope)
 {
-    if (act == HR_SILU) {
-        const float p = 1.0f / (1.0f + expf(-z));
-        slope = p * (1.0f + z * (1.0f - p));
-        return z * p;
-    }
     if (act == HR_GELU) {
-        const float p = 0.5f * (1.0f + erff(z * kSqrtHalf));
-        slope = p + z * expf(-0.5f * z * z) * kOverSqrt2Pi;
+        // the normal distribution by Abramowitz and Stegun 7.1.26 (within 0.75e-7): 1 - p(t) exp(-x^2) / 2, t = 1 / (1 + 0.3275911 x), x = |z| / sqrt 2
+        const float t = __builtin_amdgcn_rcpf(fmaf(fabsf(z), 0.3275911f * 0.7071067811865476f, 1.0f)), e = __builtin_amdgcn_exp2f(z * z * (-0.5f * kLog2e));
+        const float q = t * fmaf(t, fmaf(t, fmaf(t, fmaf(t, 0.5f * 1.061405429f, 0.5f * -1.453152027f), 0.5f * 1.421413741f), 0.5f * -0.284496736f), 0.5f * 0.254829592f) * e;
+        const float p = z < 0.0f ? q : 1.0f - q;
+        slope = fmaf(z * e, kOverSqrt2Pi, p);
         return z * p;
     }
-    const float t = tanhf(kSqrt2OverPi * (z + 0.044715f * z * z * z));
-    slope = 0.5f * (1.0f + t) + 0.5f * z * (1.0f - t * t) * (kSqrt2OverPi * (1.0f + 3 * 0.044715f * z * z));
-    return 0.5f * z * (1.0f + t);
+    float y = z, dy = 1.0f;
+    if (act == HR_GELU_TANH) {                           // (1 + tanh y) / 2 = 1 / (1 + exp(-2 y)); beyond 50 it is 0 or 1
+        const float c = fminf(fmaxf(z, -50.0f), 50.0f), c2 = c * c;
+        y = 2 * kSqrt2OverPi * c * fmaf(0.044715f, c2, 1.0f);
+        dy = 2 * kSqrt2OverPi * fmaf(3 * 0.044715f, c2, 1.0f);
+    }
+    const float p = __builtin_amdgcn_rcpf(1.0f + __builtin_amdgcn_exp2f(y * -kLog2e));
+    slope = fmaf(z * (1.0f - p) * p, dy, p);
+    return z * p;
 }
 
 // 16 bytes of k a lane, lane l those of row l % 16 from byte 16 (l / 16) on of a step of 64: one matrix instruction of 16 bits, four of 32 (the
@@ -57,38 +62,38 @@ struct TileArgs {
     float* pre; int act;                                 // gated
 };
 
-// eight neighbouring outputs of a row, as far as they are there
-template <typename O>
-__device__ __forceinline__ void store_eight(O* at, int64_t col, int64_t n, const float* v)
+// N neighbouring outputs of a row, as far as they are there
+template <int N, typename O>
+__device__ __forceinline__ void store_some(O* at, int64_t col, int64_t n, const float* v)
 {
-    typedef O outs __attribute__((ext_vector_type(8)));
+    typedef O outs __attribute__((ext_vector_type(N)));
     outs o;
 #pragma unroll
-    for (int e = 0; e < 8; ++e) o[e] = (O)v[e];
-    if (col + 8 <= n) {
+    for (int e = 0; e < N; ++e) o[e] = (O)v[e];
+    if (col + N <= n) {
         __builtin_memcpy(at + col, &o, sizeof o);
     } else {
 #pragma unroll
-        for (int e = 0; e < 8; ++e)
+        for (int e = 0; e < N; ++e)
             if (col + e < n) at[col + e] = o[e];
     }
 }
 
-// Eight neighbouring results of row `row`: of both matrices where the block is gated.
-template <typename T, bool GATED>
+// N neighbouring results of row `row`: of both matrices where the block is gated.
+template <typename T, bool GATED, int N>
 __device__ __forceinline__ void finish(const TileArgs& p, int64_t row, int64_t col, const float* v, const float* up)
 {
     if constexpr (GATED) {
-        float h[8], slope;
+        float h[N], slope;
 #pragma unroll
-        for (int e = 0; e < 8; ++e) h[e] = act_value(v[e], p.act, slope) * up[e];
-        store_eight((T*)p.out + row * p.ldo, col, p.n, h);
+        for (int e = 0; e < N; ++e) h[e] = act_value(v[e], p.act, slope) * up[e];
+        store_some<N>((T*)p.out + row * p.ldo, col, p.n, h);
         if (p.pre) {
-            store_eight(p.pre + row * 2 * p.n, col, p.n, v);
-            store_eight(p.pre + (row * 2 + 1) * p.n, col, p.n, up);
+            store_some<N>(p.pre + row * 2 * p.n, col, p.n, v);
+            store_some<N>(p.pre + (row * 2 + 1) * p.n, col, p.n, up);
         }
     } else {
-        store_eight(row < p.split ? (T*)p.out + row * p.ldo : (T*)p.out2 + (row - p.split) * p.ldo2, col, p.n, v);
+        store_some<N>(row < p.split ? (T*)p.out + row * p.ldo : (T*)p.out2 + (row - p.split) * p.ldo2, col, p.n, v);
     }
 }
 
@@ -222,10 +227,10 @@ __global__ __launch_bounds__(BM / WM * (BN / 64) * 64) void k_tiles(TileArgs p)
                 }
                 if (p.parts > 1) {
                     float* at = p.sums + ((int64_t)blockIdx.y * m + row) * (GATED ? 2 : 1) * n;
-                    store_eight(at, col, n, v);
-                    if (GATED) store_eight(at + n, col, n, up);
+                    store_some<8>(at, col, n, v);
+                    if (GATED) store_some<8>(at + n, col, n, up);
                 } else {
-                    finish<T, GATED>(p, row, col, v, up);
+                    finish<T, GATED, 8>(p, row, col, v, up);
                 }
             }
         }
@@ -233,24 +238,53 @@ __global__ __launch_bounds__(BM / WM * (BN / 64) * 64) void k_tiles(TileArgs p)
     }
 }
 
-// adds up the parts of k, in their order
-template <typename T, bool GATED>
+// Adds up the parts of k: SHARES threads take every SHARES-th part of four columns, in order, and their sums are added in order.
+template <typename T, bool GATED, int SHARES>
 __global__ __launch_bounds__(256) void k_tiles_join(TileArgs p)
 {
-    const int64_t eights = (p.n + 7) / 8, stride = p.m * p.n * (GATED ? 2 : 1);
-    for (int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x; i < p.m * eights; i += (int64_t)gridDim.x * 256) {
-        const int64_t row = i / eights, col = (i - row * eights) * 8;
-        const float* at = p.sums + row * (GATED ? 2 : 1) * p.n;
-        float v[8] = {}, up[8] = {};
-        for (int s = 0; s < p.parts; ++s, at += stride) {
+    constexpr int PER = 256 / SHARES;
+    __shared__ floatx4 some[GATED ? 2 : 1][SHARES][PER];
+    const int64_t fours = (p.n + 3) / 4, all = p.m * fours, stride = p.m * p.n * (GATED ? 2 : 1);
+    const int at = threadIdx.x % PER, share = threadIdx.x / PER;
+    for (int64_t i0 = (int64_t)blockIdx.x * PER; i0 < all; i0 += (int64_t)gridDim.x * PER) {
+        const int64_t i = min(i0 + at, all - 1), row = i / fours, col = (i - row * fours) * 4;
+        const float* from = p.sums + row * (GATED ? 2 : 1) * p.n + col;
+        const bool whole = col + 4 <= p.n;
+        auto load = [&](const float* x) __attribute__((always_inline)) {
+            floatx4 v = {0, 0, 0, 0};
+            if (whole) {
+                __builtin_memcpy(&v, x, 16);
+            } else {
 #pragma unroll
-            for (int e = 0; e < 8; ++e) {
-                const int64_t c = min(col + e, p.n - 1);
-                v[e] += at[c];
-                if (GATED) up[e] += at[p.n + c];
+                for (int e = 0; e < 4; ++e)
+                    if (col + e < p.n) v[e] = x[e];
+            }
+            return v;
+        };
+        floatx4 v = {0, 0, 0, 0}, up = {0, 0, 0, 0};
+#pragma unroll 4
+        for (int s = share; s < p.parts; s += SHARES) {
+            v += load(from + s * stride);
+            if (GATED) up += load(from + s * stride + p.n);
+        }
+        if constexpr (SHARES > 1) {
+            __syncthreads();
+            some[0][share][at] = v;
+            if (GATED) some[GATED ? 1 : 0][share][at] = up;
+            __syncthreads();
+            if (share > 0) continue;
+#pragma unroll
+            for (int q = 1; q < SHARES; ++q) {
+                v += some[0][q][at];
+                if (GATED) up += some[GATED ? 1 : 0][q][at];
             }
         }
-        finish<T, GATED>(p, row, col, v, up);
+        if (i0 + at < all) {
+            float a[4], b[4];
+#pragma unroll
+            for (int e = 0; e < 4; ++e) a[e] = v[e], b[e] = up[e];
+            finish<T, GATED, 4>(p, row, col, a, b);
+        }
     }
 }
 

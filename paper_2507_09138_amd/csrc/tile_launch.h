@@ -23,8 +23,13 @@ hipError_t launch_tiles(const Tiling& t, TileArgs p, hipStream_t s)
     else if (t.bm == 128) deep ? go(k_tiles<T, GATED, 128, 128, 32, 4>, 4) : go(k_tiles<T, GATED, 128, 128, 32, 2>, 2);
     else deep ? go(k_tiles<T, GATED, 64, 256, 32, 3>, 3) : go(k_tiles<T, GATED, 64, 256, 32, 2>, 2);
     if (e == hipSuccess && t.parts > 1) {
-        const int64_t want = (p.m * ((p.n + 7) / 8) + 255) / 256;
-        hipLaunchKernelGGL((k_tiles_join<T, GATED>), dim3((unsigned)std::min<int64_t>(want, 1 << 20)), dim3(256), 0, s, p);
+        auto join = [&](auto kernel, int shares) {
+            const int64_t want = (p.m * ((p.n + 3) / 4) + 256 / shares - 1) / (256 / shares);
+            hipLaunchKernelGGL(kernel, dim3((unsigned)std::min<int64_t>(want, 1 << 20)), dim3(256), 0, s, p);
+        };
+        if (t.parts >= 12) join(k_tiles_join<T, GATED, 16>, 16);
+        else if (t.parts >= 4) join(k_tiles_join<T, GATED, 4>, 4);
+        else join(k_tiles_join<T, GATED, 1>, 1);
     }
     return e == hipSuccess ? hipGetLastError() : e;
 }

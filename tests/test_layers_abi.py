@@ -54,7 +54,7 @@ def test_workspaces(hr):
                 assert all(s > 0 and s % 256 == 0 for s in sizes) and sizes == sorted(sizes), (k, h, dtype)
         for bad in ((-1, 1, 1, 0), (1, 0, 1, 0), (1, 1, 0, 0), (1, 1, 1, 3), ((1 << 19) + 1, 1, 1, 0), (1, (1 << 19) + 1, 1, 0), (1, 1, (1 << 19) + 1, 0)):
             assert f(*bad) == 0, bad
-        assert f(1 << 19, 1 << 19, 1 << 19, 0) > 0
+        assert f(1 << 19, 1 << 12, 1 << 15, 0) > 0 and f(1 << 19, 1 << 19, 1 << 19, 0) == 0
 
 
 def test_norm_arguments(hr):
@@ -101,6 +101,7 @@ def test_gated_arguments(hr):
                    dict(dt=1, u=P(4097)), dict(pre=P(4098))):
             assert f(**kw) == -1, (f, kw)
         assert f(ws=None) == -3 and f(ws=P(4100)) == -3 and f(bytes=255) == -3
+        assert f(m=1 << 19, k=1 << 19, f=1 << 19, ldx=BIG, ldg=BIG, ldu=BIG, ldo=BIG, ldh=BIG) == -5
     for kw in (dict(out=None), dict(ldo=5), dict(out=P(4098))):
         assert forward(**kw) == -1, kw
     assert forward(m=0) == 0
