@@ -157,8 +157,9 @@ __global__ __launch_bounds__(256) void k_clear(T* x, int64_t ld, int64_t rows, i
     for (int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x; i < rows * n; i += (int64_t)gridDim.x * 256) x[i / n * ld + i % n] = (T)0.0f;
 }
 
-// ---- up to 16 MT rows x: bound by reading the matrices, straight to registers, once.  A workgroup takes 8 NT columns of the result, its waves
-// parts of k; the first operand of a matrix instruction is eight rows of each matrix.  Rows may begin anywhere.  U steps are asked for at once.
+// ---- up to 16 MT rows x: bound by reading the matrices once.  A workgroup takes 8 NT columns of the result, its waves parts of k; the first operand of
+// a matrix instruction is eight rows of each matrix.  Here straight to registers, U steps at once, from rows that may begin anywhere: 64 bytes of a
+// line at a time, and where a row begins inside 16 bytes twice that (one row of 4096 bfloat16 against 10752 of each matrix 35 us, of 4097 80).
 constexpr int kFewRows = 32;
 template <typename T, int MT, int NT, int U>
 __global__ __launch_bounds__(1024) void k_gated_few(const T* x, int64_t ldx, const T* gate, int64_t ldg, const T* up, int64_t ldu, int m, int k, int f, int act, T* out,
@@ -238,6 +239,102 @@ __global__ __launch_bounds__(1024) void k_gated_few(const T* x, int64_t ldx, con
     }
 }
 
+// ---- the same for rows at multiples of 16 bytes: whole lines, straight to LDS.  Every wave has a ring of D blocks of 128 bytes of k of its own: of NT times
+// eight rows of each matrix, and of 8 XT rows x; no barrier but for the sums of the waves.  A load brings 8 rows, the 16-byte pieces of row r at
+// place piece ^ r % 8, so that the lanes of a read lie in different banks.  k 4096, f 10752, bfloat16, us (through registers): 1 row 31.5 (35.4), 4 rows 31.9 (41),
+// 16 rows 34.3 (56), 32 rows 41.6 (55); 5.6 TB/s for one row, start and end among them.
+template <typename T, int NT, int XT, int D>
+__global__ __launch_bounds__(512) void k_gated_ring(const T* x, int64_t ldx, const T* gate, int64_t ldg, const T* up, int64_t ldu, int m, int k, int f, int act, T* out,
+                                                    int64_t ldo, float* pre)
+{
+    constexpr int MT = (XT + 1) / 2, LOADS = 2 * NT + XT;
+    extern __shared__ __align__(1024) char lds[];
+    const int lane = lane_id(), wave = __builtin_amdgcn_readfirstlane(threadIdx.x / 64), share = blockDim.x / 64, row = lane % 16, first = blockIdx.x * 8 * NT;
+    const int bytes = k * (int)sizeof(T), blocks = (bytes + 127) / 128, begin = blocks * wave / share, end = blocks * (wave + 1) / share;
+    const int piece = ((lane & 7) ^ (lane >> 3)) * 16;
+    char* const ring = lds + wave * D * LOADS * 1024;
+    // (offsets of rows from the first one: within 2^31 bytes, the host sees to it)
+    uint32_t off[LOADS];
+    const char *g0 = (const char*)(gate + (int64_t)first * ldg), *u0 = (const char*)(up + (int64_t)first * ldu);
+#pragma unroll
+    for (int j = 0; j < NT; ++j) {
+        const uint32_t r = min(8 * j + lane / 8, f - 1 - first);
+        off[2 * j] = r * (uint32_t)(ldg * sizeof(T)) + piece;
+        off[2 * j + 1] = r * (uint32_t)(ldu * sizeof(T)) + piece;
+    }
+#pragma unroll
+    for (int i = 0; i < XT; ++i) off[2 * NT + i] = min(8 * i + lane / 8, m - 1) * (uint32_t)(ldx * sizeof(T)) + piece;
+    auto request = [&](int block, int slot) __attribute__((always_inline)) {
+        const int k0 = block * 128;
+        const uint32_t back = k0 + piece < bytes ? 0 : piece;            // (pieces behind the rows' end: the block's first instead, and zeros later)
+#pragma unroll
+        for (int i = 0; i < LOADS; ++i)
+            lds_dma16((i >= 2 * NT ? (const char*)x : (i & 1 ? u0 : g0)) + k0, off[i] - back, lds_addr(ring) + (slot * LOADS + i) * 1024);
+    };
+#pragma unroll
+    for (int u = 0; u < D; ++u)
+        if (begin + u < end) request(begin + u, u);
+    floatx4 acc[MT][NT] = {};
+    const int frag = row * 128, xfrag = 2 * NT * 1024 + row % (8 * min(XT, 2)) * 128, place = ((lane / 16) ^ (lane & 7)) * 16;
+    for (int s0 = begin; s0 < end; s0 += D) {
+#pragma unroll
+        for (int u = 0; u < D; ++u) {
+            const int s = s0 + u;
+            if (s >= end) break;
+            if (s + D <= end) wait_vmcnt<(D - 1) * LOADS>();
+            else wait_vmcnt<0>();
+            char* at = ring + u * LOADS * 1024;
+            if (s == blocks - 1 && bytes % 128 && s * 128 + piece >= bytes) {
+#pragma unroll
+                for (int i = 0; i < LOADS; ++i) *(u32x4*)(at + i * 1024 + lane * 16) = u32x4{0, 0, 0, 0};
+            }
+            wave_sync();
+            u32x4 a[2][MT], b[2][NT];
+#pragma unroll
+            for (int h = 0; h < 2; ++h) {
+#pragma unroll
+                for (int j = 0; j < NT; ++j) b[h][j] = *(const u32x4*)(at + j * 2048 + frag + (place ^ (h * 64)));
+#pragma unroll
+                for (int i = 0; i < MT; ++i) a[h][i] = *(const u32x4*)(at + xfrag + i * 2048 + (place ^ (h * 64)));
+            }
+            asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");           // the block is in registers: its place may be filled again
+            if (s + D < end) request(s + D, u);
+#pragma unroll
+            for (int h = 0; h < 2; ++h)
+#pragma unroll
+                for (int i = 0; i < MT; ++i)
+#pragma unroll
+                    for (int j = 0; j < NT; ++j) acc[i][j] = multiply(T{}, b[h][j], a[h][i], acc[i][j]);
+        }
+    }
+    __syncthreads();                                     // (every wave's requests have landed and its blocks have been read)
+    floatx4(*sums)[MT * NT][64] = (floatx4(*)[MT * NT][64])lds;
+#pragma unroll
+    for (int i = 0; i < MT; ++i)
+#pragma unroll
+        for (int j = 0; j < NT; ++j) sums[wave][i * NT + j][lane] = acc[i][j];
+    __syncthreads();
+    for (int q = wave; q < MT * NT; q += share) {
+        floatx4 v = sums[0][q][lane];
+        for (int p = 1; p < share; ++p) v += sums[p][q][lane];
+        float u[4];
+#pragma unroll
+        for (int e = 0; e < 4; ++e) u[e] = __shfl(v[e], lane ^ 32);         // (lanes 32 .. 63 hold up's sums)
+        const int r = row + q / NT * 16, c = first + q % NT * 8 + lane / 16 * 4;
+        if (lane >= 32 || r >= m) continue;
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+            if (c + e >= f) continue;
+            float slope;
+            out[r * ldo + c + e] = (T)(act_value(v[e], act, slope) * u[e]);
+            if (pre) {
+                pre[(int64_t)r * 2 * f + c + e] = v[e];
+                pre[((int64_t)r * 2 + 1) * f + c + e] = u[e];
+            }
+        }
+    }
+}
+
 // ---- rows of any alignment, or further apart than tiles reach, that are not copied: tiles of 64 rows and 32 columns of the result, staged through
 // registers, one block of 64 bytes of k at a time
 template <typename T>
@@ -281,31 +378,45 @@ __global__ __launch_bounds__(256) void k_gated_any(const T* x, int64_t ldx, cons
 
 // ---- which kernel
 
-// Tiles (rows x columns): 256 x 256 or 128 x 128, whichever takes less time, or 64 x 256 for few rows; in parts of k where the tiles are
-// few.  Large tiles come in rounds of one for every compute unit, a round taking as long as about 780 small ones.  k_bytes: of a row.
-Tiling tiling_for(bool gated, int64_t m, int64_t n, int64_t k_bytes)
+// Tiles (rows x columns of both matrices): 256 x 256, 128 x 128 or, for up to 64 rows, 64 x 256, in parts of k or not: what takes least by this count of
+// microseconds.  A block of 128 bytes of k takes a tile of 256 x 256 1.6 (16 bits; one at a time on a compute unit; an unfilled last round runs at a higher
+// clock), the smaller ones 0.48, and 0.5 where a tile has a compute unit for itself; in float32 1.9 and 2.0 (large tiles are no faster there).
+// Start and end take 6 to 8, parts are written and read at 5 MB/us, by another launch.  Measured, here (the other choices): 4096 x 4096 x 4096 bfloat16 102 .. 112 (128 x 128 118), 2048 x 4096 x 4096 61 (256 x 256
+// 86, two parts 84), 512 x 512 x 4096 in eight parts 15.4 (one 32.6), float32 2048 x 768 x 4096 in five 112 (one 260, two 144).
+Tiling tiling_for(bool gated, int64_t m, int64_t n, int64_t k_bytes, size_t es)
 {
-    auto tiles = [&](int bm, int bn) { return (m + bm - 1) / bm * ((n + bn / (gated ? 2 : 1) - 1) / (bn / (gated ? 2 : 1))); };
-    Tiling t{128, 128, 1, (int)k_bytes};
-    if (m <= 64) t.bm = 64, t.bn = 256;
-    else if (tiles(128, 128) >= (tiles(256, 256) + kComputeUnits - 1) / kComputeUnits * 780) t.bm = t.bn = 256;
-    const int64_t all = tiles(t.bm, t.bn);
-    if (all < kComputeUnits) {
-        const int64_t blocks = k_bytes / 128, parts = std::min(kComputeUnits / all, blocks / 4);        // (four blocks of k at least)
-        if (parts > 1) {
-            t.part_k = (int)((blocks + parts - 1) / parts * 128);
-            t.parts = (int)((k_bytes + t.part_k - 1) / t.part_k);
+    const int64_t blocks = k_bytes / 128, sums = m * n * (gated ? 2 : 1) * 8;
+    Tiling best{};
+    double least = 0;
+    auto consider = [&](int bm, int bn, double each, double alone, double ends) {
+        const int64_t cols = bn / (gated ? 2 : 1), tiles = (m + bm - 1) / bm * ((n + cols - 1) / cols);
+        for (int64_t parts = 1; parts <= 64; ++parts) {
+            const int64_t of = (blocks + parts - 1) / parts, all = tiles * parts;
+            if (parts > 1 && (of < 2 || parts * sums > (1LL << 29))) break;
+            if (parts > 1 && (blocks + of - 1) / of != parts) continue;                      // (fewer parts as long as these)
+            const double rounds = (double)((all + kComputeUnits - 1) / kComputeUnits), t = std::max((bm == 256 ? (rounds + (double)all / kComputeUnits) / 2 : rounds) * of * each, of * alone) + ends + (parts > 1 ? 3 + parts * sums / 5e6 : 0);
+            if (!best.parts || t < least) {
+                least = t;
+                best = {bm, bn, (int)parts, (int)(of * 128)};
+            }
         }
+    };
+    if (es == 4) {
+        if (m <= 64) consider(64, 256, 1.9, 2.0, 6);
+        else consider(128, 128, 1.9, 2.0, 6);
+    } else if (m <= 64) {
+        consider(64, 256, 0.48, 0.5, 6);
+    } else {
+        consider(128, 128, 0.48, 0.5, 6);
+        consider(256, 256, 1.6, 1.2, 8);
     }
-    return t;
+    return best;
 }
-// Room for the sums of parts of k of a product with m rows or fewer: tiles times parts are never more than the compute units, and a tile is
-// 128 x 128 or 64 x 256 sums.
-static size_t sums_bytes(int64_t m, int64_t columns, int64_t k_bytes)
+// room for the sums of parts of k
+static size_t sums_bytes(bool gated, int64_t m, int64_t n, int64_t k_bytes, size_t es)
 {
-    const int64_t most = std::max<int64_t>(1, k_bytes / 128 / 4);
-    if (most == 1) return 0;
-    return aligned((size_t)(std::min<int64_t>((int64_t)kComputeUnits * 128 * 128, most * ((m + 63) / 64 * 64) * columns) * 4));
+    const Tiling t = tiling_for(gated, m, n, k_bytes, es);
+    return t.parts > 1 ? aligned((size_t)(t.parts * m * n * (gated ? 2 : 1)) * 4) : 0;
 }
 
 static int64_t padded(int64_t n, size_t es) { return (n * (int64_t)es + 127) / 128 * 128; }             // bytes of a row
@@ -357,11 +468,21 @@ static hipError_t launch_gated(const GatedArgs& g, char* ws, hipStream_t s)
 {
     constexpr size_t es = sizeof(T);
     if (g.m <= kFewRows) {
+        auto ring = [&](auto kernel, int nt, int xt, int depth) {
+            const int64_t groups = (g.f + 8 * nt - 1) / (8 * nt);
+            const int share = few_share(groups, g.k * es, 4), lds = share * depth * (2 * nt + xt) * 1024;
+            if (lds > 64 * 1024)
+                if (hipError_t e = hipFuncSetAttribute((const void*)kernel, hipFuncAttributeMaxDynamicSharedMemorySize, 160 * 1024)) return e;
+            hipLaunchKernelGGL(kernel, dim3((unsigned)groups), dim3(64 * share), lds, s, (const T*)g.x, g.ldx, (const T*)g.gate, g.ldg, (const T*)g.up, g.ldu, (int)g.m, (int)g.k, (int)g.f,
+                               g.act, (T*)g.out, g.ldo, g.pre);
+            return hipGetLastError();
+        };
         auto go = [&](auto kernel, int columns, int most) {
             const int64_t groups = (g.f + columns - 1) / columns;
             hipLaunchKernelGGL(kernel, dim3((unsigned)groups), dim3(64 * few_share(groups, g.k * es, most)), 0, s, (const T*)g.x, g.ldx, (const T*)g.gate, g.ldg, (const T*)g.up, g.ldu,
                                (int)g.m, (int)g.k, (int)g.f, g.act, (T*)g.out, g.ldo, g.pre);
         };
+        if (g.k * es % 16 == 0 && in_tiles(g.x, g.ldx, es) && in_tiles(g.gate, g.ldg, es) && in_tiles(g.up, g.ldu, es)) return g.m <= 16 ? ring(k_gated_ring<T, 2, 2, 2>, 2, 2, 2) : ring(k_gated_ring<T, 2, 4, 3>, 2, 4, 3);
         if (g.m <= 16) go(k_gated_few<T, 1, 1, 8>, 8, 16);
         else go(k_gated_few<T, 2, 2, 4>, 16, 4);
         return hipGetLastError();
@@ -396,7 +517,7 @@ static hipError_t launch_gated(const GatedArgs& g, char* ws, hipStream_t s)
     p.pre = g.pre;
     p.act = g.act;
     p.sums = (float*)(ws + x_bytes(g.m, g.k, es) + w_bytes(g.k, g.f, es));
-    return launch_tiles<T, true>(tiling_for(true, g.m, g.f, p.k), p, s);
+    return launch_tiles<T, true>(tiling_for(true, g.m, g.f, p.k, es), p, s);
 }
 
 // workspace of the gradients: those of gate and up as rows, [m][2 fp], and as columns, [2 f][mp]; both matrices turned, [k][2 fp]; x turned, [k][mp];
@@ -416,7 +537,7 @@ static BackwardPlan backward_plan(int64_t m, int64_t k, int64_t f, size_t es)
     p.w = p.cols + aligned((size_t)(2 * f * mb));
     p.x = p.w + aligned((size_t)(k * 2 * fb));
     p.sums = p.x + aligned((size_t)(k * mb));
-    p.all = p.sums + std::max(sums_bytes(m, k, 2 * fb), sums_bytes(2 * f, k, mb)) + HR_WORKSPACE_ALIGN;
+    p.all = p.sums + (m ? std::max(sums_bytes(false, m, k, 2 * fb, es), sums_bytes(false, 2 * f, k, mb, es)) : 0) + HR_WORKSPACE_ALIGN;
     return p;
 }
 
@@ -432,7 +553,7 @@ size_t hr_gated_workspace_bytes(int64_t m, int64_t k, int64_t f, int32_t dtype)
     if (check_gated(m, k, f, dtype, HR_SILU)) return 0;
     const size_t es = element_bytes(dtype);
     if (m <= kFewRows) return HR_WORKSPACE_ALIGN;
-    return x_bytes(m, k, es) + w_bytes(k, f, es) + sums_bytes(m, 2 * f, padded(k, es)) + HR_WORKSPACE_ALIGN;
+    return x_bytes(m, k, es) + w_bytes(k, f, es) + sums_bytes(true, m, f, padded(k, es), es) + HR_WORKSPACE_ALIGN;
 }
 
 int hr_gated(const void* x, int64_t ldx, const void* w_gate, int64_t ldwg, const void* w_up, int64_t ldwu, int32_t dtype, int64_t m, int64_t k,
@@ -511,7 +632,7 @@ int hr_gated_backward(const void* x, int64_t ldx, const void* w_gate, int64_t ld
             p.n = k;
             p.out = grad_x;
             p.ldo = ldgx;
-            if (hipError_t e = launch_tiles<T, false>(tiling_for(false, p.m, p.n, p.k), p, s)) return e;
+            if (hipError_t e = launch_tiles<T, false>(tiling_for(false, p.m, p.n, p.k, sizeof(T)), p, s)) return e;
         }
         if (grad_w_gate) {
             p.a = cols;
@@ -524,7 +645,7 @@ int hr_gated_backward(const void* x, int64_t ldx, const void* w_gate, int64_t ld
             p.out2 = grad_w_up;
             p.ldo = ldgg;
             p.ldo2 = ldgu;
-            if (hipError_t e = launch_tiles<T, false>(tiling_for(false, p.m, p.n, p.k), p, s)) return e;
+            if (hipError_t e = launch_tiles<T, false>(tiling_for(false, p.m, p.n, p.k, sizeof(T)), p, s)) return e;
         }
         return hipGetLastError();
     }));

@@ -28,42 +28,85 @@ struct NormArgs {
 template <typename T> constexpr int kE = 16 / (int)sizeof(T);               // elements of a chunk
 template <typename T> using Chunk = T __attribute__((ext_vector_type(16 / sizeof(T))));
 
-// Chunk c of a row of n elements; zeros behind its end.  (Rows may begin at any element.)
+// Piece c of a row of n elements: E of them from `start` on, of which those from element `skip` of the piece on are its own (the others are the piece's
+// before: what does not end with a whole piece ends with one that begins earlier, and pieces behind the row's end have none of their own).
+// Rows may begin at any element.
 template <typename T>
-__device__ __forceinline__ Chunk<T> load_chunk(const T* row, int c, int n)
+struct Piece {
+    Chunk<T> v;
+    int start, skip;
+};
+template <typename T>
+__device__ __forceinline__ void place(Piece<T>& p, int c, int n)
 {
-    constexpr int E = kE<T>;
-    Chunk<T> v = {};
-    if (c * E + E <= n) {
-        __builtin_memcpy(&v, row + c * E, 16);
+    p.start = min(c * kE<T>, n - kE<T>);
+    p.skip = min(c * kE<T> - p.start, kE<T>);
+}
+// (TINY: rows shorter than a piece.  The loads of other rows stand in no branch: the compiler waits for a load where a branch ends.)
+template <int E, bool TINY, typename W>
+__device__ __forceinline__ void load_some(const W* at, int start, W* x)
+{
+    if constexpr (!TINY) {
+        __builtin_memcpy(x, at + start, E * sizeof(W));
     } else {
 #pragma unroll
-        for (int e = 0; e < E; ++e)
-            if (c * E + e < n) v[e] = row[c * E + e];
+        for (int e = 0; e < E; ++e) x[e] = start + e >= 0 ? at[start + e] : (W)0.0f;
     }
-    return v;
+}
+template <bool TINY = false, typename T>
+__device__ __forceinline__ Piece<T> load_piece(const T* row, int c, int n)
+{
+    Piece<T> p;
+    place(p, c, n);
+    T x[kE<T>];
+    load_some<kE<T>, TINY>(row, p.start, x);
+    __builtin_memcpy(&p.v, x, 16);
+    return p;
 }
 template <typename T>
-__device__ __forceinline__ void store_chunk(T* row, int c, int n, const float* x)
+__device__ __forceinline__ void store_piece(T* row, const Piece<T>& p, const float* x)
 {
-    constexpr int E = kE<T>;
     Chunk<T> v;
 #pragma unroll
-    for (int e = 0; e < E; ++e) v[e] = (T)x[e];
-    if (c * E + E <= n) {
-        __builtin_memcpy(row + c * E, &v, 16);
+    for (int e = 0; e < kE<T>; ++e) v[e] = (T)x[e];
+    if (p.skip == 0) {
+        __builtin_memcpy(row + p.start, &v, 16);
     } else {
 #pragma unroll
-        for (int e = 0; e < E; ++e)
-            if (c * E + e < n) row[c * E + e] = v[e];
+        for (int e = 0; e < kE<T>; ++e)
+            if (e >= p.skip) row[p.start + e] = v[e];
     }
 }
-// E numbers of a vector of n, as floats; `other` where there is no vector or behind its end
-template <int E, typename W>
-__device__ __forceinline__ void load_weights(const void* at, int first, int n, float other, float* w)
+// the numbers of a vector that lie at a piece, as floats; `other` where there is no vector
+template <int E, typename W, bool TINY = false>
+__device__ __forceinline__ void load_weights(const void* at, int start, float other, float* w)
 {
+    W x[E];
+    if (at) load_some<E, TINY>((const W*)at, start, x);
 #pragma unroll
-    for (int e = 0; e < E; ++e) w[e] = at && first + e < n ? (float)((const W*)at)[first + e] : other;
+    for (int e = 0; e < E; ++e) w[e] = at ? (float)x[e] : other;
+}
+// Forgets what a chunk's elements were as floats, and where its piece lies: between two passes over many pieces the chunks alone stay in registers.
+template <typename T>
+__device__ __forceinline__ void forget(Chunk<T>& x)
+{
+    u32x4 v = __builtin_bit_cast(u32x4, x);
+    asm volatile("" : "+v"(v));
+    x = __builtin_bit_cast(Chunk<T>, v);
+}
+__device__ __forceinline__ int anew(int t)
+{
+    asm volatile("" : "+v"(t));
+    return t;
+}
+// piece c, with the elements it has
+template <typename T>
+__device__ __forceinline__ Piece<T> piece_of(const Chunk<T>& v, int c, int n)
+{
+    Piece<T> p;
+    place(p, c, n);
+    p.v = v;
+    return p;
 }
 
 template <typename C>
@@ -110,7 +153,7 @@ __device__ __forceinline__ void fold_two(float& a, float& b, Folds& s, int& turn
 
 // ---- rows that LANES lanes hold, CH chunks of 16 bytes each, between their one read and their one write.  The mean is found first and the
 // spread from what is left: the second fold also finds what the first mean is off by, so that a row far from 0 loses nothing.
-template <typename T, typename W, int LANES, int CH>
+template <typename T, typename W, int LANES, int CH, bool TINY = false>
 __global__ __launch_bounds__(LANES > 256 ? LANES : 256) void k_norm(NormArgs a)
 {
     constexpr int E = kE<T>, THREADS = LANES > 256 ? LANES : 256, ROWS = THREADS / LANES;
@@ -120,35 +163,42 @@ __global__ __launch_bounds__(LANES > 256 ? LANES : 256) void k_norm(NormArgs a)
     const int t = threadIdx.x % LANES, n = a.n;
     const float over = 1.0f / (float)n;
     float w[KEEP ? CH : 1][E], b[KEEP ? CH : 1][E];
-    auto weights = [&](int i, float* wi, float* bi) __attribute__((always_inline)) {
-        load_weights<E, W>(a.weight, (i * LANES + t) * E, n, 1.0f, wi);
-        load_weights<E, W>(a.bias, (i * LANES + t) * E, n, 0.0f, bi);
+    auto weights = [&](const Piece<T>& p, float* wi, float* bi) __attribute__((always_inline)) {
+        load_weights<E, W, TINY>(a.weight, p.start, 1.0f, wi);
+        load_weights<E, W, TINY>(a.bias, p.start, 0.0f, bi);
     };
     if constexpr (KEEP)
-        for (int i = 0; i < CH; ++i) weights(i, w[i], b[i]);
+        for (int i = 0; i < CH; ++i) weights(piece_of<T>(Chunk<T>{}, i * LANES + t, n), w[i], b[i]);
     for (int64_t r0 = (int64_t)blockIdx.x * ROWS; r0 < a.rows; r0 += (int64_t)gridDim.x * ROWS) {
         const int64_t r = r0 + threadIdx.x / LANES;
         const bool in = r < a.rows;
         const T* row = (const T*)a.x + (in ? r : a.rows - 1) * a.ldx;
         Chunk<T> x[CH];
+        int at = t;
 #pragma unroll
-        for (int i = 0; i < CH; ++i) x[i] = load_chunk(row, i * LANES + t, n);
+        for (int i = 0; i < CH; ++i) x[i] = load_piece<TINY>(row, i * LANES + at, n).v;
         float s0 = 0.0f, s1 = 0.0f;
 #pragma unroll
-        for (int i = 0; i < CH; ++i)
+        for (int i = 0; i < CH; ++i) {
+            const Piece<T> p = piece_of<T>(x[i], i * LANES + at, n);
 #pragma unroll
-            for (int e = 0; e < E; ++e) s0 += (float)x[i][e];
+            for (int e = 0; e < E; ++e) s0 += e >= p.skip ? (float)p.v[e] : 0.0f;
+        }
         fold_two<LANES>(s0, s1, folds, turn);
         const float first = s0 * over;
         s0 = s1 = 0.0f;
+        if constexpr (!KEEP) at = anew(t);
 #pragma unroll
-        for (int i = 0; i < CH; ++i)
+        for (int i = 0; i < CH; ++i) {
+            if constexpr (!KEEP) forget<T>(x[i]);
+            const Piece<T> p = piece_of<T>(x[i], i * LANES + at, n);
 #pragma unroll
             for (int e = 0; e < E; ++e) {
-                const float d = (i * LANES + t) * E + e < n ? (float)x[i][e] - first : 0.0f;
+                const float d = e >= p.skip ? (float)p.v[e] - first : 0.0f;
                 s0 += d;
                 s1 = fmaf(d, d, s1);
             }
+        }
         fold_two<LANES>(s0, s1, folds, turn);
         const float off = s0 * over, rstd = 1.0f / sqrtf(s1 * over - off * off + a.eps);
         if (!in) continue;
@@ -157,17 +207,22 @@ __global__ __launch_bounds__(LANES > 256 ? LANES : 256) void k_norm(NormArgs a)
             a.stats[2 * r + 1] = rstd;
         }
         T* out = (T*)a.out + r * a.ldo;
+        if constexpr (!KEEP) at = anew(t);
 #pragma unroll
         for (int i = 0; i < CH; ++i) {
-            if ((i * LANES + t) * E >= n) continue;
             float wi[E], bi[E], y[E];
-            if constexpr (!KEEP) weights(i, wi, bi);
+            if constexpr (!KEEP) {
+                forget<T>(x[i]);
+                asm volatile("" ::: "memory");           // (the weights of one piece at a time)
+            }
+            const Piece<T> p = piece_of<T>(x[i], i * LANES + at, n);
+            if constexpr (!KEEP) weights(p, wi, bi);
 #pragma unroll
             for (int e = 0; e < E; ++e) {
                 if constexpr (KEEP) wi[e] = w[i][e], bi[e] = b[i][e];
-                y[e] = fmaf(((float)x[i][e] - first - off) * rstd, wi[e], bi[e]);
+                y[e] = fmaf(((float)p.v[e] - first - off) * rstd, wi[e], bi[e]);
             }
-            store_chunk(out, i * LANES + t, n, y);
+            if (p.skip < E) store_piece(out, p, y);
         }
     }
 }
@@ -185,18 +240,18 @@ __global__ __launch_bounds__(1024) void k_norm_long(NormArgs a)
         const T* row = (const T*)a.x + r * a.ldx;
         float s0 = 0.0f, s1 = 0.0f;
         for (int c = threadIdx.x; c < chunks; c += 1024) {
-            const Chunk<T> x = load_chunk(row, c, n);
+            const Piece<T> x = load_piece(row, c, n);
 #pragma unroll
-            for (int e = 0; e < E; ++e) s0 += (float)x[e];
+            for (int e = 0; e < E; ++e) s0 += e >= x.skip ? (float)x.v[e] : 0.0f;
         }
         fold_two<1024>(s0, s1, folds, turn);
         const float first = s0 * over;
         s0 = s1 = 0.0f;
         for (int c = threadIdx.x; c < chunks; c += 1024) {
-            const Chunk<T> x = load_chunk(row, c, n);
+            const Piece<T> x = load_piece(row, c, n);
 #pragma unroll
             for (int e = 0; e < E; ++e) {
-                const float d = c * E + e < n ? (float)x[e] - first : 0.0f;
+                const float d = e >= x.skip ? (float)x.v[e] - first : 0.0f;
                 s0 += d;
                 s1 = fmaf(d, d, s1);
             }
@@ -209,19 +264,19 @@ __global__ __launch_bounds__(1024) void k_norm_long(NormArgs a)
         }
         T* out = (T*)a.out + r * a.ldo;
         for (int c = threadIdx.x; c < chunks; c += 1024) {
-            const Chunk<T> x = load_chunk(row, c, n);
+            const Piece<T> x = load_piece(row, c, n);
             float w[E], b[E], y[E];
-            load_weights<E, W>(a.weight, c * E, n, 1.0f, w);
-            load_weights<E, W>(a.bias, c * E, n, 0.0f, b);
+            load_weights<E, W>(a.weight, x.start, 1.0f, w);
+            load_weights<E, W>(a.bias, x.start, 0.0f, b);
 #pragma unroll
-            for (int e = 0; e < E; ++e) y[e] = fmaf(((float)x[e] - first - off) * rstd, w[e], b[e]);
-            store_chunk(out, c, n, y);
+            for (int e = 0; e < E; ++e) y[e] = fmaf(((float)x.v[e] - first - off) * rstd, w[e], b[e]);
+            store_piece(out, x, y);
         }
     }
 }
 
 // ---- gradients of rows that LANES lanes hold; sums over the workgroup's rows stay in registers until its last
-template <typename T, typename W, int LANES, int CH>
+template <typename T, typename W, int LANES, int CH, bool TINY = false>
 __global__ __launch_bounds__(LANES > 256 ? LANES : 256) void k_norm_backward(NormArgs a)
 {
     constexpr int E = kE<T>, THREADS = LANES > 256 ? LANES : 256, ROWS = THREADS / LANES;
@@ -231,24 +286,30 @@ __global__ __launch_bounds__(LANES > 256 ? LANES : 256) void k_norm_backward(Nor
     const int t = threadIdx.x % LANES, n = a.n;
     const float over = 1.0f / (float)n;
     float w[CH][E], dw[CH][E] = {}, db[CH][E] = {};
-    for (int i = 0; i < CH; ++i) load_weights<E, W>(a.weight, (i * LANES + t) * E, n, 1.0f, w[i]);
+    for (int i = 0; i < CH; ++i) {
+        Piece<T> p;
+        place(p, i * LANES + t, n);
+        load_weights<E, W, TINY>(a.weight, p.start, 1.0f, w[i]);
+    }
     for (int64_t r0 = (int64_t)blockIdx.x * ROWS; r0 < a.rows; r0 += (int64_t)gridDim.x * ROWS) {
         const int64_t r = r0 + threadIdx.x / LANES, at = min(r, a.rows - 1);
         const bool in = r < a.rows;
         Chunk<T> x[CH], dy[CH];
+        int lane = t;
 #pragma unroll
         for (int i = 0; i < CH; ++i) {
-            x[i] = load_chunk((const T*)a.x + at * a.ldx, i * LANES + t, n);
-            dy[i] = load_chunk((const T*)a.dy + at * a.ldg, i * LANES + t, n);
+            x[i] = load_piece<TINY>((const T*)a.x + at * a.ldx, i * LANES + lane, n).v;
+            dy[i] = load_piece<TINY>((const T*)a.dy + at * a.ldg, i * LANES + lane, n).v;
         }
         const float mean = a.stats[2 * at], rstd = a.stats[2 * at + 1];
         float s0 = 0.0f, s1 = 0.0f;
 #pragma unroll
-        for (int i = 0; i < CH; ++i)
+        for (int i = 0; i < CH; ++i) {
+            const Piece<T> p = piece_of<T>(x[i], i * LANES + lane, n);
 #pragma unroll
             for (int e = 0; e < E; ++e) {
-                // (behind the row's end dy is 0, and u has to be a number)
-                const float u = (i * LANES + t) * E + e < n ? ((float)x[i][e] - mean) * rstd : 0.0f, d = (float)dy[i][e], g = d * w[i][e];
+                const bool own = e >= p.skip;
+                const float u = own ? ((float)p.v[e] - mean) * rstd : 0.0f, d = own ? (float)dy[i][e] : 0.0f, g = own ? d * w[i][e] : 0.0f;
                 s0 += g;
                 s1 = fmaf(g, u, s1);
                 if (in) {
@@ -256,31 +317,40 @@ __global__ __launch_bounds__(LANES > 256 ? LANES : 256) void k_norm_backward(Nor
                     db[i][e] += d;
                 }
             }
+        }
         fold_two<LANES>(s0, s1, folds, turn);
         const float c1 = s0 * over, c2 = s1 * over;
         if (!in || !a.dx) continue;
         T* out = (T*)a.dx + r * a.ldgx;
+        lane = anew(t);
 #pragma unroll
         for (int i = 0; i < CH; ++i) {
-            if ((i * LANES + t) * E >= n) continue;
+            forget<T>(x[i]);
+            forget<T>(dy[i]);
+            const Piece<T> p = piece_of<T>(x[i], i * LANES + lane, n);
+            if (p.skip >= E) continue;
             float y[E];
 #pragma unroll
             for (int e = 0; e < E; ++e) {
-                const float u = ((float)x[i][e] - mean) * rstd, g = (float)dy[i][e] * w[i][e];
+                const float u = ((float)p.v[e] - mean) * rstd, g = (float)dy[i][e] * w[i][e];
                 y[e] = rstd * (g - c1 - u * c2);
             }
-            store_chunk(out, i * LANES + t, n, y);
+            store_piece(out, p, y);
         }
     }
     if (!a.parts) return;
     float* to = a.parts + (int64_t)blockIdx.x * 2 * n;
     auto write = [&](float(*x)[E], float* at) __attribute__((always_inline)) {
+        Piece<T> p;
         if constexpr (ROWS > 1) {                        // the rows of the workgroup, in their order
             __syncthreads();
 #pragma unroll
-            for (int i = 0; i < CH; ++i)
+            for (int i = 0; i < CH; ++i) {
+                place(p, i * LANES + t, n);
 #pragma unroll
-                for (int e = 0; e < E; ++e) sums[(threadIdx.x / LANES) * LANES * CH * E + (i * LANES + t) * E + e] = x[i][e];
+                for (int e = 0; e < E; ++e)
+                    if (e >= p.skip) sums[(threadIdx.x / LANES) * LANES * CH * E + p.start + e] = x[i][e];
+            }
             __syncthreads();
             for (int j = threadIdx.x; j < n; j += THREADS) {
                 float s = 0.0f;
@@ -290,10 +360,16 @@ __global__ __launch_bounds__(LANES > 256 ? LANES : 256) void k_norm_backward(Nor
             }
         } else {
 #pragma unroll
-            for (int i = 0; i < CH; ++i)
+            for (int i = 0; i < CH; ++i) {
+                place(p, i * LANES + t, n);
+                if (p.skip == 0) {
+                    __builtin_memcpy(at + p.start, x[i], E * 4);
+                } else {
 #pragma unroll
-                for (int e = 0; e < E; ++e)
-                    if ((i * LANES + t) * E + e < n) at[(i * LANES + t) * E + e] = x[i][e];
+                    for (int e = 0; e < E; ++e)
+                        if (e >= p.skip) at[p.start + e] = x[i][e];
+                }
+            }
         }
     };
     write(dw, to);
@@ -304,24 +380,34 @@ __global__ __launch_bounds__(LANES > 256 ? LANES : 256) void k_norm_backward(Nor
 template <typename T, typename W>
 __global__ __launch_bounds__(1024) void k_norm_sums(NormArgs a)
 {
-    constexpr int E = kE<T>;
+    constexpr int E = kE<T>, U = 4;
     __shared__ Folds folds;
     int turn = 0;
     const int n = a.n, chunks = (n + E - 1) / E;
     const float over = 1.0f / (float)n;
     for (int64_t r = blockIdx.x; r < a.rows; r += gridDim.x) {
+        const T *xr = (const T*)a.x + r * a.ldx, *dr = (const T*)a.dy + r * a.ldg;
         const float mean = a.stats[2 * r], rstd = a.stats[2 * r + 1];
         float s0 = 0.0f, s1 = 0.0f;
-        for (int c = threadIdx.x; c < chunks; c += 1024) {
-            const Chunk<T> x = load_chunk((const T*)a.x + r * a.ldx, c, n), dy = load_chunk((const T*)a.dy + r * a.ldg, c, n);
-            float w[E];
-            load_weights<E, W>(a.weight, c * E, n, 1.0f, w);
+        for (int c0 = threadIdx.x; c0 < chunks; c0 += 1024 * U) {
+            Piece<T> x[U], dy[U];
+            float w[U][E];
 #pragma unroll
-            for (int e = 0; e < E; ++e) {
-                const float u = c * E + e < n ? ((float)x[e] - mean) * rstd : 0.0f, g = (float)dy[e] * w[e];
-                s0 += g;
-                s1 = fmaf(g, u, s1);
+            for (int u = 0; u < U; ++u) {
+                const int c = min(c0 + u * 1024, chunks);                        // (behind the row's end: a piece without elements)
+                x[u] = load_piece(xr, c, n);
+                dy[u] = load_piece(dr, c, n);
+                load_weights<E, W>(a.weight, x[u].start, 1.0f, w[u]);
             }
+#pragma unroll
+            for (int u = 0; u < U; ++u)
+#pragma unroll
+                for (int e = 0; e < E; ++e) {
+                    const bool own = e >= x[u].skip;
+                    const float v = own ? ((float)x[u].v[e] - mean) * rstd : 0.0f, g = own ? (float)dy[u].v[e] * w[u][e] : 0.0f;
+                    s0 += g;
+                    s1 = fmaf(g, v, s1);
+                }
         }
         fold_two<1024>(s0, s1, folds, turn);
         if (threadIdx.x == 0) {
@@ -337,47 +423,81 @@ __global__ __launch_bounds__(256) void k_norm_stripe(NormArgs a)
     const int n = a.n, c = blockIdx.x * 256 + threadIdx.x;
     if (c * (int64_t)E >= n) return;
     float w[E], dw[E] = {}, db[E] = {};
-    load_weights<E, W>(a.weight, c * E, n, 1.0f, w);
-    for (int64_t r = blockIdx.y; r < a.rows; r += gridDim.y) {
-        const Chunk<T> x = load_chunk((const T*)a.x + r * a.ldx, c, n), dy = load_chunk((const T*)a.dy + r * a.ldg, c, n);
-        const float mean = a.stats[2 * r], rstd = a.stats[2 * r + 1], c1 = a.sums[2 * r], c2 = a.sums[2 * r + 1];
-        float y[E];
+    Piece<T> p;
+    place(p, c, n);
+    load_weights<E, W>(a.weight, p.start, 1.0f, w);
+    constexpr int U = 4;                                 // rows at once; those behind the last one are it again, and take no part
+    for (int64_t r0 = blockIdx.y; r0 < a.rows; r0 += U * (int64_t)gridDim.y) {
+        Piece<T> x[U], dy[U];
 #pragma unroll
-        for (int e = 0; e < E; ++e) {
-            const float u = ((float)x[e] - mean) * rstd, d = (float)dy[e];
-            dw[e] = fmaf(d, u, dw[e]);
-            db[e] += d;
-            y[e] = rstd * (d * w[e] - c1 - u * c2);
+        for (int i = 0; i < U; ++i) {
+            const int64_t r = min(r0 + i * (int64_t)gridDim.y, a.rows - 1);
+            x[i] = load_piece((const T*)a.x + r * a.ldx, c, n);
+            dy[i] = load_piece((const T*)a.dy + r * a.ldg, c, n);
         }
-        if (a.dx) store_chunk((T*)a.dx + r * a.ldgx, c, n, y);
+#pragma unroll
+        for (int i = 0; i < U; ++i) {
+            const int64_t r = r0 + i * (int64_t)gridDim.y;
+            if (r >= a.rows) break;
+            const float mean = a.stats[2 * r], rstd = a.stats[2 * r + 1], c1 = a.sums[2 * r], c2 = a.sums[2 * r + 1];
+            float y[E];
+#pragma unroll
+            for (int e = 0; e < E; ++e) {
+                const float u = ((float)x[i].v[e] - mean) * rstd, d = (float)dy[i].v[e];
+                dw[e] = fmaf(d, u, dw[e]);
+                db[e] += d;
+                y[e] = rstd * (d * w[e] - c1 - u * c2);
+            }
+            if (a.dx) store_piece((T*)a.dx + r * a.ldgx, x[i], y);
+        }
     }
     if (!a.parts) return;
     float* to = a.parts + (int64_t)blockIdx.y * 2 * n;
+#pragma unroll
     for (int e = 0; e < E; ++e)
-        if (c * E + e < n) to[c * E + e] = dw[e], to[n + c * E + e] = db[e];
+        if (e >= p.skip) to[p.start + e] = dw[e], to[n + p.start + e] = db[e];
 }
 
-// ---- the sums of the groups of rows, in their order: 16 threads for 64 columns, 16 shares of the groups
+// ---- the sums of the groups of rows, in an order that depends on nothing but their number: eight threads for 32 columns, 128 shares of the groups
+// (32 shares: 8.6 us instead of 4 for 359 groups of 67 columns, a chain of round trips)
 template <typename W>
-__global__ __launch_bounds__(256) void k_norm_join(const float* parts, int groups, int n, void* grad_weight, void* grad_bias)
+__global__ __launch_bounds__(1024) void k_norm_join(const float* parts, int groups, int n, void* grad_weight, void* grad_bias)
 {
-    __shared__ float sums[16][64];
-    const int64_t all = 2 * (int64_t)n, col = (int64_t)blockIdx.x * 64;
-    const int lane = threadIdx.x % 16 * 4, share = threadIdx.x / 16;
-    float s[4] = {0, 0, 0, 0};
-    for (int g = share; g < groups; g += 16)
+    __shared__ floatx4 sums[128][8];
+    __shared__ float some[8][32];
+    const int64_t all = 2 * (int64_t)n, col = (int64_t)blockIdx.x * 32 + threadIdx.x % 8 * 4;
+    const int share = threadIdx.x / 8;
+    floatx4 s = {0, 0, 0, 0};
+    if (col + 4 <= all) {
+#pragma unroll 4
+        for (int g = share; g < groups; g += 128) {
+            floatx4 v;
+            __builtin_memcpy(&v, parts + g * all + col, 16);
+            s += v;
+        }
+    } else {
+        for (int g = share; g < groups; g += 128)
 #pragma unroll
-        for (int e = 0; e < 4; ++e)
-            if (col + lane + e < all) s[e] += parts[g * all + col + lane + e];
-#pragma unroll
-    for (int e = 0; e < 4; ++e) sums[share][lane + e] = s[e];
+            for (int e = 0; e < 4; ++e)
+                if (col + e < all) s[e] += parts[g * all + col + e];
+    }
+    sums[share][threadIdx.x % 8] = s;
     __syncthreads();
-    if (threadIdx.x < 64 && col + threadIdx.x < all) {
+    const int c = threadIdx.x % 32;
+    if (threadIdx.x < 256) {
         float v = 0.0f;
-        for (int q = 0; q < 16; ++q) v += sums[q][threadIdx.x];
-        const int64_t j = col + threadIdx.x;
+#pragma unroll
+        for (int q = 0; q < 16; ++q) v += sums[threadIdx.x / 32 * 16 + q][c / 4][c % 4];
+        some[threadIdx.x / 32][c] = v;
+    }
+    __syncthreads();
+    if (threadIdx.x < 32) {
+        const int64_t j = (int64_t)blockIdx.x * 32 + c;
+        float v = 0.0f;
+#pragma unroll
+        for (int q = 0; q < 8; ++q) v += some[q][c];
         void* to = j < n ? grad_weight : grad_bias;
-        if (to) ((W*)to)[j < n ? j : j - n] = (W)v;
+        if (j < all && to) ((W*)to)[j < n ? j : j - n] = (W)v;
     }
 }
 
@@ -408,7 +528,8 @@ static void launch_norm(const NormArgs& a, hipStream_t s)
         const int64_t want = (a.rows + rows - 1) / rows, most = 256 * (2048 / threads);
         hipLaunchKernelGGL(kernel, dim3((unsigned)std::min(want, most)), dim3(threads), 0, s, a);
     };
-    if (chunks <= 16) go(k_norm<T, W, 16, 1>, 256, 16);
+    if (a.n < kE<T>) go(k_norm<T, W, 16, 1, true>, 256, 16);
+    else if (chunks <= 16) go(k_norm<T, W, 16, 1>, 256, 16);
     else if (chunks <= 32) go(k_norm<T, W, 16, 2>, 256, 16);
     else if (chunks <= 64) go(k_norm<T, W, 64, 1>, 256, 4);
     else if (chunks <= 128) go(k_norm<T, W, 64, 2>, 256, 4);
@@ -416,6 +537,8 @@ static void launch_norm(const NormArgs& a, hipStream_t s)
     else if (chunks <= 512) go(k_norm<T, W, 256, 2>, 256, 1);
     else if (chunks <= 1024) go(k_norm<T, W, 256, 4>, 256, 1);
     else if (chunks <= 4096) go(k_norm<T, W, 1024, 4>, 1024, 1);
+    else if (chunks <= 8192) go(k_norm<T, W, 1024, 8>, 1024, 1);
+    else if (chunks <= 16384) go(k_norm<T, W, 1024, 16>, 1024, 1);
     else go(k_norm_long<T, W>, 1024, 1);
 }
 
@@ -433,7 +556,8 @@ static void launch_norm_backward(const NormArgs& a, void* grad_weight, void* gra
         hipLaunchKernelGGL((k_norm_sums<T, W>), dim3((unsigned)std::min<int64_t>(a.rows, 512)), dim3(1024), 0, s, a);
         groups = most;
         hipLaunchKernelGGL((k_norm_stripe<T, W>), dim3((unsigned)((chunks + 255) / 256), (unsigned)groups), dim3(256), 0, s, a);
-    } else if (chunks <= 16) go(k_norm_backward<T, W, 16, 1>, 256, 16);
+    } else if (a.n < kE<T>) go(k_norm_backward<T, W, 16, 1, true>, 256, 16);
+    else if (chunks <= 16) go(k_norm_backward<T, W, 16, 1>, 256, 16);
     else if (chunks <= 32) go(k_norm_backward<T, W, 16, 2>, 256, 16);
     else if (chunks <= 64) go(k_norm_backward<T, W, 64, 1>, 256, 4);
     else if (chunks <= 128) go(k_norm_backward<T, W, 64, 2>, 256, 4);
@@ -444,7 +568,7 @@ static void launch_norm_backward(const NormArgs& a, void* grad_weight, void* gra
     else if constexpr (sizeof(T) == 4) go(k_norm_backward<T, W, 1024, 4>, 1024, 1);
     if (a.parts || a.rows == 0) {
         if (!grad_weight && !grad_bias) return;
-        hipLaunchKernelGGL(k_norm_join<W>, dim3((unsigned)((2 * (int64_t)a.n + 63) / 64)), dim3(256), 0, s, a.parts, (int)groups, a.n, grad_weight, grad_bias);
+        hipLaunchKernelGGL(k_norm_join<W>, dim3((unsigned)((2 * (int64_t)a.n + 31) / 32)), dim3(1024), 0, s, a.parts, (int)groups, a.n, grad_weight, grad_bias);
     }
 }
 

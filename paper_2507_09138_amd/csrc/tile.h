@@ -291,7 +291,7 @@ __global__ __launch_bounds__(256) void k_tiles_join(TileArgs p)
 // ---- which tiles (host): see gated.hip
 constexpr int kComputeUnits = 256;
 struct Tiling { int bm, bn, parts, part_k; };
-Tiling tiling_for(bool gated, int64_t m, int64_t n, int64_t k_bytes);
+Tiling tiling_for(bool gated, int64_t m, int64_t n, int64_t k_bytes, size_t es);
 template <typename T, bool GATED>
 hipError_t launch_tiles(const Tiling& t, TileArgs p, hipStream_t s);
 

@@ -8,7 +8,9 @@ Nothing here is recorded by autograd: a training step calls the ``..._backward``
 ``adamw`` updates, counts as a change in place of that tensor.
 """
 import ctypes
+import functools
 import struct
+from itertools import chain
 from typing import NamedTuple, Optional
 
 import torch
@@ -42,8 +44,10 @@ class hr_adamw_tensor(ctypes.Structure):
                 ("param_dtype", _i32), ("grad_dtype", _i32)]
 
 
-_TENSOR = struct.Struct("@6Pqfii")                        # the same, but for the padding behind it
-_TENSOR_BYTES = ctypes.sizeof(hr_adamw_tensor)
+@functools.lru_cache(64)
+def _tables(n):
+    """n of these, as struct packs them."""
+    return struct.Struct("@" + "6Pqfii4x" * n)
 
 
 # ---- the C entry points by name
@@ -235,7 +239,7 @@ def adamw_state(param, bits=32):
 
 
 def _refuse(i, p, g, w, m, v, e, device):
-    """Says what is wrong with the i-th tensor of a step."""
+    """Says what is wrong with the i-th tensor of a step, if anything is."""
     for name, t in (("params", p), ("grads", g), ("m", m), ("v", v), ("masters", w), ("exponents", e)):
         if t is None and name in ("masters", "exponents"):
             continue
@@ -255,8 +259,13 @@ def _refuse(i, p, g, w, m, v, e, device):
     want = torch.float32 if e is None else torch.uint8
     if m.dtype != want or v.dtype != want:
         raise HrError(-1, f"m[{i}] and v[{i}] are {m.dtype} and {v.dtype}, want {want}" + (": exponents are None" if e is None else ""))
-    blocks = (p.numel() + HR_ADAMW_BLOCK - 1) // HR_ADAMW_BLOCK
-    raise HrError(-1, f"exponents[{i}] is {e.dtype} {tuple(e.shape)}, want {torch.uint8} {(blocks, 2)}")
+    shape = ((p.numel() + HR_ADAMW_BLOCK - 1) // HR_ADAMW_BLOCK, 2)
+    if e is not None and (e.dtype != torch.uint8 or e.shape != shape):
+        raise HrError(-1, f"exponents[{i}] is {e.dtype} {tuple(e.shape)}, want {torch.uint8} {shape}")
+
+
+_numel, _get_device, _is_contiguous, _data_ptr = torch.Tensor.numel, torch.Tensor.get_device, torch.Tensor.is_contiguous, torch.Tensor.data_ptr
+_F32, _U8 = torch.float32, torch.uint8
 
 
 def _lists(n, **named):
@@ -295,40 +304,38 @@ def adamw(params, grads, m, v, step, lr, betas=(0.9, 0.999), eps=1e-8, weight_de
         scale = _like(grad_scale, "grad_scale", torch.float32, grad_scale.shape if isinstance(grad_scale, torch.Tensor) else (), dev)
         if scale.numel() != 1:
             raise HrError(-1, f"grad_scale has {scale.numel()} elements, want 1")
-    table = bytearray(n * _TENSOR_BYTES)
-    count, kept, changed, f32, u8, pack = 0, [], [], torch.float32, torch.uint8, _TENSOR.pack_into
-    for i, (p, g, w, a, b, e) in enumerate(zip(params, grads, masters, m, v, exponents)):
-        if g is None:
-            continue
-        try:
-            size = p.numel()
-            kind = f32 if e is None else u8
-            fine = (p.device == dev and g.device == dev and a.device == dev and b.device == dev and g.shape == p.shape and a.dtype is kind and b.dtype is kind
-                    and a.numel() == size and b.numel() == size and p.is_contiguous() and a.is_contiguous() and b.is_contiguous()
-                    and (w is None or (w.device == dev and w.dtype is f32 and p.dtype is not f32 and w.numel() == size and w.is_contiguous()))
-                    and (e is None or (e.device == dev and e.dtype is u8 and e.is_contiguous() and e.shape == ((size + HR_ADAMW_BLOCK - 1) // HR_ADAMW_BLOCK, 2))))
-            kinds = _DTYPE[p.dtype], _DTYPE[g.dtype]
-        except (AttributeError, KeyError):
-            fine = False
-        if not fine:
-            _refuse(i, p, g, w, a, b, e, dev)
-        if not g.is_contiguous():
-            g = g.contiguous()
-            kept.append(g)
-        changed += (p, a, b) if w is None else (p, w, a, b)
-        if e is not None:
-            changed.append(e)
-        pack(table, count * _TENSOR_BYTES, p.data_ptr(), g.data_ptr(), 0 if w is None else w.data_ptr(), a.data_ptr(), b.data_ptr(), 0 if e is None else e.data_ptr(),
-             size, decay[i], *kinds)
-        count += 1
-    places = [t.data_ptr() for t in changed if t.numel()]
+    if any(g is None for g in grads):
+        kept = [i for i, g in enumerate(grads) if g is not None]
+        params, grads, m, v, exponents, masters, decay = ([x[i] for i in kept] for x in (params, grads, m, v, exponents, masters, decay))
+        n = len(params)
+    # (hundreds of tensors: what is asked of each is asked of whole lists, by functions that are not Python's)
+    has_e, has_w = [e for e in exponents if e is not None], [w for w in masters if w is not None]
+    try:
+        sizes, kinds, shapes = list(map(_numel, params)), [p.dtype for p in params], [p.shape for p in params]
+        wants = [_F32] * n if not has_e else [_F32 if e is None else _U8 for e in exponents]
+        fine = (set(map(_get_device, chain(params, grads, m, v, has_e, has_w))) <= {dev.index} and all(map(_is_contiguous, chain(params, m, v, has_e, has_w)))
+                and [g.shape for g in grads] == shapes and list(map(_numel, m)) == sizes and list(map(_numel, v)) == sizes
+                and [t.dtype for t in m] == wants and [t.dtype for t in v] == wants
+                and (not has_e or [(e.dtype, *e.shape) for e in has_e] == [(_U8, (k + HR_ADAMW_BLOCK - 1) // HR_ADAMW_BLOCK, 2) for k, e in zip(sizes, exponents) if e is not None])
+                and (not has_w or [(w.dtype, w.numel(), False) for w in has_w] == [(_F32, k, d is _F32) for k, d, w in zip(sizes, kinds, masters) if w is not None]))
+        ptypes, gtypes = [_DTYPE[d] for d in kinds], [_DTYPE[g.dtype] for g in grads]
+    except (AttributeError, KeyError, TypeError):
+        fine = False
+    if not fine:
+        for i, x in enumerate(zip(params, grads, masters, m, v, exponents)):
+            _refuse(i, *x, dev)
+    if not all(map(_is_contiguous, grads)):
+        grads = [g.contiguous() for g in grads]
+    at = [list(map(_data_ptr, x)) for x in (params, grads, m, v)]
+    wat, eat = ([0 if t is None else t.data_ptr() for t in x] if has else [0] * n for x, has in ((masters, has_w), (exponents, has_e)))
+    places = [x for x, k in zip(chain(at[0], at[2], at[3], wat, eat), sizes * 5) if k and x]
     if len(set(places)) != len(places):
         raise HrError(-1, "a tensor is in the lists twice")
-    at = (ctypes.c_char * len(table)).from_buffer(table)
+    table = _tables(n).pack(*chain.from_iterable(zip(at[0], at[1], wat, at[2], at[3], eat, sizes, decay, ptypes, gtypes)))
     beta1, beta2 = betas
     with torch.cuda.device(dev):
-        _check(lib.hr_adamw(ctypes.addressof(at), count, lr, beta1, beta2, eps, step, _at(device_step), _at(scale), _raw_stream(dev.index)))
-    torch.autograd.graph.increment_version(changed)
+        _check(lib.hr_adamw(table, n, lr, beta1, beta2, eps, step, _at(device_step), _at(scale), _raw_stream(dev.index)))
+    torch.autograd.graph.increment_version(list(chain(params, m, v, has_e, has_w)))
 
 
 @_on_device
