@@ -16,7 +16,7 @@ from typing import NamedTuple, Optional
 import torch
 
 from .binding import _DTYPE, _addr, _check, _stream, HR_F32, HrError, lib
-from .scores import _at, _kept, _like, _matrix, _on_device, _raw_stream, _result, _workspace, _written
+from .scores import _at, _current_device, _kept, _like, _matrix, _on_device, _raw_stream, _result, _workspace, _written
 
 HR_SILU, HR_GELU, HR_GELU_TANH = 0, 1, 2
 HR_GATED_MAX, HR_ADAMW_BLOCK = 1 << 19, 256
@@ -122,9 +122,9 @@ def _vector(t, name, n, dtype, device):
         return None
     if not isinstance(t, torch.Tensor) or t.device != device:
         raise HrError(-1, f"{name} must be a tensor on {device}")
-    if t.dtype not in (torch.float32, dtype) or t.shape != (n,):
+    if (t.dtype is not torch.float32 and t.dtype is not dtype) or t.shape != (n,):
         raise HrError(-1, f"{name} is {t.dtype} {tuple(t.shape)}, want {torch.float32} or {dtype} {(n,)}")
-    return t.contiguous()
+    return t if t.is_contiguous() else t.contiguous()
 
 
 @_on_device
@@ -333,8 +333,11 @@ def adamw(params, grads, m, v, step, lr, betas=(0.9, 0.999), eps=1e-8, weight_de
         raise HrError(-1, "a tensor is in the lists twice")
     table = _tables(n).pack(*chain.from_iterable(zip(at[0], at[1], wat, at[2], at[3], eat, sizes, decay, ptypes, gtypes)))
     beta1, beta2 = betas
-    with torch.cuda.device(dev):
+    if dev.index == _current_device():
         _check(lib.hr_adamw(table, n, lr, beta1, beta2, eps, step, _at(device_step), _at(scale), _raw_stream(dev.index)))
+    else:
+        with torch.cuda.device(dev):
+            _check(lib.hr_adamw(table, n, lr, beta1, beta2, eps, step, _at(device_step), _at(scale), _raw_stream(dev.index)))
     torch.autograd.graph.increment_version(list(chain(params, m, v, has_e, has_w)))
 
 

@@ -103,6 +103,7 @@ def hr_distill_step(logits, ld, dtype, rows, n, scale, ids, teacher, k, weights,
 # plain numbers, sizes of workspaces are kept by shape, and the library is called without another function in between.
 
 _raw_stream = torch._C._cuda_getCurrentRawStream          # (current_stream() makes an object first: 3 us)
+_current_device = torch._C._cuda_getDevice
 
 
 def _kept(f):
@@ -128,10 +129,13 @@ def _on_device(f):
 
     @functools.wraps(f)
     def call(*args, **kw):
-        t = args[0] if args else kw.get(name)
-        if not isinstance(t, torch.Tensor) or not t.is_cuda or t.device.index == torch._C._cuda_getDevice():
+        try:
+            index = (args[0] if args else kw.get(name)).get_device()
+        except AttributeError:                            # (no tensor: f says so)
             return f(*args, **kw)
-        with torch.cuda.device(t.device):
+        if index < 0 or index == _current_device():
+            return f(*args, **kw)
+        with torch.cuda.device(index):
             return f(*args, **kw)
     return call
 
