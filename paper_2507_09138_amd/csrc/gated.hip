@@ -26,6 +26,26 @@ __device__ __forceinline__ u32x4 load16(const T* row, int t, int n)
     return v;
 }
 
+// 16 bytes of a row from an element on that may lie anywhere: whole words of 4 bytes and a shift (a load of 16 bytes that begins inside a word takes
+// four times as long; the word behind them is read only where it holds some of them)
+template <typename T>
+__device__ __forceinline__ u32x4 load16_words(const T* at)
+{
+    u32x4 v;
+    if constexpr (sizeof(T) == 4) {
+        __builtin_memcpy(&v, at, 16);
+    } else {
+        const uint32_t* from = (const uint32_t*)((uintptr_t)at & ~(uintptr_t)3);
+        const uint32_t shift = (uint32_t)(uintptr_t)at & 3;
+        uint32_t w[5];
+        __builtin_memcpy(w, __builtin_assume_aligned(from, 4), 16);
+        w[4] = from[shift ? 4 : 3];
+#pragma unroll
+        for (int i = 0; i < 4; ++i) v[i] = __builtin_amdgcn_alignbyte(w[i + 1], w[i], shift);
+    }
+    return v;
+}
+
 // ---- rows that tiles cannot take as they are, copied with zeros behind them to multiples of 128 bytes
 template <typename T>
 __global__ __launch_bounds__(256) void k_pad(const T* x, int64_t ldx, int64_t rows, int n, char* out, int64_t ldo)
@@ -185,9 +205,9 @@ __global__ __launch_bounds__(1024) void k_gated_few(const T* x, int64_t ldx, con
         for (int u = 0; u < U; ++u) {
             const int t = (decltype(full)::value ? s + u : min(s + u, end - 1)) * K;
 #pragma unroll
-            for (int j = 0; j < NT; ++j) __builtin_memcpy(&b[u][j], w[j] + t, 16);
+            for (int j = 0; j < NT; ++j) b[u][j] = load16_words(w[j] + t);
 #pragma unroll
-            for (int i = 0; i < MT; ++i) __builtin_memcpy(&a[u][i], xr[i] + t, 16);
+            for (int i = 0; i < MT; ++i) a[u][i] = load16_words(xr[i] + t);
         }
 #pragma unroll
         for (int u = 0; u < U; ++u) {
@@ -483,7 +503,8 @@ static hipError_t launch_gated(const GatedArgs& g, char* ws, hipStream_t s)
                                (int)g.m, (int)g.k, (int)g.f, g.act, (T*)g.out, g.ldo, g.pre);
         };
         if (g.k * es % 16 == 0 && in_tiles(g.x, g.ldx, es) && in_tiles(g.gate, g.ldg, es) && in_tiles(g.up, g.ldu, es)) return g.m <= 16 ? ring(k_gated_ring<T, 2, 2, 2>, 2, 2, 2) : ring(k_gated_ring<T, 2, 4, 3>, 2, 4, 3);
-        if (g.m <= 16) go(k_gated_few<T, 1, 1, 8>, 8, 16);
+        if (g.m <= 4) go(k_gated_few<T, 1, 1, 8>, 8, 16);
+        else if (g.m <= 16) go(k_gated_few<T, 1, 2, 4>, 16, 8);
         else go(k_gated_few<T, 2, 2, 4>, 16, 4);
         return hipGetLastError();
     }
