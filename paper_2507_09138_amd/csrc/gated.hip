@@ -398,46 +398,70 @@ __global__ __launch_bounds__(256) void k_gated_any(const T* x, int64_t ldx, cons
 
 // ---- which kernel
 
-// Tiles (rows x columns of both matrices): 256 x 256, 128 x 128 or, for up to 64 rows, 64 x 256, in parts of k or not: what takes least by this count of
-// microseconds.  A block of 128 bytes of k takes a tile of 256 x 256 1.6 (16 bits; one at a time on a compute unit; an unfilled last round runs at a higher
-// clock), the smaller ones 0.48, and 0.5 where a tile has a compute unit for itself; in float32 1.9 and 2.0 (large tiles are no faster there).
-// Start and end take 6 to 8, parts are written and read at 5 MB/us, by another launch.  Measured, here (the other choices): 4096 x 4096 x 4096 bfloat16 102 .. 112 (128 x 128 118), 2048 x 4096 x 4096 61 (256 x 256
-// 86, two parts 84), 512 x 512 x 4096 in eight parts 15.4 (one 32.6), float32 2048 x 768 x 4096 in five 112 (one 260, two 144).
-Tiling tiling_for(bool gated, int64_t m, int64_t n, int64_t k_bytes, size_t es)
+// Tiles (rows x columns of both matrices): 256 x 256, 128 x 128 or, for up to 64 rows of a gated block, 64 x 256, in parts of k or not: what takes least by
+// this count of microseconds.  Workgroups come in rounds: one of 256 x 256 on a compute unit at a time, two of the smaller ones; those of two products in
+// one launch, of parts about as long as each other, in common rounds or one product's after the other's.  A block of 128 bytes of k takes a large tile 1.6 (16 bits; an unfilled last round runs at a higher
+// clock), two small ones 0.96, and one that has a compute unit for itself 0.5; in float32 3.8 and 2.0 (large tiles are no faster there).  Start and end
+// take 6 to 8, parts are written and read at 4 MB/us, by another launch.
+// Measured, here (the other choices): 4096 x 4096 x 4096 bfloat16 102 .. 112 (128 x 128 118), 2048 x 4096 x 4096 61 (256 x 256
+// 86, two parts 84), 512 x 512 x 4096 in eight parts 15.4 (one 32.6), float32 2048 x 768 x 4096 in five 113 (one 260, two 148), that and 4096 x 768 x 2048
+// in eight and four parts 219 (one after the other 228; four and two 209, six and one, unlike lengths, 325).
+// m, n and k of the products are there; parts and part_k are set.
+static Tiling plan_tiles(bool gated, size_t es, TileArgs* p, int count)
 {
-    const int64_t blocks = k_bytes / 128, sums = m * n * (gated ? 2 : 1) * 8;
     Tiling best{};
     double least = 0;
+    int64_t longest_k = 0, chosen = 0;
+    for (int i = 0; i < count; ++i) longest_k = std::max<int64_t>(longest_k, p[i].k / 128);
     auto consider = [&](int bm, int bn, double each, double alone, double ends) {
-        const int64_t cols = bn / (gated ? 2 : 1), tiles = (m + bm - 1) / bm * ((n + cols - 1) / cols);
-        for (int64_t parts = 1; parts <= 64; ++parts) {
-            const int64_t of = (blocks + parts - 1) / parts, all = tiles * parts;
-            if (parts > 1 && (of < 2 || parts * sums > (1LL << 29))) break;
-            if (parts > 1 && (blocks + of - 1) / of != parts) continue;                      // (fewer parts as long as these)
-            const double rounds = (double)((all + kComputeUnits - 1) / kComputeUnits), t = std::max((bm == 256 ? (rounds + (double)all / kComputeUnits) / 2 : rounds) * of * each, of * alone) + ends + (parts > 1 ? 3 + parts * sums / 5e6 : 0);
-            if (!best.parts || t < least) {
+        const int64_t cols = bn / (gated ? 2 : 1), at_once = bm == 256 ? kComputeUnits : 2 * kComputeUnits;
+        int64_t last = 0;
+        for (int64_t n = 1; n <= 64; ++n) {
+            const int64_t length = (longest_k + n - 1) / n;                  // blocks of the longest part
+            if (n > 1 && (length < 2 || length == last)) continue;
+            last = length;
+            int64_t all = 0, most = 0;
+            double work = 0, joins = 0, in_turn = 0;
+            bool fits = true;
+            for (int i = 0; i < count; ++i) {
+                const int64_t blocks = p[i].k / 128, parts = (blocks + length - 1) / length, of = (blocks + parts - 1) / parts;
+                const int64_t groups = (p[i].m + bm - 1) / bm * ((p[i].n + cols - 1) / cols) * parts;
+                const double sums = (double)parts * p[i].m * p[i].n * (gated ? 8 : 4);
+                all += groups;
+                most = std::max(most, of);
+                work += (double)groups * of;
+                in_turn += groups <= kComputeUnits ? of * alone : (double)((groups + at_once - 1) / at_once * of) * each;
+                if (parts > 1) {
+                    joins += 2 * sums / 4e6;
+                    fits &= groups <= 8 * kComputeUnits && sums <= 0x1p28;
+                }
+            }
+            if (!fits) break;
+            double t = all <= kComputeUnits ? most * alone : std::min(in_turn, (double)((all + at_once - 1) / at_once * most) * each);
+            if (bm == 256) t = std::max(most * alone, (t + work / kComputeUnits * each) / 2);
+            t += ends + joins + (joins > 0 ? 4 : 0);
+            if (!best.bm || t < least) {
                 least = t;
-                best = {bm, bn, (int)parts, (int)(of * 128)};
+                best = {bm, bn};
+                chosen = length;
             }
         }
     };
-    if (es == 4) {
-        if (m <= 64) consider(64, 256, 1.9, 2.0, 6);
-        else consider(128, 128, 1.9, 2.0, 6);
-    } else if (m <= 64) {
-        consider(64, 256, 0.48, 0.5, 6);
+    if (gated && p[0].m <= 64) {
+        consider(64, 256, es == 4 ? 3.8 : 0.96, es == 4 ? 2.0 : 0.5, 6);
     } else {
-        consider(128, 128, 0.48, 0.5, 6);
-        consider(256, 256, 1.6, 1.2, 8);
+        consider(128, 128, es == 4 ? 3.8 : 0.96, es == 4 ? 2.0 : 0.5, 6);
+        if (es < 4) consider(256, 256, 1.6, 1.2, 8);
+    }
+    for (int i = 0; i < count; ++i) {
+        const int64_t blocks = p[i].k / 128, parts = (blocks + chosen - 1) / chosen, of = (blocks + parts - 1) / parts;
+        p[i].parts = (int)((blocks + of - 1) / of);
+        p[i].part_k = (int)of * 128;
     }
     return best;
 }
 // room for the sums of parts of k
-static size_t sums_bytes(bool gated, int64_t m, int64_t n, int64_t k_bytes, size_t es)
-{
-    const Tiling t = tiling_for(gated, m, n, k_bytes, es);
-    return t.parts > 1 ? aligned((size_t)(t.parts * m * n * (gated ? 2 : 1)) * 4) : 0;
-}
+static size_t sums_bytes(bool gated, const TileArgs& p) { return p.parts > 1 ? aligned((size_t)(p.parts * p.m * p.n * (gated ? 2 : 1)) * 4) : 0; }
 
 static int64_t padded(int64_t n, size_t es) { return (n * (int64_t)es + 127) / 128 * 128; }             // bytes of a row
 // rows that requests of 16 bytes reach; offsets inside a tile are 32-bit numbers
@@ -538,7 +562,8 @@ static hipError_t launch_gated(const GatedArgs& g, char* ws, hipStream_t s)
     p.pre = g.pre;
     p.act = g.act;
     p.sums = (float*)(ws + x_bytes(g.m, g.k, es) + w_bytes(g.k, g.f, es));
-    return launch_tiles<T, true>(tiling_for(true, g.m, g.f, p.k, es), p, s);
+    const Tiling t = plan_tiles(true, es, &p, 1);
+    return launch_tiles<T, true>(t, TilePair{{p}}, 1, s);
 }
 
 // workspace of the gradients: those of gate and up as rows, [m][2 fp], and as columns, [2 f][mp]; both matrices turned, [k][2 fp]; x turned, [k][mp];
@@ -546,10 +571,12 @@ static hipError_t launch_gated(const GatedArgs& g, char* ws, hipStream_t s)
 struct BackwardPlan {
     int64_t fp, mp;                                      // elements
     size_t rows, cols, w, x, sums, all;                  // where each begins, and the end
+    Tiling tiling;
+    TileArgs p[2];                                       // the product for x's gradient, the one for the matrices' (the same parts whichever are wanted)
 };
 static BackwardPlan backward_plan(int64_t m, int64_t k, int64_t f, size_t es)
 {
-    BackwardPlan p;
+    BackwardPlan p{};
     const int64_t fb = padded(f, es), mb = padded(m, es);
     p.fp = fb / es;
     p.mp = mb / es;
@@ -558,7 +585,17 @@ static BackwardPlan backward_plan(int64_t m, int64_t k, int64_t f, size_t es)
     p.w = p.cols + aligned((size_t)(2 * f * mb));
     p.x = p.w + aligned((size_t)(k * 2 * fb));
     p.sums = p.x + aligned((size_t)(k * mb));
-    p.all = p.sums + (m ? std::max(sums_bytes(false, m, k, 2 * fb, es), sums_bytes(false, 2 * f, k, mb, es)) : 0) + HR_WORKSPACE_ALIGN;
+    p.all = p.sums + HR_WORKSPACE_ALIGN;
+    if (m == 0) return p;
+    for (int i = 0; i < 2; ++i) {
+        TileArgs& t = p.p[i];
+        t.m = i ? 2 * f : m;
+        t.n = k;
+        t.k = (int)(i ? mb : 2 * fb);
+        t.lda = t.ldb = t.k;
+    }
+    p.tiling = plan_tiles(false, es, p.p, 2);
+    p.all += sums_bytes(false, p.p[0]) + sums_bytes(false, p.p[1]);
     return p;
 }
 
@@ -574,7 +611,12 @@ size_t hr_gated_workspace_bytes(int64_t m, int64_t k, int64_t f, int32_t dtype)
     if (check_gated(m, k, f, dtype, HR_SILU)) return 0;
     const size_t es = element_bytes(dtype);
     if (m <= kFewRows) return HR_WORKSPACE_ALIGN;
-    return x_bytes(m, k, es) + w_bytes(k, f, es) + sums_bytes(true, m, f, padded(k, es), es) + HR_WORKSPACE_ALIGN;
+    TileArgs p{};
+    p.m = m;
+    p.n = f;
+    p.k = (int)padded(k, es);
+    plan_tiles(true, es, &p, 1);
+    return x_bytes(m, k, es) + w_bytes(k, f, es) + sums_bytes(true, p) + HR_WORKSPACE_ALIGN;
 }
 
 int hr_gated(const void* x, int64_t ldx, const void* w_gate, int64_t ldwg, const void* w_up, int64_t ldwu, int32_t dtype, int64_t m, int64_t k,
@@ -620,10 +662,10 @@ int hr_gated_backward(const void* x, int64_t ldx, const void* w_gate, int64_t ld
         if (int rc = check_matrix("grad_w_gate", grad_w_gate, f, k, ldgg, es)) return rc;
         if (int rc = check_matrix("grad_w_up", grad_w_up, f, k, ldgu, es)) return rc;
     }
-    if (int rc = check_workspace(workspace, workspace_bytes, hr_gated_backward_workspace_bytes(m, k, f, dtype))) return rc;
+    const BackwardPlan plan = backward_plan(m, k, f, es);
+    if (int rc = check_workspace(workspace, workspace_bytes, plan.all)) return rc;
     if (!grad_x && !grad_w_gate) return HR_OK;
     hipStream_t s = (hipStream_t)stream;
-    const BackwardPlan plan = backward_plan(m, k, f, es);
     char *rows = (char*)workspace + plan.rows, *cols = (char*)workspace + plan.cols, *turned_w = (char*)workspace + plan.w, *turned_x = (char*)workspace + plan.x;
     HR_HIP(with_type(dtype, [&](auto t) -> hipError_t {
         using T = decltype(t);
@@ -643,31 +685,30 @@ int hr_gated_backward(const void* x, int64_t ldx, const void* w_gate, int64_t ld
         l.blocks_d = blocks(plan.mp, plan.fp);
         l.blocks_w = blocks(plan.fp, k);
         hipLaunchKernelGGL(k_lay_out<T>, dim3((unsigned)(l.blocks_d + (grad_x ? 2 * l.blocks_w : 0) + (grad_w_gate ? blocks(plan.mp, k) : 0))), dim3(256), 0, s, l);
-        TileArgs p{};
-        p.sums = (float*)((char*)workspace + plan.sums);
+        TilePair pair{};
+        int count = 0;
+        char* sums = (char*)workspace + plan.sums;
         if (grad_x) {
+            TileArgs& p = pair.p[count++] = plan.p[0];
+            p.sums = (float*)sums;
             p.a = rows;
             p.b = turned_w;
-            p.lda = p.ldb = p.k = (int)(2 * plan.fp * sizeof(T));
-            p.m = p.split = m;
-            p.n = k;
             p.out = grad_x;
             p.ldo = ldgx;
-            if (hipError_t e = launch_tiles<T, false>(tiling_for(false, p.m, p.n, p.k, sizeof(T)), p, s)) return e;
+            p.split = m;
         }
         if (grad_w_gate) {
+            TileArgs& p = pair.p[count++] = plan.p[1];
+            p.sums = (float*)(sums + sums_bytes(false, plan.p[0]));
             p.a = cols;
             p.b = turned_x;
-            p.lda = p.ldb = p.k = (int)(plan.mp * sizeof(T));
-            p.m = 2 * f;
-            p.split = f;
-            p.n = k;
             p.out = grad_w_gate;
             p.out2 = grad_w_up;
             p.ldo = ldgg;
             p.ldo2 = ldgu;
-            if (hipError_t e = launch_tiles<T, false>(tiling_for(false, p.m, p.n, p.k, sizeof(T)), p, s)) return e;
+            p.split = f;
         }
+        if (hipError_t e = launch_tiles<T, false>(plan.tiling, pair, count, s)) return e;
         return hipGetLastError();
     }));
     return HR_OK;

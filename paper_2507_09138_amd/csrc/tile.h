@@ -56,10 +56,17 @@ struct TileArgs {
     const char* up; int64_t ldup;                        // gated: up's
     int64_t m, n; int k;                                 // n: columns of the result
     int parts, part_k;                                   // parts of k (part_k bytes each, a multiple of 128), and where there are more than one
+    int slots;                                           // workgroups of each part, a multiple of 8
     float* sums;                                         // their sums, [parts][m][n], gated [parts][m][2][n]
     void* out; int64_t ldo;                              // elements apart
     void* out2; int64_t ldo2, split;                     // rows from `split` on go to out2
     float* pre; int act;                                 // gated
+};
+
+// One product, or two in one launch: workgroups from `first` on are the second's.
+struct TilePair {
+    TileArgs p[2];
+    unsigned first;
 };
 
 // N neighbouring outputs of a row, as far as they are there
@@ -104,22 +111,25 @@ __device__ __forceinline__ void finish(const TileArgs& p, int64_t row, int64_t c
 // filled again: one barrier a block.  Where there is no more than a tile for every compute unit nothing else hides the time that loads take: NB
 // buffers, all but one on their way.  Else a workgroup goes from tile to tile and asks for the next one's first blocks before it writes its outputs.
 template <typename T, bool GATED, int BM, int BN, int WM, int NB>
-__global__ __launch_bounds__(BM / WM * (BN / 64) * 64) void k_tiles(TileArgs p)
+__global__ __launch_bounds__(BM / WM * (BN / 64) * 64) void k_tiles(TilePair pair)
 {
+    const bool second = blockIdx.x >= pair.first;
+    const TileArgs& p = pair.p[second];
+    const int wg = (int)(blockIdx.x - (second ? pair.first : 0)), part = wg / p.slots, slot = wg - part * p.slots;
     constexpr int WN = 64, WAVES = BM / WM * (BN / WN), TM = WM / 16, TN = 4, BK = 128, UNITS = (BM + BN) / 8 / WAVES, BUF = (BM + BN) * BK;
     constexpr int COLS = GATED ? BN / 2 : BN;            // of the result
     static_assert(BM / 8 % WAVES == 0 && BN / 8 % WAVES == 0 && NB >= 2 && NB <= 4);
     extern __shared__ __align__(1024) char lds[];
     const int lane = lane_id(), wave = __builtin_amdgcn_readfirstlane(threadIdx.x / 64);
     const int wm = wave / (BN / WN) * WM, wn = wave % (BN / WN) * WN;
-    const int k_begin = blockIdx.y * p.part_k, k_end = min(p.k, k_begin + p.part_k), blocks = (k_end - k_begin) / BK;
+    const int k_begin = part * p.part_k, k_end = min(p.k, k_begin + p.part_k), blocks = (k_end - k_begin) / BK;
     const int piece = ((lane & 7) ^ (lane >> 3)) * 16;
     const uint32_t lds0 = lds_addr(lds);
 
     // Tiles that run at the same time on an XCD share its L2: each has a stretch of the tiles, and takes them in blocks of four rows of tiles.
     const int m = (int)p.m, n = (int)p.n, tiles_m = (m + BM - 1) / BM, tiles_n = (n + COLS - 1) / COLS, tiles = tiles_m * tiles_n;
-    const int stretch = (tiles + 7) / 8, tile0 = (int)(blockIdx.x % 8) * stretch, end = min(stretch, tiles - tile0);
-    int tile = blockIdx.x / 8, m0 = 0, n0 = 0;
+    const int stretch = (tiles + 7) / 8, tile0 = slot % 8 * stretch, end = min(stretch, tiles - tile0);
+    int tile = slot / 8, m0 = 0, n0 = 0;
     uint32_t off[UNITS];                                 // (rows of a tile lie within 2^31 bytes: the host sees to it)
     const char *ga = p.a, *gb = p.b, *gu = p.up;
     // What lies in row r of b's part of a buffer.  Rows 0 .. 15 and 16 .. 31 of 32 are four of each eight columns, so that a lane has eight neighbouring
@@ -205,7 +215,7 @@ __global__ __launch_bounds__(BM / WM * (BN / 64) * 64) void k_tiles(TileArgs p)
             step(b1, place(b + 1, 0));
         }
         const int mt = m0, nt = n0;
-        tile += gridDim.x / 8;
+        tile += p.slots / 8;
         const bool more = NB == 2 && tile < end;         // (with more buffers the host launches a workgroup for every tile)
         if (more) {
             aim(tile);
@@ -226,7 +236,7 @@ __global__ __launch_bounds__(BM / WM * (BN / 64) * 64) void k_tiles(TileArgs p)
                     if (GATED) up[e] = acc[i][(j + 2 + e / 4) % TN][e % 4];
                 }
                 if (p.parts > 1) {
-                    float* at = p.sums + ((int64_t)blockIdx.y * m + row) * (GATED ? 2 : 1) * n;
+                    float* at = p.sums + ((int64_t)part * m + row) * (GATED ? 2 : 1) * n;
                     store_some<8>(at, col, n, v);
                     if (GATED) store_some<8>(at + n, col, n, up);
                 } else {
@@ -240,13 +250,16 @@ __global__ __launch_bounds__(BM / WM * (BN / 64) * 64) void k_tiles(TileArgs p)
 
 // Adds up the parts of k: SHARES threads take every SHARES-th part of four columns, in order, and their sums are added in order.
 template <typename T, bool GATED, int SHARES>
-__global__ __launch_bounds__(256) void k_tiles_join(TileArgs p)
+__global__ __launch_bounds__(256) void k_tiles_join(TilePair pair)
 {
+    const bool second = blockIdx.x >= pair.first;
+    const TileArgs& p = pair.p[second];
+    const int64_t block = blockIdx.x - (second ? pair.first : 0), blocks = second ? gridDim.x - pair.first : pair.first;
     constexpr int PER = 256 / SHARES;
     __shared__ floatx4 some[GATED ? 2 : 1][SHARES][PER];
     const int64_t fours = (p.n + 3) / 4, all = p.m * fours, stride = p.m * p.n * (GATED ? 2 : 1);
     const int at = threadIdx.x % PER, share = threadIdx.x / PER;
-    for (int64_t i0 = (int64_t)blockIdx.x * PER; i0 < all; i0 += (int64_t)gridDim.x * PER) {
+    for (int64_t i0 = block * PER; i0 < all; i0 += blocks * PER) {
         const int64_t i = min(i0 + at, all - 1), row = i / fours, col = (i - row * fours) * 4;
         const float* from = p.sums + row * (GATED ? 2 : 1) * p.n + col;
         const bool whole = col + 4 <= p.n;
@@ -288,11 +301,11 @@ __global__ __launch_bounds__(256) void k_tiles_join(TileArgs p)
     }
 }
 
-// ---- which tiles (host): see gated.hip
+// ---- host: which tiles (gated.hip), and their launches
 constexpr int kComputeUnits = 256;
-struct Tiling { int bm, bn, parts, part_k; };
-Tiling tiling_for(bool gated, int64_t m, int64_t n, int64_t k_bytes, size_t es);
+struct Tiling { int bm, bn; };
+// Of count products, 1 or 2; slots are set here.
 template <typename T, bool GATED>
-hipError_t launch_tiles(const Tiling& t, TileArgs p, hipStream_t s);
+hipError_t launch_tiles(const Tiling& t, TilePair pair, int count, hipStream_t s);
 
 }  // namespace hr

@@ -7,28 +7,43 @@
 namespace hr {
 
 template <typename T, bool GATED>
-hipError_t launch_tiles(const Tiling& t, TileArgs p, hipStream_t s)
+hipError_t launch_tiles(const Tiling& t, TilePair pair, int count, hipStream_t s)
 {
     hipError_t e = hipSuccess;
-    const int64_t cols = GATED ? t.bn / 2 : t.bn, tiles = (p.m + t.bm - 1) / t.bm * ((p.n + cols - 1) / cols);
-    const bool deep = t.bm < 256 && tiles * t.parts <= kComputeUnits;
+    const int64_t cols = GATED ? t.bn / 2 : t.bn;
+    auto tiles = [&](const TileArgs& p) { return (p.m + t.bm - 1) / t.bm * ((p.n + cols - 1) / cols); };
+    int64_t all = 0;
+    for (int i = 0; i < count; ++i) all += tiles(pair.p[i]) * pair.p[i].parts;
+    const bool deep = t.bm < 256 && all <= kComputeUnits;
     auto go = [&](auto kernel, int buffers) {
         const size_t lds = (size_t)(t.bm + t.bn) * 128 * buffers;
+        unsigned groups[2] = {0, 0};
+        for (int i = 0; i < count; ++i) {
+            pair.p[i].slots = (int)std::min((tiles(pair.p[i]) + 7) / 8, (int64_t)kComputeUnits / 8 * (lds <= 80 * 1024 ? 2 : 1)) * 8;
+            groups[i] = (unsigned)(pair.p[i].slots * pair.p[i].parts);
+        }
+        pair.first = groups[0];
         if (lds > 64 * 1024) e = hipFuncSetAttribute((const void*)kernel, hipFuncAttributeMaxDynamicSharedMemorySize, (int)lds);
-        if (e == hipSuccess) hipLaunchKernelGGL(kernel, dim3((unsigned)(std::min((tiles + 7) / 8, (int64_t)kComputeUnits / 8 * (lds <= 80 * 1024 ? 2 : 1)) * 8), t.parts), dim3(512), lds, s, p);
+        if (e == hipSuccess) hipLaunchKernelGGL(kernel, dim3(groups[0] + groups[1]), dim3(512), lds, s, pair);
     };
-    p.parts = t.parts;
-    p.part_k = t.part_k;
-    if (t.bm == 256) go(k_tiles<T, GATED, 256, 256, 128, 2>, 2);
-    else if (t.bm == 128) deep ? go(k_tiles<T, GATED, 128, 128, 32, 4>, 4) : go(k_tiles<T, GATED, 128, 128, 32, 2>, 2);
-    else deep ? go(k_tiles<T, GATED, 64, 256, 32, 3>, 3) : go(k_tiles<T, GATED, 64, 256, 32, 2>, 2);
-    if (e == hipSuccess && t.parts > 1) {
+    if (t.bm == 256) {
+        if constexpr (sizeof(T) == 2) go(k_tiles<T, GATED, 256, 256, 128, 2>, 2);
+    } else if (t.bm == 128) {
+        deep ? go(k_tiles<T, GATED, 128, 128, 32, 4>, 4) : go(k_tiles<T, GATED, 128, 128, 32, 2>, 2);
+    } else if constexpr (GATED) {
+        deep ? go(k_tiles<T, GATED, 64, 256, 32, 3>, 3) : go(k_tiles<T, GATED, 64, 256, 32, 2>, 2);
+    }
+    const int most = std::max(pair.p[0].parts, count > 1 ? pair.p[1].parts : 1);
+    if (e == hipSuccess && most > 1) {
         auto join = [&](auto kernel, int shares) {
-            const int64_t want = (p.m * ((p.n + 3) / 4) + 256 / shares - 1) / (256 / shares);
-            hipLaunchKernelGGL(kernel, dim3((unsigned)std::min<int64_t>(want, 1 << 20)), dim3(256), 0, s, p);
+            unsigned groups[2] = {0, 0};
+            for (int i = 0; i < count; ++i)
+                if (pair.p[i].parts > 1) groups[i] = (unsigned)std::min<int64_t>((pair.p[i].m * ((pair.p[i].n + 3) / 4) + 256 / shares - 1) / (256 / shares), 1 << 20);
+            pair.first = groups[0];
+            hipLaunchKernelGGL(kernel, dim3(groups[0] + groups[1]), dim3(256), 0, s, pair);
         };
-        if (t.parts >= 12) join(k_tiles_join<T, GATED, 16>, 16);
-        else if (t.parts >= 4) join(k_tiles_join<T, GATED, 4>, 4);
+        if (most >= 12) join(k_tiles_join<T, GATED, 16>, 16);
+        else if (most >= 4) join(k_tiles_join<T, GATED, 4>, 4);
         else join(k_tiles_join<T, GATED, 1>, 1);
     }
     return e == hipSuccess ? hipGetLastError() : e;
