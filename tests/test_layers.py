@@ -585,3 +585,39 @@ def test_what_is_refused():
         assert err.value.code in (-1, -5), i
     torch.cuda.synchronize()
     assert torch.equal(x, kept)                            # nothing was enqueued by the refused calls
+
+
+def _example():
+    import importlib.util
+    import os
+    path = os.path.join(os.path.dirname(os.path.dirname(os.path.abspath(__file__))), "examples", "train_encoder_layers.py")
+    spec = importlib.util.spec_from_file_location("train_encoder_layers", path)
+    example = importlib.util.module_from_spec(spec)
+    spec.loader.exec_module(example)
+    return example
+
+
+def test_the_example_runs(capsys):
+    """examples/train_encoder_layers.py, small: search, layers, distillation, gradients and steps together."""
+    encoder, losses = _example().main(passages=8192, d=128, hidden=200, layers=2, nlist=64, batch=128, k=16, probes=8, steps=6)
+    assert len(losses) == 6 and all(math.isfinite(x) for x in losses) and encoder.steps == 6
+    assert all(bool(t.isfinite().all()) for t in encoder.tensors) and "step 5" in capsys.readouterr().out
+
+
+def test_the_examples_gradients():
+    """Of its encoder in float32, two layers, against autograd in 64 bits."""
+    e = _example().Encoder(2, 48, 80, dtype=F32, bits=32)
+    x, dy = _randn(1, 60, 48), _randn(2, 60, 48)
+    y, kept = e.forward(x)
+    grads = e.backward(dy, kept)
+    leaves = [t.double().cpu().requires_grad_(True) for t in e.tensors]
+    z = x.double().cpu()
+    for i in range(0, 10, 5):
+        w, b, wg, wu, wd = leaves[i:i + 5]
+        u = torch.nn.functional.layer_norm(z, (48,), w, b, 1e-5)
+        z = z + (torch.nn.functional.silu(u @ wg.T) * (u @ wu.T)) @ wd.T
+    (z * dy.double().cpu()).sum().backward()
+    # chains of up to ten sums of at most 80 products, of factors near 1 in size, by the norm of the result
+    assert float((y.double().cpu() - z.detach()).norm() / z.detach().norm()) < 10 * 90 * ref.U
+    for got, leaf in zip(grads, leaves):
+        assert float((got.double().cpu() - leaf.grad).norm() / leaf.grad.norm()) < 10 * 90 * ref.U
