@@ -398,20 +398,22 @@ __global__ __launch_bounds__(256) void k_gated_any(const T* x, int64_t ldx, cons
 
 // ---- which kernel
 
-// Tiles (rows x columns of both matrices): 256 x 256, 128 x 128 or, for up to 64 rows of a gated block, 64 x 256, in parts of k or not: what takes least by
-// this count of microseconds.  Workgroups come in rounds: one of 256 x 256 on a compute unit at a time, two of the smaller ones; those of two products in
-// one launch, of parts about as long as each other, in common rounds or one product's after the other's.  A block of 128 bytes of k takes a large tile 1.6 (16 bits; an unfilled last round runs at a higher
-// clock), two small ones 0.96, and one that has a compute unit for itself 0.5; in float32 3.8 and 2.0 (large tiles are no faster there).  Start and end
-// take 6 to 8, parts are written and read at 4 MB/us, by another launch.
-// Measured, here (the other choices): 4096 x 4096 x 4096 bfloat16 102 .. 112 (128 x 128 118), 2048 x 4096 x 4096 61 (256 x 256
-// 86, two parts 84), 512 x 512 x 4096 in eight parts 15.4 (one 32.6), float32 2048 x 768 x 4096 in five 113 (one 260, two 148), that and 4096 x 768 x 2048
-// in eight and four parts 219 (one after the other 228; four and two 209, six and one, unlike lengths, 325).
-// m, n and k of the products are there; parts and part_k are set.
+// Tiles (rows x columns of both matrices): 256 x 256, 128 x 128 or, for up to 64 rows of a gated block, 64 x 256, in parts of k or not: what takes
+// least by this count of microseconds.  Workgroups come in rounds: one of 256 x 256 on a compute unit at a time, two of the smaller ones; those of
+// two products in one launch, of parts about as long as each other, in common rounds or one product's after the other's.  A block of 128 bytes of k
+// takes a large tile 1.6 (16 bits), two small ones 0.96, and one that has a compute unit for itself 0.5; in float32 3.8 and 2.0 (large tiles are no
+// faster there).  Start and end take 6 to 8, parts are written and read at 4 MB/us, by another launch.
+// Measured, here (the other choices): 4096 x 4096 x 4096 bfloat16 102 .. 112 (128 x 128 118), 2048 x 4096 x 4096 61 (256 x 256 86, two parts 84),
+// 512 x 512 x 4096 in eight parts 15.4 (one 32.6), float32 2048 x 768 x 4096 in five 113 (one 260, two 148), that and 4096 x 768 x 2048 in eight and
+// four parts 219 (one after the other 228; four and two 209, six and one, unlike lengths, 325).
+// Where large tiles leave much of a last round empty, the rows of that round are left to small ones, in a second launch: 8192 x 4096 x 21504 and
+// 21504 x 4096 x 8192, 2 and 5.25 rounds, 2283 -> 2190.
+// m, n and k of the products are there; parts, part_k and large are set.
 static Tiling plan_tiles(bool gated, size_t es, TileArgs* p, int count)
 {
     Tiling best{};
     double least = 0;
-    int64_t longest_k = 0, chosen = 0;
+    int64_t longest_k = 0, chosen = 0, large[2] = {p[0].m, count > 1 ? p[1].m : 0};
     for (int i = 0; i < count; ++i) longest_k = std::max<int64_t>(longest_k, p[i].k / 128);
     auto consider = [&](int bm, int bn, double each, double alone, double ends) {
         const int64_t cols = bn / (gated ? 2 : 1), at_once = bm == 256 ? kComputeUnits : 2 * kComputeUnits;
@@ -438,7 +440,35 @@ static Tiling plan_tiles(bool gated, size_t es, TileArgs* p, int count)
             }
             if (!fits) break;
             double t = all <= kComputeUnits ? most * alone : std::min(in_turn, (double)((all + at_once - 1) / at_once * most) * each);
-            if (bm == 256) t = std::max(most * alone, (t + work / kComputeUnits * each) / 2);
+            // (16 bits: an unfilled last round runs at a higher clock)
+            if (es < 4 && all > kComputeUnits) t = (t + work / at_once * each) / 2;
+            if (bm == 256) {
+                if (all <= kComputeUnits) t = std::max(t, (most * each + work / kComputeUnits * each) / 2);
+                // (rows that fill whole rounds, the others in small tiles)
+                if (n == 1) {
+                    double mixed = 0;
+                    int64_t kept[2];
+                    for (int i = 0; i < count; ++i) {
+                        const int64_t blocks = p[i].k / 128, across = (p[i].n + cols - 1) / cols, down = (p[i].m + bm - 1) / bm;
+                        const int64_t full = across * down / kComputeUnits * kComputeUnits / across, left = p[i].m - full * bm;
+                        kept[i] = left > 0 ? full * bm : p[i].m;
+                        mixed += (double)((std::min(full, down) * across + kComputeUnits - 1) / kComputeUnits * blocks) * each;
+                        if (left > 0) {
+                            const int64_t small = (left + 127) / 128 * ((p[i].n + cols / 2 - 1) / (cols / 2));
+                            mixed += small <= kComputeUnits ? blocks * 0.5 : (double)((small + 2 * kComputeUnits - 1) / (2 * kComputeUnits) * blocks) * 0.96;
+                        }
+                    }
+                    mixed += 6;
+                    if (mixed < t) {
+                        t = mixed;
+                        large[0] = kept[0];
+                        large[1] = kept[1];
+                    } else {
+                        large[0] = p[0].m;
+                        large[1] = count > 1 ? p[1].m : 0;
+                    }
+                }
+            }
             t += ends + joins + (joins > 0 ? 4 : 0);
             if (!best.bm || t < least) {
                 least = t;
@@ -457,6 +487,7 @@ static Tiling plan_tiles(bool gated, size_t es, TileArgs* p, int count)
         const int64_t blocks = p[i].k / 128, parts = (blocks + chosen - 1) / chosen, of = (blocks + parts - 1) / parts;
         p[i].parts = (int)((blocks + of - 1) / of);
         p[i].part_k = (int)of * 128;
+        p[i].large = best.bm == 256 && p[i].parts == 1 ? large[i] : p[i].m;
     }
     return best;
 }

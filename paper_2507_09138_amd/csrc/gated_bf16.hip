@@ -2,6 +2,6 @@
 #include "tile_launch.h"
 
 namespace hr {
-template hipError_t launch_tiles<__bf16, false>(const Tiling&, TilePair, int, hipStream_t);
-template hipError_t launch_tiles<__bf16, true>(const Tiling&, TilePair, int, hipStream_t);
+template hipError_t launch_tiles<__bf16, false>(const Tiling&, const TilePair&, int, hipStream_t);
+template hipError_t launch_tiles<__bf16, true>(const Tiling&, const TilePair&, int, hipStream_t);
 }  // namespace hr

@@ -2,6 +2,6 @@
 #include "tile_launch.h"
 
 namespace hr {
-template hipError_t launch_tiles<float, false>(const Tiling&, TilePair, int, hipStream_t);
-template hipError_t launch_tiles<float, true>(const Tiling&, TilePair, int, hipStream_t);
+template hipError_t launch_tiles<float, false>(const Tiling&, const TilePair&, int, hipStream_t);
+template hipError_t launch_tiles<float, true>(const Tiling&, const TilePair&, int, hipStream_t);
 }  // namespace hr

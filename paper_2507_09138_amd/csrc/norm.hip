@@ -465,39 +465,41 @@ __global__ __launch_bounds__(1024) void k_norm_join(const float* parts, int grou
 {
     __shared__ floatx4 sums[128][8];
     __shared__ float some[8][32];
-    const int64_t all = 2 * (int64_t)n, col = (int64_t)blockIdx.x * 32 + threadIdx.x % 8 * 4;
-    const int share = threadIdx.x / 8;
-    floatx4 s = {0, 0, 0, 0};
-    if (col + 4 <= all) {
+    const int64_t all = 2 * (int64_t)n;
+    const int share = threadIdx.x / 8, c = threadIdx.x % 32;
+    for (int64_t first = (int64_t)blockIdx.x * 32; first < all; first += (int64_t)gridDim.x * 32) {
+        const int64_t col = first + threadIdx.x % 8 * 4;
+        floatx4 s = {0, 0, 0, 0};
+        if (col + 4 <= all) {
 #pragma unroll 4
-        for (int g = share; g < groups; g += 128) {
-            floatx4 v;
-            __builtin_memcpy(&v, parts + g * all + col, 16);
-            s += v;
+            for (int g = share; g < groups; g += 128) {
+                floatx4 v;
+                __builtin_memcpy(&v, parts + g * all + col, 16);
+                s += v;
+            }
+        } else {
+            for (int g = share; g < groups; g += 128)
+#pragma unroll
+                for (int e = 0; e < 4; ++e)
+                    if (col + e < all) s[e] += parts[g * all + col + e];
         }
-    } else {
-        for (int g = share; g < groups; g += 128)
+        sums[share][threadIdx.x % 8] = s;
+        __syncthreads();
+        if (threadIdx.x < 256) {
+            float v = 0.0f;
 #pragma unroll
-            for (int e = 0; e < 4; ++e)
-                if (col + e < all) s[e] += parts[g * all + col + e];
-    }
-    sums[share][threadIdx.x % 8] = s;
-    __syncthreads();
-    const int c = threadIdx.x % 32;
-    if (threadIdx.x < 256) {
-        float v = 0.0f;
+            for (int q = 0; q < 16; ++q) v += sums[threadIdx.x / 32 * 16 + q][c / 4][c % 4];
+            some[threadIdx.x / 32][c] = v;
+        }
+        __syncthreads();
+        if (threadIdx.x < 32) {
+            const int64_t j = first + c;
+            float v = 0.0f;
 #pragma unroll
-        for (int q = 0; q < 16; ++q) v += sums[threadIdx.x / 32 * 16 + q][c / 4][c % 4];
-        some[threadIdx.x / 32][c] = v;
-    }
-    __syncthreads();
-    if (threadIdx.x < 32) {
-        const int64_t j = (int64_t)blockIdx.x * 32 + c;
-        float v = 0.0f;
-#pragma unroll
-        for (int q = 0; q < 8; ++q) v += some[q][c];
-        void* to = j < n ? grad_weight : grad_bias;
-        if (j < all && to) ((W*)to)[j < n ? j : j - n] = (W)v;
+            for (int q = 0; q < 8; ++q) v += some[q][c];
+            void* to = j < n ? grad_weight : grad_bias;
+            if (j < all && to) ((W*)to)[j < n ? j : j - n] = (W)v;
+        }
     }
 }
 
@@ -568,7 +570,7 @@ static void launch_norm_backward(const NormArgs& a, void* grad_weight, void* gra
     else if constexpr (sizeof(T) == 4) go(k_norm_backward<T, W, 1024, 4>, 1024, 1);
     if (a.parts || a.rows == 0) {
         if (!grad_weight && !grad_bias) return;
-        hipLaunchKernelGGL(k_norm_join<W>, dim3((unsigned)((2 * (int64_t)a.n + 31) / 32)), dim3(1024), 0, s, a.parts, (int)groups, a.n, grad_weight, grad_bias);
+        hipLaunchKernelGGL(k_norm_join<W>, dim3((unsigned)std::min<int64_t>((2 * (int64_t)a.n + 31) / 32, 1 << 20)), dim3(1024), 0, s, a.parts, (int)groups, a.n, grad_weight, grad_bias);
     }
 }
 

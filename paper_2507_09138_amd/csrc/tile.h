@@ -55,6 +55,7 @@ struct TileArgs {
     const char* b; int64_t ldb;                          // gated: the gate's matrix
     const char* up; int64_t ldup;                        // gated: up's
     int64_t m, n; int k;                                 // n: columns of the result
+    int64_t row0, large;                                 // its first row here; how many rows large tiles take, the others small ones (set by plan_tiles)
     int parts, part_k;                                   // parts of k (part_k bytes each, a multiple of 128), and where there are more than one
     int slots;                                           // workgroups of each part, a multiple of 8
     float* sums;                                         // their sums, [parts][m][n], gated [parts][m][2][n]
@@ -86,10 +87,11 @@ __device__ __forceinline__ void store_some(O* at, int64_t col, int64_t n, const 
     }
 }
 
-// N neighbouring results of row `row`: of both matrices where the block is gated.
+// N neighbouring results of a row: of both matrices where the block is gated.
 template <typename T, bool GATED, int N>
 __device__ __forceinline__ void finish(const TileArgs& p, int64_t row, int64_t col, const float* v, const float* up)
 {
+    row += p.row0;
     if constexpr (GATED) {
         float h[N], slope;
 #pragma unroll
@@ -304,8 +306,8 @@ __global__ __launch_bounds__(256) void k_tiles_join(TilePair pair)
 // ---- host: which tiles (gated.hip), and their launches
 constexpr int kComputeUnits = 256;
 struct Tiling { int bm, bn; };
-// Of count products, 1 or 2; slots are set here.
+// Of count products, 1 or 2.
 template <typename T, bool GATED>
-hipError_t launch_tiles(const Tiling& t, TilePair pair, int count, hipStream_t s);
+hipError_t launch_tiles(const Tiling& t, const TilePair& pair, int count, hipStream_t s);
 
 }  // namespace hr

@@ -7,7 +7,7 @@
 namespace hr {
 
 template <typename T, bool GATED>
-hipError_t launch_tiles(const Tiling& t, TilePair pair, int count, hipStream_t s)
+static hipError_t launch_one_size(const Tiling& t, TilePair pair, int count, hipStream_t s)
 {
     hipError_t e = hipSuccess;
     const int64_t cols = GATED ? t.bn / 2 : t.bn;
@@ -47,6 +47,29 @@ hipError_t launch_tiles(const Tiling& t, TilePair pair, int count, hipStream_t s
         else join(k_tiles_join<T, GATED, 1>, 1);
     }
     return e == hipSuccess ? hipGetLastError() : e;
+}
+
+template <typename T, bool GATED>
+hipError_t launch_tiles(const Tiling& t, const TilePair& pair, int count, hipStream_t s)
+{
+    TilePair first{}, rest{};
+    int firsts = 0, rests = 0;
+    for (int i = 0; i < count; ++i) {
+        const TileArgs& p = pair.p[i];
+        if (p.large > 0) {
+            first.p[firsts] = p;
+            first.p[firsts++].m = p.large;
+        }
+        if (p.large < p.m) {
+            TileArgs& r = rest.p[rests++] = p;
+            r.row0 = p.large;
+            r.a += p.large * p.lda;
+            r.m -= p.large;
+        }
+    }
+    if (firsts)
+        if (hipError_t e = launch_one_size<T, GATED>(t, first, firsts, s)) return e;
+    return rests ? launch_one_size<T, GATED>(Tiling{128, 128}, rest, rests, s) : hipSuccess;
 }
 
 }  // namespace hr

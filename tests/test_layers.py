@@ -542,6 +542,40 @@ def test_a_block_with_its_gradients_and_step_against_autograd():
     _check_adamw(before, {**lists, "exponents": [None] * 5, "masters": [None] * 5}, 1, 1e-3, (0.9, 0.999), 1e-8, [0.01] * 5)
 
 
+def test_offsets_beyond_32_bits():
+    """Rows, columns and numbers that lie more than 2^32 bytes and 2^31 elements from the first equal those of a call that begins with them."""
+    hr = _hr()
+    rows, n = 33000, 65537
+    x = torch.empty(rows, n, dtype=BF16, device="cuda").normal_(generator=_gen(1))
+    w = 1 + 0.1 * _randn(2, n)
+    got = hr.layer_norm(x, w)
+    alone = hr.layer_norm(x[-3:], w)
+    assert torch.equal(got.out[-3:], alone.out) and torch.equal(got.stats[-3:], alone.stats)
+    g = hr.layer_norm_backward(x, w, got.stats, got.out)
+    assert torch.equal(g.x[-3:], hr.layer_norm_backward(x[-3:], w, alone.stats, alone.out).x)
+    del x, got, g, alone
+    f, k = 1 << 19, 4104
+    wg, wu = (torch.empty(f, k, dtype=BF16, device="cuda").normal_(generator=_gen(i)) for i in (3, 4))
+    for m in (1, 20, 70):                                  # (the last 256 columns begin a tile, and a workgroup of every kernel)
+        x = (_randn(m, m, k) / 64).to(BF16)
+        got, tail = hr.gated(x, wg, wu, keep=True), hr.gated(x, wg[-256:], wu[-256:], keep=True)
+        _, gate, up, _, g_tol, u_tol = ref.gated(x, wg[-256:], wu[-256:], "silu")
+        for r in (got.pre[:, :, -256:], tail.pre):
+            ref.close(r[:, 0], gate, g_tol, F32)
+            ref.close(r[:, 1], up, u_tol, F32)
+    del wg, wu, got, tail
+    n = (1 << 31) + 1000
+    p, g = (torch.empty(n, dtype=BF16, device="cuda").normal_(generator=_gen(i)) for i in (5, 6))
+    m, v, e = hr.adamw_state(p, 8)
+    cut = (1 << 31) - 512
+    small = [t[cut:].clone() for t in (p, g, m, v)] + [e[cut // 256:].clone()]
+    hr.adamw([p], [g], [m], [v], 1, 1e-2, exponents=[e])
+    hr.adamw(*[[t] for t in small[:4]], 1, 1e-2, exponents=[small[4]])
+    assert torch.equal(p[cut:], small[0]) and torch.equal(m[cut:], small[2]) and torch.equal(v[cut:], small[3]) and torch.equal(e[cut // 256:], small[4])
+    fm, fv = hr.adamw_moments(m, v, e)
+    assert all(torch.equal(a[cut:], b) for a, b in zip((fm, fv), hr.adamw_moments(*small[2:])))
+
+
 def test_keyword_calls_give_the_same():
     hr = _hr()
     x, wg, wu, dh = _gated_inputs(5, 40, 24, BF16)
