@@ -398,90 +398,103 @@ __global__ __launch_bounds__(256) void k_gated_any(const T* x, int64_t ldx, cons
 
 // ---- which kernel
 
+// Blocks of k that a compute unit, or one of its halves, multiplies one after the other until all workgroups are done: first those of `long_` blocks, then
+// the shorter ones, each on the first of `places` that is free.
+static double rounds(int64_t places, int64_t longs, int64_t long_, int64_t shorts, int64_t short_)
+{
+    const int64_t later = longs % places;                // places that take one of the long ones more
+    int64_t early_free = longs / places * long_, late_free = early_free + long_, last = later ? late_free : early_free;
+    while (shorts > 0) {
+        const bool early = later == 0 || early_free <= late_free;
+        shorts -= early ? places - later : later;
+        int64_t& free = early ? early_free : late_free;
+        free += short_;
+        last = std::max(last, free);
+    }
+    return (double)last;
+}
+
 // Tiles (rows x columns of both matrices): 256 x 256, 128 x 128 or, for up to 64 rows of a gated block, 64 x 256, in parts of k or not: what takes
-// least by this count of microseconds.  Workgroups come in rounds: one of 256 x 256 on a compute unit at a time, two of the smaller ones; those of
-// two products in one launch, of parts about as long as each other, in common rounds or one product's after the other's.  A block of 128 bytes of k
-// takes a large tile 1.6 (16 bits), two small ones 0.96, and one that has a compute unit for itself 0.5; in float32 3.8 and 2.0 (large tiles are no
-// faster there).  Start and end take 6 to 8, parts are written and read at 4 MB/us, by another launch.
+// least by this count of microseconds.  A compute unit takes one workgroup with a large tile at a time, two with small ones, or one with four buffers,
+// which costs more where there are many, and less where they do not fill the last round.  A block of 128 bytes of k takes a large tile 1.6 (16 bits), two
+// small ones 0.96, one alone 0.5; in float32 3.8 and 2.0 (large tiles are no faster there).  Start and end take 6 to 8, for workgroups that come
+// alone 4 more a round; parts are written and read at 4 MB/us, by another launch.  Parts of two products in one launch are about as long as each other.
 // Measured, here (the other choices): 4096 x 4096 x 4096 bfloat16 102 .. 112 (128 x 128 118), 2048 x 4096 x 4096 61 (256 x 256 86, two parts 84),
-// 512 x 512 x 4096 in eight parts 15.4 (one 32.6), float32 2048 x 768 x 4096 in five 113 (one 260, two 148), that and 4096 x 768 x 2048 in eight and
-// four parts 219 (one after the other 228; four and two 209, six and one, unlike lengths, 325).
+// 512 x 512 x 4096 in eight parts 15.4 (one 32.6), float32 2048 x 768 x 4096 in five 113 (one 260, two 148), that and 4096 x 768 x 2048 in one launch
+// 219 (one after the other 228; in six parts and one, unlike lengths, 325).
 // Where large tiles leave much of a last round empty, the rows of that round are left to small ones, in a second launch: 8192 x 4096 x 21504 and
 // 21504 x 4096 x 8192, 2 and 5.25 rounds, 2283 -> 2190.
 // m, n and k of the products are there; parts, part_k and large are set.
 static Tiling plan_tiles(bool gated, size_t es, TileArgs* p, int count)
 {
+    const double pair = es == 4 ? 3.8 : 0.96, one = es == 4 ? 2.0 : 0.5;             // of small tiles
     Tiling best{};
     double least = 0;
     int64_t longest_k = 0, chosen = 0, large[2] = {p[0].m, count > 1 ? p[1].m : 0};
     for (int i = 0; i < count; ++i) longest_k = std::max<int64_t>(longest_k, p[i].k / 128);
-    auto consider = [&](int bm, int bn, double each, double alone, double ends) {
-        const int64_t cols = bn / (gated ? 2 : 1), at_once = bm == 256 ? kComputeUnits : 2 * kComputeUnits;
+    auto consider = [&](int bm, int bn) {
+        const int64_t cols = bn / (gated ? 2 : 1);
         int64_t last = 0;
         for (int64_t n = 1; n <= 64; ++n) {
             const int64_t length = (longest_k + n - 1) / n;                  // blocks of the longest part
             if (n > 1 && (length < 2 || length == last)) continue;
             last = length;
-            int64_t all = 0, most = 0;
-            double work = 0, joins = 0, in_turn = 0;
+            int64_t groups[2] = {0, 0}, of[2] = {0, 0};
+            double work = 0, joins = 0;
             bool fits = true;
             for (int i = 0; i < count; ++i) {
-                const int64_t blocks = p[i].k / 128, parts = (blocks + length - 1) / length, of = (blocks + parts - 1) / parts;
-                const int64_t groups = (p[i].m + bm - 1) / bm * ((p[i].n + cols - 1) / cols) * parts;
+                const int64_t blocks = p[i].k / 128, parts = (blocks + length - 1) / length;
                 const double sums = (double)parts * p[i].m * p[i].n * (gated ? 8 : 4);
-                all += groups;
-                most = std::max(most, of);
-                work += (double)groups * of;
-                in_turn += groups <= kComputeUnits ? of * alone : (double)((groups + at_once - 1) / at_once * of) * each;
+                of[i] = (blocks + parts - 1) / parts;
+                groups[i] = (p[i].m + bm - 1) / bm * ((p[i].n + cols - 1) / cols) * parts;
+                work += (double)groups[i] * of[i];
                 if (parts > 1) {
                     joins += 2 * sums / 4e6;
-                    fits &= groups <= 8 * kComputeUnits && sums <= 0x1p28;
+                    fits &= groups[i] <= 8 * kComputeUnits && sums <= 0x1p28;
                 }
             }
             if (!fits) break;
-            double t = all <= kComputeUnits ? most * alone : std::min(in_turn, (double)((all + at_once - 1) / at_once * most) * each);
-            // (16 bits: an unfilled last round runs at a higher clock)
-            if (es < 4 && all > kComputeUnits) t = (t + work / at_once * each) / 2;
-            if (bm == 256) {
-                if (all <= kComputeUnits) t = std::max(t, (most * each + work / kComputeUnits * each) / 2);
-                // (rows that fill whole rounds, the others in small tiles)
-                if (n == 1) {
-                    double mixed = 0;
-                    int64_t kept[2];
-                    for (int i = 0; i < count; ++i) {
-                        const int64_t blocks = p[i].k / 128, across = (p[i].n + cols - 1) / cols, down = (p[i].m + bm - 1) / bm;
-                        const int64_t full = across * down / kComputeUnits * kComputeUnits / across, left = p[i].m - full * bm;
-                        kept[i] = left > 0 ? full * bm : p[i].m;
-                        mixed += (double)((std::min(full, down) * across + kComputeUnits - 1) / kComputeUnits * blocks) * each;
-                        if (left > 0) {
-                            const int64_t small = (left + 127) / 128 * ((p[i].n + cols / 2 - 1) / (cols / 2));
-                            mixed += small <= kComputeUnits ? blocks * 0.5 : (double)((small + 2 * kComputeUnits - 1) / (2 * kComputeUnits) * blocks) * 0.96;
-                        }
-                    }
-                    mixed += 6;
-                    if (mixed < t) {
-                        t = mixed;
-                        large[0] = kept[0];
-                        large[1] = kept[1];
-                    } else {
-                        large[0] = p[0].m;
-                        large[1] = count > 1 ? p[1].m : 0;
-                    }
+            if (joins > 0) joins += 4;
+            const int l = of[1] > of[0];                 // the product of the longer parts
+            const int64_t all = groups[0] + groups[1];
+            auto try_one = [&](bool alone, double t) {
+                if (!best.bm || t < least) {
+                    least = t;
+                    best = {bm, bn, alone};
+                    chosen = length;
                 }
+            };
+            if (bm < 256) {
+                // (16 bits: an unfilled last round of pairs runs at a higher clock)
+                double t = rounds(2 * kComputeUnits, groups[l], of[l], groups[1 - l], of[1 - l]) * pair;
+                if (es < 4) t = (t + work / (2 * kComputeUnits) * pair) / 2;
+                if (all > kComputeUnits) try_one(false, t + 6 + joins);
+                try_one(true, rounds(kComputeUnits, groups[l], of[l], groups[1 - l], of[1 - l]) * one + 2 + 4 * (double)((all + kComputeUnits - 1) / kComputeUnits) + joins);
+                continue;
             }
-            t += ends + joins + (joins > 0 ? 4 : 0);
-            if (!best.bm || t < least) {
-                least = t;
-                best = {bm, bn};
-                chosen = length;
+            double t = rounds(kComputeUnits, groups[l], of[l], groups[1 - l], of[1 - l]) * 1.6;
+            t = std::max(std::max(of[0], of[1]) * 1.2, (t + work / kComputeUnits * 1.6) / 2) + 8 + joins;
+            if (n == 1) {                                // rows that fill whole rounds, the others in small tiles
+                double mixed = 14;
+                int64_t kept[2] = {0, 0};
+                for (int i = 0; i < count; ++i) {
+                    const int64_t across = (p[i].n + cols - 1) / cols, down = (p[i].m + bm - 1) / bm, full = across * down / kComputeUnits * kComputeUnits / across, left = p[i].m - full * bm;
+                    kept[i] = left > 0 ? full * bm : p[i].m;
+                    mixed += (double)((std::min(full, down) * across + kComputeUnits - 1) / kComputeUnits * of[i]) * 1.6;
+                    if (left > 0) mixed += rounds(2 * kComputeUnits, (left + 127) / 128 * ((p[i].n + cols / 2 - 1) / (cols / 2)), of[i], 0, 0) * pair;
+                }
+                const bool mix = mixed < t;
+                for (int i = 0; i < count; ++i) large[i] = mix ? kept[i] : p[i].m;
+                t = std::min(t, mixed);
             }
+            try_one(false, t);
         }
     };
     if (gated && p[0].m <= 64) {
-        consider(64, 256, es == 4 ? 3.8 : 0.96, es == 4 ? 2.0 : 0.5, 6);
+        consider(64, 256);
     } else {
-        consider(128, 128, es == 4 ? 3.8 : 0.96, es == 4 ? 2.0 : 0.5, 6);
-        if (es < 4) consider(256, 256, 1.6, 1.2, 8);
+        consider(128, 128);
+        if (es < 4) consider(256, 256);
     }
     for (int i = 0; i < count; ++i) {
         const int64_t blocks = p[i].k / 128, parts = (blocks + chosen - 1) / chosen, of = (blocks + parts - 1) / parts;

@@ -57,7 +57,7 @@ struct TileArgs {
     int64_t m, n; int k;                                 // n: columns of the result
     int64_t row0, large;                                 // its first row here; how many rows large tiles take, the others small ones (set by plan_tiles)
     int parts, part_k;                                   // parts of k (part_k bytes each, a multiple of 128), and where there are more than one
-    int slots;                                           // workgroups of each part, a multiple of 8
+    int slots;                                           // workgroups, a multiple of 8
     float* sums;                                         // their sums, [parts][m][n], gated [parts][m][2][n]
     void* out; int64_t ldo;                              // elements apart
     void* out2; int64_t ldo2, split;                     // rows from `split` on go to out2
@@ -117,21 +117,20 @@ __global__ __launch_bounds__(BM / WM * (BN / 64) * 64) void k_tiles(TilePair pai
 {
     const bool second = blockIdx.x >= pair.first;
     const TileArgs& p = pair.p[second];
-    const int wg = (int)(blockIdx.x - (second ? pair.first : 0)), part = wg / p.slots, slot = wg - part * p.slots;
+    const int slot = (int)(blockIdx.x - (second ? pair.first : 0));
     constexpr int WN = 64, WAVES = BM / WM * (BN / WN), TM = WM / 16, TN = 4, BK = 128, UNITS = (BM + BN) / 8 / WAVES, BUF = (BM + BN) * BK;
     constexpr int COLS = GATED ? BN / 2 : BN;            // of the result
     static_assert(BM / 8 % WAVES == 0 && BN / 8 % WAVES == 0 && NB >= 2 && NB <= 4);
     extern __shared__ __align__(1024) char lds[];
     const int lane = lane_id(), wave = __builtin_amdgcn_readfirstlane(threadIdx.x / 64);
     const int wm = wave / (BN / WN) * WM, wn = wave % (BN / WN) * WN;
-    const int k_begin = part * p.part_k, k_end = min(p.k, k_begin + p.part_k), blocks = (k_end - k_begin) / BK;
     const int piece = ((lane & 7) ^ (lane >> 3)) * 16;
     const uint32_t lds0 = lds_addr(lds);
 
-    // Tiles that run at the same time on an XCD share its L2: each has a stretch of the tiles, and takes them in blocks of four rows of tiles.
+    // Tiles that run at the same time on an XCD share its L2: each has a stretch of the parts' tiles, and takes them in blocks of four rows of tiles.
     const int m = (int)p.m, n = (int)p.n, tiles_m = (m + BM - 1) / BM, tiles_n = (n + COLS - 1) / COLS, tiles = tiles_m * tiles_n;
-    const int stretch = (tiles + 7) / 8, tile0 = slot % 8 * stretch, end = min(stretch, tiles - tile0);
-    int tile = slot / 8, m0 = 0, n0 = 0;
+    const int stretch = (tiles * p.parts + 7) / 8, item0 = slot % 8 * stretch, end = min(stretch, tiles * p.parts - item0);
+    int item = slot / 8, part = 0, k_begin = 0, blocks = 0, m0 = 0, n0 = 0;
     uint32_t off[UNITS];                                 // (rows of a tile lie within 2^31 bytes: the host sees to it)
     const char *ga = p.a, *gb = p.b, *gu = p.up;
     // What lies in row r of b's part of a buffer.  Rows 0 .. 15 and 16 .. 31 of 32 are four of each eight columns, so that a lane has eight neighbouring
@@ -142,7 +141,10 @@ __global__ __launch_bounds__(BM / WM * (BN / 64) * 64) void k_tiles(TilePair pai
     };
     auto is_up = [&](int i) __attribute__((always_inline)) { return GATED && (((i * WAVES + wave) * 8 - BM) & 32) != 0; };       // (of a load: the same for its 8 rows)
     auto aim = [&](int t) __attribute__((always_inline)) {
-        t += tile0;
+        part = (t + item0) / tiles;
+        k_begin = part * p.part_k;
+        blocks = (min(p.k, k_begin + p.part_k) - k_begin) / BK;
+        t = t + item0 - part * tiles;
         const int g = t / (4 * tiles_n), rest = t - g * 4 * tiles_n, high = min(4, tiles_m - g * 4);
         m0 = (g * 4 + rest % high) * BM;
         n0 = rest / high * COLS;
@@ -194,8 +196,8 @@ __global__ __launch_bounds__(BM / WM * (BN / 64) * 64) void k_tiles(TilePair pai
         asm volatile("" ::: "memory");
     };
 
-    if (tile >= end) return;
-    aim(tile);
+    if (item >= end) return;
+    aim(item);
 #pragma unroll
     for (int b = 0; b < NB; ++b)
         if (b < blocks) request(b);
@@ -216,11 +218,11 @@ __global__ __launch_bounds__(BM / WM * (BN / 64) * 64) void k_tiles(TilePair pai
             read_b(b0, b + 1, 0);                        // (behind the last block: whatever the buffer holds, not multiplied)
             step(b1, place(b + 1, 0));
         }
-        const int mt = m0, nt = n0;
-        tile += p.slots / 8;
-        const bool more = NB == 2 && tile < end;         // (with more buffers the host launches a workgroup for every tile)
+        const int mt = m0, nt = n0, of = part;
+        item += p.slots / 8;
+        const bool more = NB == 2 && item < end;         // (with more buffers the host launches a workgroup for every tile)
         if (more) {
-            aim(tile);
+            aim(item);
             request(0);                                  // (both buffers are free since the last meeting)
             if (blocks > 1) request(1);
         }
@@ -238,7 +240,7 @@ __global__ __launch_bounds__(BM / WM * (BN / 64) * 64) void k_tiles(TilePair pai
                     if (GATED) up[e] = acc[i][(j + 2 + e / 4) % TN][e % 4];
                 }
                 if (p.parts > 1) {
-                    float* at = p.sums + ((int64_t)part * m + row) * (GATED ? 2 : 1) * n;
+                    float* at = p.sums + ((int64_t)of * m + row) * (GATED ? 2 : 1) * n;
                     store_some<8>(at, col, n, v);
                     if (GATED) store_some<8>(at + n, col, n, up);
                 } else {
@@ -305,7 +307,10 @@ __global__ __launch_bounds__(256) void k_tiles_join(TilePair pair)
 
 // ---- host: which tiles (gated.hip), and their launches
 constexpr int kComputeUnits = 256;
-struct Tiling { int bm, bn; };
+struct Tiling {
+    int bm, bn;
+    bool alone;                                          // one workgroup on a compute unit at a time
+};
 // Of count products, 1 or 2.
 template <typename T, bool GATED>
 hipError_t launch_tiles(const Tiling& t, const TilePair& pair, int count, hipStream_t s);

@@ -1,6 +1,7 @@
 // Launches of k_tiles for one type of elements: the body of gated_f16.hip, gated_bf16.hip and gated_f32.hip.
 #pragma once
 #include <algorithm>
+#include <utility>
 
 #include "tile.h"
 
@@ -12,15 +13,15 @@ static hipError_t launch_one_size(const Tiling& t, TilePair pair, int count, hip
     hipError_t e = hipSuccess;
     const int64_t cols = GATED ? t.bn / 2 : t.bn;
     auto tiles = [&](const TileArgs& p) { return (p.m + t.bm - 1) / t.bm * ((p.n + cols - 1) / cols); };
-    int64_t all = 0;
-    for (int i = 0; i < count; ++i) all += tiles(pair.p[i]) * pair.p[i].parts;
-    const bool deep = t.bm < 256 && all <= kComputeUnits;
+    if (count > 1 && pair.p[1].part_k > pair.p[0].part_k) std::swap(pair.p[0], pair.p[1]);               // (long parts first)
     auto go = [&](auto kernel, int buffers) {
         const size_t lds = (size_t)(t.bm + t.bn) * 128 * buffers;
         unsigned groups[2] = {0, 0};
         for (int i = 0; i < count; ++i) {
-            pair.p[i].slots = (int)std::min((tiles(pair.p[i]) + 7) / 8, (int64_t)kComputeUnits / 8 * (lds <= 80 * 1024 ? 2 : 1)) * 8;
-            groups[i] = (unsigned)(pair.p[i].slots * pair.p[i].parts);
+            // (where there are more than two buffers every part of a tile has a workgroup of its own)
+            const int64_t of_eight = (tiles(pair.p[i]) * pair.p[i].parts + 7) / 8;
+            pair.p[i].slots = (int)(buffers > 2 ? of_eight : std::min(of_eight, (int64_t)kComputeUnits / 8 * (lds <= 80 * 1024 ? 2 : 1))) * 8;
+            groups[i] = (unsigned)pair.p[i].slots;
         }
         pair.first = groups[0];
         if (lds > 64 * 1024) e = hipFuncSetAttribute((const void*)kernel, hipFuncAttributeMaxDynamicSharedMemorySize, (int)lds);
@@ -29,9 +30,9 @@ static hipError_t launch_one_size(const Tiling& t, TilePair pair, int count, hip
     if (t.bm == 256) {
         if constexpr (sizeof(T) == 2) go(k_tiles<T, GATED, 256, 256, 128, 2>, 2);
     } else if (t.bm == 128) {
-        deep ? go(k_tiles<T, GATED, 128, 128, 32, 4>, 4) : go(k_tiles<T, GATED, 128, 128, 32, 2>, 2);
+        t.alone ? go(k_tiles<T, GATED, 128, 128, 32, 4>, 4) : go(k_tiles<T, GATED, 128, 128, 32, 2>, 2);
     } else if constexpr (GATED) {
-        deep ? go(k_tiles<T, GATED, 64, 256, 32, 3>, 3) : go(k_tiles<T, GATED, 64, 256, 32, 2>, 2);
+        t.alone ? go(k_tiles<T, GATED, 64, 256, 32, 3>, 3) : go(k_tiles<T, GATED, 64, 256, 32, 2>, 2);
     }
     const int most = std::max(pair.p[0].parts, count > 1 ? pair.p[1].parts : 1);
     if (e == hipSuccess && most > 1) {
@@ -69,7 +70,7 @@ hipError_t launch_tiles(const Tiling& t, const TilePair& pair, int count, hipStr
     }
     if (firsts)
         if (hipError_t e = launch_one_size<T, GATED>(t, first, firsts, s)) return e;
-    return rests ? launch_one_size<T, GATED>(Tiling{128, 128}, rest, rests, s) : hipSuccess;
+    return rests ? launch_one_size<T, GATED>(Tiling{128, 128, t.alone}, rest, rests, s) : hipSuccess;
 }
 
 }  // namespace hr
