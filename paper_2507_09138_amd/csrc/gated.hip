@@ -398,8 +398,8 @@ __global__ __launch_bounds__(256) void k_gated_any(const T* x, int64_t ldx, cons
 
 // ---- which kernel
 
-// Blocks of k that a compute unit, or one of its halves, multiplies one after the other until all workgroups are done: first those of `long_` blocks, then
-// the shorter ones, each on the first of `places` that is free.
+// Blocks of k that a place for a workgroup multiplies one after the other until all workgroups are done: first those of `long_` blocks, then the
+// shorter ones, each on the first of `places` that is free.
 static double rounds(int64_t places, int64_t longs, int64_t long_, int64_t shorts, int64_t short_)
 {
     const int64_t later = longs % places;                // places that take one of the long ones more
@@ -415,10 +415,10 @@ static double rounds(int64_t places, int64_t longs, int64_t long_, int64_t short
 }
 
 // Tiles (rows x columns of both matrices): 256 x 256, 128 x 128 or, for up to 64 rows of a gated block, 64 x 256, in parts of k or not: what takes
-// least by this count of microseconds.  A compute unit takes one workgroup with a large tile at a time, two with small ones, or one with four buffers,
-// which costs more where there are many, and less where they do not fill the last round.  A block of 128 bytes of k takes a large tile 1.6 (16 bits), two
-// small ones 0.96, one alone 0.5; in float32 3.8 and 2.0 (large tiles are no faster there).  Start and end take 6 to 8, for workgroups that come
-// alone 4 more a round; parts are written and read at 4 MB/us, by another launch.  Parts of two products in one launch are about as long as each other.
+// least by this count of microseconds.  A compute unit takes one workgroup with a large tile at a time, two with small ones; a block of 128 bytes of k
+// takes a large tile 1.6 (16 bits), two small ones 0.96, and one alone, where up to 256 are left or there are no more, 0.5; in float32 3.8 and 2.0
+// (large tiles are no faster there).  Start and end take 6 to 8, parts are written and read at 4 MB/us, by another launch.  Parts of two products in one
+// launch are about as long as each other.
 // Measured, here (the other choices): 4096 x 4096 x 4096 bfloat16 102 .. 112 (128 x 128 118), 2048 x 4096 x 4096 61 (256 x 256 86, two parts 84),
 // 512 x 512 x 4096 in eight parts 15.4 (one 32.6), float32 2048 x 768 x 4096 in five 113 (one 260, two 148), that and 4096 x 768 x 2048 in one launch
 // 219 (one after the other 228; in six parts and one, unlike lengths, 325).
@@ -457,19 +457,18 @@ static Tiling plan_tiles(bool gated, size_t es, TileArgs* p, int count)
             if (joins > 0) joins += 4;
             const int l = of[1] > of[0];                 // the product of the longer parts
             const int64_t all = groups[0] + groups[1];
-            auto try_one = [&](bool alone, double t) {
+            auto try_one = [&](double t) {
                 if (!best.bm || t < least) {
                     least = t;
-                    best = {bm, bn, alone};
+                    best = {bm, bn};
                     chosen = length;
                 }
             };
             if (bm < 256) {
-                // (16 bits: an unfilled last round of pairs runs at a higher clock)
-                double t = rounds(2 * kComputeUnits, groups[l], of[l], groups[1 - l], of[1 - l]) * pair;
-                if (es < 4) t = (t + work / (2 * kComputeUnits) * pair) / 2;
-                if (all > kComputeUnits) try_one(false, t + 6 + joins);
-                try_one(true, rounds(kComputeUnits, groups[l], of[l], groups[1 - l], of[1 - l]) * one + 2 + 4 * (double)((all + kComputeUnits - 1) / kComputeUnits) + joins);
+                const int64_t at_once = 2 * kComputeUnits, left = all % at_once;
+                if (all <= kComputeUnits) try_one(std::max(of[0], of[1]) * one + 6 + joins);
+                else if (count > 1 && of[0] != of[1]) try_one(rounds(at_once, groups[l], of[l], groups[1 - l], of[1 - l]) * pair + 6 + joins);
+                else try_one((double)(all / at_once * of[0]) * pair + (left == 0 ? 0 : left <= kComputeUnits ? of[0] * one : of[0] * pair) + 6 + joins);
                 continue;
             }
             double t = rounds(kComputeUnits, groups[l], of[l], groups[1 - l], of[1 - l]) * 1.6;
@@ -487,7 +486,7 @@ static Tiling plan_tiles(bool gated, size_t es, TileArgs* p, int count)
                 for (int i = 0; i < count; ++i) large[i] = mix ? kept[i] : p[i].m;
                 t = std::min(t, mixed);
             }
-            try_one(false, t);
+            try_one(t);
         }
     };
     if (gated && p[0].m <= 64) {

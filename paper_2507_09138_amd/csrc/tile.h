@@ -307,10 +307,7 @@ __global__ __launch_bounds__(256) void k_tiles_join(TilePair pair)
 
 // ---- host: which tiles (gated.hip), and their launches
 constexpr int kComputeUnits = 256;
-struct Tiling {
-    int bm, bn;
-    bool alone;                                          // one workgroup on a compute unit at a time
-};
+struct Tiling { int bm, bn; };
 // Of count products, 1 or 2.
 template <typename T, bool GATED>
 hipError_t launch_tiles(const Tiling& t, const TilePair& pair, int count, hipStream_t s);

@@ -13,6 +13,9 @@ static hipError_t launch_one_size(const Tiling& t, TilePair pair, int count, hip
     hipError_t e = hipSuccess;
     const int64_t cols = GATED ? t.bn / 2 : t.bn;
     auto tiles = [&](const TileArgs& p) { return (p.m + t.bm - 1) / t.bm * ((p.n + cols - 1) / cols); };
+    int64_t all = 0;
+    for (int i = 0; i < count; ++i) all += tiles(pair.p[i]) * pair.p[i].parts;
+    const bool deep = all <= kComputeUnits;              // (nothing but requests of its own hides the time that a workgroup's loads take)
     if (count > 1 && pair.p[1].part_k > pair.p[0].part_k) std::swap(pair.p[0], pair.p[1]);               // (long parts first)
     auto go = [&](auto kernel, int buffers) {
         const size_t lds = (size_t)(t.bm + t.bn) * 128 * buffers;
@@ -30,9 +33,9 @@ static hipError_t launch_one_size(const Tiling& t, TilePair pair, int count, hip
     if (t.bm == 256) {
         if constexpr (sizeof(T) == 2) go(k_tiles<T, GATED, 256, 256, 128, 2>, 2);
     } else if (t.bm == 128) {
-        t.alone ? go(k_tiles<T, GATED, 128, 128, 32, 4>, 4) : go(k_tiles<T, GATED, 128, 128, 32, 2>, 2);
+        deep ? go(k_tiles<T, GATED, 128, 128, 32, 4>, 4) : go(k_tiles<T, GATED, 128, 128, 32, 2>, 2);
     } else if constexpr (GATED) {
-        t.alone ? go(k_tiles<T, GATED, 64, 256, 32, 3>, 3) : go(k_tiles<T, GATED, 64, 256, 32, 2>, 2);
+        deep ? go(k_tiles<T, GATED, 64, 256, 32, 3>, 3) : go(k_tiles<T, GATED, 64, 256, 32, 2>, 2);
     }
     const int most = std::max(pair.p[0].parts, count > 1 ? pair.p[1].parts : 1);
     if (e == hipSuccess && most > 1) {
@@ -70,7 +73,7 @@ hipError_t launch_tiles(const Tiling& t, const TilePair& pair, int count, hipStr
     }
     if (firsts)
         if (hipError_t e = launch_one_size<T, GATED>(t, first, firsts, s)) return e;
-    return rests ? launch_one_size<T, GATED>(Tiling{128, 128, t.alone}, rest, rests, s) : hipSuccess;
+    return rests ? launch_one_size<T, GATED>(Tiling{128, 128}, rest, rests, s) : hipSuccess;
 }
 
 }  // namespace hr
