@@ -140,6 +140,7 @@ __device__ __forceinline__ void fold_two(float& a, float& b, Folds& s, int& turn
         constexpr int WAVES = LANES / 64;
         float(*part)[2] = s.part[turn];
         turn ^= 1;
+        const int first = threadIdx.x / LANES * WAVES;   // (of this row)
         if (lane_id() == 0) {
             part[threadIdx.x / 64][0] = a;
             part[threadIdx.x / 64][1] = b;
@@ -147,7 +148,7 @@ __device__ __forceinline__ void fold_two(float& a, float& b, Folds& s, int& turn
         __syncthreads();
         a = b = 0.0f;
 #pragma unroll
-        for (int w = 0; w < WAVES; ++w) a += part[w][0], b += part[w][1];
+        for (int w = 0; w < WAVES; ++w) a += part[first + w][0], b += part[first + w][1];
     }
 }
 
@@ -276,10 +277,10 @@ __global__ __launch_bounds__(1024) void k_norm_long(NormArgs a)
 }
 
 // ---- gradients of rows that LANES lanes hold; sums over the workgroup's rows stay in registers until its last
-template <typename T, typename W, int LANES, int CH, bool TINY = false>
-__global__ __launch_bounds__(LANES > 256 ? LANES : 256) void k_norm_backward(NormArgs a)
+template <typename T, typename W, int LANES, int CH, bool TINY = false, int THREADS = (LANES > 256 ? LANES : 256)>
+__global__ __launch_bounds__(THREADS, THREADS == 512 && LANES == 256 ? 4 : 1) void k_norm_backward(NormArgs a)
 {
-    constexpr int E = kE<T>, THREADS = LANES > 256 ? LANES : 256, ROWS = THREADS / LANES;
+    constexpr int E = kE<T>, ROWS = THREADS / LANES;
     __shared__ Folds folds;
     __shared__ float sums[ROWS > 1 ? ROWS * LANES * CH * E : 1];
     int turn = 0;
@@ -564,7 +565,7 @@ static void launch_norm_backward(const NormArgs& a, void* grad_weight, void* gra
     else if (chunks <= 64) go(k_norm_backward<T, W, 64, 1>, 256, 4);
     else if (chunks <= 128) go(k_norm_backward<T, W, 64, 2>, 256, 4);
     else if (chunks <= 256) go(k_norm_backward<T, W, 256, 1>, 256, 1);
-    else if (chunks <= 512) go(k_norm_backward<T, W, 256, 2>, 256, 1);
+    else if (chunks <= 512) go(k_norm_backward<T, W, 256, 2, false, 512>, 512, 2);
     else if (chunks <= 1024) go(k_norm_backward<T, W, 512, 2>, 512, 1);
     else if (chunks <= 2048) go(k_norm_backward<T, W, 1024, 2>, 1024, 1);
     else if constexpr (sizeof(T) == 4) go(k_norm_backward<T, W, 1024, 4>, 1024, 1);
