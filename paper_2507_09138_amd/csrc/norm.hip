@@ -170,14 +170,26 @@ __global__ __launch_bounds__(LANES > 256 ? LANES : 256) void k_norm(NormArgs a)
     };
     if constexpr (KEEP)
         for (int i = 0; i < CH; ++i) weights(piece_of<T>(Chunk<T>{}, i * LANES + t, n), w[i], b[i]);
+    // (AHEAD: large workgroups are few on a compute unit, and ask for their next row before they fold the last one's sums)
+    constexpr bool AHEAD = LANES >= 512 && CH <= 4;
+    auto load = [&](int64_t r0, Chunk<T>* x) __attribute__((always_inline)) {
+        const T* row = (const T*)a.x + min(r0 + threadIdx.x / LANES, a.rows - 1) * a.ldx;
+#pragma unroll
+        for (int i = 0; i < CH; ++i) x[i] = load_piece<TINY>(row, i * LANES + t, n).v;
+    };
+    Chunk<T> x[CH], next[CH];
+    if constexpr (AHEAD) load((int64_t)blockIdx.x * ROWS, next);
     for (int64_t r0 = (int64_t)blockIdx.x * ROWS; r0 < a.rows; r0 += (int64_t)gridDim.x * ROWS) {
         const int64_t r = r0 + threadIdx.x / LANES;
         const bool in = r < a.rows;
-        const T* row = (const T*)a.x + (in ? r : a.rows - 1) * a.ldx;
-        Chunk<T> x[CH];
         int at = t;
+        if constexpr (AHEAD) {
 #pragma unroll
-        for (int i = 0; i < CH; ++i) x[i] = load_piece<TINY>(row, i * LANES + at, n).v;
+            for (int i = 0; i < CH; ++i) x[i] = next[i];
+            load(r0 + (int64_t)gridDim.x * ROWS, next);
+        } else {
+            load(r0, x);
+        }
         float s0 = 0.0f, s1 = 0.0f;
 #pragma unroll
         for (int i = 0; i < CH; ++i) {
@@ -278,7 +290,7 @@ __global__ __launch_bounds__(1024) void k_norm_long(NormArgs a)
 
 // ---- gradients of rows that LANES lanes hold; sums over the workgroup's rows stay in registers until its last
 template <typename T, typename W, int LANES, int CH, bool TINY = false, int THREADS = (LANES > 256 ? LANES : 256)>
-__global__ __launch_bounds__(THREADS, THREADS == 512 && LANES == 256 ? 4 : 1) void k_norm_backward(NormArgs a)
+__global__ __launch_bounds__(THREADS, THREADS == 512 ? 4 : 1) void k_norm_backward(NormArgs a)
 {
     constexpr int E = kE<T>, ROWS = THREADS / LANES;
     __shared__ Folds folds;
@@ -539,6 +551,7 @@ static void launch_norm(const NormArgs& a, hipStream_t s)
     else if (chunks <= 256) go(k_norm<T, W, 256, 1>, 256, 1);
     else if (chunks <= 512) go(k_norm<T, W, 256, 2>, 256, 1);
     else if (chunks <= 1024) go(k_norm<T, W, 256, 4>, 256, 1);
+    else if (chunks <= 2048) go(k_norm<T, W, 512, 4>, 512, 1);
     else if (chunks <= 4096) go(k_norm<T, W, 1024, 4>, 1024, 1);
     else if (chunks <= 8192) go(k_norm<T, W, 1024, 8>, 1024, 1);
     else if (chunks <= 16384) go(k_norm<T, W, 1024, 16>, 1024, 1);
@@ -551,7 +564,7 @@ static void launch_norm_backward(const NormArgs& a, void* grad_weight, void* gra
     const int64_t chunks = (a.n + kE<T> - 1) / kE<T>, most = groups_for(a.rows, a.n);
     int64_t groups = 0;
     auto go = [&](auto kernel, int threads, int rows) {
-        groups = std::min((a.rows + rows - 1) / rows, most);
+        groups = std::min((a.rows + rows - 1) / rows, threads == 1024 && rows == 1 ? std::min<int64_t>(most, 256) : most);
         hipLaunchKernelGGL(kernel, dim3((unsigned)groups), dim3(threads), 0, s, a);
     };
     if (a.rows == 0) {
@@ -562,9 +575,9 @@ static void launch_norm_backward(const NormArgs& a, void* grad_weight, void* gra
     } else if (a.n < kE<T>) go(k_norm_backward<T, W, 16, 1, true>, 256, 16);
     else if (chunks <= 16) go(k_norm_backward<T, W, 16, 1>, 256, 16);
     else if (chunks <= 32) go(k_norm_backward<T, W, 16, 2>, 256, 16);
-    else if (chunks <= 64) go(k_norm_backward<T, W, 64, 1>, 256, 4);
-    else if (chunks <= 128) go(k_norm_backward<T, W, 64, 2>, 256, 4);
-    else if (chunks <= 256) go(k_norm_backward<T, W, 256, 1>, 256, 1);
+    else if (chunks <= 64) go(k_norm_backward<T, W, 64, 1, false, 512>, 512, 8);
+    else if (chunks <= 128) go(k_norm_backward<T, W, 64, 2, false, 512>, 512, 8);
+    else if (chunks <= 256) go(k_norm_backward<T, W, 256, 1, false, 512>, 512, 2);
     else if (chunks <= 512) go(k_norm_backward<T, W, 256, 2, false, 512>, 512, 2);
     else if (chunks <= 1024) go(k_norm_backward<T, W, 512, 2>, 512, 1);
     else if (chunks <= 2048) go(k_norm_backward<T, W, 1024, 2>, 1024, 1);
