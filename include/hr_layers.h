@@ -86,13 +86,13 @@ typedef struct {
     void* m;                 /* first moment: float32, or uint8 codes; updated */
     void* v;                 /* second moment: the same */
     uint8_t* exponents;      /* moments in 8 bits: [ceil(n / HR_ADAMW_BLOCK), 2], updated; NULL: moments in 32 bits */
-    int64_t n;               /* 0 .. 2^40 */
+    int64_t n;               /* 0 .. 2^36 */
     float weight_decay;      /* finite */
     int32_t param_dtype, grad_dtype;
 } hr_adamw_tensor;
 
 /*
- * hr_adamw — one step of AdamW over `count` tensors, in one launch for every 48 of them:
+ * hr_adamw — one step of AdamW over `count` tensors, in one launch for every 48 of them that have numbers:
  *   g = grad * *grad_scale,   m = beta1 m + (1 - beta1) g,   v = beta2 v + (1 - beta2) g^2,
  *   param = param (1 - lr weight_decay) - lr / (1 - beta1^step) * m / (sqrt(v / (1 - beta2^step)) + eps).
  * The arithmetic is float32, (1 - beta...) and what depends on step are taken in 64 bits and rounded.

@@ -152,6 +152,9 @@ __device__ __forceinline__ void fold_two(float& a, float& b, Folds& s, int& turn
     }
 }
 
+// 1 / sqrt(spread^2 + eps).  (Of a row of equal numbers far from 0 the difference of two squares may come out below 0, by more than eps; a NaN stays one.)
+__device__ __forceinline__ float over_spread(float square, float eps) { return 1.0f / sqrtf((square < 0.0f ? 0.0f : square) + eps); }
+
 // ---- rows that LANES lanes hold, CH chunks of 16 bytes each, between their one read and their one write.  The mean is found first and the
 // spread from what is left: the second fold also finds what the first mean is off by, so that a row far from 0 loses nothing.
 template <typename T, typename W, int LANES, int CH, bool TINY = false>
@@ -213,7 +216,7 @@ __global__ __launch_bounds__(LANES > 256 ? LANES : 256) void k_norm(NormArgs a)
             }
         }
         fold_two<LANES>(s0, s1, folds, turn);
-        const float off = s0 * over, rstd = 1.0f / sqrtf(s1 * over - off * off + a.eps);
+        const float off = s0 * over, rstd = over_spread(s1 * over - off * off, a.eps);
         if (!in) continue;
         if (t == 0 && a.stats) {
             a.stats[2 * r] = first + off;
@@ -270,7 +273,7 @@ __global__ __launch_bounds__(1024) void k_norm_long(NormArgs a)
             }
         }
         fold_two<1024>(s0, s1, folds, turn);
-        const float off = s0 * over, rstd = 1.0f / sqrtf(s1 * over - off * off + a.eps);
+        const float off = s0 * over, rstd = over_spread(s1 * over - off * off, a.eps);
         if (threadIdx.x == 0 && a.stats) {
             a.stats[2 * r] = first + off;
             a.stats[2 * r + 1] = rstd;

@@ -149,6 +149,27 @@ def test_norm_of_rows_without_spread_and_without_numbers(n, dtype):
     assert dx[0].isnan().any() and dx[4].isnan().all() and not dx[[1, 2, 3, 5]].isnan().any()
 
 
+@pytest.mark.parametrize("n", [3, 67, 300, 768, 1500, 3000, 5000, 17000, 40000, 70001, 100000])
+def test_norm_of_equal_numbers_far_from_zero(n):
+    """Their spread is 0, but the first mean is off by a rounding, and the squares of what is left are larger than eps."""
+    c = 10.0 ** (6 + 8 * torch.rand(200, generator=_gen(n), device="cuda"))
+    x = (c * torch.sign(_randn(n + 1, 200)))[:, None].expand(200, n).contiguous()
+    eps = 1e-5
+    r = _hr().layer_norm(x, eps=eps)
+    # K additions one after the other (160 at most here: 128 of a lane and the folds): the first mean is within K u |c| of c, what is left is exact, its
+    # mean within K u of itself; so what is divided by the spread is within (K u)^2 |c| of 0, and the spread is at least sqrt eps
+    bound = (162 * 2.0 ** -24) ** 2 * c / math.sqrt(eps) * 1.01
+    assert torch.isfinite(r.out).all()
+    assert (r.out.abs() <= bound[:, None]).all()
+    assert (r.stats[:, 1] > 0).all() and (r.stats[:, 1] <= 1.0001 / math.sqrt(eps)).all()
+    # one of them next to the others: the spread is far below what its square is off by
+    x[:, 0] = torch.nextafter(x[:, 0], torch.zeros_like(x[:, 0]))
+    r = _hr().layer_norm(x, eps=eps)
+    assert torch.isfinite(r.out).all() and torch.isfinite(r.stats).all()
+    g = _hr().layer_norm_backward(x, None, r.stats, torch.ones(200, n, device="cuda"))
+    assert torch.isfinite(g.x).all()
+
+
 def test_norm_without_rows_and_many_rows():
     hr = _hr()
     for n in (5, 3000, 40000):
