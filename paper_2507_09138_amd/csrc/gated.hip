@@ -10,22 +10,6 @@ namespace hr {
 
 template <typename T> constexpr int kE = 16 / (int)sizeof(T);            // elements of 16 bytes
 
-// 16 bytes of a row from element t on, zeros from element n on; rows may begin at any element
-template <typename T>
-__device__ __forceinline__ u32x4 load16(const T* row, int t, int n)
-{
-    u32x4 v = {0, 0, 0, 0};
-    if (t + kE<T> <= n) {
-        __builtin_memcpy(&v, row + t, 16);
-    } else if (t < n) {
-        T x[kE<T>];
-#pragma unroll
-        for (int e = 0; e < kE<T>; ++e) x[e] = t + e < n ? row[t + e] : (T)0.0f;
-        __builtin_memcpy(&v, x, 16);
-    }
-    return v;
-}
-
 // 16 bytes of a row from an element on that may lie anywhere: whole words of 4 bytes and a shift (a load of 16 bytes that begins inside a word takes
 // four times as long; the word behind them is read only where it holds some of them)
 template <typename T>
@@ -46,14 +30,40 @@ __device__ __forceinline__ u32x4 load16_words(const T* at)
     return v;
 }
 
-// ---- rows that tiles cannot take as they are, copied with zeros behind them to multiples of 128 bytes
+// 16 bytes of a row from element t on, zeros from element n on; rows may begin at any element
 template <typename T>
-__global__ __launch_bounds__(256) void k_pad(const T* x, int64_t ldx, int64_t rows, int n, char* out, int64_t ldo)
+__device__ __forceinline__ u32x4 load16(const T* row, int t, int n)
 {
-    const int64_t pieces = ldo / 16;
-    for (int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x; i < rows * pieces; i += (int64_t)gridDim.x * 256) {
+    u32x4 v;
+    if (t + kE<T> <= n) {
+        __builtin_memcpy(&v, row + t, 16);
+    } else {                                             // (every load is one: with a branch around each they would wait for each other)
+        T x[kE<T>];
+#pragma unroll
+        for (int e = 0; e < kE<T>; ++e) x[e] = row[min(t + e, n - 1)];
+#pragma unroll
+        for (int e = 0; e < kE<T>; ++e)
+            if (t + e >= n) x[e] = (T)0.0f;
+        __builtin_memcpy(&v, x, 16);
+    }
+    return v;
+}
+
+// ---- rows that tiles cannot take as they are, copied with zeros behind them to multiples of 128 bytes: those of up to three matrices, one after the other
+struct PadArgs {
+    const void* x[3]; int64_t ld[3], rows[3];
+    int n;
+    char* out; int64_t ldo;                              // (in bytes)
+};
+template <typename T>
+__global__ __launch_bounds__(256) void k_pad(PadArgs a)
+{
+    const int64_t pieces = a.ldo / 16, to1 = a.rows[0], to2 = to1 + a.rows[1], all = (to2 + a.rows[2]) * pieces;
+    for (int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x; i < all; i += (int64_t)gridDim.x * 256) {
         const int64_t r = i / pieces;
-        *(u32x4*)(out + i * 16) = load16(x + r * ldx, (int)(i - r * pieces) * kE<T>, n);
+        const int of = r < to1 ? 0 : r < to2 ? 1 : 2;
+        const T* row = (const T*)a.x[of] + (r - (of == 0 ? 0 : of == 1 ? to1 : to2)) * a.ld[of];
+        *(u32x4*)(a.out + i * 16) = load16(row, (int)(i - r * pieces) * kE<T>, a.n);
     }
 }
 
@@ -97,49 +107,70 @@ __device__ __forceinline__ void load_floats(const float* row, int t, int n, floa
         __builtin_memcpy(v, row + t, E * 4);
     } else {
 #pragma unroll
-        for (int e = 0; e < E; ++e) v[e] = t + e < n ? row[t + e] : 0.0f;
+        for (int e = 0; e < E; ++e) v[e] = row[min(t + e, n - 1)];
+#pragma unroll
+        for (int e = 0; e < E; ++e)
+            if (t + e >= n) v[e] = 0.0f;
     }
 }
 template <typename T>
 __global__ __launch_bounds__(256) void k_lay_out(LayOutArgs a)
 {
     __shared__ __align__(16) T tiles[2][64 * kTurn<T>];
-    constexpr int E = kE<T>, PER = 64 / E;
+    constexpr int E = kE<T>, PER = 64 / E, N = 64 * PER / 256;
     int block = blockIdx.x;
     if (block < a.blocks_d) {
         const int across = (a.fp + 63) / 64, r0 = block / across * 64, c0 = block % across * 64;
+        auto gradients = [&](auto whole) __attribute__((always_inline)) {
+            u32x4 raw[N];
+            float z[N][E], w[N][E];
 #pragma unroll
-        for (int i = threadIdx.x; i < 64 * PER; i += 256) {
-            const int r = i / PER, c = i % PER * E;
-            const bool in = r0 + r < a.m;
-            u32x4 raw = {0, 0, 0, 0};
-            float z[E] = {}, w[E] = {};
-            if (in) {
+            for (int j = 0; j < N; ++j) {
+                const int i = threadIdx.x + j * 256, r = i / PER, c = i % PER * E;
                 const float* at = a.pre + (int64_t)(r0 + r) * 2 * a.f;
-                raw = load16((const T*)a.dh + (int64_t)(r0 + r) * a.ldh, c0 + c, a.f);
-                load_floats<E>(at, c0 + c, a.f, z);
-                load_floats<E>(at + a.f, c0 + c, a.f, w);
-            }
-            T d[E], dg[E], du[E];
-            __builtin_memcpy(d, &raw, 16);
+                const T* dh = (const T*)a.dh + (int64_t)(r0 + r) * a.ldh;
+                if constexpr (decltype(whole)::value) {
+                    __builtin_memcpy(&raw[j], dh + c0 + c, 16);
+                    __builtin_memcpy(z[j], at + c0 + c, E * 4);
+                    __builtin_memcpy(w[j], at + a.f + c0 + c, E * 4);
+                } else {
+                    raw[j] = u32x4{0, 0, 0, 0};
 #pragma unroll
-            for (int e = 0; e < E; ++e) {                // (behind a row's end all three are 0, and so are both gradients)
-                float slope;
-                const float v = act_value(z[e], a.act, slope);
-                dg[e] = (T)((float)d[e] * w[e] * slope);
-                du[e] = (T)((float)d[e] * v);
+                    for (int e = 0; e < E; ++e) z[j][e] = w[j][e] = 0.0f;
+                    if (r0 + r < a.m) {
+                        raw[j] = load16(dh, c0 + c, a.f);
+                        load_floats<E>(at, c0 + c, a.f, z[j]);
+                        load_floats<E>(at + a.f, c0 + c, a.f, w[j]);
+                    }
+                }
             }
-            u32x4 g, u;
-            __builtin_memcpy(&g, dg, 16);
-            __builtin_memcpy(&u, du, 16);
-            if (a.rows && in && c0 + c < a.fp) {
-                T* at = (T*)a.rows + (int64_t)(r0 + r) * 2 * a.fp + c0 + c;
-                *(u32x4*)at = g;
-                *(u32x4*)(at + a.fp) = u;
+#pragma unroll
+            for (int j = 0; j < N; ++j) {
+                const int i = threadIdx.x + j * 256, r = i / PER, c = i % PER * E;
+                T d[E], dg[E], du[E];
+                __builtin_memcpy(d, &raw[j], 16);
+#pragma unroll
+                for (int e = 0; e < E; ++e) {            // (behind a row's end all three are 0, and so are both gradients)
+                    float slope;
+                    const float v = act_value(z[j][e], a.act, slope);
+                    dg[e] = (T)((float)d[e] * w[j][e] * slope);
+                    du[e] = (T)((float)d[e] * v);
+                }
+                u32x4 g, u;
+                __builtin_memcpy(&g, dg, 16);
+                __builtin_memcpy(&u, du, 16);
+                if (a.rows && r0 + r < a.m && c0 + c < a.fp) {
+                    T* at = (T*)a.rows + (int64_t)(r0 + r) * 2 * a.fp + c0 + c;
+                    *(u32x4*)at = g;
+                    *(u32x4*)(at + a.fp) = u;
+                }
+                turn_in(tiles[0], r, c, g);
+                turn_in(tiles[1], r, c, u);
             }
-            turn_in(tiles[0], r, c, g);
-            turn_in(tiles[1], r, c, u);
-        }
+        };
+        // (no branch between the loads of blocks that are whole: the compiler waits where one ends)
+        if (r0 + 64 <= a.m && c0 + 64 <= a.f) gradients(std::true_type{});
+        else gradients(std::false_type{});
         if (!a.cols) return;
         __syncthreads();
         for (int i = threadIdx.x; i < 2 * 64 * PER; i += 256) {
@@ -158,11 +189,22 @@ __global__ __launch_bounds__(256) void k_lay_out(LayOutArgs a)
     T* out = of_w ? (T*)a.turned_w + (of_up ? a.fp : 0) : (T*)a.turned_x;
     const int64_t ldo = of_w ? 2 * a.fp : a.mp;
     const int across = (a.k + 63) / 64, r0 = block / across * 64, c0 = block % across * 64;
+    u32x4 some[N];
+    if (r0 + 64 <= n && c0 + 64 <= a.k) {
 #pragma unroll
-    for (int i = threadIdx.x; i < 64 * PER; i += 256) {
-        const int r = i / PER, c = i % PER * E;
-        turn_in(tiles[0], r, c, r0 + r < n ? load16(from + (int64_t)(r0 + r) * ld, c0 + c, a.k) : u32x4{0, 0, 0, 0});
+        for (int j = 0; j < N; ++j) {
+            const int i = threadIdx.x + j * 256;
+            __builtin_memcpy(&some[j], from + (int64_t)(r0 + i / PER) * ld + c0 + i % PER * E, 16);
+        }
+    } else {
+#pragma unroll
+        for (int j = 0; j < N; ++j) {
+            const int i = threadIdx.x + j * 256, r = i / PER;
+            some[j] = r0 + r < n ? load16(from + (int64_t)(r0 + r) * ld, c0 + i % PER * E, a.k) : u32x4{0, 0, 0, 0};
+        }
     }
+#pragma unroll
+    for (int j = 0; j < N; ++j) turn_in(tiles[0], (threadIdx.x + j * 256) / PER, (threadIdx.x + j * 256) % PER * E, some[j]);
     __syncthreads();
 #pragma unroll
     for (int i = threadIdx.x; i < 64 * PER; i += 256) {
@@ -522,14 +564,6 @@ static int check_gated(int64_t m, int64_t k, int64_t f, int32_t dtype, int32_t a
     return HR_OK;
 }
 
-template <typename T>
-static hipError_t launch_pad(const void* x, int64_t ldx, int64_t rows, int64_t n, void* out, hipStream_t s)
-{
-    const int64_t ldo = padded(n, sizeof(T));
-    hipLaunchKernelGGL(k_pad<T>, dim3((unsigned)std::min<int64_t>((rows * (ldo / 16) + 255) / 256, 1 << 20)), dim3(256), 0, s, (const T*)x, ldx, rows, (int)n, (char*)out, ldo);
-    return hipGetLastError();
-}
-
 // waves that take parts of k of the same columns: enough for the chip to be busy, eight steps each at least
 static int few_share(int64_t groups, int64_t k_bytes, int most)
 {
@@ -547,8 +581,7 @@ struct GatedArgs {
 };
 
 // workspace: x and both matrices with padded rows, where rows of k elements are not whole blocks; sums of the parts of k
-static size_t x_bytes(int64_t m, int64_t k, size_t es) { return k * es % 128 ? aligned((size_t)(m * padded(k, es))) : 0; }
-static size_t w_bytes(int64_t k, int64_t f, size_t es) { return k * es % 128 ? aligned((size_t)(2 * f * padded(k, es))) : 0; }
+static size_t padded_bytes(int64_t m, int64_t k, int64_t f, size_t es) { return k * es % 128 ? aligned((size_t)((m + 2 * f) * padded(k, es))) : 0; }
 
 template <typename T>
 static hipError_t launch_gated(const GatedArgs& g, char* ws, hipStream_t s)
@@ -578,13 +611,12 @@ static hipError_t launch_gated(const GatedArgs& g, char* ws, hipStream_t s)
     TileArgs p{};
     p.k = (int)padded(g.k, es);
     if (g.k * es % 128) {
-        char *px = ws, *pw = ws + x_bytes(g.m, g.k, es);
-        if (hipError_t e = launch_pad<T>(g.x, g.ldx, g.m, g.k, px, s)) return e;
-        if (hipError_t e = launch_pad<T>(g.gate, g.ldg, g.f, g.k, pw, s)) return e;
-        if (hipError_t e = launch_pad<T>(g.up, g.ldu, g.f, g.k, pw + g.f * p.k, s)) return e;
-        p.a = px;
-        p.b = pw;
-        p.up = pw + g.f * p.k;
+        const PadArgs pad{{g.x, g.gate, g.up}, {g.ldx, g.ldg, g.ldu}, {g.m, g.f, g.f}, (int)g.k, ws, p.k};
+        hipLaunchKernelGGL(k_pad<T>, dim3((unsigned)std::min<int64_t>(((g.m + 2 * g.f) * (p.k / 16) + 255) / 256, 1 << 20)), dim3(256), 0, s, pad);
+        if (hipError_t e = hipGetLastError()) return e;
+        p.a = ws;
+        p.b = ws + g.m * p.k;
+        p.up = p.b + g.f * p.k;
         p.lda = p.ldb = p.ldup = p.k;
     } else if (in_tiles(g.x, g.ldx, es) && in_tiles(g.gate, g.ldg, es) && in_tiles(g.up, g.ldu, es)) {
         p.a = (const char*)g.x;
@@ -604,7 +636,7 @@ static hipError_t launch_gated(const GatedArgs& g, char* ws, hipStream_t s)
     p.ldo = g.ldo;
     p.pre = g.pre;
     p.act = g.act;
-    p.sums = (float*)(ws + x_bytes(g.m, g.k, es) + w_bytes(g.k, g.f, es));
+    p.sums = (float*)(ws + padded_bytes(g.m, g.k, g.f, es));
     const Tiling t = plan_tiles(true, es, &p, 1);
     return launch_tiles<T, true>(t, TilePair{{p}}, 1, s);
 }
@@ -659,7 +691,7 @@ size_t hr_gated_workspace_bytes(int64_t m, int64_t k, int64_t f, int32_t dtype)
     p.n = f;
     p.k = (int)padded(k, es);
     plan_tiles(true, es, &p, 1);
-    return x_bytes(m, k, es) + w_bytes(k, f, es) + sums_bytes(true, p) + HR_WORKSPACE_ALIGN;
+    return padded_bytes(m, k, f, es) + sums_bytes(true, p) + HR_WORKSPACE_ALIGN;
 }
 
 int hr_gated(const void* x, int64_t ldx, const void* w_gate, int64_t ldwg, const void* w_up, int64_t ldwu, int32_t dtype, int64_t m, int64_t k,
