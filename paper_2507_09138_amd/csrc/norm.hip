@@ -474,45 +474,46 @@ __global__ __launch_bounds__(256) void k_norm_stripe(NormArgs a)
         if (e >= p.skip) to[p.start + e] = dw[e], to[n + p.start + e] = db[e];
 }
 
-// ---- the sums of the groups of rows, in an order that depends on nothing but their number: eight threads for 32 columns, 128 shares of the groups
-// (32 shares: 8.6 us instead of 4 for 359 groups of 67 columns, a chain of round trips)
-template <typename W>
+// ---- the sums of the groups of rows, in an order that depends on nothing but their number: SHARES threads take every SHARES-th group of four columns.
+// 128 where there may be many groups (with 32 shares 8.6 us instead of 4 for 359 groups of 67 columns, a chain of round trips), 16 for the few of long rows.
+template <typename W, int SHARES>
 __global__ __launch_bounds__(1024) void k_norm_join(const float* parts, int groups, int n, void* grad_weight, void* grad_bias)
 {
-    __shared__ floatx4 sums[128][8];
-    __shared__ float some[8][32];
+    constexpr int FOURS = 1024 / SHARES, COLS = 4 * FOURS, PARTS = 256 / COLS;            // (256 threads add 16 shares each)
+    __shared__ floatx4 sums[SHARES][FOURS];
+    __shared__ float some[PARTS][COLS];
     const int64_t all = 2 * (int64_t)n;
-    const int share = threadIdx.x / 8, c = threadIdx.x % 32;
-    for (int64_t first = (int64_t)blockIdx.x * 32; first < all; first += (int64_t)gridDim.x * 32) {
-        const int64_t col = first + threadIdx.x % 8 * 4;
+    const int share = threadIdx.x / FOURS, c = threadIdx.x % COLS;
+    for (int64_t first = (int64_t)blockIdx.x * COLS; first < all; first += (int64_t)gridDim.x * COLS) {
+        const int64_t col = first + threadIdx.x % FOURS * 4;
         floatx4 s = {0, 0, 0, 0};
         if (col + 4 <= all) {
 #pragma unroll 4
-            for (int g = share; g < groups; g += 128) {
+            for (int g = share; g < groups; g += SHARES) {
                 floatx4 v;
                 __builtin_memcpy(&v, parts + g * all + col, 16);
                 s += v;
             }
         } else {
-            for (int g = share; g < groups; g += 128)
+            for (int g = share; g < groups; g += SHARES)
 #pragma unroll
                 for (int e = 0; e < 4; ++e)
                     if (col + e < all) s[e] += parts[g * all + col + e];
         }
-        sums[share][threadIdx.x % 8] = s;
+        sums[share][threadIdx.x % FOURS] = s;
         __syncthreads();
         if (threadIdx.x < 256) {
             float v = 0.0f;
 #pragma unroll
-            for (int q = 0; q < 16; ++q) v += sums[threadIdx.x / 32 * 16 + q][c / 4][c % 4];
-            some[threadIdx.x / 32][c] = v;
+            for (int q = 0; q < 16; ++q) v += sums[threadIdx.x / COLS * 16 + q][c / 4][c % 4];
+            some[threadIdx.x / COLS][c] = v;
         }
         __syncthreads();
-        if (threadIdx.x < 32) {
+        if (threadIdx.x < COLS) {
             const int64_t j = first + c;
             float v = 0.0f;
 #pragma unroll
-            for (int q = 0; q < 8; ++q) v += some[q][c];
+            for (int q = 0; q < PARTS; ++q) v += some[q][c];
             void* to = j < n ? grad_weight : grad_bias;
             if (j < all && to) ((W*)to)[j < n ? j : j - n] = (W)v;
         }
@@ -573,7 +574,7 @@ static void launch_norm_backward(const NormArgs& a, void* grad_weight, void* gra
     if (a.rows == 0) {
     } else if (a.n > kHeldColumns) {
         hipLaunchKernelGGL((k_norm_sums<T, W>), dim3((unsigned)std::min<int64_t>(a.rows, 512)), dim3(1024), 0, s, a);
-        groups = most;
+        groups = std::min<int64_t>(most, std::max<int64_t>(1, 768 / ((chunks + 255) / 256)));     // (three workgroups a compute unit: 58 us instead of 66 with eight, 512 x 50021 float32)
         hipLaunchKernelGGL((k_norm_stripe<T, W>), dim3((unsigned)((chunks + 255) / 256), (unsigned)groups), dim3(256), 0, s, a);
     } else if (a.n < kE<T>) go(k_norm_backward<T, W, 16, 1, true>, 256, 16);
     else if (chunks <= 16) go(k_norm_backward<T, W, 16, 1>, 256, 16);
@@ -587,7 +588,10 @@ static void launch_norm_backward(const NormArgs& a, void* grad_weight, void* gra
     else if constexpr (sizeof(T) == 4) go(k_norm_backward<T, W, 1024, 4>, 1024, 1);
     if (a.parts || a.rows == 0) {
         if (!grad_weight && !grad_bias) return;
-        hipLaunchKernelGGL(k_norm_join<W>, dim3((unsigned)std::min<int64_t>((2 * (int64_t)a.n + 31) / 32, 1 << 20)), dim3(1024), 0, s, a.parts, (int)groups, a.n, grad_weight, grad_bias);
+        auto join = [&](auto kernel, int columns) {
+            hipLaunchKernelGGL(kernel, dim3((unsigned)std::min<int64_t>((2 * (int64_t)a.n + columns - 1) / columns, 1 << 20)), dim3(1024), 0, s, a.parts, (int)groups, a.n, grad_weight, grad_bias);
+        };
+        a.n > kHeldColumns ? join(k_norm_join<W, 16>, 256) : join(k_norm_join<W, 128>, 32);
     }
 }
 
