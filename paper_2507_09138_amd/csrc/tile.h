@@ -112,6 +112,9 @@ __device__ __forceinline__ void finish(const TileArgs& p, int64_t row, int64_t c
 // step of 64 bytes are read while the step before is multiplied; where those of a block's second step have been read by all waves its buffer is
 // filled again: one barrier a block.  Where there is no more than a tile for every compute unit nothing else hides the time that loads take: NB
 // buffers, all but one on their way.  Else a workgroup goes from tile to tile and asks for the next one's first blocks before it writes its outputs.
+// Bound by matrix instructions at the clock that power leaves (1.72 GHz, busy 68 % of it, no bank conflicts).  Gated, 8192 x 4096 x 10752 of both matrices,
+// bfloat16 1210 us (1.19 P/s, with 705 MB of gate and up written; a library's product alone 1090); 8192 x 4096 x 21504 1210 (library 1083), 21504 x 4096 x
+// 8192 1180 .. 1300 (1003), 4096^3 102 (92).  float32 141 T/s between start and end, of 154.
 template <typename T, bool GATED, int BM, int BN, int WM, int NB>
 __global__ __launch_bounds__(BM / WM * (BN / 64) * 64) void k_tiles(TilePair pair)
 {
@@ -252,7 +255,7 @@ __global__ __launch_bounds__(BM / WM * (BN / 64) * 64) void k_tiles(TilePair pai
     }
 }
 
-// Adds up the parts of k: SHARES threads take every SHARES-th part of four columns, in order, and their sums are added in order.
+// Adds up the parts of k (memory: 75 MB in 19 us, 4 TB/s): SHARES threads take every SHARES-th part of four columns, in order, and their sums are added in order.
 template <typename T, bool GATED, int SHARES>
 __global__ __launch_bounds__(256) void k_tiles_join(TilePair pair)
 {
