@@ -476,6 +476,11 @@ static Tiling plan_tiles(bool gated, size_t es, TileArgs* p, int count)
     double least = 0;
     int64_t longest_k = 0, chosen = 0, large[2] = {p[0].m, count > 1 ? p[1].m : 0};
     for (int i = 0; i < count; ++i) longest_k = std::max<int64_t>(longest_k, p[i].k / 128);
+    // small tiles of so many blocks each: rounds of two on every compute unit, the last one half as long where it has one at most for each
+    auto small = [&](int64_t tiles, int64_t of) {
+        const int64_t at_once = 2 * kComputeUnits, left = tiles % at_once;
+        return (double)(tiles / at_once * of) * pair + (left == 0 ? 0 : left <= kComputeUnits ? of * one : of * pair);
+    };
     auto consider = [&](int bm, int bn) {
         const int64_t cols = bn / (gated ? 2 : 1);
         int64_t last = 0;
@@ -509,10 +514,9 @@ static Tiling plan_tiles(bool gated, size_t es, TileArgs* p, int count)
                 }
             };
             if (bm < 256) {
-                const int64_t at_once = 2 * kComputeUnits, left = all % at_once;
                 if (all <= kComputeUnits) try_one(std::max(of[0], of[1]) * one + 6 + joins);
-                else if (count > 1 && of[0] != of[1]) try_one(rounds(at_once, groups[l], of[l], groups[1 - l], of[1 - l]) * pair + 6 + joins);
-                else try_one((double)(all / at_once * of[0]) * pair + (left == 0 ? 0 : left <= kComputeUnits ? of[0] * one : of[0] * pair) + 6 + joins);
+                else if (count > 1 && of[0] != of[1]) try_one(rounds(2 * kComputeUnits, groups[l], of[l], groups[1 - l], of[1 - l]) * pair + 6 + joins);
+                else try_one(small(all, of[0]) + 6 + joins);
                 continue;
             }
             double t = rounds(kComputeUnits, groups[l], of[l], groups[1 - l], of[1 - l]) * 1.6;
@@ -521,10 +525,11 @@ static Tiling plan_tiles(bool gated, size_t es, TileArgs* p, int count)
                 double mixed = 14;
                 int64_t kept[2] = {0, 0};
                 for (int i = 0; i < count; ++i) {
-                    const int64_t across = (p[i].n + cols - 1) / cols, down = (p[i].m + bm - 1) / bm, full = across * down / kComputeUnits * kComputeUnits / across, left = p[i].m - full * bm;
+                    const int64_t across = (p[i].n + cols - 1) / cols, down = (p[i].m + bm - 1) / bm, full = across * down / kComputeUnits * kComputeUnits / across,
+                                  left = p[i].m - full * bm;
                     kept[i] = left > 0 ? full * bm : p[i].m;
                     mixed += (double)((std::min(full, down) * across + kComputeUnits - 1) / kComputeUnits * of[i]) * 1.6;
-                    if (left > 0) mixed += rounds(2 * kComputeUnits, (left + 127) / 128 * ((p[i].n + cols / 2 - 1) / (cols / 2)), of[i], 0, 0) * pair;
+                    if (left > 0) mixed += small((left + 127) / 128 * ((p[i].n + cols / 2 - 1) / (cols / 2)), of[i]);
                 }
                 const bool mix = mixed < t;
                 for (int i = 0; i < count; ++i) large[i] = mix ? kept[i] : p[i].m;
