@@ -160,7 +160,7 @@ __device__ __forceinline__ float over_spread(float square, float eps) { return 1
 // Bound by memory, in and out: 16384 x 4096 bfloat16 57 us (4.7 TB/s, a copy's rate), 65536 x 768 39 (5.1), 262144 x 128 24 (5.6), 8192 x 8192 float32 91 (5.9);
 // 512 x 50021 float32 58 (3.5: a row fills a compute unit's registers, and the next one waits until it has been written).  One row of 768 takes 3.
 template <typename T, typename W, int LANES, int CH, bool TINY = false>
-__global__ __launch_bounds__(LANES > 256 ? LANES : 256) void k_norm(NormArgs a)
+__global__ __launch_bounds__(LANES > 256 ? LANES : 256, LANES == 1024 && CH == 4 && sizeof(T) == 2 ? 8 : 1) void k_norm(NormArgs a)
 {
     constexpr int E = kE<T>, THREADS = LANES > 256 ? LANES : 256, ROWS = THREADS / LANES;
     constexpr bool KEEP = CH * E <= 16;                  // weights stay in registers from row to row
@@ -175,8 +175,9 @@ __global__ __launch_bounds__(LANES > 256 ? LANES : 256) void k_norm(NormArgs a)
     };
     if constexpr (KEEP)
         for (int i = 0; i < CH; ++i) weights(piece_of<T>(Chunk<T>{}, i * LANES + t, n), w[i], b[i]);
-    // (AHEAD: large workgroups are few on a compute unit, and ask for their next row before they fold the last one's sums)
-    constexpr bool AHEAD = LANES >= 512 && CH <= 4;
+    // (AHEAD: large workgroups are few on a compute unit, and ask for their next row before they fold the last one's sums; where two of 1024 threads fit
+    // without, as those of 16 bits do, that is faster: 2048 x 32768 bfloat16 65 us for 71)
+    constexpr bool AHEAD = (LANES == 512 || (LANES == 1024 && sizeof(T) == 4)) && CH <= 4;
     auto load = [&](int64_t r0, Chunk<T>* x) __attribute__((always_inline)) {
         const T* row = (const T*)a.x + min(r0 + threadIdx.x / LANES, a.rows - 1) * a.ldx;
 #pragma unroll
