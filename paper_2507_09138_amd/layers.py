@@ -161,7 +161,8 @@ def layer_norm_backward(x, weight, stats, grad_out, parameters=True, out=None):
     dx, ldgx = _result(out, "out", dtype, (rows, n), dev)
     dw = db = None
     if parameters:
-        dw, db = torch.empty(n, dtype=kind, device=dev), torch.empty(n, dtype=kind, device=dev)
+        dw = torch.empty(n, dtype=kind, device=dev)
+        db = torch.empty_like(dw)
     ws = _workspace(_norm_bytes(rows, n), dev)
     _check(lib.hr_layer_norm_backward(x.data_ptr(), ldx, _DTYPE[dtype], rows, n, _at(weight), _DTYPE[kind], stats.data_ptr(), dy.data_ptr(), ldg,
                                       dx.data_ptr(), ldgx, _at(dw), _at(db), ws.data_ptr(), ws.numel(), _raw_stream(dev.index)))
@@ -222,7 +223,10 @@ def gated_backward(x, w_gate, w_up, pre, grad_out, activation="silu", rows=True,
         raise HrError(-1, f"grad_out must be a {(m, f)} tensor on {dev}")
     ws = _workspace(_gated_backward_bytes(m, k, f, kind), dev)
     dx = torch.empty(m, k, dtype=x.dtype, device=dev) if rows else None
-    dg, du = torch.empty(2, f, k, dtype=x.dtype, device=dev) if matrices else (None, None)
+    dg = du = None
+    if matrices:
+        dg = torch.empty(f, k, dtype=x.dtype, device=dev)
+        du = torch.empty_like(dg)
     _check(lib.hr_gated_backward(x.data_ptr(), ldx, w_gate.data_ptr(), ldwg, w_up.data_ptr(), ldwu, kind, m, k, f, _ACT[activation], pre.data_ptr(),
                                  dh.data_ptr(), ldgo, _at(dx), k, _at(dg), k, _at(du), k, ws.data_ptr(), ws.numel(), _raw_stream(dev.index)))
     return GatedGrads(dx, dg, du)
