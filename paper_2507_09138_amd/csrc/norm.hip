@@ -250,31 +250,39 @@ __global__ __launch_bounds__(LANES > 256 ? LANES : 256, LANES == 1024 && CH == 4
 template <typename T, typename W>
 __global__ __launch_bounds__(1024) void k_norm_long(NormArgs a)
 {
-    constexpr int E = kE<T>;
+    constexpr int E = kE<T>, U = 4;
     __shared__ Folds folds;
     int turn = 0;
     const int n = a.n, chunks = (n + E - 1) / E;
     const float over = 1.0f / (float)n;
     for (int64_t r = blockIdx.x; r < a.rows; r += gridDim.x) {
         const T* row = (const T*)a.x + r * a.ldx;
+        // f of every piece, U of them asked for at once (behind the row's end: pieces without elements)
+        auto pass = [&](auto f) __attribute__((always_inline)) {
+            for (int c0 = threadIdx.x; c0 < chunks; c0 += 1024 * U) {
+                Piece<T> x[U];
+#pragma unroll
+                for (int u = 0; u < U; ++u) x[u] = load_piece(row, min(c0 + u * 1024, chunks), n);
+#pragma unroll
+                for (int u = 0; u < U; ++u) f(x[u]);
+            }
+        };
         float s0 = 0.0f, s1 = 0.0f;
-        for (int c = threadIdx.x; c < chunks; c += 1024) {
-            const Piece<T> x = load_piece(row, c, n);
+        pass([&](const Piece<T>& x) __attribute__((always_inline)) {
 #pragma unroll
             for (int e = 0; e < E; ++e) s0 += e >= x.skip ? (float)x.v[e] : 0.0f;
-        }
+        });
         fold_two<1024>(s0, s1, folds, turn);
         const float first = s0 * over;
         s0 = s1 = 0.0f;
-        for (int c = threadIdx.x; c < chunks; c += 1024) {
-            const Piece<T> x = load_piece(row, c, n);
+        pass([&](const Piece<T>& x) __attribute__((always_inline)) {
 #pragma unroll
             for (int e = 0; e < E; ++e) {
                 const float d = e >= x.skip ? (float)x.v[e] - first : 0.0f;
                 s0 += d;
                 s1 = fmaf(d, d, s1);
             }
-        }
+        });
         fold_two<1024>(s0, s1, folds, turn);
         const float off = s0 * over, rstd = over_spread(s1 * over - off * off, a.eps);
         if (threadIdx.x == 0 && a.stats) {
@@ -282,15 +290,14 @@ __global__ __launch_bounds__(1024) void k_norm_long(NormArgs a)
             a.stats[2 * r + 1] = rstd;
         }
         T* out = (T*)a.out + r * a.ldo;
-        for (int c = threadIdx.x; c < chunks; c += 1024) {
-            const Piece<T> x = load_piece(row, c, n);
+        pass([&](const Piece<T>& x) __attribute__((always_inline)) {
             float w[E], b[E], y[E];
             load_weights<E, W>(a.weight, x.start, 1.0f, w);
             load_weights<E, W>(a.bias, x.start, 0.0f, b);
 #pragma unroll
             for (int e = 0; e < E; ++e) y[e] = fmaf(((float)x.v[e] - first - off) * rstd, w[e], b[e]);
             store_piece(out, x, y);
-        }
+        });
     }
 }
 
