@@ -49,7 +49,9 @@ __device__ __forceinline__ u32x4 load16(const T* row, int t, int n)
     return v;
 }
 
-// ---- rows that tiles cannot take as they are, copied with zeros behind them to multiples of 128 bytes: those of up to three matrices, one after the other
+// ---- rows that tiles cannot take as they are (they begin at other places than multiples of 16 bytes, are no whole blocks of 128, or lie too far apart for
+// 32-bit offsets), copied with zeros behind them to multiples of 128 bytes: those of up to three matrices, one after the other.  8192 x 4096 and 2 x 10752 x 4096
+// bfloat16 75 us beside 1110 for the products, 777 x 1024 and 2 x 1333 x 1024 binary16 9 beside 14 (tiles that stage such rows through registers: 28).
 struct PadArgs {
     const void* x[3]; int64_t ld[3], rows[3];
     int n;
@@ -399,47 +401,6 @@ __global__ __launch_bounds__(512) void k_gated_ring(const T* x, int64_t ldx, con
     }
 }
 
-// ---- rows of any alignment, or further apart than tiles reach, that are not copied: tiles of 64 rows and 32 columns of the result, staged through
-// registers, one block of 64 bytes of k at a time.  777 x 1024 x 1333 binary16 28 us, aligned in tiles 13.5 (a copy, 5 us here, would want room in every call's workspace).
-template <typename T>
-__global__ __launch_bounds__(256) void k_gated_any(const T* x, int64_t ldx, const T* gate, int64_t ldg, const T* up, int64_t ldu, int m, int k, int f, int act, T* out,
-                                                   int64_t ldo, float* pre)
-{
-    constexpr int E = kE<T>, K = 4 * E, S = K + E;
-    __shared__ __align__(16) T ta[64 * S], tb[64 * S];
-    const int m0 = blockIdx.x * 64, n0 = blockIdx.y * 32;
-    const int lane = lane_id(), wave = threadIdx.x / 64, r = threadIdx.x / 4, t = threadIdx.x % 4 * E;
-    const T* ra = x + (int64_t)min(m0 + r, m - 1) * ldx;
-    const T* rb = r < 32 ? gate + (int64_t)min(n0 + r, f - 1) * ldg : up + (int64_t)min(n0 + r - 32, f - 1) * ldu;
-    floatx4 acc[4] = {};
-    for (int k0 = 0; k0 < k; k0 += K) {
-        const u32x4 va = load16(ra, k0 + t, k), vb = load16(rb, k0 + t, k);
-        __syncthreads();
-        *(u32x4*)(ta + r * S + t) = va;
-        *(u32x4*)(tb + r * S + t) = vb;
-        __syncthreads();
-        const u32x4 fa = *(const u32x4*)(ta + (wave * 16 + lane % 16) * S + lane / 16 * E);
-#pragma unroll
-        for (int j = 0; j < 4; ++j) acc[j] = multiply(T{}, *(const u32x4*)(tb + (j * 16 + lane % 16) * S + lane / 16 * E), fa, acc[j]);
-    }
-    const int row = m0 + wave * 16 + lane % 16;
-    if (row >= m) return;
-#pragma unroll
-    for (int j = 0; j < 2; ++j)
-#pragma unroll
-        for (int e = 0; e < 4; ++e) {
-            const int col = n0 + j * 16 + lane / 16 * 4 + e;
-            if (col >= f) continue;
-            float slope;
-            const float g = acc[j][e], u = acc[j + 2][e];
-            out[(int64_t)row * ldo + col] = (T)(act_value(g, act, slope) * u);
-            if (pre) {
-                pre[(int64_t)row * 2 * f + col] = g;
-                pre[((int64_t)row * 2 + 1) * f + col] = u;
-            }
-        }
-}
-
 // ---- which kernel
 
 // Blocks of k that a place for a workgroup multiplies one after the other until all workgroups are done: first those of `long_` blocks, then the
@@ -588,8 +549,8 @@ struct GatedArgs {
     void* out; int64_t ldo; float* pre;
 };
 
-// workspace: x and both matrices with padded rows, where rows of k elements are not whole blocks; sums of the parts of k
-static size_t padded_bytes(int64_t m, int64_t k, int64_t f, size_t es) { return k * es % 128 ? aligned((size_t)((m + 2 * f) * padded(k, es))) : 0; }
+// workspace: x and both matrices with padded rows (whether a call copies them is known by its addresses only); sums of the parts of k
+static size_t padded_bytes(int64_t m, int64_t k, int64_t f, size_t es) { return aligned((size_t)((m + 2 * f) * padded(k, es))); }
 
 template <typename T>
 static hipError_t launch_gated(const GatedArgs& g, char* ws, hipStream_t s)
@@ -619,25 +580,25 @@ static hipError_t launch_gated(const GatedArgs& g, char* ws, hipStream_t s)
     }
     TileArgs p{};
     p.k = (int)padded(g.k, es);
-    if (g.k * es % 128) {
-        const PadArgs pad{{g.x, g.gate, g.up}, {g.ldx, g.ldg, g.ldu}, {g.m, g.f, g.f}, (int)g.k, ws, p.k};
-        hipLaunchKernelGGL(k_pad<T>, dim3((unsigned)std::min<int64_t>(((g.m + 2 * g.f) * (p.k / 16) + 255) / 256, 1 << 20)), dim3(256), 0, s, pad);
+    // what tiles cannot take as it is is copied first, row by row
+    struct { const void* at; int64_t ld, rows; const char** to; int64_t* lds; } in[3] = {{g.x, g.ldx, g.m, &p.a, &p.lda}, {g.gate, g.ldg, g.f, &p.b, &p.ldb}, {g.up, g.ldu, g.f, &p.up, &p.ldup}};
+    PadArgs pad{};
+    pad.n = (int)g.k;
+    pad.out = ws;
+    pad.ldo = p.k;
+    int64_t copied = 0;
+    for (int i = 0; i < 3; ++i) {
+        const bool fits = g.k * es % 128 == 0 && in_tiles(in[i].at, in[i].ld, es);
+        pad.x[i] = in[i].at;
+        pad.ld[i] = in[i].ld;
+        pad.rows[i] = fits ? 0 : in[i].rows;
+        *in[i].to = fits ? (const char*)in[i].at : ws + copied * p.k;
+        *in[i].lds = fits ? in[i].ld * (int64_t)es : p.k;
+        copied += pad.rows[i];
+    }
+    if (copied > 0) {
+        hipLaunchKernelGGL(k_pad<T>, dim3((unsigned)std::min<int64_t>((copied * (p.k / 16) + 255) / 256, 1 << 20)), dim3(256), 0, s, pad);
         if (hipError_t e = hipGetLastError()) return e;
-        p.a = ws;
-        p.b = ws + g.m * p.k;
-        p.up = p.b + g.f * p.k;
-        p.lda = p.ldb = p.ldup = p.k;
-    } else if (in_tiles(g.x, g.ldx, es) && in_tiles(g.gate, g.ldg, es) && in_tiles(g.up, g.ldu, es)) {
-        p.a = (const char*)g.x;
-        p.b = (const char*)g.gate;
-        p.up = (const char*)g.up;
-        p.lda = g.ldx * es;
-        p.ldb = g.ldg * es;
-        p.ldup = g.ldu * es;
-    } else {
-        hipLaunchKernelGGL(k_gated_any<T>, dim3((unsigned)((g.m + 63) / 64), (unsigned)((g.f + 31) / 32)), dim3(256), 0, s, (const T*)g.x, g.ldx, (const T*)g.gate, g.ldg,
-                           (const T*)g.up, g.ldu, (int)g.m, (int)g.k, (int)g.f, g.act, (T*)g.out, g.ldo, g.pre);
-        return hipGetLastError();
     }
     p.m = g.m;
     p.n = g.f;
