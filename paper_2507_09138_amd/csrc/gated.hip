@@ -49,7 +49,7 @@ __device__ __forceinline__ u32x4 load16(const T* row, int t, int n)
     return v;
 }
 
-// ---- rows that tiles cannot take as they are (they begin at other places than multiples of 16 bytes, are no whole blocks of 128, or lie too far apart for
+// ---- rows that tiles cannot take as they are (they begin at other places than multiples of 16 bytes, are no multiple of that long, or lie too far apart for
 // 32-bit offsets), copied with zeros behind them to multiples of 128 bytes: those of up to three matrices, one after the other.  8192 x 4096 and 2 x 10752 x 4096
 // bfloat16 75 us beside 1110 for the products, 777 x 1024 and 2 x 1333 x 1024 binary16 9 beside 14 (tiles that stage such rows through registers: 28).
 struct PadArgs {
@@ -580,15 +580,17 @@ static hipError_t launch_gated(const GatedArgs& g, char* ws, hipStream_t s)
     }
     TileArgs p{};
     p.k = (int)padded(g.k, es);
+    p.end = g.k * es % 16 == 0 ? (int)(g.k * es) : p.k;  // (behind it a copy has zeros, where there is one)
     // what tiles cannot take as it is is copied first, row by row
-    struct { const void* at; int64_t ld, rows; const char** to; int64_t* lds; } in[3] = {{g.x, g.ldx, g.m, &p.a, &p.lda}, {g.gate, g.ldg, g.f, &p.b, &p.ldb}, {g.up, g.ldu, g.f, &p.up, &p.ldup}};
+    struct { const void* at; int64_t ld, rows; const char** to; int64_t* lds; } in[3] = {
+        {g.x, g.ldx, g.m, &p.a, &p.lda}, {g.gate, g.ldg, g.f, &p.b, &p.ldb}, {g.up, g.ldu, g.f, &p.up, &p.ldup}};
     PadArgs pad{};
     pad.n = (int)g.k;
     pad.out = ws;
     pad.ldo = p.k;
     int64_t copied = 0;
     for (int i = 0; i < 3; ++i) {
-        const bool fits = g.k * es % 128 == 0 && in_tiles(in[i].at, in[i].ld, es);
+        const bool fits = g.k * es % 16 == 0 && in_tiles(in[i].at, in[i].ld, es);
         pad.x[i] = in[i].at;
         pad.ld[i] = in[i].ld;
         pad.rows[i] = fits ? 0 : in[i].rows;
@@ -636,7 +638,7 @@ static BackwardPlan backward_plan(int64_t m, int64_t k, int64_t f, size_t es)
         TileArgs& t = p.p[i];
         t.m = i ? 2 * f : m;
         t.n = k;
-        t.k = (int)(i ? mb : 2 * fb);
+        t.k = t.end = (int)(i ? mb : 2 * fb);
         t.lda = t.ldb = t.k;
     }
     p.tiling = plan_tiles(false, es, p.p, 2);

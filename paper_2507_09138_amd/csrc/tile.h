@@ -49,12 +49,12 @@ __device__ __forceinline__ floatx4 multiply(float, u32x4 b, u32x4 a, floatx4 c)
     return c;
 }
 
-// What tiles take: out[i, j] = sum_t a[i, t] b[j, t], all distances in bytes.  Rows begin at multiples of 16 bytes, `k` is a multiple of 128.
+// What tiles take: out[i, j] = sum_t a[i, t] b[j, t], all distances in bytes.  Rows begin at multiples of 16 bytes and are a multiple of 16 long.
 struct TileArgs {
     const char* a; int64_t lda;
     const char* b; int64_t ldb;                          // gated: the gate's matrix
     const char* up; int64_t ldup;                        // gated: up's
-    int64_t m, n; int k;                                 // n: columns of the result
+    int64_t m, n; int k, end;                            // n: columns of the result; end: the length of a row, k: that in whole blocks of 128
     int64_t row0, large;                                 // its first row here; how many rows large tiles take, the others small ones (set by plan_tiles)
     int parts, part_k;                                   // parts of k (part_k bytes each, a multiple of 128), and where there are more than one
     int slots;                                           // workgroups, a multiple of 8
@@ -115,7 +115,8 @@ __device__ __forceinline__ void finish(const TileArgs& p, int64_t row, int64_t c
 // Bound by matrix instructions at the clock that power leaves (1.72 GHz, busy 68 % of it, no bank conflicts).  Gated, 8192 x 4096 x 10752 of both matrices,
 // bfloat16 1210 us (1.19 P/s, with 705 MB of gate and up written; a library's product alone 1090); 8192 x 4096 x 21504 1210 (library 1083), 21504 x 4096 x
 // 8192 1180 .. 1300 (1003), 4096^3 102 (92).  float32 141 T/s between start and end, of 154.
-template <typename T, bool GATED, int BM, int BN, int WM, int NB>
+// TAIL: rows that are no whole blocks; with what they need for it the others would be 4 % slower.
+template <typename T, bool GATED, int BM, int BN, int WM, int NB, bool TAIL>
 __global__ __launch_bounds__(BM / WM * (BN / 64) * 64) void k_tiles(TilePair pair)
 {
     const bool second = blockIdx.x >= pair.first;
@@ -163,9 +164,10 @@ __global__ __launch_bounds__(BM / WM * (BN / 64) * 64) void k_tiles(TilePair pai
     };
     auto request = [&](int block) __attribute__((always_inline)) {
         const int k0 = k_begin + block * BK;
+        const uint32_t back = TAIL && k0 + piece >= p.end ? piece : 0;        // (pieces behind the rows' end: the block's first instead, and zeros later)
 #pragma unroll
         for (int i = 0; i < UNITS; ++i)
-            lds_dma16((i * WAVES * 8 < BM ? ga : (is_up(i) ? gu : gb)) + k0, off[i], lds0 + (uint32_t)block % NB * BUF + (i * WAVES + wave) * 1024);
+            lds_dma16((i * WAVES * 8 < BM ? ga : (is_up(i) ? gu : gb)) + k0, off[i] - back, lds0 + (uint32_t)block % NB * BUF + (i * WAVES + wave) * 1024);
     };
 
     const int frag = (lane % 16) * BK + ((lane / 16) ^ (lane & 7)) * 16;
@@ -189,11 +191,17 @@ __global__ __launch_bounds__(BM / WM * (BN / 64) * 64) void k_tiles(TilePair pai
         }
         __builtin_amdgcn_s_setprio(0);
     };
-    // Everything asked for has landed, but for `behind` blocks that were asked for last, everything read is in registers: of all waves.
-    auto meet = [&](int behind) __attribute__((always_inline)) {
+    // Everything asked for has landed, up to block `next`, but for `behind` blocks that were asked for last, everything read is in registers: of all waves.
+    auto meet = [&](int next, int behind) __attribute__((always_inline)) {
         if (NB > 2 && behind >= 2) wait_vmcnt<2 * UNITS>();
         else if (NB > 2 && behind == 1) wait_vmcnt<UNITS>();
         else wait_vmcnt<0>();
+        if (const int k0 = k_begin + next * BK; TAIL && k0 + BK > p.end && next < blocks) {      // (what this wave asked for behind the rows' end)
+            if (k0 + piece >= p.end) {
+#pragma unroll
+                for (int i = 0; i < UNITS; ++i) *(u32x4*)(lds + (uint32_t)next % NB * BUF + (i * WAVES + wave) * 1024 + lane * 16) = u32x4{0, 0, 0, 0};
+            }
+        }
         asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
         __builtin_amdgcn_s_barrier();
         asm volatile("" ::: "memory");
@@ -205,7 +213,7 @@ __global__ __launch_bounds__(BM / WM * (BN / 64) * 64) void k_tiles(TilePair pai
     for (int b = 0; b < NB; ++b)
         if (b < blocks) request(b);
     for (;;) {
-        meet(min(blocks, NB) - 1);
+        meet(0, min(blocks, NB) - 1);
         read_b(b0, 0, 0);
 #pragma unroll
         for (int i = 0; i < TM; ++i) a[i] = *(const u32x4*)(place(0, 0) + (wm + i * 16) * BK);
@@ -216,7 +224,7 @@ __global__ __launch_bounds__(BM / WM * (BN / 64) * 64) void k_tiles(TilePair pai
         for (int b = 0; b < blocks; ++b) {
             read_b(b1, b, 1);
             step(b0, place(b, 1));
-            meet(min(blocks - 2 - b, NB - 2));           // (nobody reads this block's buffer any more, the next block has landed)
+            meet(b + 1, min(blocks - 2 - b, NB - 2));           // (nobody reads this block's buffer any more, the next block has landed)
             if (b + NB < blocks) request(b + NB);
             read_b(b0, b + 1, 0);                        // (behind the last block: whatever the buffer holds, not multiplied)
             step(b1, place(b + 1, 0));

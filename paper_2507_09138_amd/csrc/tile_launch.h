@@ -1,6 +1,7 @@
 // Launches of k_tiles for one type of elements: the body of gated_f16.hip, gated_bf16.hip and gated_f32.hip.
 #pragma once
 #include <algorithm>
+#include <type_traits>
 #include <utility>
 
 #include "tile.h"
@@ -30,12 +31,20 @@ static hipError_t launch_one_size(const Tiling& t, TilePair pair, int count, hip
         if (lds > 64 * 1024) e = hipFuncSetAttribute((const void*)kernel, hipFuncAttributeMaxDynamicSharedMemorySize, (int)lds);
         if (e == hipSuccess) hipLaunchKernelGGL(kernel, dim3(groups[0] + groups[1]), dim3(512), lds, s, pair);
     };
-    if (t.bm == 256) {
-        if constexpr (sizeof(T) == 2) go(k_tiles<T, GATED, 256, 256, 128, 2>, 2);
-    } else if (t.bm == 128) {
-        deep ? go(k_tiles<T, GATED, 128, 128, 32, 4>, 4) : go(k_tiles<T, GATED, 128, 128, 32, 2>, 2);
-    } else if constexpr (GATED) {
-        deep ? go(k_tiles<T, GATED, 64, 256, 32, 3>, 3) : go(k_tiles<T, GATED, 64, 256, 32, 2>, 2);
+    auto of_size = [&](auto tail) {
+        constexpr bool TAIL = decltype(tail)::value;
+        if (t.bm == 256) {
+            if constexpr (sizeof(T) == 2) go(k_tiles<T, GATED, 256, 256, 128, 2, TAIL>, 2);
+        } else if (t.bm == 128) {
+            deep ? go(k_tiles<T, GATED, 128, 128, 32, 4, TAIL>, 4) : go(k_tiles<T, GATED, 128, 128, 32, 2, TAIL>, 2);
+        } else if constexpr (GATED) {
+            deep ? go(k_tiles<T, GATED, 64, 256, 32, 3, TAIL>, 3) : go(k_tiles<T, GATED, 64, 256, 32, 2, TAIL>, 2);
+        }
+    };
+    if constexpr (GATED) {                               // (operands of the gradients are laid out in whole blocks)
+        pair.p[0].end < pair.p[0].k ? of_size(std::true_type{}) : of_size(std::false_type{});
+    } else {
+        of_size(std::false_type{});
     }
     const int most = std::max(pair.p[0].parts, count > 1 ? pair.p[1].parts : 1);
     if (e == hipSuccess && most > 1) {

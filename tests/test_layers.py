@@ -274,6 +274,15 @@ def test_gated_keeps_what_is_no_number_where_it_is(m, k, f, dtype):
     assert torch.equal(back.x, grads.x) and back.w_gate[:, k - 1].isnan().all() and torch.equal(back.w_gate[:, 1:k - 1], grads.w_gate[:, 1:k - 1])
 
 
+# tiles of 256 x 256, whole blocks of k and not, with rows that are left to small ones and without
+@pytest.mark.parametrize("m,k,f,dtype", [(4100, 1032, 4104, BF16), (4352, 1024, 4352, F16), (8200, 520, 5128, F16), (4100, 1033, 4104, BF16)])
+def test_gated_in_large_tiles(m, k, f, dtype):
+    hr = _hr()
+    x, wg, wu, dh = _gated_inputs(m, k, f, dtype)
+    got = hr.gated(x, wg, wu, "gelu", keep=True)
+    _check_gated(x, wg, wu, dh, "gelu", got, hr.gated_backward(x, wg, wu, got.pre, dh, "gelu"))
+
+
 @pytest.mark.parametrize("act", ACTS)
 def test_gated_far_arguments(act):
     """Arguments at which exponentials leave their range: 0 or the argument, slope 0 or 1, no NaN."""
