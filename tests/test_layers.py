@@ -274,6 +274,25 @@ def test_gated_keeps_what_is_no_number_where_it_is(m, k, f, dtype):
     assert torch.equal(back.x, grads.x) and back.w_gate[:, k - 1].isnan().all() and torch.equal(back.w_gate[:, 1:k - 1], grads.w_gate[:, 1:k - 1])
 
 
+@pytest.mark.parametrize("dtype", TYPES)
+@pytest.mark.parametrize("m,k,f", [(70, 128, 96), (40, 136, 70), (300, 200, 130), (33, 136, 40)])
+def test_gated_with_some_operands_at_odd_places(m, k, f, dtype):
+    """Whichever they are, or rows that lie far apart: the same bits (more than 32 rows take one way), and nothing beside the results is written."""
+    hr = _hr()
+    x, wg, wu, _ = _gated_inputs(m, k, f, dtype)
+    want = hr.gated(x, wg, wu, keep=True)
+    odd = [_strided(t, 1, 2, NAN)[0] for t in (x, wg, wu)]
+    for which in ((0,), (1,), (2,), (0, 1), (1, 2), (0, 1, 2)):
+        ops = [odd[i] if i in which else t for i, t in enumerate((x, wg, wu))]
+        wide = torch.full((m, f + 5), 7.0, dtype=dtype, device="cuda")
+        got = hr.gated(*ops, keep=True, out=wide[:, 3:3 + f])
+        assert torch.equal(got.out, want.out) and torch.equal(got.pre, want.pre) and _around(wide, 3, f, 7.0)
+    if m < 100:
+        far = torch.zeros(m, (1 << 21) + 64, dtype=dtype, device="cuda")[:, :k]
+        got = hr.gated(far.copy_(x), wg, wu, keep=True)
+        assert torch.equal(got.out, want.out) and torch.equal(got.pre, want.pre)
+
+
 # tiles of 256 x 256, whole blocks of k and not, with rows that are left to small ones and without
 @pytest.mark.parametrize("m,k,f,dtype", [(4100, 1032, 4104, BF16), (4352, 1024, 4352, F16), (8200, 520, 5128, F16), (4100, 1033, 4104, BF16)])
 def test_gated_in_large_tiles(m, k, f, dtype):
