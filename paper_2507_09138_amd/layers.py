@@ -332,7 +332,9 @@ def adamw(params, grads, m, v, step, lr, betas=(0.9, 0.999), eps=1e-8, weight_de
         grads = [g.contiguous() for g in grads]
     at = [list(map(_data_ptr, x)) for x in (params, grads, m, v)]
     wat, eat = ([0 if t is None else t.data_ptr() for t in x] if has else [0] * n for x, has in ((masters, has_w), (exponents, has_e)))
-    places = [x for x, k in zip(chain(at[0], at[2], at[3], wat, eat), sizes * 5) if k and x]
+    places = at[0] + at[2] + at[3] + (wat if has_w else []) + (eat if has_e else [])
+    if 0 in sizes or 0 < len(has_w) < n or 0 < len(has_e) < n:           # (addresses of nothing are no places)
+        places = [x for x, k in zip(places, sizes * 5) if k and x]
     if len(set(places)) != len(places):
         raise HrError(-1, "a tensor is in the lists twice")
     table = _tables(n).pack(*chain.from_iterable(zip(at[0], at[1], wat, at[2], at[3], eat, sizes, decay, ptypes, gtypes)))

@@ -440,6 +440,23 @@ def test_adamw_mixed_lists_equal_calls_for_each():
         assert all(x is None or torch.equal(x, y) for x, y in zip(a[name], b[name])), name
 
 
+def test_adamw_leaves_alone_what_has_no_gradient():
+    hr = _hr()
+    params = [_randn(1, 300), _randn(2, 0), _randn(3, 7).half()]
+    state = [hr.adamw_state(p, b) for p, b in zip(params, (8, 32, 32))]
+    masters = [None, None, params[2].float()]
+    before = [p.clone() for p in params]
+    lists = [[s[i] for s in state] for i in range(3)]
+
+    def step(grads):
+        hr.adamw(params, grads, lists[0], lists[1], 1, 1e-2, exponents=lists[2], masters=masters)
+
+    step([None, None, None])
+    assert all(torch.equal(p, b) for p, b in zip(params, before)) and not any(bool(t.any()) for s in state for t in s if t is not None)
+    step([None, params[1].clone(), torch.ones_like(params[2])])
+    assert torch.equal(params[0], before[0]) and not bool((params[2] == before[2]).any()) and not bool(state[0][0].any())
+
+
 def test_adamw_strange_numbers():
     """Moments in 8 bits: a NaN or an infinity makes its block's NaN and no other's; gradients so small or so large that their squares leave the range."""
     hr = _hr()
