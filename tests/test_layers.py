@@ -85,7 +85,7 @@ def test_norm_and_gradients(rows, n, dtype):
 
 
 @pytest.mark.parametrize("dtype", TYPES)
-@pytest.mark.parametrize("rows,n", [(37, 100), (5, 1003), (3, 5001), (2, 40001)])
+@pytest.mark.parametrize("rows,n", [(37, 100), (5, 1003), (3, 5001), (2, 20003), (2, 40001), (2, 140001)])
 def test_norm_of_slices_and_in_place(rows, n, dtype):
     """Rows that begin anywhere, NaN beside them; results in the place of the inputs; what lies beside a result stays as it was."""
     hr = _hr()
