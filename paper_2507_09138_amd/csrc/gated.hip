@@ -428,7 +428,7 @@ static double rounds(int64_t places, int64_t longs, int64_t long_, int64_t short
 // 512 x 512 x 4096 in eight parts 15.4 (one 32.6), float32 2048 x 768 x 4096 in five 113 (one 260, two 148), that and 4096 x 768 x 2048 in one launch
 // 219 (one after the other 228; in six parts and one, unlike lengths, 325).
 // Where large tiles leave much of a last round empty, the rows of that round are left to small ones, in a second launch: 8192 x 4096 x 21504 and
-// 21504 x 4096 x 8192, 2 and 5.25 rounds, 2283 -> 2190.
+// 21504 x 4096 x 8192, 2 and 5.25 rounds, 2283 -> 2150.
 // m, n and k of the products are there; parts, part_k and large are set.
 static Tiling plan_tiles(bool gated, size_t es, TileArgs* p, int count)
 {
