@@ -64,10 +64,12 @@ int hr_gated(const void* x, int64_t ldx, const void* w_gate, int64_t ldwg, const
              int64_t f, int32_t activation, void* out, int64_t ldo, float* out_pre, void* workspace, size_t workspace_bytes, void* stream);
 
 /*
- * hr_gated_backward — with d_up = grad_out * act(gate) and d_gate = grad_out * up * act'(gate), both rounded to `dtype` once, for the
+ * hr_gated_backward — with d_up = grad_out * act(gate) and d_gate = grad_out * up * act'(gate), both rounded to as many bits as `dtype` has once, for the
  * matrix instructions that take them:
  *   grad_x = d_gate w_gate + d_up w_up,   grad_w_gate = d_gate' x,   grad_w_up = d_up' x.
  *   pre   DEV [m, 2, f] float32, as hr_gated wrote it.   grad_out  DEV [m, f] in `dtype`.
+ * In binary16 each row of d_gate and d_up (for grad_x) and each column (for the matrices) is held times a power of two, so that they may be of any size that
+ * float32 has: only the results have to fit the type.  What is less than 2^-28 of the largest of its row (column) has fewer bits, below 2^-40 none.
  *   grad_x  DEV [m, k] or NULL: not wanted.   grad_w_gate, grad_w_up  DEV [f, k], both or neither (NULL); overwritten; all in `dtype`, rounded once.
  */
 size_t hr_gated_backward_workspace_bytes(int64_t m, int64_t k, int64_t f, int32_t dtype);        /* as above */

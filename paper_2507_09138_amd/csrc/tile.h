@@ -1,5 +1,7 @@
 // Products of floating point matrices in tiles (16-bit types and float32), and the gated block's arithmetic: what gated*.hip share.
 #pragma once
+#include <type_traits>
+
 #include "common.h"
 #include "hr_layers.h"
 #include "wave.h"
@@ -30,6 +32,15 @@ __device__ __forceinline__ float act_value(float z, int act, float& slope)
     slope = fmaf(z * (1.0f - p) * p, dy, p);
     return z * p;
 }
+
+// Gradients of gate and up in binary16 have a power of two for each of their rows, and in the copy that is turned for each of their columns: with it the
+// largest of them lies in 2^14 .. 2^15, so that none is too large for the type and those that are too small for it are less than a rounding of what they
+// are added to.  Here its exponent, from the bits of that largest magnitude (0 where it is 0, infinite or NaN).  Multiplying by it is exact.
+__device__ __forceinline__ int raised_by(uint32_t largest)
+{
+    return largest == 0 || largest >= 0x7f800000u ? 0 : 141 - (int)(largest >> 23);
+}
+template <typename T> constexpr bool kRaised = std::is_same_v<T, _Float16>;
 
 // 16 bytes of k a lane, lane l those of row l % 16 from byte 16 (l / 16) on of a step of 64: one matrix instruction of 16 bits, four of 32 (the
 // k of a step in another order, the same for both operands).  The first operand's rows are the result's rows, four of them in the registers of
@@ -62,6 +73,7 @@ struct TileArgs {
     void* out; int64_t ldo;                              // elements apart
     void* out2; int64_t ldo2, split;                     // rows from `split` on go to out2
     float* pre; int act;                                 // gated
+    const uint32_t* largest;                             // kRaised gradients: bits of the largest magnitude of each row of a, which is raised by its power of two
 };
 
 // One product, or two in one launch: workgroups from `first` on are the second's.
@@ -101,6 +113,12 @@ __device__ __forceinline__ void finish(const TileArgs& p, int64_t row, int64_t c
             store_some<N>(p.pre + row * 2 * p.n, col, p.n, v);
             store_some<N>(p.pre + (row * 2 + 1) * p.n, col, p.n, up);
         }
+    } else if constexpr (kRaised<T>) {
+        const int by = raised_by(p.largest[row]);
+        float x[N];
+#pragma unroll
+        for (int e = 0; e < N; ++e) x[e] = __builtin_ldexpf(v[e], -by);
+        store_some<N>(row < p.split ? (T*)p.out + row * p.ldo : (T*)p.out2 + (row - p.split) * p.ldo2, col, p.n, x);
     } else {
         store_some<N>(row < p.split ? (T*)p.out + row * p.ldo : (T*)p.out2 + (row - p.split) * p.ldo2, col, p.n, v);
     }
