@@ -9,16 +9,31 @@
 namespace hr {
 
 // ---- activations: the value and the slope.  All three are z times a share p of 0 .. 1 that one exponential gives; 2^x and 1 / x as the hardware has them
-// (within two units of the last place): what they are off by is a few units of the last place of z, and less than a rounding to 16 bits.
-constexpr float kLog2e = 1.4426950408889634f, kSqrt2OverPi = 0.7978845608028654f, kOverSqrt2Pi = 0.3989422804014327f;
+// (within a unit of the last place).  GELU is off by at most 8 units of its own last place wherever it is a normal number; the other two by a few units of the
+// last place of z, below 0 relative to themselves by |z| of them.
+constexpr float kLog2e = 1.4426950408889634f, kSqrt2OverPi = 0.7978845608028654f, kOverSqrt2Pi = 0.3989422804014327f, kLn2 = 0.6931471805599453f;
+
+// The normal distribution p(z) and e = exp(-z^2 / 2), from polynomials fitted for this (least largest relative error).  |z| <= 1: (p - 1 / 2) / z, even, in z^2
+// (1e-9).  Beyond: p(-|z|) = e t P(t), t = 1 / (1 + 0.4 |z|), up to 13.4, where e leaves float32's range (0.8e-7).  e is taken with what z^2 and its
+// product with log2 e are off by (without: 5e-6 of e at 12).
+__device__ __forceinline__ float normal_share(float z, float& e)
+{
+    constexpr float kHalf = -0.5f * kLog2e, kHalfRest = -9.62981517e-9f;                     // -log2 e / 2, and what float32 lacks of it
+    const float x = fminf(fabsf(z), 16.0f), t = __builtin_amdgcn_rcpf(fmaf(x, 0.4f, 1.0f));
+    const float square = x * x, rest = fmaf(x, x, -square), power = square * kHalf;
+    const float off = fmaf(square, kHalf, -power) + fmaf(rest, kHalf, square * kHalfRest);
+    e = __builtin_amdgcn_exp2f(power);
+    e = fmaf(e, off * kLn2, e);
+    const float q = fmaf(t, fmaf(t, fmaf(t, fmaf(t, fmaf(t, fmaf(t, 0.0681211948f, -0.186427504f), 0.105362579f), 0.0555409156f), 0.139002189f), 0.159100011f), 0.159595788f) * t * e;
+    const float s = fmaf(square, fmaf(square, fmaf(square, fmaf(square, fmaf(square, -7.65420828e-06f, 0.000113486371f), -0.00118632999f), 0.00997332297f), -0.0664903596f), 0.398942292f);
+    return x <= 1.0f ? fmaf(z, s, 0.5f) : z < 0.0f ? q : 1.0f - q;
+}
 
 __device__ __forceinline__ float act_value(float z, int act, float& slope)
 {
     if (act == HR_GELU) {
-        // the normal distribution by Abramowitz and Stegun 7.1.26 (within 0.75e-7): 1 - p(t) exp(-x^2) / 2, t = 1 / (1 + 0.3275911 x), x = |z| / sqrt 2
-        const float t = __builtin_amdgcn_rcpf(fmaf(fabsf(z), 0.3275911f * 0.7071067811865476f, 1.0f)), e = __builtin_amdgcn_exp2f(z * z * (-0.5f * kLog2e));
-        const float q = t * fmaf(t, fmaf(t, fmaf(t, fmaf(t, 0.5f * 1.061405429f, 0.5f * -1.453152027f), 0.5f * 1.421413741f), 0.5f * -0.284496736f), 0.5f * 0.254829592f) * e;
-        const float p = z < 0.0f ? q : 1.0f - q;
+        float e;
+        const float p = normal_share(z, e);
         slope = fmaf(z * e, kOverSqrt2Pi, p);
         return z * p;
     }
