@@ -18,7 +18,7 @@ LIB = os.path.join(HERE, "libhr_ivf.so")
 SOURCES = ["api.hip", "aux_kernels.hip", "scan_f16.hip", "scan_bf16.hip", "scan_f32.hip", "scan_f32x2.hip",
            "i8.hip", "rows.hip", "norm.hip", "gated.hip",
            "gated_f16.hip", "gated_bf16.hip", "gated_f32.hip", "adamw.hip"]
-HEADERS = [os.path.join(CSRC, h) for h in ("common.h", "wave.h", "group.h", "scan_kernel.h", "entry.h", "row_math.h", "i8_few.h", "tile.h", "tile_launch.h")] + \
+HEADERS = [os.path.join(CSRC, h) for h in ("common.h", "wave.h", "group.h", "scan_kernel.h", "entry.h", "row_math.h", "i8_few.h", "tile.h", "tile_launch.h", "tile_plan.h")] + \
           [os.path.join(ROOT, "include", h) for h in ("hr_ivf.h", "hr_scores.h", "hr_layers.h")]
 FLAGS = ["--offload-arch=gfx950", "-O3", "-std=c++17", "-fPIC", "-Wall", "-Wno-unused-function",
          "-Xclang", "-target-feature", "-Xclang", "-packed-fp32-ops",
