@@ -59,7 +59,7 @@ int hr_layer_norm_backward(const void* x, int64_t ldx, int32_t dtype, int64_t ro
  * Products are summed in float32, act and its product with up taken in float32, out rounded once.
  *   1 <= k, f <= HR_GATED_MAX, 0 <= m <= HR_GATED_MAX; HR_ERR_UNSUPPORTED where [m, 2 f], [2 f, k] and [m, k] together have about 2^36 elements or more.
  */
-size_t hr_gated_workspace_bytes(int64_t m, int64_t k, int64_t f, int32_t dtype);       /* of this shape, with room for copies of rows at odd places; 0 on invalid arguments */
+size_t hr_gated_workspace_bytes(int64_t m, int64_t k, int64_t f, int32_t dtype);       /* 0 on invalid arguments; enough for fewer rows as well; has room for copies of rows at odd places */
 int hr_gated(const void* x, int64_t ldx, const void* w_gate, int64_t ldwg, const void* w_up, int64_t ldwu, int32_t dtype, int64_t m, int64_t k,
              int64_t f, int32_t activation, void* out, int64_t ldo, float* out_pre, void* workspace, size_t workspace_bytes, void* stream);
 

@@ -517,8 +517,38 @@ struct GatedArgs {
 // workspace: x and both matrices with padded rows (whether a call copies them is known by its addresses only); sums of the parts of k
 static size_t padded_bytes(int64_t m, int64_t k, int64_t f, size_t es) { return aligned((size_t)((m + 2 * f) * padded(k, es))); }
 
+// Tiles and workspace of more than kFewRows rows.  The tiles are those of the next multiple of 64 rows, so that a workspace for fewer rows is found without
+// asking for every number of them.
+struct GatedPlan {
+    Tiling tiling;
+    TileArgs p;
+    size_t sums, all;                                    // where they begin, and the end
+};
+static int64_t next_64(int64_t m) { return (m + 63) / 64 * 64; }
+static GatedPlan gated_plan(int64_t m, int64_t k, int64_t f, size_t es)
+{
+    GatedPlan g{};
+    g.p.m = next_64(m);
+    g.p.n = f;
+    g.p.k = (int)padded(k, es);
+    g.tiling = plan_tiles(true, es, &g.p, 1);
+    g.sums = padded_bytes(m, k, f, es);
+    g.all = g.sums + sums_bytes(true, g.p) + HR_WORKSPACE_ALIGN;
+    g.p.m = m;
+    g.p.large = std::min(g.p.large, m);
+    return g;
+}
+// The most that m rows or fewer take; a multiple of `step` rows takes as much as the fewer ones that go with it.  at_most(rows): a bound that falls with them.
+template <typename F, typename G>
+static size_t for_fewer_too(int64_t m, int64_t step, F&& takes, G&& at_most)
+{
+    size_t most = takes(m);
+    for (int64_t rows = (m - 1) / step * step; rows > 0 && at_most(rows) > most; rows -= step) most = std::max(most, takes(rows));
+    return most;
+}
+
 template <typename T>
-static hipError_t launch_gated(const GatedArgs& g, char* ws, hipStream_t s)
+static hipError_t launch_gated(const GatedArgs& g, const GatedPlan& plan, char* ws, hipStream_t s)
 {
     constexpr size_t es = sizeof(T);
     if (g.m <= kFewRows) {
@@ -543,8 +573,7 @@ static hipError_t launch_gated(const GatedArgs& g, char* ws, hipStream_t s)
         else go(k_gated_few<T, 2, 2, 4>, 16, 4);
         return hipGetLastError();
     }
-    TileArgs p{};
-    p.k = (int)padded(g.k, es);
+    TileArgs p = plan.p;
     p.end = g.k * es % 16 == 0 ? (int)(g.k * es) : p.k;  // (behind it a copy has zeros, where there is one)
     // what tiles cannot take as it is is copied first, row by row
     struct { const void* at; int64_t ld, rows; const char** to; int64_t* lds; } in[3] = {
@@ -567,26 +596,23 @@ static hipError_t launch_gated(const GatedArgs& g, char* ws, hipStream_t s)
         hipLaunchKernelGGL(k_pad<T>, dim3((unsigned)std::min<int64_t>((copied * (p.k / 16) + 255) / 256, 1 << 20)), dim3(256), 0, s, pad);
         if (hipError_t e = hipGetLastError()) return e;
     }
-    p.m = g.m;
-    p.n = g.f;
     p.out = g.out;
     p.ldo = g.ldo;
     p.pre = g.pre;
     p.act = g.act;
-    p.sums = (float*)(ws + padded_bytes(g.m, g.k, g.f, es));
-    const Tiling t = plan_tiles(true, es, &p, 1);
-    return launch_tiles<T, true>(t, TilePair{{p}}, 1, s);
+    p.sums = (float*)(ws + plan.sums);
+    return launch_tiles<T, true>(plan.tiling, TilePair{{p}}, 1, s);
 }
 
 // workspace of the gradients: those of gate and up as rows, [m][2 fp], and as columns, [2 f][mp]; both matrices turned, [k][2 fp]; x turned, [k][mp];
 // bits of the largest of each row and of each column (binary16), sums of the parts of the products' k.  fp, mp: whole blocks.
 struct BackwardPlan {
     int64_t fp, mp;                                      // elements
-    size_t rows, cols, w, x, largest, sums, all;         // where each begins, and the end
+    size_t rows, cols, w, x, largest, sums, sums2, all;  // where each begins, and the end
     Tiling tiling;
     TileArgs p[2];                                       // the product for x's gradient, the one for the matrices' (the same parts whichever are wanted)
 };
-static BackwardPlan backward_plan(int64_t m, int64_t k, int64_t f, int32_t dtype)
+static BackwardPlan backward_plan(int64_t m, int64_t k, int64_t f, int32_t dtype, bool tiles = true)
 {
     const size_t es = element_bytes(dtype);
     const bool raised = dtype == HR_F16;
@@ -601,18 +627,24 @@ static BackwardPlan backward_plan(int64_t m, int64_t k, int64_t f, int32_t dtype
     p.largest = p.x + aligned((size_t)(k * mb));
     p.sums = p.largest + (raised ? aligned((size_t)(m + 2 * f) * 4) : 0);
     p.all = p.sums + HR_WORKSPACE_ALIGN;
-    if (m == 0) return p;
+    if (m == 0 || !tiles) return p;
     for (int i = 0; i < 2; ++i) {
         TileArgs& t = p.p[i];
-        t.m = i ? 2 * f : m;
+        t.m = i ? 2 * f : p.mp;                          // (whole blocks of rows: see gated_plan)
         t.n = k;
         t.k = t.end = (int)(i ? mb : 2 * fb);
         t.lda = t.ldb = t.k;
     }
     p.tiling = plan_tiles(false, es, p.p, 2);
-    p.all += sums_bytes(false, p.p[0]) + sums_bytes(false, p.p[1]);
+    p.sums2 = p.sums + sums_bytes(false, p.p[0]);
+    p.all = p.sums2 + sums_bytes(false, p.p[1]) + HR_WORKSPACE_ALIGN;
+    p.p[0].m = m;
+    p.p[0].large = std::min(p.p[0].large, m);
     return p;
 }
+
+// most that the sums of parts of k of a product take: see plan_tiles
+static size_t most_sums(int64_t m, int64_t n, size_t es) { return (size_t)std::min<int64_t>(kMostSums, kMostParts * m * n * (int64_t)es) + HR_WORKSPACE_ALIGN; }
 
 }  // namespace hr
 
@@ -626,12 +658,8 @@ size_t hr_gated_workspace_bytes(int64_t m, int64_t k, int64_t f, int32_t dtype)
     if (check_gated(m, k, f, dtype, HR_SILU)) return 0;
     const size_t es = element_bytes(dtype);
     if (m <= kFewRows) return HR_WORKSPACE_ALIGN;
-    TileArgs p{};
-    p.m = m;
-    p.n = f;
-    p.k = (int)padded(k, es);
-    plan_tiles(true, es, &p, 1);
-    return padded_bytes(m, k, f, es) + sums_bytes(true, p) + HR_WORKSPACE_ALIGN;
+    return for_fewer_too(m, 64, [&](int64_t rows) { return gated_plan(rows, k, f, es).all; },
+                         [&](int64_t rows) { return padded_bytes(rows, k, f, es) + most_sums(rows, f, 8) + HR_WORKSPACE_ALIGN; });
 }
 
 int hr_gated(const void* x, int64_t ldx, const void* w_gate, int64_t ldwg, const void* w_up, int64_t ldwu, int32_t dtype, int64_t m, int64_t k,
@@ -645,16 +673,22 @@ int hr_gated(const void* x, int64_t ldx, const void* w_gate, int64_t ldwg, const
     if (int rc = check_matrix("out", out, m, f, ldo, es)) return rc;
     if ((uintptr_t)out_pre % 4) return fail(HR_ERR_ARG, "out_pre is not aligned to its elements");
     if (m == 0) return HR_OK;
-    if (int rc = check_workspace(workspace, workspace_bytes, hr_gated_workspace_bytes(m, k, f, dtype))) return rc;
+    const GatedPlan plan = m > kFewRows ? gated_plan(m, k, f, es) : GatedPlan{};
+    if (int rc = check_workspace(workspace, workspace_bytes, std::max<size_t>(plan.all, HR_WORKSPACE_ALIGN))) return rc;
     const GatedArgs g{x, ldx, w_gate, ldwg, w_up, ldwu, m, k, f, activation, out, ldo, out_pre};
-    HR_HIP(with_type(dtype, [&](auto t) { return launch_gated<decltype(t)>(g, (char*)workspace, (hipStream_t)stream); }));
+    HR_HIP(with_type(dtype, [&](auto t) { return launch_gated<decltype(t)>(g, plan, (char*)workspace, (hipStream_t)stream); }));
     return HR_OK;
 }
 
 size_t hr_gated_backward_workspace_bytes(int64_t m, int64_t k, int64_t f, int32_t dtype)
 {
     if (check_gated(m, k, f, dtype, HR_SILU)) return 0;
-    return backward_plan(m, k, f, dtype).all;
+    const int64_t step = 128 / (int64_t)element_bytes(dtype);
+    return for_fewer_too(m, step, [&](int64_t rows) { return backward_plan(rows, k, f, dtype).all; },
+                         [&](int64_t rows) {
+                             const BackwardPlan p = backward_plan(rows, k, f, dtype, false);
+                             return p.sums + most_sums(rows, k, 4) + most_sums(2 * f, k, 4) + HR_WORKSPACE_ALIGN;
+                         });
 }
 
 int hr_gated_backward(const void* x, int64_t ldx, const void* w_gate, int64_t ldwg, const void* w_up, int64_t ldwu, int32_t dtype, int64_t m,
@@ -713,10 +747,9 @@ int hr_gated_backward(const void* x, int64_t ldx, const void* w_gate, int64_t ld
         hipLaunchKernelGGL(k_lay_out<T>, dim3((unsigned)(l.blocks_d + (grad_x ? 2 * l.blocks_w : 0) + (grad_w_gate ? blocks(plan.mp, k) : 0))), dim3(256), 0, s, l);
         TilePair pair{};
         int count = 0;
-        char* sums = (char*)workspace + plan.sums;
         if (grad_x) {
             TileArgs& p = pair.p[count++] = plan.p[0];
-            p.sums = (float*)sums;
+            p.sums = (float*)((char*)workspace + plan.sums);
             p.a = rows;
             p.largest = largest;
             p.b = turned_w;
@@ -726,7 +759,7 @@ int hr_gated_backward(const void* x, int64_t ldx, const void* w_gate, int64_t ld
         }
         if (grad_w_gate) {
             TileArgs& p = pair.p[count++] = plan.p[1];
-            p.sums = (float*)(sums + sums_bytes(false, plan.p[0]));
+            p.sums = (float*)((char*)workspace + plan.sums2);
             p.a = cols;
             p.largest = largest + m;
             p.b = turned_x;

@@ -7,6 +7,8 @@
 
 namespace hr {
 
+constexpr int64_t kMostParts = 64, kMostSums = 1 << 28;              // of k, and bytes of their sums
+
 // Blocks of k that a place for a workgroup multiplies one after the other until all workgroups are done: first those of `long_` blocks, then the
 // shorter ones, each on the first of `places` that is free.
 inline double rounds(int64_t places, int64_t longs, int64_t long_, int64_t shorts, int64_t short_)
@@ -50,7 +52,7 @@ inline Tiling plan_tiles(bool gated, size_t es, TileArgs* p, int count)
     auto consider = [&](int bm, int bn) {
         const int64_t cols = bn / (gated ? 2 : 1);
         int64_t last = 0;
-        for (int64_t n = 1; n <= 64; ++n) {
+        for (int64_t n = 1; n <= kMostParts; ++n) {
             const int64_t length = (longest_k + n - 1) / n;                  // blocks of the longest part
             if (n > 1 && (length < 2 || length == last)) continue;
             last = length;
@@ -65,7 +67,7 @@ inline Tiling plan_tiles(bool gated, size_t es, TileArgs* p, int count)
                 work += (double)groups[i] * of[i];
                 if (parts > 1) {
                     joins += 2 * sums / 4e6;
-                    fits &= groups[i] <= 8 * kComputeUnits && sums <= 0x1p28;
+                    fits &= groups[i] <= 8 * kComputeUnits && sums <= kMostSums;
                 }
             }
             if (!fits) break;
