@@ -9,7 +9,8 @@
  * Conventions are those of hr_scores.h: DEV pointers on the current device, row-major matrices with the distance between rows in elements, types
  * HR_F32 / HR_F16 / HR_BF16, error codes and hr_last_error(), nothing enqueued on any error but HR_ERR_HIP, kernels only (no allocation, no
  * host synchronisation, no memset or copy nodes; capture in a HIP graph is fine), bit-identical results for the same inputs.  Outputs must not
- * overlap inputs or each other, except where it says so.  Zero rows are a no-op, but for gradients that sum over rows: those are zeros.
+ * overlap inputs or each other, except where it says so.  Of 16-bit rows that begin or end inside an aligned word of 4 bytes the whole word may be read; what is
+ * not the row's is not used, and may be written meanwhile.  Zero rows are a no-op, but for gradients that sum over rows: those are zeros.
  */
 #ifndef HR_LAYERS_H
 #define HR_LAYERS_H
@@ -68,6 +69,7 @@ int hr_gated(const void* x, int64_t ldx, const void* w_gate, int64_t ldwg, const
  * matrix instructions that take them:
  *   grad_x = d_gate w_gate + d_up w_up,   grad_w_gate = d_gate' x,   grad_w_up = d_up' x.
  *   pre   DEV [m, 2, f] float32, as hr_gated wrote it.   grad_out  DEV [m, f] in `dtype`.
+ * (The rounding is as large as that of the result: together they are 1.4 times as far off as one of them.)
  * In binary16 each row of d_gate and d_up (for grad_x) and each column (for the matrices) is held times a power of two, so that they may be of any size that
  * float32 has: only the results have to fit the type.  What is less than 2^-28 of the largest of its row (column) has fewer bits, below 2^-40 none.
  *   grad_x  DEV [m, k] or NULL: not wanted.   grad_w_gate, grad_w_up  DEV [f, k], both or neither (NULL); overwritten; all in `dtype`, rounded once.

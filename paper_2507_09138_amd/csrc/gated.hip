@@ -312,7 +312,8 @@ __global__ __launch_bounds__(256) void k_clear(T* x, int64_t ld, int64_t rows, i
 
 // ---- up to 16 MT rows x: bound by reading the matrices once.  A workgroup takes 8 NT columns of the result, its waves parts of k; the first operand of
 // a matrix instruction is eight rows of each matrix.  Here straight to registers, U steps at once, from rows that may begin anywhere: 64 bytes of a
-// line at a time, and where a row begins inside 16 bytes twice that (one row of 4096 bfloat16 against 10752 of each matrix 35 us, of 4097 80).
+// line at a time (one row of 4096 bfloat16 against 10752 of each matrix 35 us), and of rows that begin inside a word whole words and a shift (of 4097 70, 16
+// rows 90).
 constexpr int kFewRows = 32;
 template <typename T, int MT, int NT, int U>
 __global__ __launch_bounds__(1024) void k_gated_few(const T* x, int64_t ldx, const T* gate, int64_t ldg, const T* up, int64_t ldu, int m, int k, int f, int act, T* out,
