@@ -1,12 +1,15 @@
 """Workspaces of gated blocks: what is enough for a batch is enough for every smaller one (no GPU), and the calls on the GPU use no more than they ask for."""
+import os
+
 import pytest
 import torch
-
-import layers_reference as ref  # noqa: F401  (beside the other tests of hr_layers.h)
 
 
 def _hr():
     import paper_2507_09138_amd as hr
+    from paper_2507_09138_amd import build
+    if not os.path.exists(build.LIB):
+        build.build()
     return hr
 
 
